@@ -1,0 +1,380 @@
+// Products of the gated feed-forward block: C[i][j] = sum_k P[i][k] Q[j][k] in tiles of BM x BN on the matrix cores, with the
+// block's activation, gating and row maps in the loads and the epilogue.
+#pragma once
+#include "ffn_act.hpp"
+#include "ffn_params.hpp"
+#include "mma_common.hpp"
+
+namespace sc {
+
+// ---- LDS tiles ------------------------------------------------------------------------------------------------------------------
+// 128 bytes of k a row of an operand along k (64 entries of 16 bits, 32 floats); an operand across k has as many rows of k.
+// A 16-byte group lies at its index XOR a key of its row, so that the lanes that read together touch every bank once.
+template <int EB> struct FfnTile {
+  static constexpr int BK = 128 / EB, V = 16 / EB, STEPS = 4, KSTEP = BK / STEPS;
+  static __device__ __forceinline__ int key_along(int row) { return (row & 3) | ((((row >> 2) ^ (row >> 4)) & 1) << 2); }
+  static __device__ __forceinline__ int key_across(int k) {
+    if constexpr (EB == 2) return ((k & 3) << 2) | ((k >> 1) & 1);
+    return ((k >> 2) & 1) << 3;
+  }
+};
+
+// A 32 x 32 block of results leaves 16 registers a lane: with the Q rows of a block read in this order, they are 16 consecutive
+// columns of the lane's row.
+__device__ __forceinline__ int ffn_q_order(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
+
+static __device__ __align__(16) v4i ffn_zeros = {0, 0, 0, 0};      // what is read beyond an operand's end
+
+// 16 bytes a lane from memory into LDS at base + 16 lane.  Written out, because the compiler would let every later LDS read wait
+// for all transfers in flight; their arrival is waited for at the barriers below.
+__device__ __forceinline__ void ffn_dma16(const void* src, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src));
+}
+
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const FfnGemm p) {
+  using E = Elem<DT>;
+  using T = typename E::T;
+  constexpr int EB = sizeof(T);
+  using L = FfnTile<EB>;
+  constexpr int V = L::V, BK = L::BK;
+  constexpr int W = WAVES_M * WAVES_N, NT = 64 * W;
+  constexpr int MI = BM / WAVES_M / 32, NI = BN / WAVES_N / 32;
+  constexpr int JP = BM * 8 / NT, JQ = BN * 8 / NT;            // transfers a lane and K tile
+  constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
+  constexpr bool GATED = WHAT == kFfnUp;
+  constexpr int HALF = GATED ? NI / 2 : NI;                    // blocks of columns that a wavefront leaves
+  constexpr int COLS = GATED ? BN / 2 : BN;                    // result columns of a tile
+  extern __shared__ __align__(16) unsigned char smem[];
+
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+  const int l32 = lane & 31, h = lane >> 5;
+
+  // consecutive workgroups go round the eight dies: renumbered so that a die has neighbouring tiles, `group` tiles high
+  const int tiles = p.m_tiles * p.n_tiles, total = tiles * p.batch * p.splits;
+  const int per_xcd = (total + 7) >> 3;
+  int at = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_xcd || at >= total) return;
+  const int part = at / tiles;
+  at -= part * tiles;
+  const int z = part / p.splits, split = part - z * p.splits;
+  const int band = at / (p.group * p.n_tiles), in_band = at - band * p.group * p.n_tiles;
+  const int high = min(p.group, p.m_tiles - band * p.group);
+  const int m0 = (band * p.group + in_band % high) * BM, n0 = (in_band / high) * COLS;
+
+  // K tiles of this workgroup: every segment is a whole number of tiles, the last one padded with zeros
+  const int seg_tiles = (p.k + BK - 1) / BK, all_tiles = seg_tiles * p.segments;
+  const int kt_lo = (int)((int64_t)all_tiles * split / p.splits), kt_hi = (int)((int64_t)all_tiles * (split + 1) / p.splits);
+
+  // ---- loads ----
+  // slot s of an operand's tile (16 bytes): along k, row s / 8, group s % 8; across k, row s / CPR of k, group s % CPR
+  auto column_of = [&](int qrow, int& which) -> int {          // column of the result that a row of the Q tile belongs to
+    which = GATED && qrow >= COLS ? 1 : 0;
+    return n0 + (which ? qrow - COLS : qrow);
+  };
+  auto p_row = [&](int i) -> int64_t { return p.p_rows ? p.p_rows[i] : i; };
+  auto q_row = [&](int i) -> int64_t { return p.q_rows ? p.q_rows[i] : i; };
+
+  const T* pp[JP];
+  const T* qq[JQ];
+  int p_at = 0, q_at = 0;                                      // k (along) or result row / column (across) of the lane's group
+  int p_k[JP], q_k[JQ];                                        // k of its row (across)
+  if constexpr (P_ALONG) {
+    const int row = wave * 8 + (lane >> 3);
+    p_at = ((lane & 7) ^ L::key_along(row)) * V;
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      const int i = min(m0 + row + j * W * 8, p.m - 1);
+      pp[j] = static_cast<const T*>(p.p[0]) + p_row(i) * p.ldp;
+    }
+  } else {
+    constexpr int CPR = BM / V, RPL = 64 / CPR;
+    const int k0 = wave * RPL + lane / CPR;
+    p_at = m0 + ((lane % CPR) ^ L::key_across(k0)) * V;
+#pragma unroll
+    for (int j = 0; j < JP; ++j) p_k[j] = k0 + j * W * RPL;
+  }
+  if constexpr (Q_ALONG) {
+    const int row = wave * 8 + (lane >> 3);
+    q_at = ((lane & 7) ^ L::key_along(row)) * V;
+#pragma unroll
+    for (int j = 0; j < JQ; ++j) {
+      int which;
+      const int c = min(column_of(row + j * W * 8, which), p.n - 1);
+      qq[j] = static_cast<const T*>(p.q[which]) + (int64_t)c * p.ldq;
+    }
+  } else {
+    constexpr int CPR = BN / V, RPL = 64 / CPR;
+    const int k0 = wave * RPL + lane / CPR;
+    q_at = n0 + ((lane % CPR) ^ L::key_across(k0)) * V;
+#pragma unroll
+    for (int j = 0; j < JQ; ++j) q_k[j] = k0 + j * W * RPL;
+  }
+  // the source of transfer j of K tile kt, and how many of its entries there are
+  auto p_src = [&](int kt, int j, int& have) -> const T* {
+    const int seg = kt / seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    if constexpr (P_ALONG) {
+      have = min(V, p.k - (k0 + p_at));
+      const T* base = pp[j] + k0 + p_at;
+      if (p.segments > 1 && seg) base += static_cast<const T*>(p.p[1]) - static_cast<const T*>(p.p[0]);
+      return base;
+    } else {
+      const int k = k0 + p_k[j];
+      have = k < p.k ? min(V, p.m - p_at) : 0;
+      return static_cast<const T*>(p.p[z]) + (have > 0 ? p_row(k) * p.ldp + p_at : 0);
+    }
+  };
+  auto q_src = [&](int kt, int j, int& have) -> const T* {
+    const int seg = kt / seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    if constexpr (Q_ALONG) {
+      have = min(V, p.k - (k0 + q_at));
+      return qq[j] + k0 + q_at;
+    } else {
+      const int k = k0 + q_k[j];
+      have = k < p.k ? min(V, p.n - q_at) : 0;
+      return static_cast<const T*>(p.q[p.segments > 1 ? seg : 0]) + (have > 0 ? q_row(k) * p.ldq + q_at : 0);
+    }
+  };
+  const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
+  auto request = [&](int kt, int stage) {                      // whole groups: straight into LDS
+    const unsigned at_p = lds0 + stage * STAGE + wave * 1024, at_q = at_p + P_BYTES;
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      int have;
+      const T* s = p_src(kt, j, have);
+      ffn_dma16(have > 0 ? (const void*)s : (const void*)&ffn_zeros, at_p + j * NT * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < JQ; ++j) {
+      int have;
+      const T* s = q_src(kt, j, have);
+      ffn_dma16(have > 0 ? (const void*)s : (const void*)&ffn_zeros, at_q + j * NT * 16);
+    }
+  };
+  v4i held[JP + JQ];                                           // rows of any length: through registers
+  auto load_group = [=](const T* s, int have) -> v4i {
+    if (have >= V) {
+      v4i g;
+      __builtin_memcpy(&g, s, 16);
+      return g;
+    }
+    T e[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = i < have ? s[i] : T(0);
+    v4i g;
+    __builtin_memcpy(&g, e, 16);
+    return g;
+  };
+  auto hold = [&](int kt) {
+#pragma unroll
+    for (int j = 0; j < JP; ++j) {
+      int have;
+      const T* s = p_src(kt, j, have);
+      held[j] = load_group(s, have);
+    }
+#pragma unroll
+    for (int j = 0; j < JQ; ++j) {
+      int have;
+      const T* s = q_src(kt, j, have);
+      held[JP + j] = load_group(s, have);
+    }
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int j = 0; j < JP; ++j) *reinterpret_cast<v4i*>(smem + (j * NT + t) * 16) = held[j];
+#pragma unroll
+    for (int j = 0; j < JQ; ++j) *reinterpret_cast<v4i*>(smem + P_BYTES + (j * NT + t) * 16) = held[JP + j];
+  };
+
+  // ---- fragments ----
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  // 32 rows r0 .. r0 + 31 of an operand's tile (of BR rows), KSTEP entries of k
+  auto fragment = [&](auto along, auto is_q, const unsigned char* tile, auto br, int r0, int ks) -> v4i {
+    constexpr int BR = decltype(br)::value;
+    if constexpr (decltype(along)::value) {
+      const int r = decltype(is_q)::value ? ffn_q_order(l32) : l32;
+      return *reinterpret_cast<const v4i*>(tile + (r0 + r) * 128 + (((2 * ks + h) ^ L::key_along(r)) << 4));
+    } else if constexpr (EB == 2) {
+      // within 16 lanes the transposing read gives lane j element t of source lane 4 t + j / 4, entry j % 4: source lane s
+      // points at row s / 4 of k, columns of the four lanes from 4 (s % 4) on
+      const int l16 = lane & 15, k = ks * L::KSTEP + 8 * h + (l16 >> 2);
+      const int r = 16 * ((lane >> 4) & 1) + 4 * (l16 & 3), c = r0 + (decltype(is_q)::value ? ffn_q_order(r) : r);
+      const unsigned char* a = tile + k * (BR * 2) + (((c >> 3) ^ L::key_across(k)) << 4) + (c & 7) * 2;
+      struct { s16x4 lo, hi; } both = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a),
+                                       __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 4 * BR * 2))};
+      return __builtin_bit_cast(v4i, both);
+    } else {
+      const int k = ks * L::KSTEP + 4 * h, c = r0 + (decltype(is_q)::value ? ffn_q_order(l32) : l32);
+      v4i f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        f[e] = *reinterpret_cast<const int*>(tile + (k + e) * (BR * 4) + (((c >> 2) ^ L::key_across(k)) << 4) + (c & 3) * 4);
+      return f;
+    }
+  };
+
+  floatx16 acc[MI][NI];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
+
+  auto contract = [&](int stage) {
+    const unsigned char* tp = smem + stage * STAGE;
+    const unsigned char* tq = tp + P_BYTES;
+#pragma unroll
+    for (int ks = 0; ks < L::STEPS; ++ks) {
+      v4i pf[MI], qf[NI];
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+        pf[mi] = fragment(std::bool_constant<P_ALONG>{}, std::false_type{}, tp, std::integral_constant<int, BM>{}, (wm * MI + mi) * 32, ks);
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) {
+        const int r0 = GATED ? (ni < HALF ? (wn * HALF + ni) * 32 : COLS + (wn * HALF + ni - HALF) * 32) : (wn * NI + ni) * 32;
+        qf[ni] = fragment(std::bool_constant<Q_ALONG>{}, std::true_type{}, tq, std::integral_constant<int, BN>{}, r0, ks);
+      }
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) E::mma(acc[mi][ni], qf[ni], pf[mi]);
+    }
+  };
+
+  if constexpr (ALIGNED) {
+    if (kt_lo < kt_hi) request(kt_lo, 0);
+    for (int kt = kt_lo; kt < kt_hi; ++kt) {
+      const int stage = (kt - kt_lo) & 1;
+      // this tile has landed, for every wavefront, and all have left the one before, whose place the next takes
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (kt + 1 < kt_hi) request(kt + 1, stage ^ 1);
+      contract(stage);
+    }
+  } else {
+    if (kt_lo < kt_hi) hold(kt_lo);
+    for (int kt = kt_lo; kt < kt_hi; ++kt) {
+      __syncthreads();
+      put();
+      __syncthreads();
+      if (kt + 1 < kt_hi) hold(kt + 1);
+      contract(0);
+    }
+  }
+
+  // ---- results: the lane has row l32 of a block, its columns 16 h .. 16 h + 15 ----
+  const int n = p.n, m = p.m;
+  auto store = [&](T* c, int64_t ldc, int row, int col, const floatx16& v) {      // row < 0: none
+    if constexpr (ALIGNED) {
+      store_block_pairs<DT, false>(v, row, false, col, c, nullptr, 0, (int)ldc);
+    } else if (row >= 0) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (col + e < n) c[(int64_t)row * ldc + col + e] = E::from_float(v[e]);
+    }
+  };
+  auto load16 = [&](const T* c, int64_t ldc, int row, int col, float (&out)[16]) {
+    const T* s = c + (int64_t)row * ldc + col;
+#pragma unroll
+    for (int g = 0; g < 16 / V; ++g) {
+      const v4i q = load_group(s + g * V, row < 0 ? 0 : n - col - g * V);
+      T e[V];
+      __builtin_memcpy(e, &q, 16);
+#pragma unroll
+      for (int i = 0; i < V; ++i) out[g * V + i] = (float)e[i];
+    }
+  };
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) {
+    const int i = m0 + (wm * MI + mi) * 32 + l32;
+    const int row = i < m ? i : -1;
+    int out_row = row;
+    if (row >= 0 && p.c_rows) out_row = p.c_rows[row];
+#pragma unroll
+    for (int ni = 0; ni < HALF; ++ni) {
+      const int col = n0 + (wn * HALF + ni) * 32 + 16 * h;
+      if constexpr (WHAT == kFfnUp) {
+        floatx16 hidden;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a, da;
+          ffn_act(p.activation, acc[mi][ni][e], a, da);
+          hidden[e] = a * acc[mi][ni + HALF][e];
+        }
+        store(static_cast<T*>(p.c[0]), p.ldc, row, col, hidden);
+        if (p.saved) {
+          T* g = static_cast<T*>(p.saved);
+          store(g, p.ldc, row, col, acc[mi][ni]);
+          store(g + (int64_t)m * n, p.ldc, row, col, acc[mi][ni + HALF]);
+        }
+      } else if constexpr (WHAT == kFfnGateGrad) {
+        float g[16], u[16];
+        const T* sv = static_cast<const T*>(p.saved);
+        load16(sv, p.ldc, row, col, g);
+        load16(sv + (int64_t)m * n, p.ldc, row, col, u);
+        floatx16 dg, du;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a, da;
+          ffn_act(p.activation, g[e], a, da);
+          dg[e] = acc[mi][ni][e] * u[e] * da;
+          du[e] = acc[mi][ni][e] * a;
+        }
+        store(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
+        store(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
+      } else {
+        if (WHAT == kFfnWGrad && p.splits > 1) {
+          if (row >= 0) {
+            float* dst = p.partial + (((int64_t)z * p.splits + split) * m + row) * n + col;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (col + e < n) dst[e] = acc[mi][ni][e];
+          }
+        } else {
+          store(static_cast<T*>(p.c[z]), p.ldc, out_row, col, acc[mi][ni]);
+        }
+      }
+    }
+  }
+}
+
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
+hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
+  auto kernel = ffn_gemm_kernel<DT, P_ALONG, Q_ALONG, WHAT, BM, BN, WAVES_M, WAVES_N, ALIGNED>;
+  constexpr int cols = WHAT == kFfnUp ? BN / 2 : BN;
+  g.m_tiles = (g.m + BM - 1) / BM;
+  g.n_tiles = (g.n + cols - 1) / cols;
+  g.group = 8;
+  constexpr int lds = (BM + BN) * 128 * (ALIGNED ? 2 : 1);
+  if constexpr (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t total = (int64_t)g.m_tiles * g.n_tiles * g.batch * g.splits;
+  kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WAVES_M * WAVES_N), lds, s>>>(g);
+  return hipGetLastError();
+}
+
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT>
+hipError_t ffn_launch_what(const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
+  if (!aligned) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, false>(g, s);
+  if (tile == 1) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 256, 2, 4, true>(g, s);
+  return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, true>(g, s);
+}
+
+template <int DT> hipError_t ffn_launch_type(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
+  switch (what) {
+    case kFfnUp: return ffn_launch_what<DT, true, true, kFfnUp>(g, tile, aligned, s);
+    case kFfnDown: return ffn_launch_what<DT, true, true, kFfnDown>(g, tile, aligned, s);
+    case kFfnGateGrad: return ffn_launch_what<DT, true, false, kFfnGateGrad>(g, tile, aligned, s);
+    case kFfnInGrad: return ffn_launch_what<DT, true, false, kFfnInGrad>(g, tile, aligned, s);
+    case kFfnWGrad: return ffn_launch_what<DT, false, false, kFfnWGrad>(g, tile, aligned, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace sc

@@ -1,0 +1,44 @@
+// Host-side description of the products of the gated feed-forward block, and the launchers of each element type.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sc {
+
+// C[i][j] = sum_k P[i][k] Q[j][k].  An operand is "along k" (its rows are those of the result, k runs within them) or "across k"
+// (its rows are those of the contraction).
+enum FfnProduct : int32_t {
+  kFfnUp = 0,       // P along, Q = gate and up weights along: act(P Wg') * (P Wu'), and with `saved` the two products
+  kFfnDown = 1,     // P along, Q along
+  kFfnGateGrad = 2, // P along, Q across: the product is the gradient of the hidden rows; leaves those of gate and up
+  kFfnInGrad = 3,   // P along, Q across, two pairs of operands summed
+  kFfnWGrad = 4,    // P across, Q across, one or two P with results of their own
+  kFfnProducts = 5
+};
+
+struct FfnGemm {
+  const void* p[2];
+  const void* q[2];
+  int64_t ldp, ldq;            // elements from row to row
+  const int32_t* p_rows;       // row of p that row i (of the result, or of the contraction) stands for; null: i
+  const int32_t* q_rows;
+  int32_t m, n, k;             // result rows and columns, contraction
+  int32_t segments;            // pairs (p[s], q[s]) whose products are summed
+  int32_t batch;               // results c[z] of p[z] with q[0]
+  void* c[2];
+  int64_t ldc;
+  const int32_t* c_rows;       // row of c that receives result row i; null: i
+  void* saved;                 // kFfnUp: [3][m][n] or null, c[0] is then its third matrix.  kFfnGateGrad: read
+  int32_t activation;
+  int32_t splits;              // kFfnWGrad: parts of the contraction, each with partial sums in `partial`
+  float* partial;              // [batch][splits][m][n]
+  // set by the launcher
+  int32_t m_tiles, n_tiles, group;
+};
+
+// tile: index into the launcher's list of tile shapes; aligned: rows of all operands are whole 16-byte groups
+hipError_t ffn_launch_bf16(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
+hipError_t ffn_launch_f16(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
+hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
+
+}  // namespace sc

@@ -1,0 +1,451 @@
+"""Block operators against the 64-bit oracle: types, odd sizes, masks from nothing to everything, gradients also against differences."""
+import math
+
+import pytest
+import torch
+
+import block_oracle as O
+from paper_2309_06626_amd import binding as B
+from paper_2309_06626_amd import block as K
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def normal(g, *shape, dtype="f32", std=1.0, mean=0.0):
+    """On the host, rounded to the type and widened to float64."""
+    return (torch.randn(*shape, generator=g) * std + mean).to(O.TORCH[dtype]).double()
+
+
+def dev(t, dtype="f32"):
+    return None if t is None else t.to(O.TORCH[dtype]).to(DEV)
+
+
+def nan_like(*shape, dtype="f32"):
+    return torch.full(shape, float("nan"), dtype=O.TORCH[dtype], device=DEV)
+
+
+def inside(got, want, bound, what):
+    got = got.double().cpu()
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), what
+    over = ((got - want).abs() / bound).max().item() if got.numel() else 0.0
+    assert over <= 1.0, f"{what}: {over:.3g} times the bound"
+
+
+def mask_of(kind, rows, g):
+    m = torch.ones(rows, dtype=torch.uint8)
+    if kind == "half":
+        m[torch.randperm(rows, generator=g)[: rows // 2]] = 0
+    elif kind == "nothing":
+        m.zero_()
+    elif kind == "ends":
+        m[1:-1] = 0
+    elif kind == "block":
+        m[rows // 4: rows // 4 + rows // 2] = 0
+    return m
+
+
+# ---- row sets ----------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows", [0, 1, 63, 64, 4095, 4096, 4097, 70001])
+@pytest.mark.parametrize("kind", ["half", "nothing", "all", "ends"])
+def test_row_lists(rows, kind):
+    g = gen(rows)
+    mask = mask_of(kind, rows, g) * 5      # any byte but 0 keeps
+    rs = K.sparse_rows_plan(mask.to(DEV))
+    for m in (mask, mask_of("half", rows, g)):
+        K.sparse_rows_set_mask(rs, m.to(DEV))
+        want = m.nonzero()[:, 0]
+        got = K.sparse_rows_info(rs)
+        assert got[0] == rows and got[1] == rs.kept == len(want)
+        assert torch.equal(got[2].cpu().long(), want)
+        slot = torch.full((rows,), -1, dtype=torch.int64)
+        slot[want] = torch.arange(len(want))
+        assert torch.equal(got[3].cpu().long(), slot)
+
+
+# ---- norms -------------------------------------------------------------------------------------------------------------
+
+NORMS = [  # rows, d, dtype, post, pre, rows_per_gate (None: no gate), masks of f and h, a, b
+    (1, 1, "f32", "rms", "rms", None, "all", "all", 1.0, 1.0),
+    (1, 2048, "bf16", "rms", "rms", None, "all", "all", 1.0, 1.0),
+    (3, 7, "bf16", "layer", "layer", 2, "all", "all", 1.0, 1.0),
+    (70, 64, "f16", "layer", "rms", 9, "half", "half", 0.5, 2.0),
+    (33, 410, "f32", "layer", "layer", 0, "half", "block", 1.0, 1.0),
+    (1100, 513, "bf16", "rms", "layer", 196, "block", "half", 1.0, 1.0),
+    (600, 1000, "f16", "none", "layer", 1, "half", "half", 1.0, -1.0),
+    (40, 1028, "f32", "rms", "none", 7, "nothing", "half", 1.0, 1.0),
+    (40, 2056, "bf16", "rms", "rms", 5, "half", "nothing", 0.7, 1.0),
+    (1030, 96, "bf16", "layer", "rms", 600, "ends", "ends", 1.0, 1.0),
+    (21, 4099, "bf16", "layer", "layer", 4, "half", "half", 1.0, 1.0),
+    (530, 4100, "f32", "rms", "layer", 530, "half", "half", 1.0, 1.0),
+    (13, 8191, "f16", "layer", "rms", 3, "half", "all", 1.0, 1.0),
+    (520, 8192, "bf16", "rms", "rms", 2, "all", "half", 1.0, 1.0),
+]
+
+
+def norm_inputs(rows, d, dtype, post, pre, per, f_mask, h_mask, seed):
+    g = gen(seed)
+    fm, hm = mask_of(f_mask, rows, g), mask_of(h_mask, rows, g)
+    t = dict(x=normal(g, rows, d, dtype=dtype), f=normal(g, int(fm.sum()), d, dtype=dtype, std=0.5, mean=0.2))
+    t["gate"] = None if per is None else normal(g, -(-rows // (per or rows)), d, dtype=dtype, std=0.5, mean=0.5)
+    t["w_post"], t["w_pre"] = normal(g, d, std=0.1, mean=1.0), normal(g, d, std=0.1, mean=1.0)
+    t["b_post"] = normal(g, d, std=0.1) if post == "layer" else None
+    t["b_pre"] = normal(g, d, std=0.1) if pre == "layer" else None
+    return g, t, fm, hm
+
+
+def norm_call(c, t, fm, hm, **over):
+    rows, d, dtype, post, pre, per, _, _, a, b = c
+    desc = K.make_norm_desc(d, K.DTYPE_CODE[dtype], K.NORM_CODE[post], K.NORM_CODE[pre], 1e-5, a, b, per or 0)
+    dt = {n: dev(v, dtype if n in ("x", "f", "gate") else "f32") for n, v in t.items()}
+    fr = None if fm.all() else K.sparse_rows_plan(fm.to(DEV))
+    hr = None if hm.all() else K.sparse_rows_plan(hm.to(DEV))
+    out = dict(x_new=nan_like(rows, d, dtype=dtype), h=nan_like(int(hm.sum()), d, dtype=dtype), stats=nan_like(rows, 4))
+    K.sparse_norm_run(desc, *[dt[n] for n in ("x", "f", "gate", "w_post", "b_post", "w_pre", "b_pre")], out["x_new"], out["h"],
+                      f_rows=fr, h_rows=hr, stats=out["stats"])
+    return desc, dt, fr, hr, out
+
+
+def norm_oracle(c, t, fm, hm):
+    rows, d, dtype, post, pre, per, _, _, a, b = c
+    return O.norm_forward(t["x"], t["f"], t["gate"], t["w_post"], t["b_post"], t["w_pre"], t["b_pre"], post, pre, 1e-5, a, b,
+                          per or max(rows, 1), fm.bool(), hm.bool())
+
+
+def rowwise(want, d, u):
+    """A normalised row's float error is a few units of its largest terms, the sums over d included."""
+    return u * want.abs() + O.acc(d) * (want.abs().amax(-1, keepdim=True) + 1) * 4 + 1e-37
+
+
+@pytest.mark.parametrize("c", NORMS, ids=lambda c: "-".join(map(str, c[:8])))
+def test_norm_forward_and_gradients(c):
+    rows, d, dtype, post, pre, per, f_mask, h_mask, a, b = c
+    g, t, fm, hm = norm_inputs(rows, d, dtype, post, pre, per, f_mask, h_mask, 11 * rows + d)
+    desc, dt, fr, hr, out = norm_call(c, t, fm, hm)
+    x_new, h = norm_oracle(c, t, fm, hm)
+    u = O.U[dtype] + (2.0 ** -24 if dtype == "f16" else 0)
+    inside(out["x_new"], x_new, rowwise(x_new, d, u) + O.TINY[dtype], "x_new")
+    inside(out["h"], h, rowwise(h, d, u) + O.TINY[dtype], "h")
+
+    dx_new, dh = normal(g, rows, d, dtype=dtype), normal(g, int(hm.sum()), d, dtype=dtype)
+    names = [n for n in ("x", "f", "gate", "w_post", "b_post", "w_pre", "b_pre") if t[n] is not None]
+    leaves = {n: (t[n].clone().requires_grad_(True) if n in names else None) for n in t}
+    want = torch.autograd.grad(norm_oracle(c, leaves, fm, hm), [leaves[n] for n in names], [dx_new, dh], allow_unused=True)
+    want = {n: torch.zeros_like(t[n]) if w is None else w for n, w in zip(names, want)}
+    got = {n: torch.full_like(dt[n], float("nan")) for n in names}
+    ws = torch.empty(K.sparse_norm_workspace_bytes(desc, rows), dtype=torch.uint8, device=DEV)
+    args = [dt[n] for n in ("x", "f", "gate", "w_post", "b_post", "w_pre")] + [out["stats"], dev(dx_new, dtype), dev(dh, dtype)]
+    grads = lambda into: [into.get(n) for n in ("x", "f", "gate", "w_post", "b_post", "w_pre", "b_pre")]  # noqa: E731
+    K.sparse_norm_backward(desc, *args, *grads(got), ws, f_rows=fr, h_rows=hr)
+    # magnitudes that enter: gradients of a row scale with 1 / spread
+    spread = lambda v, kind: 1.0 if kind == "none" or not v.numel() else float(  # noqa: E731
+        (1 / torch.sqrt(((v - (v.mean(-1, keepdim=True) if kind == "layer" else 0)) ** 2).mean(-1) + 1e-5)).max())
+    big = (1 + abs(a) + abs(b)) * (1 + spread(x_new, pre)) * (1 + spread(t["f"], post)) * 8
+    for n in names:
+        w = want[n]
+        terms = rows if n.startswith(("w_", "b_")) else (per or rows) if n == "gate" else 1
+        scale = (w.abs().amax() if w.numel() else 0.0) + 1 + math.sqrt(terms)
+        uu = u if n in ("x", "f", "gate") else O.E
+        inside(got[n], w, uu * w.abs() + O.acc(d) * big * scale + O.TINY[dtype], "d" + n)
+    # the same bits again, into other buffers, with only some of the gradients wanted
+    again = {n: torch.full_like(dt[n], float("nan")) for n in names}
+    K.sparse_norm_backward(desc, *args, *grads(again), ws, f_rows=fr, h_rows=hr)
+    assert all(torch.equal(got[n].view(torch.uint8), again[n].view(torch.uint8)) for n in names)
+    some = {"x": torch.full_like(dt["x"], float("nan"))}
+    K.sparse_norm_backward(desc, *args, *grads(some), ws, f_rows=fr, h_rows=hr)
+    assert torch.equal(some["x"], got["x"])
+
+
+def test_norm_before_a_block_alone_and_in_place():
+    c = (50, 200, "bf16", "rms", "rms", None, "all", "all", 1.0, 1.0)
+    g, t, fm, hm = norm_inputs(*c[:8], 5)
+    desc = K.make_norm_desc(200, B.SC_BF16)
+    x, h = dev(t["x"], "bf16"), nan_like(50, 200, dtype="bf16")
+    K.sparse_norm_run(desc, x, None, None, None, None, dev(t["w_pre"]), None, None, h)
+    want = O.normed(t["x"], "rms", 1e-6) * t["w_pre"]
+    inside(h, want, rowwise(want, 200, O.U["bf16"]), "h")
+    _, dt, _, _, out = norm_call(c, t, fm, hm)
+    K.sparse_norm_run(K.make_norm_desc(200, B.SC_BF16, eps=1e-5), dt["x"], dt["f"], None, dt["w_post"], None, dt["w_pre"], None,
+                      dt["x"], h)
+    assert torch.equal(dt["x"], out["x_new"]) and torch.equal(h, out["h"])
+
+
+def test_norm_gradient_against_differences():
+    c = (6, 20, "f32", "layer", "rms", 4, "half", "all", 0.5, 2.0)
+    g, t, fm, hm = norm_inputs(*c[:8], 3)
+    desc, dt, fr, hr, out = norm_call(c, t, fm, hm)
+    dx_new, dh = normal(g, 6, 20), normal(g, 6, 20)
+    got = {n: torch.empty_like(v) for n, v in dt.items() if v is not None}
+    ws = torch.empty(K.sparse_norm_workspace_bytes(desc, 6), dtype=torch.uint8, device=DEV)
+    K.sparse_norm_backward(desc, *[dt[n] for n in ("x", "f", "gate", "w_post", "b_post", "w_pre")], out["stats"], dev(dx_new), dev(dh),
+                           *[got.get(n) for n in ("x", "f", "gate", "w_post", "b_post", "w_pre", "b_pre")], ws, f_rows=fr, h_rows=hr)
+
+    def loss(v):
+        x_new, h = norm_oracle(c, v, fm, hm)
+        return float((x_new * dx_new).sum() + (h * dh).sum())
+
+    for n in got:
+        way = normal(g, *t[n].shape)
+        step = 1e-5
+        slope = (loss({**t, n: t[n] + step * way}) - loss({**t, n: t[n] - step * way})) / (2 * step)
+        have = float((got[n].double().cpu() * way).sum())
+        assert abs(have - slope) <= 1e-5 * (1 + float((got[n].double().cpu() * way).abs().sum())), n
+
+
+def test_rows_that_the_mask_drops_are_not_looked_at():
+    """f and h hold kept rows only; what lies in x's other rows stays in its own row."""
+    c = (64, 96, "bf16", "rms", "rms", 8, "half", "half", 1.0, 1.0)
+    g, t, fm, hm = norm_inputs(*c[:8], 9)
+    _, _, _, _, clean = norm_call(c, t, fm, hm)
+    lost = (hm == 0).nonzero()[:, 0]
+    t["x"][lost] = float("nan")
+    _, _, _, _, out = norm_call(c, t, fm, hm)
+    assert torch.equal(out["h"], clean["h"])
+    assert torch.equal(out["x_new"][hm.bool().to(DEV)], clean["x_new"][hm.bool().to(DEV)])
+
+
+# ---- feed-forward block ------------------------------------------------------------------------------------------------
+
+FFNS = [  # rows, d_in, d_hidden, d_out, dtype, activation, mask, x_rows, y_rows
+    (1, 1, 1, 1, "f32", "silu", "all", 0, 0),
+    (1, 64, 128, 64, "bf16", "silu", "all", 0, 0),
+    (2, 200, 88, 72, "f16", "gelu", "all", 0, 0),
+    (5, 51, 102, 205, "bf16", "gelu_tanh", "half", 0, 0),
+    (16, 256, 520, 256, "bf16", "silu", "all", 0, 0),
+    (17, 264, 136, 8, "f16", "silu", "half", 1, 0),
+    (33, 65, 129, 63, "f32", "gelu", "half", 0, 1),
+    (64, 512, 96, 512, "bf16", "gelu", "ends", 0, 0),
+    (100, 128, 256, 128, "f32", "silu", "half", 0, 0),
+    (130, 96, 160, 224, "f16", "gelu_tanh", "block", 1, 1),
+    (257, 264, 392, 264, "bf16", "silu", "half", 0, 0),
+    (300, 320, 640, 192, "bf16", "gelu", "nothing", 0, 0),
+    (700, 136, 328, 136, "f32", "gelu_tanh", "half", 0, 0),
+    (1030, 72, 1160, 2056, "f16", "silu", "half", 0, 0),
+    (2000, 410, 300, 410, "bf16", "silu", "block", 0, 0),
+]
+
+
+def ffn_case(c, seed):
+    rows, di, dh, do, dtype, kind, mask, x_rows, y_rows = c
+    g = gen(seed)
+    m = mask_of(mask, rows, g)
+    keep = m.bool()
+    full = dict(x=normal(g, rows, di, dtype=dtype), wg=normal(g, dh, di, dtype=dtype, std=di ** -0.5),
+                wu=normal(g, dh, di, dtype=dtype, std=di ** -0.5), wd=normal(g, do, dh, dtype=dtype, std=dh ** -0.5),
+                dy=normal(g, rows, do, dtype=dtype))
+    return m, keep, full
+
+
+def ffn_call(c, m, keep, full, backward=True):
+    rows, di, dh, do, dtype, kind, mask, x_rows, y_rows = c
+    kept = int(keep.sum())
+    rs = None if mask == "all" else K.sparse_rows_plan(m.to(DEV))
+    desc = K.make_ffn_desc(di, dh, do, K.DTYPE_CODE[dtype], K.ACT_CODE[kind])
+    t = {n: dev(v, dtype) for n, v in full.items()}
+    if rs is not None:      # what dropped rows hold must not matter
+        t["x"][~keep.to(DEV)] = float("nan")
+        t["dy"][~keep.to(DEV)] = float("nan")
+    x = t["x"][keep.to(DEV)].contiguous() if x_rows else t["x"]
+    dy = t["dy"][keep.to(DEV)].contiguous() if y_rows else t["dy"]
+    y, saved = nan_like(kept if y_rows else rows, do, dtype=dtype), nan_like(3, kept, dh, dtype=dtype)
+    ws = torch.empty(K.sparse_ffn_workspace_bytes(desc, kept, True), dtype=torch.uint8, device=DEV)
+    K.sparse_ffn_run(desc, x, t["wg"], t["wu"], t["wd"], y, ws, rows=rs, x_rows=x_rows, y_rows=y_rows, saved=saved)
+    plain = nan_like(*y.shape, dtype=dtype)
+    K.sparse_ffn_run(desc, x, t["wg"], t["wu"], t["wd"], plain, ws, rows=rs, x_rows=x_rows, y_rows=y_rows)
+    assert torch.equal(plain, y)
+    if not backward:
+        return y
+    grads = [nan_like(*s.shape, dtype=dtype) for s in (x, t["wg"], t["wu"], t["wd"])]
+    K.sparse_ffn_backward(desc, x, t["wg"], t["wu"], t["wd"], saved, dy, *grads, ws, rows=rs, x_rows=x_rows, y_rows=y_rows)
+    again = [nan_like(*s.shape, dtype=dtype) for s in grads]
+    K.sparse_ffn_backward(desc, x, t["wg"], t["wu"], t["wd"], saved, dy, *again, ws, rows=rs, x_rows=x_rows, y_rows=y_rows)
+    assert all(torch.equal(p, q) for p, q in zip(grads, again))
+    only = nan_like(*x.shape, dtype=dtype)
+    K.sparse_ffn_backward(desc, x, t["wg"], t["wu"], t["wd"], saved, dy, only, None, None, None, ws, rows=rs, x_rows=x_rows, y_rows=y_rows)
+    assert torch.equal(only, grads[0])
+    return [y] + grads
+
+
+@pytest.mark.parametrize("c", FFNS, ids=lambda c: "-".join(map(str, c)))
+def test_ffn_forward_and_gradients(c):
+    rows, di, dh, do, dtype, kind, mask, x_rows, y_rows = c
+    m, keep, full = ffn_case(c, 7 * rows + dh)
+    got = ffn_call(c, m, keep, full)
+    x, dy = full["x"][keep], full["dy"][keep]
+    leaves = [v.clone().requires_grad_(True) for v in (x, full["wg"], full["wu"], full["wd"])]
+    y = O.ffn_forward(*leaves, kind)
+    want = [y.detach(), *torch.autograd.grad(y, leaves, dy)]
+    bounds = O.ffn_bounds(x, full["wg"], full["wu"], full["wd"], kind, dtype, dy)
+    for name, v, w, b in zip(("y", "dx", "dw_gate", "dw_up", "dw_down"), got, want, bounds):
+        if name in ("y", "dx") and not (y_rows if name == "y" else x_rows):
+            dropped = v[~keep.to(DEV)]
+            assert (dropped.view(torch.int32 if dtype == "f32" else torch.int16) == 0).all(), name
+            v = v[keep.to(DEV)]
+        inside(v, w, b, name)
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+def test_ffn_gradient_against_differences(kind):
+    c = (9, 12, 20, 8, "f32", kind, "half", 0, 0)
+    m, keep, full = ffn_case(c, 21)
+    got = ffn_call(c, m, keep, full)
+    g = gen(4)
+
+    def loss(v):
+        return float((O.ffn_forward(v["x"][keep], v["wg"], v["wu"], v["wd"], kind) * full["dy"][keep]).sum())
+
+    for n, have in zip(("x", "wg", "wu", "wd"), got[1:]):
+        way, step = normal(g, *full[n].shape), 1e-5
+        slope = (loss({**full, n: full[n] + step * way}) - loss({**full, n: full[n] - step * way})) / (2 * step)
+        terms = have.double().cpu() * way
+        assert abs(float(terms.sum()) - slope) <= 1e-5 * (1 + float(terms.abs().sum())), n
+
+
+def test_ffn_far_out_activations():
+    """Products of +-100: the activations saturate, nothing overflows."""
+    full = dict(x=torch.tensor([[100.0] * 8, [-100.0] * 8]).double(), wg=torch.eye(8).double(), wu=torch.ones(8, 8).double() / 8,
+                wd=torch.eye(8).double(), dy=torch.ones(2, 8).double())
+    for kind in ("silu", "gelu", "gelu_tanh"):
+        c = (2, 8, 8, 8, "f32", kind, "all", 0, 0)
+        got = ffn_call(c, torch.ones(2, dtype=torch.uint8), torch.ones(2, dtype=torch.bool), full)
+        y = got[0].double().cpu()
+        assert torch.allclose(y[0], torch.full((8,), 10000.0, dtype=torch.float64), rtol=1e-6)
+        assert y[1].abs().max() <= 1e-30 and torch.isfinite(got[1]).all()
+
+
+def test_ffn_on_another_stream_and_in_a_graph():
+    c = (96, 128, 256, 128, "bf16", "silu", "half", 0, 0)
+    m, keep, full = ffn_case(c, 2)
+    want = ffn_call(c, m, keep, full, backward=False)
+    t = {n: dev(v, "bf16") for n, v in full.items()}
+    rs = K.sparse_rows_plan(m.to(DEV))
+    desc = K.make_ffn_desc(128, 256, 128)
+    ws = torch.empty(K.sparse_ffn_workspace_bytes(desc, rs.kept), dtype=torch.uint8, device=DEV)
+    y = nan_like(96, 128, dtype="bf16")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        K.sparse_ffn_run(desc, t["x"], t["wg"], t["wu"], t["wd"], y, ws, rows=rs)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(y, want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        K.sparse_ffn_run(desc, t["x"], t["wg"], t["wu"], t["wd"], y, ws, rows=rs)
+    for _ in range(3):
+        y.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+
+
+# ---- 4-bit weights -----------------------------------------------------------------------------------------------------
+
+Q4S = [  # rows, n, k, group, dtype, zeros
+    (1, 1, 1, 32, "bf16", True), (1, 16, 128, 128, "bf16", True), (1, 100, 260, 64, "f16", True), (2, 33, 127, 32, "f16", False),
+    (5, 17, 1000, 128, "bf16", False), (16, 64, 1024, 64, "bf16", True), (17, 48, 515, 32, "bf16", True),
+    (33, 130, 640, 128, "f16", True), (64, 96, 2049, 64, "bf16", True), (65, 40, 300, 128, "f16", True), (150, 24, 96, 32, "bf16", True)]
+
+
+def q4_matrix(g, n, k, group, dtype, zeros):
+    groups = -(-k // group)
+    codes = torch.randint(0, 256, (n, -(-k // 2)), generator=g, dtype=torch.uint8)
+    scales = (torch.rand(n, groups, generator=g) * 0.02 + 0.001).to(O.TORCH[dtype])
+    z = torch.randint(0, 16, (n, groups), generator=g).to(O.TORCH[dtype]) if zeros else None
+    return codes, scales, z
+
+
+@pytest.mark.parametrize("c", Q4S, ids=lambda c: "-".join(map(str, c)))
+def test_q4_products(c):
+    rows, n, k, group, dtype, zeros = c
+    g = gen(n + k)
+    x = normal(g, rows, k, dtype=dtype)
+    codes, scales, z = q4_matrix(g, n, k, group, dtype, zeros)
+    desc = K.make_q4_desc(k, n, group, K.DTYPE_CODE[dtype])
+    held = [v.to(DEV) if v is not None else None for v in (codes, scales, z)]
+    plan = K.sparse_q4_plan(desc, *held)
+    torch.cuda.synchronize()
+    for v in held:      # not needed any more
+        if v is not None:
+            v.zero_()
+    y = nan_like(rows, n, dtype=dtype)
+    K.sparse_q4_run(plan, dev(x, dtype), y)
+    want, bound = O.q4_bound(x, codes, scales, z, k, group, dtype)
+    inside(y, want, bound, "y")
+    again = nan_like(rows, n, dtype=dtype)
+    K.sparse_q4_run(plan, dev(x, dtype), again)
+    assert torch.equal(y, again)
+
+
+@pytest.mark.parametrize("rows,n,k,group,dtype,kind", [(1, 40, 192, 64, "bf16", "silu"), (3, 33, 100, 32, "f16", "gelu"),
+                                                       (20, 80, 512, 128, "bf16", "gelu_tanh"), (70, 16, 140, 64, "f16", "silu")])
+def test_q4_gated_products(rows, n, k, group, dtype, kind):
+    g = gen(rows)
+    x = normal(g, rows, k, dtype=dtype)
+    mats = [q4_matrix(g, n, k, group, dtype, True) for _ in range(2)]
+    desc = K.make_q4_desc(k, n, group, K.DTYPE_CODE[dtype])
+    sides = [dict(codes=c.to(DEV), scales=s.to(DEV), zeros=z.to(DEV)) for c, s, z in mats]
+    plan = K.sparse_q4_plan_gated(desc, *sides, activation=K.ACT_CODE[kind])
+    y = K.sparse_q4_run(plan, dev(x, dtype), nan_like(rows, n, dtype=dtype))
+    (a, ea), (p, ep) = (O.q4_bound(x, *mt, k, group, dtype) for mt in mats)
+    ea, ep = ea - O.U[dtype] * a.abs(), ep - O.U[dtype] * p.abs()      # the two products are not rounded
+    want = O.act(a, kind) * p
+    bound = O.U[dtype] * want.abs() + 1.2 * ea * p.abs() + O.act(a, kind).abs() * ep + 1.2 * ea * ep + O.TINY[dtype]
+    bound = bound + 64 * O.E * (1 + a.abs()) * a.abs().clamp_max(8) * p.abs()
+    inside(y, want, bound, "y")
+
+
+# ---- refusals of the binding -------------------------------------------------------------------------------------------
+
+
+def test_wrong_tensors_are_refused():
+    desc = K.make_ffn_desc(64, 128, 64)
+    w, wd = torch.zeros(128, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(64, 128, dtype=torch.bfloat16, device=DEV)
+    x, y = torch.zeros(4, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(4, 64, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    K.sparse_ffn_run(desc, x, w, w, wd, y, ws)
+    for bad in (dict(x=x.float()), dict(x=x[:, :32]), dict(w_gate=w[:64]), dict(w_gate=w.t()), dict(y=y[:3]), dict(x=x.cpu()),
+                dict(y_rows=B.SC_ROWS_COMPACT, rows=K.sparse_rows_plan(torch.tensor([1, 0, 0, 1], dtype=torch.uint8, device=DEV)))):
+        a = dict(x=x, w_gate=w, w_up=w, w_down=wd, y=y, workspace=ws)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            K.sparse_ffn_run(desc, **a)
+    with pytest.raises(K.ScError):
+        K.sparse_ffn_run(desc, x, w, w, wd, y, ws[:100])
+    with pytest.raises(ValueError):
+        K.sparse_rows_plan(torch.zeros(4, device=DEV))
+    nd = K.make_norm_desc(64)
+    with pytest.raises(ValueError):
+        K.sparse_norm_run(nd, x, y[:2], None, None, None, None, None, y, y)
+    q = K.sparse_q4_plan(K.make_q4_desc(64, 32, 32), torch.zeros(32, 32, dtype=torch.uint8, device=DEV),
+                         torch.zeros(32, 2, dtype=torch.bfloat16, device=DEV))
+    with pytest.raises(ValueError):
+        K.sparse_q4_run(q, x, y)
+
+
+def test_empty_calls():
+    desc = K.make_ffn_desc(64, 128, 64)
+    e = lambda *s, dtype="bf16": torch.empty(*s, dtype=O.TORCH[dtype], device=DEV)  # noqa: E731
+    w, wd = nan_like(128, 64, dtype="bf16"), nan_like(64, 128, dtype="bf16")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    K.sparse_ffn_run(desc, e(0, 64), w, w, wd, e(0, 64), ws)
+    grads = [nan_like(128, 64, dtype="bf16"), nan_like(128, 64, dtype="bf16"), nan_like(64, 128, dtype="bf16")]
+    K.sparse_ffn_backward(desc, e(0, 64), w, w, wd, e(3, 0, 128), e(0, 64), e(0, 64), *grads, ws)
+    assert all((g == 0).all() for g in grads)
+    nd = K.make_norm_desc(64)
+    K.sparse_norm_run(nd, e(0, 64), e(0, 64), None, None, None, None, None, e(0, 64), e(0, 64))
+    dw = [nan_like(64) for _ in range(2)]
+    K.sparse_norm_backward(nd, e(0, 64), e(0, 64), None, None, None, None, e(0, 4, dtype="f32"), e(0, 64), e(0, 64), e(0, 64), e(0, 64),
+                           None, dw[0], None, dw[1], None, ws)
+    assert all((v == 0).all() for v in dw)
+    plan = K.sparse_q4_plan(K.make_q4_desc(64, 32, 32), torch.zeros(32, 32, dtype=torch.uint8, device=DEV),
+                            torch.zeros(32, 2, dtype=torch.bfloat16, device=DEV))
+    K.sparse_q4_run(plan, e(0, 64), e(0, 32))
