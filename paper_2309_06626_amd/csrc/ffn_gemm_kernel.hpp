@@ -23,6 +23,7 @@ template <int EB> struct FfnTile {
 // columns of the lane's row.
 __device__ __forceinline__ int ffn_q_order(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
 
+constexpr int kFfnList = 4096;      // rows of the contraction whose list entries lie in LDS
 static __device__ __align__(16) v4i ffn_zeros = {0, 0, 0, 0};      // what is read beyond an operand's end
 
 // 16 bytes a lane from memory into LDS at base + 16 lane.  Written out, because the compiler would let every later LDS read wait
@@ -64,92 +65,113 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   const int m0 = (band * p.group + in_band % high) * BM, n0 = (in_band / high) * COLS;
 
   // K tiles of this workgroup: every segment is a whole number of tiles, the last one padded with zeros
+  const int n_last = p.n - 1;
+  const bool q_listed = p.q_rows != nullptr;
   const int seg_tiles = (p.k + BK - 1) / BK, all_tiles = seg_tiles * p.segments;
   const int kt_lo = (int)((int64_t)all_tiles * split / p.splits), kt_hi = (int)((int64_t)all_tiles * (split + 1) / p.splits);
 
   // ---- loads ----
   // slot s of an operand's tile (16 bytes): along k, row s / 8, group s % 8; across k, row s / CPR of k, group s % CPR
-  auto column_of = [&](int qrow, int& which) -> int {          // column of the result that a row of the Q tile belongs to
-    which = GATED && qrow >= COLS ? 1 : 0;
-    return n0 + (which ? qrow - COLS : qrow);
-  };
-  auto p_row = [&](int i) -> int64_t { return p.p_rows ? p.p_rows[i] : i; };
-  auto q_row = [&](int i) -> int64_t { return p.q_rows ? p.q_rows[i] : i; };
-
-  const T* pp[JP];
-  const T* qq[JQ];
-  int p_at = 0, q_at = 0;                                      // k (along) or result row / column (across) of the lane's group
-  int p_k[JP], q_k[JQ];                                        // k of its row (across)
+  constexpr int P_CPR = P_ALONG ? 8 : BM / V, Q_CPR = Q_ALONG ? 8 : BN / V;
+  const int p_row = wave * (64 / P_CPR) + lane / P_CPR, q_row = wave * (64 / Q_CPR) + lane / Q_CPR;      // of transfer 0
+  constexpr int P_NEXT = W * (64 / P_CPR), Q_NEXT = W * (64 / Q_CPR);                                    // rows from transfer to transfer
+  // k (along) or result row / column (across) of the lane's group; the same for all its transfers, whose rows have one key
+  const int p_at = P_ALONG ? ((lane & 7) ^ L::key_along(p_row)) * V : m0 + ((lane % P_CPR) ^ L::key_across(p_row)) * V;
+  const int q_at = Q_ALONG ? ((lane & 7) ^ L::key_along(q_row)) * V : n0 + ((lane % Q_CPR) ^ L::key_across(q_row)) * V;
+  const T* pp[P_ALONG ? JP : 1];
+  const T* qq[Q_ALONG ? JQ : 1];
   if constexpr (P_ALONG) {
-    const int row = wave * 8 + (lane >> 3);
-    p_at = ((lane & 7) ^ L::key_along(row)) * V;
 #pragma unroll
     for (int j = 0; j < JP; ++j) {
-      const int i = min(m0 + row + j * W * 8, p.m - 1);
-      pp[j] = static_cast<const T*>(p.p[0]) + p_row(i) * p.ldp;
+      const int i = min(m0 + p_row + j * P_NEXT, p.m - 1);      // rows beyond the end: results that are not stored
+      pp[j] = static_cast<const T*>(p.p[0]) + (p.p_rows ? (int64_t)p.p_rows[i] : i) * p.ldp + p_at;
     }
-  } else {
-    constexpr int CPR = BM / V, RPL = 64 / CPR;
-    const int k0 = wave * RPL + lane / CPR;
-    p_at = m0 + ((lane % CPR) ^ L::key_across(k0)) * V;
-#pragma unroll
-    for (int j = 0; j < JP; ++j) p_k[j] = k0 + j * W * RPL;
   }
   if constexpr (Q_ALONG) {
-    const int row = wave * 8 + (lane >> 3);
-    q_at = ((lane & 7) ^ L::key_along(row)) * V;
 #pragma unroll
     for (int j = 0; j < JQ; ++j) {
-      int which;
-      const int c = min(column_of(row + j * W * 8, which), p.n - 1);
-      qq[j] = static_cast<const T*>(p.q[which]) + (int64_t)c * p.ldq;
+      const int r = q_row + j * Q_NEXT, up = GATED && r >= COLS;
+      const int c = min(n0 + (up ? r - COLS : r), n_last);
+      qq[j] = static_cast<const T*>(p.q[up]) + (int64_t)c * p.ldq + q_at;
     }
-  } else {
-    constexpr int CPR = BN / V, RPL = 64 / CPR;
-    const int k0 = wave * RPL + lane / CPR;
-    q_at = n0 + ((lane % CPR) ^ L::key_across(k0)) * V;
-#pragma unroll
-    for (int j = 0; j < JQ; ++j) q_k[j] = k0 + j * W * RPL;
   }
-  // the source of transfer j of K tile kt, and how many of its entries there are
+  // rows of the contraction that stand for others: a stretch of the list at a time in LDS (a look-up in memory would have to wait
+  // for the transfers before it)
+  constexpr bool LISTED = WHAT == kFfnWGrad;
+  int32_t* const s_list = reinterpret_cast<int32_t*>(smem + (ALIGNED ? 2 : 1) * STAGE);
+  const int32_t* const list = LISTED ? (p.p_rows ? p.p_rows : p.q_rows) : nullptr;
+  int list_base = 0;
+  auto stretch = [&](int kt) {      // called by all
+    list_base = kt * BK;
+    for (int i = t; i < kFfnList && list_base + i < p.k; i += NT) s_list[i] = list[list_base + i];
+  };
+  auto p_k = [&](int k) -> int64_t { return LISTED && p.p_rows ? s_list[k - list_base] : k; };
+  auto q_k = [&](int k) -> int64_t { return LISTED && q_listed ? s_list[k - list_base] : k; };
+
+  const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
+  // columns beyond the end across k: any that exist
+  const int p_in = min(p_at, p.m - V), q_in = min(q_at, p.n - V);
+  auto request = [&](int kt, int stage) {                      // whole groups: straight into LDS
+    const unsigned at_p = lds0 + stage * STAGE + wave * 1024, at_q = at_p + P_BYTES;
+    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    const T* const pb = static_cast<const T*>(p.p[P_ALONG ? seg : z]);
+    const T* const qb = static_cast<const T*>(p.q[p.segments > 1 ? seg : 0]);
+    const int64_t p_off = P_ALONG ? (seg ? pb - static_cast<const T*>(p.p[0]) : 0) + k0 : (int64_t)k0 * p.ldp;
+    auto all = [&](auto whole) {
+      constexpr bool WHOLE = decltype(whole)::value;           // no k beyond the end in this tile
+#pragma unroll
+      for (int j = 0; j < JP; ++j) {
+        const T* src;
+        bool in = true;
+        if constexpr (P_ALONG) {
+          src = pp[j] + p_off;
+          if constexpr (!WHOLE) in = k0 + p_at < p.k;
+        } else {
+          const int k = k0 + p_row + j * P_NEXT;
+          if constexpr (!WHOLE) in = k < p.k;
+          src = pb + p_k(in ? k : k0) * p.ldp + p_in;
+        }
+        ffn_dma16(WHOLE || in ? (const void*)src : (const void*)&ffn_zeros, at_p + j * NT * 16);
+      }
+#pragma unroll
+      for (int j = 0; j < JQ; ++j) {
+        const T* src;
+        bool in = true;
+        if constexpr (Q_ALONG) {
+          src = qq[j] + k0;
+          if constexpr (!WHOLE) in = k0 + q_at < p.k;
+        } else {
+          const int k = k0 + q_row + j * Q_NEXT;
+          if constexpr (!WHOLE) in = k < p.k;
+          src = qb + q_k(in ? k : k0) * p.ldq + q_in;
+        }
+        ffn_dma16(WHOLE || in ? (const void*)src : (const void*)&ffn_zeros, at_q + j * NT * 16);
+      }
+    };
+    if (k0 + BK <= p.k) all(std::true_type{});
+    else all(std::false_type{});
+  };
+  // the source of transfer j of K tile kt, and how many of its entries there are (rows of any length)
   auto p_src = [&](int kt, int j, int& have) -> const T* {
-    const int seg = kt / seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     if constexpr (P_ALONG) {
       have = min(V, p.k - (k0 + p_at));
-      const T* base = pp[j] + k0 + p_at;
-      if (p.segments > 1 && seg) base += static_cast<const T*>(p.p[1]) - static_cast<const T*>(p.p[0]);
-      return base;
+      return pp[j] + (seg ? static_cast<const T*>(p.p[1]) - static_cast<const T*>(p.p[0]) : 0) + k0;
     } else {
-      const int k = k0 + p_k[j];
+      const int k = k0 + p_row + j * P_NEXT;
       have = k < p.k ? min(V, p.m - p_at) : 0;
-      return static_cast<const T*>(p.p[z]) + (have > 0 ? p_row(k) * p.ldp + p_at : 0);
+      return static_cast<const T*>(p.p[z]) + (have > 0 ? p_k(k) * p.ldp + p_at : 0);
     }
   };
   auto q_src = [&](int kt, int j, int& have) -> const T* {
-    const int seg = kt / seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     if constexpr (Q_ALONG) {
       have = min(V, p.k - (k0 + q_at));
-      return qq[j] + k0 + q_at;
+      return qq[j] + k0;
     } else {
-      const int k = k0 + q_k[j];
+      const int k = k0 + q_row + j * Q_NEXT;
       have = k < p.k ? min(V, p.n - q_at) : 0;
-      return static_cast<const T*>(p.q[p.segments > 1 ? seg : 0]) + (have > 0 ? q_row(k) * p.ldq + q_at : 0);
-    }
-  };
-  const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
-  auto request = [&](int kt, int stage) {                      // whole groups: straight into LDS
-    const unsigned at_p = lds0 + stage * STAGE + wave * 1024, at_q = at_p + P_BYTES;
-#pragma unroll
-    for (int j = 0; j < JP; ++j) {
-      int have;
-      const T* s = p_src(kt, j, have);
-      ffn_dma16(have > 0 ? (const void*)s : (const void*)&ffn_zeros, at_p + j * NT * 16);
-    }
-#pragma unroll
-    for (int j = 0; j < JQ; ++j) {
-      int have;
-      const T* s = q_src(kt, j, have);
-      ffn_dma16(have > 0 ? (const void*)s : (const void*)&ffn_zeros, at_q + j * NT * 16);
+      return static_cast<const T*>(p.q[p.segments > 1 ? seg : 0]) + (have > 0 ? q_k(k) * p.ldq + q_at : 0);
     }
   };
   v4i held[JP + JQ];                                           // rows of any length: through registers
@@ -244,24 +266,46 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     }
   };
 
+  constexpr int STRETCH = kFfnList / BK;                       // K tiles of a stretch of the list
+  auto renew_list = [&](int kt) {                              // before anything of K tile kt is asked for
+    if constexpr (LISTED) {
+      if (list && (kt - kt_lo) % STRETCH == 0) {
+        __syncthreads();
+        stretch(kt);
+        __syncthreads();
+      }
+    }
+  };
   if constexpr (ALIGNED) {
-    if (kt_lo < kt_hi) request(kt_lo, 0);
+    if (kt_lo < kt_hi) {
+      renew_list(kt_lo);
+      request(kt_lo, 0);
+    }
     for (int kt = kt_lo; kt < kt_hi; ++kt) {
       const int stage = (kt - kt_lo) & 1;
       // this tile has landed, for every wavefront, and all have left the one before, whose place the next takes
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (kt + 1 < kt_hi) request(kt + 1, stage ^ 1);
+      if (kt + 1 < kt_hi) {
+        renew_list(kt + 1);
+        request(kt + 1, stage ^ 1);
+      }
       contract(stage);
     }
   } else {
-    if (kt_lo < kt_hi) hold(kt_lo);
+    if (kt_lo < kt_hi) {
+      renew_list(kt_lo);
+      hold(kt_lo);
+    }
     for (int kt = kt_lo; kt < kt_hi; ++kt) {
       __syncthreads();
       put();
       __syncthreads();
-      if (kt + 1 < kt_hi) hold(kt + 1);
+      if (kt + 1 < kt_hi) {
+        renew_list(kt + 1);
+        hold(kt + 1);
+      }
       contract(0);
     }
   }
@@ -349,8 +393,9 @@ hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
   g.m_tiles = (g.m + BM - 1) / BM;
   g.n_tiles = (g.n + cols - 1) / cols;
   g.group = 8;
-  constexpr int lds = (BM + BN) * 128 * (ALIGNED ? 2 : 1);
-  if constexpr (lds > 65536) {
+  const bool listed = WHAT == kFfnWGrad && (g.p_rows || g.q_rows);
+  const int lds = (BM + BN) * 128 * (ALIGNED ? 2 : 1) + (listed ? kFfnList * 4 : 0);
+  if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
