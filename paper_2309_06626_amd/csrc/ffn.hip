@@ -39,6 +39,17 @@ static hipError_t launch(int dtype, FfnProduct what, const FfnGemm& g, int tile,
   }
 }
 
+constexpr int64_t kFewRows = 64;
+
+static hipError_t launch_forward(int dtype, FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
+  if (g.m > kFewRows) return launch(dtype, what, g, tile, aligned, s);
+  switch (dtype) {
+    case SC_BF16: return ffn_few_bf16(what == kFfnUp, g, aligned, s);
+    case SC_F16: return ffn_few_f16(what == kFfnUp, g, aligned, s);
+    default: return ffn_few_f32(what == kFfnUp, g, aligned, s);
+  }
+}
+
 static bool whole_groups(const sc_ffn_desc& d) {
   const int v = 16 / elem_bytes(d.dtype);
   return d.d_in % v == 0 && d.d_hidden % v == 0 && d.d_out % v == 0;
@@ -188,7 +199,7 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
   up.ldc = desc->d_hidden;
   up.saved = saved_dev;
   up.activation = desc->activation;
-  e = sc::launch(desc->dtype, sc::kFfnUp, up, sc::pick_tile(kept, 2 * (int64_t)desc->d_hidden, 1), aligned, s);
+  e = sc::launch_forward(desc->dtype, sc::kFfnUp, up, sc::pick_tile(kept, 2 * (int64_t)desc->d_hidden, 1), aligned, s);
   if (e != hipSuccess) return sc::failed(e);
 
   sc::FfnGemm down = sc::gemm_of(kept, desc->d_out, desc->d_hidden);
@@ -198,7 +209,7 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
   down.c[0] = y_dev;
   down.ldc = desc->d_out;
   down.c_rows = sc::map_of(rows, y_rows);
-  e = sc::launch(desc->dtype, sc::kFfnDown, down, sc::pick_tile(kept, desc->d_out, 1), aligned, s);
+  e = sc::launch_forward(desc->dtype, sc::kFfnDown, down, sc::pick_tile(kept, desc->d_out, 1), aligned, s);
   return e == hipSuccess ? SC_OK : sc::failed(e);
 }
 

@@ -395,10 +395,9 @@ hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
   g.group = 8;
   const bool listed = WHAT == kFfnWGrad && (g.p_rows || g.q_rows);
   const int lds = (BM + BN) * 128 * (ALIGNED ? 2 : 1) + (listed ? kFfnList * 4 : 0);
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-  }
+  static std::atomic<uint64_t> told{0};
+  const hipError_t e = ffn_allow_lds(reinterpret_cast<const void*>(kernel), (BM + BN) * 128 * (ALIGNED ? 2 : 1) + kFfnList * 4, told);
+  if (e != hipSuccess) return e;
   const int64_t total = (int64_t)g.m_tiles * g.n_tiles * g.batch * g.splits;
   kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WAVES_M * WAVES_N), lds, s>>>(g);
   return hipGetLastError();

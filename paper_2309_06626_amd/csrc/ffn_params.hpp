@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace sc {
 
 // C[i][j] = sum_k P[i][k] Q[j][k].  An operand is "along k" (its rows are those of the result, k runs within them) or "across k"
@@ -40,5 +42,23 @@ struct FfnGemm {
 hipError_t ffn_launch_bf16(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
 hipError_t ffn_launch_f16(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
 hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
+
+// kFfnUp (gated) and kFfnDown for a few rows
+hipError_t ffn_few_bf16(bool gated, const FfnGemm& g, bool whole, hipStream_t s);
+hipError_t ffn_few_f16(bool gated, const FfnGemm& g, bool whole, hipStream_t s);
+hipError_t ffn_few_f32(bool gated, const FfnGemm& g, bool whole, hipStream_t s);
+
+// Kernels with more than 64 KB of LDS have to say so, once on each device.
+inline hipError_t ffn_allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& told) {
+  if (bytes <= 65536) return hipSuccess;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (told.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) told.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 }  // namespace sc
