@@ -12,7 +12,9 @@ namespace sc {
 // A 16-byte group lies at its index XOR a key of its row, so that the lanes that read together touch every bank once.
 template <int EB> struct FfnTile {
   static constexpr int BK = 128 / EB, V = 16 / EB, STEPS = 4, KSTEP = BK / STEPS;
-  static __device__ __forceinline__ int key_along(int row) { return (row & 3) | ((((row >> 2) ^ (row >> 4)) & 1) << 2); }
+  // sixteen lanes read at once: two rows of one group side by side in the 256 bytes of the banks, eight such pairs; the rows are
+  // consecutive (P) or those of ffn_q_order, 0 .. 7 and 16 .. 23
+  static __device__ __forceinline__ int key_along(int row) { return ((row >> 1) & 3) | ((((row >> 3) ^ (row >> 4)) & 1) << 2); }
   static __device__ __forceinline__ int key_across(int k) {
     if constexpr (EB == 2) return ((k & 3) << 2) | ((k >> 1) & 1);
     return ((k >> 2) & 1) << 3;
@@ -30,6 +32,13 @@ static __device__ __align__(16) v4i ffn_zeros = {0, 0, 0, 0};      // what is re
 // for all transfers in flight; their arrival is waited for at the barriers below.
 __device__ __forceinline__ void ffn_dma16(const void* src, unsigned lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src));
+}
+
+template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    ffn_for<I + 1, N>(f);
+  }
 }
 
 template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
@@ -78,13 +87,20 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   // k (along) or result row / column (across) of the lane's group; the same for all its transfers, whose rows have one key
   const int p_at = P_ALONG ? ((lane & 7) ^ L::key_along(p_row)) * V : m0 + ((lane % P_CPR) ^ L::key_across(p_row)) * V;
   const int q_at = Q_ALONG ? ((lane & 7) ^ L::key_along(q_row)) * V : n0 + ((lane % Q_CPR) ^ L::key_across(q_row)) * V;
-  const T* pp[P_ALONG ? JP : 1];
-  const T* qq[Q_ALONG ? JQ : 1];
+  int64_t pp[P_ALONG ? JP : 1], qq_at[Q_ALONG ? JQ : 1];      // from the start of the operand
+  const T* qq[Q_ALONG && GATED ? JQ : 1];                      // two matrices: addresses
+  // held in scalar registers: a load of a kernel argument between the products would have to wait for the operands on their way
+  const T *p0 = static_cast<const T*>(p.p[P_ALONG ? 0 : z]), *p1 = static_cast<const T*>(p.p[p.segments > 1]);
+  const T *q0 = static_cast<const T*>(p.q[0]), *q1 = static_cast<const T*>(p.q[p.segments > 1]);
+  int64_t ldp = p.ldp, ldq = p.ldq;
+  int k_end = p.k;
+  const void* zeros = &ffn_zeros;
+  asm volatile("" : "+s"(p0), "+s"(p1), "+s"(q0), "+s"(q1), "+s"(ldp), "+s"(ldq), "+s"(k_end), "+s"(zeros));
   if constexpr (P_ALONG) {
 #pragma unroll
     for (int j = 0; j < JP; ++j) {
       const int i = min(m0 + p_row + j * P_NEXT, p.m - 1);      // rows beyond the end: results that are not stored
-      pp[j] = static_cast<const T*>(p.p[0]) + (p.p_rows ? (int64_t)p.p_rows[i] : i) * p.ldp + p_at;
+      pp[j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_at;
     }
   }
   if constexpr (Q_ALONG) {
@@ -92,7 +108,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     for (int j = 0; j < JQ; ++j) {
       const int r = q_row + j * Q_NEXT, up = GATED && r >= COLS;
       const int c = min(n0 + (up ? r - COLS : r), n_last);
-      qq[j] = static_cast<const T*>(p.q[up]) + (int64_t)c * p.ldq + q_at;
+      qq_at[j] = c * ldq + q_at;
+      if constexpr (GATED) qq[j] = static_cast<const T*>(p.q[up]) + qq_at[j];
     }
   }
   // rows of the contraction that stand for others: a stretch of the list at a time in LDS (a look-up in memory would have to wait
@@ -111,67 +128,76 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
   // columns beyond the end across k: any that exist
   const int p_in = min(p_at, p.m - V), q_in = min(q_at, p.n - V);
-  auto request = [&](int kt, int stage) {                      // whole groups: straight into LDS
-    const unsigned at_p = lds0 + stage * STAGE + wave * 1024, at_q = at_p + P_BYTES;
+  int32_t listed_row[P_ALONG ? JQ : (JP > JQ ? JP : JQ)];      // of the tile asked for next
+  auto look_up = [&](int kt) {
+    if constexpr (LISTED) {
+      if (!list) return;
+      const int first = kt * BK + (q_listed ? q_row : p_row), next = q_listed ? Q_NEXT : P_NEXT;
+#pragma unroll
+      for (int j = 0; j < (JP > JQ ? JP : JQ); ++j) listed_row[j] = s_list[min(first + j * next, p.k - 1) - list_base];
+    }
+  };
+  // What the transfers of a K tile share, worked out once: whole groups go straight into LDS, zeros beyond the end of k.
+  struct Ask { const T *p, *q; int k0; unsigned to; };
+  auto prepare = [&](int kt, int stage) -> Ask {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
-    const T* const pb = static_cast<const T*>(p.p[P_ALONG ? seg : z]);
-    const T* const qb = static_cast<const T*>(p.q[p.segments > 1 ? seg : 0]);
-    const int64_t p_off = P_ALONG ? (seg ? pb - static_cast<const T*>(p.p[0]) : 0) + k0 : (int64_t)k0 * p.ldp;
-    auto all = [&](auto whole) {
-      constexpr bool WHOLE = decltype(whole)::value;           // no k beyond the end in this tile
-#pragma unroll
-      for (int j = 0; j < JP; ++j) {
-        const T* src;
-        bool in = true;
-        if constexpr (P_ALONG) {
-          src = pp[j] + p_off;
-          if constexpr (!WHOLE) in = k0 + p_at < p.k;
-        } else {
-          const int k = k0 + p_row + j * P_NEXT;
-          if constexpr (!WHOLE) in = k < p.k;
-          src = pb + p_k(in ? k : k0) * p.ldp + p_in;
-        }
-        ffn_dma16(WHOLE || in ? (const void*)src : (const void*)&ffn_zeros, at_p + j * NT * 16);
+    Ask a;
+    a.k0 = k0;
+    a.to = lds0 + stage * STAGE + wave * 1024;
+    a.p = P_ALONG ? (seg ? p1 : p0) + k0 : p0;
+    a.q = (seg ? q1 : q0) + (Q_ALONG ? k0 : 0);
+    return a;
+  };
+  auto request_one = [&](const Ask& a, auto which) {
+    constexpr int j = decltype(which)::value;
+    const T* src;
+    bool in;
+    if constexpr (j < JP) {
+      if constexpr (P_ALONG) {
+        src = a.p + pp[j];
+        in = a.k0 + p_at < k_end;
+      } else {
+        const int k = a.k0 + p_row + j * P_NEXT;
+        in = k < k_end;
+        src = a.p + p_in + (LISTED && list && !q_listed ? listed_row[j] : in ? k : 0) * ldp;
       }
-#pragma unroll
-      for (int j = 0; j < JQ; ++j) {
-        const T* src;
-        bool in = true;
-        if constexpr (Q_ALONG) {
-          src = qq[j] + k0;
-          if constexpr (!WHOLE) in = k0 + q_at < p.k;
-        } else {
-          const int k = k0 + q_row + j * Q_NEXT;
-          if constexpr (!WHOLE) in = k < p.k;
-          src = qb + q_k(in ? k : k0) * p.ldq + q_in;
-        }
-        ffn_dma16(WHOLE || in ? (const void*)src : (const void*)&ffn_zeros, at_q + j * NT * 16);
+      ffn_dma16(in ? (const void*)src : zeros, a.to + j * NT * 16);
+    } else {
+      constexpr int i = j - JP;
+      if constexpr (Q_ALONG) {
+        if constexpr (GATED) src = qq[i] + a.k0;
+        else src = a.q + qq_at[i];
+        in = a.k0 + q_at < k_end;
+      } else {
+        const int k = a.k0 + q_row + i * Q_NEXT;
+        in = k < k_end;
+        src = a.q + q_in + (LISTED && q_listed ? listed_row[i] : in ? k : 0) * ldq;
       }
-    };
-    if (k0 + BK <= p.k) all(std::true_type{});
-    else all(std::false_type{});
+      ffn_dma16(in ? (const void*)src : zeros, a.to + P_BYTES + i * NT * 16);
+    }
   };
   // the source of transfer j of K tile kt, and how many of its entries there are (rows of any length)
   auto p_src = [&](int kt, int j, int& have) -> const T* {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     if constexpr (P_ALONG) {
       have = min(V, p.k - (k0 + p_at));
-      return pp[j] + (seg ? static_cast<const T*>(p.p[1]) - static_cast<const T*>(p.p[0]) : 0) + k0;
+      return (seg ? p1 : p0) + pp[j] + k0;
     } else {
       const int k = k0 + p_row + j * P_NEXT;
       have = k < p.k ? min(V, p.m - p_at) : 0;
-      return static_cast<const T*>(p.p[z]) + (have > 0 ? p_k(k) * p.ldp + p_at : 0);
+      return p0 + (have > 0 ? p_k(k) * ldp + p_at : 0);
     }
   };
   auto q_src = [&](int kt, int j, int& have) -> const T* {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     if constexpr (Q_ALONG) {
       have = min(V, p.k - (k0 + q_at));
-      return qq[j] + k0;
+      if constexpr (GATED) return qq[j] + k0;
+      else return q0 + qq_at[j] + k0;
     } else {
       const int k = k0 + q_row + j * Q_NEXT;
       have = k < p.k ? min(V, p.n - q_at) : 0;
-      return static_cast<const T*>(p.q[p.segments > 1 ? seg : 0]) + (have > 0 ? q_k(k) * p.ldq + q_at : 0);
+      return (seg ? q1 : q0) + (have > 0 ? q_k(k) * ldq + q_at : 0);
     }
   };
   v4i held[JP + JQ];                                           // rows of any length: through registers
@@ -245,29 +271,31 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
 
-  auto contract = [&](int stage) {
+  struct Step { v4i p[MI], q[NI]; };                           // operands of KSTEP entries of k
+  auto read_step = [&](int stage, int ks, Step& f) {
     const unsigned char* tp = smem + stage * STAGE;
     const unsigned char* tq = tp + P_BYTES;
 #pragma unroll
-    for (int ks = 0; ks < L::STEPS; ++ks) {
-      v4i pf[MI], qf[NI];
+    for (int mi = 0; mi < MI; ++mi)
+      f.p[mi] = fragment(std::bool_constant<P_ALONG>{}, std::false_type{}, tp, std::integral_constant<int, BM>{}, (wm * MI + mi) * 32, ks);
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi)
-        pf[mi] = fragment(std::bool_constant<P_ALONG>{}, std::false_type{}, tp, std::integral_constant<int, BM>{}, (wm * MI + mi) * 32, ks);
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni) {
-        const int r0 = GATED ? (ni < HALF ? (wn * HALF + ni) * 32 : COLS + (wn * HALF + ni - HALF) * 32) : (wn * NI + ni) * 32;
-        qf[ni] = fragment(std::bool_constant<Q_ALONG>{}, std::true_type{}, tq, std::integral_constant<int, BN>{}, r0, ks);
-      }
-#pragma unroll
-      for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-        for (int ni = 0; ni < NI; ++ni) E::mma(acc[mi][ni], qf[ni], pf[mi]);
+    for (int ni = 0; ni < NI; ++ni) {
+      const int r0 = GATED ? (ni < HALF ? (wn * HALF + ni) * 32 : COLS + (wn * HALF + ni - HALF) * 32) : (wn * NI + ni) * 32;
+      f.q[ni] = fragment(std::bool_constant<Q_ALONG>{}, std::true_type{}, tq, std::integral_constant<int, BN>{}, r0, ks);
     }
   };
+  // the products of a step; job(i) behind the i-th
+  auto multiply = [&](const Step& f, auto&& job) {
+    ffn_for<0, MI * NI>([&](auto i) {
+      constexpr int I = decltype(i)::value;
+      E::mma(acc[I / NI][I % NI], f.q[I % NI], f.p[I / NI]);
+      job(i);
+    });
+  };
+  auto no_job = [](auto) {};
 
   constexpr int STRETCH = kFfnList / BK;                       // K tiles of a stretch of the list
-  auto renew_list = [&](int kt) {                              // before anything of K tile kt is asked for
+  auto renew_list = [&](int kt) {                              // called by all, before anything of K tile kt is asked for
     if constexpr (LISTED) {
       if (list && (kt - kt_lo) % STRETCH == 0) {
         __syncthreads();
@@ -277,22 +305,61 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     }
   };
   if constexpr (ALIGNED) {
-    if (kt_lo < kt_hi) {
-      renew_list(kt_lo);
-      request(kt_lo, 0);
+    // Two tiles in LDS.  A tile has four steps, whose operands are read one step ahead, the first step's under the products of the last
+    // one of the tile before: by then all wavefronts have met, the tile has landed, and the one before is in registers, so that its
+    // place takes the tile after next.  Its transfers are asked for one at a time between products, since a wavefront that asks for
+    // several waits while the address unit takes them.
+    constexpr int JOBS = JP + JQ, EACH = (JOBS + MI * NI - 1) / (MI * NI);      // transfers behind a product
+    auto ask = [&](int kt, int stage) {
+      renew_list(kt);
+      look_up(kt);
+      const Ask a = prepare(kt, stage);
+      ffn_for<0, JOBS>([&](auto j) { request_one(a, j); });
+    };
+    if (kt_lo < kt_hi) ask(kt_lo, 0);
+    if (kt_lo + 1 < kt_hi) {
+      ask(kt_lo + 1, 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(JOBS) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    Step f0, f1;
+    if (kt_lo < kt_hi) read_step(0, 0, f0);
     for (int kt = kt_lo; kt < kt_hi; ++kt) {
       const int stage = (kt - kt_lo) & 1;
-      // this tile has landed, for every wavefront, and all have left the one before, whose place the next takes
+      read_step(stage, 1, f1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(f0, no_job);
+      __builtin_amdgcn_sched_barrier(0);
+      read_step(stage, 2, f0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(f1, no_job);
+      __builtin_amdgcn_sched_barrier(0);
+      read_step(stage, 3, f1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(f0, no_job);
+      __builtin_amdgcn_sched_barrier(0);
+      // the next tile has landed, and this one has been read, for every wavefront
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (kt + 1 < kt_hi) {
-        renew_list(kt + 1);
-        request(kt + 1, stage ^ 1);
-      }
-      contract(stage);
+      // (behind the last tile but one, the last again, which nobody reads: a branch here would cost registers)
+      const int ahead = min(kt + 2, kt_hi - 1);
+      if (kt + 2 < kt_hi) renew_list(ahead);
+      look_up(ahead);
+      const Ask a = prepare(ahead, stage);
+      read_step(stage ^ 1, 0, f0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(f1, [&](auto i) {
+        constexpr int I = decltype(i)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        ffn_for<I * EACH, (I + 1) * EACH < JOBS ? (I + 1) * EACH : JOBS>([&](auto j) { request_one(a, j); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may still be on its way into LDS when the workgroup ends
   } else {
     if (kt_lo < kt_hi) {
       renew_list(kt_lo);
@@ -306,7 +373,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
         renew_list(kt + 1);
         hold(kt + 1);
       }
-      contract(0);
+#pragma unroll
+      for (int ks = 0; ks < L::STEPS; ++ks) {
+        Step f;
+        read_step(0, ks, f);
+        multiply(f, no_job);
+      }
     }
   }
 
