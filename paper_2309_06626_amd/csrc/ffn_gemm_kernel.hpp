@@ -12,11 +12,12 @@ namespace sc {
 // A 16-byte group lies at its index XOR a key of its row, so that the lanes that read together touch every bank once.
 template <int EB> struct FfnTile {
   static constexpr int BK = 128 / EB, V = 16 / EB, STEPS = 4, KSTEP = BK / STEPS;
-  // sixteen lanes read at once: two rows of one group side by side in the 256 bytes of the banks, eight such pairs; the rows are
-  // consecutive (P) or those of ffn_q_order, 0 .. 7 and 16 .. 23
-  static __device__ __forceinline__ int key_along(int row) { return ((row >> 1) & 3) | ((((row >> 3) ^ (row >> 4)) & 1) << 2); }
-  static __device__ __forceinline__ int key_across(int k) {
-    if constexpr (EB == 2) return ((k & 3) << 2) | ((k >> 1) & 1);
+  // (row >> 1) & 7: a 16-byte read serves lanes 0-3, 12-15, 20-23 and 24-27 of a wavefront together (and their like); they then touch
+  // every bank once, for consecutive rows (P) as for those of ffn_q_order (Q): 4.0 cycles a read, 6.7 with row & 7, 24 without a key
+  static __device__ __forceinline__ int key_along(int row) { return (row >> 1) & 7; }
+  // GROUPS 16-byte groups a row
+  template <int GROUPS> static __device__ __forceinline__ int key_across(int k) {
+    if constexpr (EB == 2) return GROUPS >= 16 ? ((k & 3) << 2) | ((k >> 1) & 1) : ((k >> 1) & 1) << 2;
     return ((k >> 2) & 1) << 3;
   }
 };
@@ -49,14 +50,21 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   using L = FfnTile<EB>;
   constexpr int V = L::V, BK = L::BK;
   constexpr int W = WAVES_M * WAVES_N, NT = 64 * W;
-  constexpr int MI = BM / WAVES_M / 32, NI = BN / WAVES_N / 32;
-  constexpr int JP = BM * 8 / NT, JQ = BN * 8 / NT;            // transfers a lane and K tile
-  constexpr int P_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-  constexpr bool GATED = WHAT == kFfnUp;
-  constexpr int HALF = GATED ? NI / 2 : NI;                    // blocks of columns that a wavefront leaves
-  constexpr int COLS = GATED ? BN / 2 : BN;                    // result columns of a tile
+  // a tile is two halves of P's rows by two halves of Q's; a wavefront has MB x NB blocks of 32 x 32 in each quadrant
+  constexpr int PM = BM / 2, PN = BN / 2;
+  constexpr int MB = PM / WAVES_M / 32, NB = PN / WAVES_N / 32;
+  constexpr int JP = PM * 8 / NT, JQ = PN * 8 / NT;            // transfers a lane and half tile
+  constexpr int P_PIECE = PM * 128, Q_PIECE = PN * 128, STAGE = 2 * (P_PIECE + Q_PIECE);
+  // half h of stage s in LDS, the halves of an operand within 64 KB of each other: one address a lane, the rest is in the instructions
+  auto at_p = [](int h, int s) constexpr { return (2 * h + s) * P_PIECE; };
+  auto at_q = [](int h, int s) constexpr { return 4 * P_PIECE + (2 * h + s) * Q_PIECE; };
+  constexpr bool GATED = WHAT == kFfnUp;                       // the halves of Q: gate and up weights of the same columns
+  constexpr int COLS = GATED ? PN : BN;                        // result columns of a tile
+  static_assert(JP == JQ && JP * 6 <= 63, "the counts of transfers below");
   extern __shared__ __align__(16) unsigned char smem[];
 
+  constexpr std::integral_constant<int, 0> c0{};
+  constexpr std::integral_constant<int, 1> c1{};
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave / WAVES_N, wn = wave % WAVES_N;
   const int l32 = lane & 31, h = lane >> 5;
@@ -80,42 +88,47 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   const int kt_lo = (int)((int64_t)all_tiles * split / p.splits), kt_hi = (int)((int64_t)all_tiles * (split + 1) / p.splits);
 
   // ---- loads ----
-  // slot s of an operand's tile (16 bytes): along k, row s / 8, group s % 8; across k, row s / CPR of k, group s % CPR
-  constexpr int P_CPR = P_ALONG ? 8 : BM / V, Q_CPR = Q_ALONG ? 8 : BN / V;
+  // slot s of a half of an operand's tile (16 bytes): along k, row s / 8, group s % 8; across k, row s / CPR of k, group s % CPR
+  constexpr int P_CPR = P_ALONG ? 8 : PM / V, Q_CPR = Q_ALONG ? 8 : PN / V;
   const int p_row = wave * (64 / P_CPR) + lane / P_CPR, q_row = wave * (64 / Q_CPR) + lane / Q_CPR;      // of transfer 0
   constexpr int P_NEXT = W * (64 / P_CPR), Q_NEXT = W * (64 / Q_CPR);                                    // rows from transfer to transfer
-  // k (along) or result row / column (across) of the lane's group; the same for all its transfers, whose rows have one key
-  const int p_at = P_ALONG ? ((lane & 7) ^ L::key_along(p_row)) * V : m0 + ((lane % P_CPR) ^ L::key_across(p_row)) * V;
-  const int q_at = Q_ALONG ? ((lane & 7) ^ L::key_along(q_row)) * V : n0 + ((lane % Q_CPR) ^ L::key_across(q_row)) * V;
-  int64_t pp[P_ALONG ? JP : 1], qq_at[Q_ALONG ? JQ : 1];      // from the start of the operand
-  const T* qq[Q_ALONG && GATED ? JQ : 1];                      // two matrices: addresses
   // held in scalar registers: a load of a kernel argument between the products would have to wait for the operands on their way
   const T *p0 = static_cast<const T*>(p.p[P_ALONG ? 0 : z]), *p1 = static_cast<const T*>(p.p[p.segments > 1]);
-  const T *q0 = static_cast<const T*>(p.q[0]), *q1 = static_cast<const T*>(p.q[p.segments > 1]);
+  const T *q0 = static_cast<const T*>(p.q[0]), *q1 = static_cast<const T*>(p.q[p.segments > 1 || GATED]);
   int64_t ldp = p.ldp, ldq = p.ldq;
   int k_end = p.k;
   const void* zeros = &ffn_zeros;
   asm volatile("" : "+s"(p0), "+s"(p1), "+s"(q0), "+s"(q1), "+s"(ldp), "+s"(ldq), "+s"(k_end), "+s"(zeros));
-  if constexpr (P_ALONG) {
+  // along: k of the lane's group, and its rows from the start of the operand; rows beyond the end: results that are not stored.
+  // across: result row / column of the group in either half (beyond the end: any that exists)
+  int p_at[2], q_at[2];
+  int64_t p_off[2][P_ALONG ? JP : 1], q_off[2][Q_ALONG ? JQ : 1];
 #pragma unroll
-    for (int j = 0; j < JP; ++j) {
-      const int i = min(m0 + p_row + j * P_NEXT, p.m - 1);      // rows beyond the end: results that are not stored
-      pp[j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_at;
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (P_ALONG) {
+      p_at[h] = ((lane & 7) ^ L::key_along(p_row)) * V;
+#pragma unroll
+      for (int j = 0; j < JP; ++j) {
+        const int i = min(m0 + h * PM + p_row + j * P_NEXT, p.m - 1);
+        p_off[h][j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_at[h];
+      }
+    } else {
+      p_at[h] = m0 + h * PM + ((lane % P_CPR) ^ L::template key_across<P_CPR>(p_row)) * V;
+      if constexpr (ALIGNED) p_at[h] = min(p_at[h], p.m - V);
     }
-  }
-  if constexpr (Q_ALONG) {
+    if constexpr (Q_ALONG) {
+      q_at[h] = ((lane & 7) ^ L::key_along(q_row)) * V;
 #pragma unroll
-    for (int j = 0; j < JQ; ++j) {
-      const int r = q_row + j * Q_NEXT, up = GATED && r >= COLS;
-      const int c = min(n0 + (up ? r - COLS : r), n_last);
-      qq_at[j] = c * ldq + q_at;
-      if constexpr (GATED) qq[j] = static_cast<const T*>(p.q[up]) + qq_at[j];
+      for (int j = 0; j < JQ; ++j) q_off[h][j] = min(n0 + (GATED ? 0 : h * PN) + q_row + j * Q_NEXT, n_last) * ldq + q_at[h];
+    } else {
+      q_at[h] = n0 + h * PN + ((lane % Q_CPR) ^ L::template key_across<Q_CPR>(q_row)) * V;
+      if constexpr (ALIGNED) q_at[h] = min(q_at[h], p.n - V);
     }
   }
   // rows of the contraction that stand for others: a stretch of the list at a time in LDS (a look-up in memory would have to wait
   // for the transfers before it)
   constexpr bool LISTED = WHAT == kFfnWGrad;
-  int32_t* const s_list = reinterpret_cast<int32_t*>(smem + (ALIGNED ? 2 : 1) * STAGE);
+  int32_t* const s_list = reinterpret_cast<int32_t*>(smem + 2 * STAGE);
   const int32_t* const list = LISTED ? (p.p_rows ? p.p_rows : p.q_rows) : nullptr;
   int list_base = 0;
   auto stretch = [&](int kt) {      // called by all
@@ -126,81 +139,81 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   auto q_k = [&](int k) -> int64_t { return LISTED && q_listed ? s_list[k - list_base] : k; };
 
   const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
-  // columns beyond the end across k: any that exist
-  const int p_in = min(p_at, p.m - V), q_in = min(q_at, p.n - V);
-  int32_t listed_row[P_ALONG ? JQ : (JP > JQ ? JP : JQ)];      // of the tile asked for next
+  int listed_row[JP];                                          // of the tile asked for next; the halves share them
   auto look_up = [&](int kt) {
     if constexpr (LISTED) {
       if (!list) return;
       const int first = kt * BK + (q_listed ? q_row : p_row), next = q_listed ? Q_NEXT : P_NEXT;
 #pragma unroll
-      for (int j = 0; j < (JP > JQ ? JP : JQ); ++j) listed_row[j] = s_list[min(first + j * next, p.k - 1) - list_base];
+      for (int j = 0; j < JP; ++j) listed_row[j] = s_list[min(first + j * next, p.k - 1) - list_base];
     }
   };
   // What the transfers of a K tile share, worked out once: whole groups go straight into LDS, zeros beyond the end of k.
-  struct Ask { const T *p, *q; int k0; unsigned to; };
-  auto prepare = [&](int kt, int stage) -> Ask {
+  struct Ask { const T *p, *q[2]; int k0; };
+  auto prepare = [&](int kt) -> Ask {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     Ask a;
     a.k0 = k0;
-    a.to = lds0 + stage * STAGE + wave * 1024;
-    a.p = P_ALONG ? (seg ? p1 : p0) + k0 : p0;
-    a.q = (seg ? q1 : q0) + (Q_ALONG ? k0 : 0);
+    a.p = (seg ? p1 : p0) + (P_ALONG ? k0 : 0);
+    a.q[0] = (!GATED && seg ? q1 : q0) + (Q_ALONG ? k0 : 0);
+    a.q[1] = GATED ? q1 + k0 : a.q[0];
     return a;
   };
-  auto request_one = [&](const Ask& a, auto which) {
-    constexpr int j = decltype(which)::value;
+  const unsigned to = lds0 + wave * 1024;
+  auto request_p = [&](const Ask& a, auto half, auto stage, auto which) {
+    constexpr int h = decltype(half)::value, j = decltype(which)::value;
     const T* src;
     bool in;
-    if constexpr (j < JP) {
-      if constexpr (P_ALONG) {
-        src = a.p + pp[j];
-        in = a.k0 + p_at < k_end;
-      } else {
-        const int k = a.k0 + p_row + j * P_NEXT;
-        in = k < k_end;
-        src = a.p + p_in + (LISTED && list && !q_listed ? listed_row[j] : in ? k : 0) * ldp;
-      }
-      ffn_dma16(in ? (const void*)src : zeros, a.to + j * NT * 16);
-    } else {
-      constexpr int i = j - JP;
-      if constexpr (Q_ALONG) {
-        if constexpr (GATED) src = qq[i] + a.k0;
-        else src = a.q + qq_at[i];
-        in = a.k0 + q_at < k_end;
-      } else {
-        const int k = a.k0 + q_row + i * Q_NEXT;
-        in = k < k_end;
-        src = a.q + q_in + (LISTED && q_listed ? listed_row[i] : in ? k : 0) * ldq;
-      }
-      ffn_dma16(in ? (const void*)src : zeros, a.to + P_BYTES + i * NT * 16);
-    }
-  };
-  // the source of transfer j of K tile kt, and how many of its entries there are (rows of any length)
-  auto p_src = [&](int kt, int j, int& have) -> const T* {
-    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     if constexpr (P_ALONG) {
-      have = min(V, p.k - (k0 + p_at));
-      return (seg ? p1 : p0) + pp[j] + k0;
+      src = a.p + p_off[h][j];
+      in = a.k0 + p_at[0] < k_end;
+    } else {
+      const int k = a.k0 + p_row + j * P_NEXT;
+      in = k < k_end;
+      src = a.p + p_at[h] + (LISTED && list && !q_listed ? listed_row[j] : k) * ldp;
+    }
+    ffn_dma16(in ? (const void*)src : zeros, to + at_p(h, decltype(stage)::value) + j * NT * 16);
+  };
+  auto request_q = [&](const Ask& a, auto half, auto stage, auto which) {
+    constexpr int h = decltype(half)::value, j = decltype(which)::value;
+    const T* src;
+    bool in;
+    if constexpr (Q_ALONG) {
+      src = a.q[h] + q_off[h][j];
+      in = a.k0 + q_at[0] < k_end;
+    } else {
+      const int k = a.k0 + q_row + j * Q_NEXT;
+      in = k < k_end;
+      src = a.q[h] + q_at[h] + (LISTED && q_listed ? listed_row[j] : k) * ldq;
+    }
+    ffn_dma16(in ? (const void*)src : zeros, to + at_q(h, decltype(stage)::value) + j * NT * 16);
+  };
+  // rows of any length: through registers.  The source of a group of K tile kt, and how many of its entries there are
+  auto p_src = [&](int kt, int h, int j, int& have) -> const T* {
+    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    const T* const base = seg ? p1 : p0;
+    if constexpr (P_ALONG) {
+      have = min(V, p.k - (k0 + p_at[h]));
+      return base + p_off[h][j] + k0;
     } else {
       const int k = k0 + p_row + j * P_NEXT;
-      have = k < p.k ? min(V, p.m - p_at) : 0;
-      return p0 + (have > 0 ? p_k(k) * ldp + p_at : 0);
+      have = k < p.k ? min(V, p.m - p_at[h]) : 0;
+      return base + (have > 0 ? p_k(k) * ldp + p_at[h] : 0);
     }
   };
-  auto q_src = [&](int kt, int j, int& have) -> const T* {
+  auto q_src = [&](int kt, int h, int j, int& have) -> const T* {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
+    const T* const base = (GATED ? h : seg) ? q1 : q0;
     if constexpr (Q_ALONG) {
-      have = min(V, p.k - (k0 + q_at));
-      if constexpr (GATED) return qq[j] + k0;
-      else return q0 + qq_at[j] + k0;
+      have = min(V, p.k - (k0 + q_at[h]));
+      return base + q_off[h][j] + k0;
     } else {
       const int k = k0 + q_row + j * Q_NEXT;
-      have = k < p.k ? min(V, p.n - q_at) : 0;
-      return (seg ? q1 : q0) + (have > 0 ? q_k(k) * ldq + q_at : 0);
+      have = k < p.k ? min(V, p.n - q_at[h]) : 0;
+      return base + (have > 0 ? q_k(k) * ldq + q_at[h] : 0);
     }
   };
-  v4i held[JP + JQ];                                           // rows of any length: through registers
+  v4i held[2 * (JP + JQ)];
   auto load_group = [=](const T* s, int have) -> v4i {
     if (have >= V) {
       v4i g;
@@ -216,83 +229,127 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   };
   auto hold = [&](int kt) {
 #pragma unroll
-    for (int j = 0; j < JP; ++j) {
-      int have;
-      const T* s = p_src(kt, j, have);
-      held[j] = load_group(s, have);
-    }
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int j = 0; j < JQ; ++j) {
-      int have;
-      const T* s = q_src(kt, j, have);
-      held[JP + j] = load_group(s, have);
+      for (int j = 0; j < JP; ++j) {
+        int have;
+        const T* s = p_src(kt, h, j, have);
+        held[h * (JP + JQ) + j] = load_group(s, have);
+      }
+#pragma unroll
+      for (int j = 0; j < JQ; ++j) {
+        int have;
+        const T* s = q_src(kt, h, j, have);
+        held[h * (JP + JQ) + JP + j] = load_group(s, have);
+      }
     }
   };
   auto put = [&]() {
 #pragma unroll
-    for (int j = 0; j < JP; ++j) *reinterpret_cast<v4i*>(smem + (j * NT + t) * 16) = held[j];
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int j = 0; j < JQ; ++j) *reinterpret_cast<v4i*>(smem + P_BYTES + (j * NT + t) * 16) = held[JP + j];
+      for (int j = 0; j < JP; ++j) *reinterpret_cast<v4i*>(smem + at_p(h, 0) + (j * NT + t) * 16) = held[h * (JP + JQ) + j];
+#pragma unroll
+      for (int j = 0; j < JQ; ++j) *reinterpret_cast<v4i*>(smem + at_q(h, 0) + (j * NT + t) * 16) = held[h * (JP + JQ) + JP + j];
+    }
   };
 
-  // ---- fragments ----
+  // ---- operands of the matrix instructions, from LDS ----
+  // 32 rows of a half of an operand and KSTEP entries of k.  A lane's addresses in half 0 of stage 0: along k one for every step (the
+  // keys differ), across k one for every block of 32 rows; the rest is an offset in the instruction.
   typedef short s16x4 __attribute__((ext_vector_type(4)));
-  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-  // 32 rows r0 .. r0 + 31 of an operand's tile (of BR rows), KSTEP entries of k
-  auto fragment = [&](auto along, auto is_q, const unsigned char* tile, auto br, int r0, int ks) -> v4i {
-    constexpr int BR = decltype(br)::value;
+  typedef __attribute__((address_space(3))) const v4i lds_v4i;
+  typedef __attribute__((address_space(3))) const int lds_int;
+  auto lane_address = [&](auto along, auto is_q, auto rows, int r0, int i) -> unsigned {
+    constexpr int BR = decltype(rows)::value;
+    constexpr bool Q = decltype(is_q)::value;
     if constexpr (decltype(along)::value) {
-      const int r = decltype(is_q)::value ? ffn_q_order(l32) : l32;
-      return *reinterpret_cast<const v4i*>(tile + (r0 + r) * 128 + (((2 * ks + h) ^ L::key_along(r)) << 4));
+      const int r = r0 + (Q ? ffn_q_order(l32) : l32);
+      return r * 128 + (((2 * i + h) ^ L::key_along(r)) << 4);
     } else if constexpr (EB == 2) {
       // within 16 lanes the transposing read gives lane j element t of source lane 4 t + j / 4, entry j % 4: source lane s
       // points at row s / 4 of k, columns of the four lanes from 4 (s % 4) on
-      const int l16 = lane & 15, k = ks * L::KSTEP + 8 * h + (l16 >> 2);
-      const int r = 16 * ((lane >> 4) & 1) + 4 * (l16 & 3), c = r0 + (decltype(is_q)::value ? ffn_q_order(r) : r);
-      const unsigned char* a = tile + k * (BR * 2) + (((c >> 3) ^ L::key_across(k)) << 4) + (c & 7) * 2;
-      struct { s16x4 lo, hi; } both = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a),
-                                       __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 4 * BR * 2))};
+      const int l16 = lane & 15, k = 8 * h + (l16 >> 2), r = 16 * ((lane >> 4) & 1) + 4 * (l16 & 3);
+      const int c = r0 + 32 * i + (Q ? ffn_q_order(r) : r);
+      return k * (BR * 2) + (((c >> 3) ^ L::template key_across<BR / V>(k)) << 4) + (c & 7) * 2;
+    } else {
+      const int k = 4 * h, c = r0 + 32 * i + (Q ? ffn_q_order(l32) : l32);
+      return k * (BR * 4) + (((c >> 2) ^ L::template key_across<BR / V>(k)) << 4) + (c & 3) * 4;
+    }
+  };
+  constexpr int P_ADDR = P_ALONG ? L::STEPS : MB, Q_ADDR = Q_ALONG ? L::STEPS : NB;
+  unsigned p_addr[P_ADDR], q_addr[Q_ADDR];
+#pragma unroll
+  for (int i = 0; i < P_ADDR; ++i) {
+    p_addr[i] = lds0 + lane_address(std::bool_constant<P_ALONG>{}, std::false_type{}, std::integral_constant<int, PM>{}, wm * MB * 32, i);
+    asm volatile("" : "+v"(p_addr[i]));      // (kept as it is, so that what is added to it goes into the instructions)
+  }
+#pragma unroll
+  for (int i = 0; i < Q_ADDR; ++i) {
+    q_addr[i] = lds0 + at_q(0, 0) +
+                lane_address(std::bool_constant<Q_ALONG>{}, std::true_type{}, std::integral_constant<int, PN>{}, wn * NB * 32, i);
+    asm volatile("" : "+v"(q_addr[i]));
+  }
+  auto fragment = [&](auto along, auto rows, auto step, const auto& addr, int b, unsigned at) -> v4i {
+    constexpr int BR = decltype(rows)::value, ks = decltype(step)::value;
+    if constexpr (decltype(along)::value) {
+      return *(lds_v4i*)(uint64_t)(addr[ks] + at + b * 32 * 128);
+    } else if constexpr (EB == 2) {
+      const unsigned a = addr[b] + at + ks * L::KSTEP * BR * 2;
+      struct { s16x4 lo, hi; } both = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uint64_t)a),
+                                       __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uint64_t)(a + 4 * BR * 2))};
       return __builtin_bit_cast(v4i, both);
     } else {
-      const int k = ks * L::KSTEP + 4 * h, c = r0 + (decltype(is_q)::value ? ffn_q_order(l32) : l32);
       v4i f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        f[e] = *reinterpret_cast<const int*>(tile + (k + e) * (BR * 4) + (((c >> 2) ^ L::key_across(k)) << 4) + (c & 3) * 4);
+      for (int e = 0; e < 4; ++e) f[e] = *(lds_int*)(uint64_t)(addr[b] + at + (ks * L::KSTEP + e) * BR * 4);
       return f;
     }
   };
 
-  floatx16 acc[MI][NI];
+  floatx16 acc[2 * MB][2 * NB];
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi)
+  for (int mi = 0; mi < 2 * MB; ++mi)
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni)
+    for (int ni = 0; ni < 2 * NB; ++ni)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
 
-  struct Step { v4i p[MI], q[NI]; };                           // operands of KSTEP entries of k
-  auto read_step = [&](int stage, int ks, Step& f) {
-    const unsigned char* tp = smem + stage * STAGE;
-    const unsigned char* tq = tp + P_BYTES;
+  // operands: one half of P, both of Q, and the first half of Q of the next tile (the first and the third change places from tile to tile)
+  v4i pf[L::STEPS][MB], qf[3][L::STEPS][NB];
+  auto read_p = [&](auto stage, auto half, auto step) {
 #pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-      f.p[mi] = fragment(std::bool_constant<P_ALONG>{}, std::false_type{}, tp, std::integral_constant<int, BM>{}, (wm * MI + mi) * 32, ks);
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      const int r0 = GATED ? (ni < HALF ? (wn * HALF + ni) * 32 : COLS + (wn * HALF + ni - HALF) * 32) : (wn * NI + ni) * 32;
-      f.q[ni] = fragment(std::bool_constant<Q_ALONG>{}, std::true_type{}, tq, std::integral_constant<int, BN>{}, r0, ks);
-    }
+    for (int b = 0; b < MB; ++b)
+      pf[decltype(step)::value][b] = fragment(std::bool_constant<P_ALONG>{}, std::integral_constant<int, PM>{}, step, p_addr, b,
+                                              at_p(decltype(half)::value, decltype(stage)::value));
   };
-  // the products of a step; job(i) behind the i-th
-  auto multiply = [&](const Step& f, auto&& job) {
-    ffn_for<0, MI * NI>([&](auto i) {
-      constexpr int I = decltype(i)::value;
-      E::mma(acc[I / NI][I % NI], f.q[I % NI], f.p[I / NI]);
-      job(i);
+  auto read_q = [&](auto stage, auto half, auto into, auto step) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+      qf[decltype(into)::value][decltype(step)::value][b] =
+          fragment(std::bool_constant<Q_ALONG>{}, std::integral_constant<int, PN>{}, step, q_addr, b,
+                   at_q(decltype(half)::value, decltype(stage)::value) - at_q(0, 0));
+  };
+  // the products of a quadrant with Q in registers `set`; then(ks) behind those of a step of k
+  auto quadrant = [&](auto half_p, auto half_q, auto set, auto&& then) {
+    constexpr int hp = decltype(half_p)::value, hq = decltype(half_q)::value;
+    ffn_for<0, L::STEPS>([&](auto step) {
+      constexpr int ks = decltype(step)::value;
+#pragma unroll
+      for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int c = 0; c < NB; ++c) E::mma(acc[hp * MB + b][hq * NB + c], qf[decltype(set)::value][ks][c], pf[ks][b]);
+      __builtin_amdgcn_sched_barrier(0);
+      then(step);
+      __builtin_amdgcn_sched_barrier(0);
     });
   };
-  auto no_job = [](auto) {};
+  // all transfers but the youngest N have landed, for every wavefront, and all have come this far
+  auto meet = [&](auto youngest) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(youngest)::value) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
 
   constexpr int STRETCH = kFfnList / BK;                       // K tiles of a stretch of the list
   auto renew_list = [&](int kt) {                              // called by all, before anything of K tile kt is asked for
@@ -305,61 +362,69 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     }
   };
   if constexpr (ALIGNED) {
-    // Two tiles in LDS.  A tile has four steps, whose operands are read one step ahead, the first step's under the products of the last
-    // one of the tile before: by then all wavefronts have met, the tile has landed, and the one before is in registers, so that its
-    // place takes the tile after next.  Its transfers are asked for one at a time between products, since a wavefront that asks for
-    // several waits while the address unit takes them.
-    constexpr int JOBS = JP + JQ, EACH = (JOBS + MI * NI - 1) / (MI * NI);      // transfers behind a product
-    auto ask = [&](int kt, int stage) {
-      renew_list(kt);
-      look_up(kt);
-      const Ask a = prepare(kt, stage);
-      ffn_for<0, JOBS>([&](auto j) { request_one(a, j); });
-    };
-    if (kt_lo < kt_hi) ask(kt_lo, 0);
-    if (kt_lo + 1 < kt_hi) {
-      ask(kt_lo + 1, 1);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(JOBS) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // Two K tiles in LDS, each in four halves.  The quadrants of a tile are multiplied in the order (P0, Q0), (P0, Q1), (P1, Q1),
+    // (P1, Q0).  The operands of a quadrant are read from LDS one or two quadrants before, into registers that are free by then, and a
+    // half's place in LDS is taken by the same half of the tile after next as soon as it is in everybody's registers: wavefronts meet
+    // twice a tile, behind the first quadrant and behind the third, and a transfer has four to five quadrants (2 000 to 2 500 cycles for
+    // tiles of 256) to arrive.  64 KB take 1.1 us to arrive in a compute unit that has nothing else to do.
+    //   quadrant    1          2          3              4
+    //   reads       Q1         P1         Q0, next tile  P0, next tile
+    //   asks for    P1, next   Q0, after  P0, after      Q1, after next
+    if (kt_lo < kt_hi) {
+      const int last = kt_hi - 1;
+      const std::integral_constant<int, 2> c2{};
+      auto all_p = [&](const Ask& a, auto half, auto stage) { ffn_for<0, JP>([&](auto j) { request_p(a, half, stage, j); }); };
+      auto all_q = [&](const Ask& a, auto half, auto stage) { ffn_for<0, JQ>([&](auto j) { request_q(a, half, stage, j); }); };
+      renew_list(kt_lo);
+      look_up(kt_lo);
+      Ask a = prepare(kt_lo);
+      all_q(a, c0, c0);
+      all_p(a, c0, c0);
+      all_q(a, c1, c0);
+      all_p(a, c1, c0);
+      look_up(min(kt_lo + 1, last));
+      a = prepare(min(kt_lo + 1, last));
+      all_q(a, c0, c1);
+      all_p(a, c0, c1);
+      all_q(a, c1, c1);
+      meet(std::integral_constant<int, 5 * JP>{});
+      ffn_for<0, L::STEPS>([&](auto ks) { read_q(c0, c0, c0, ks); read_p(c0, c0, ks); });
+      meet(std::integral_constant<int, 4 * JP>{});
+      // tile kt in `stage`, its first half of Q in registers `now`, that of the next tile goes into `next`
+      auto tile = [&](int kt, auto stage, auto other, auto now, auto next) {
+        // a: the next tile's
+        quadrant(c0, c0, now, [&](auto ks) {
+          read_q(stage, c1, c1, ks);
+          if constexpr (decltype(ks)::value < JP) request_p(a, c1, other, ks);
+        });
+        meet(std::integral_constant<int, 3 * JP>{});
+        // (behind the last tiles the last one again, which nobody reads: the counts stay, and a branch would cost registers)
+        const int ahead = min(kt + 2, last);
+        if (kt + 2 <= last) renew_list(ahead);
+        look_up(ahead);
+        a = prepare(ahead);
+        quadrant(c0, c1, c1, [&](auto ks) {
+          read_p(stage, c1, ks);
+          if constexpr (decltype(ks)::value < JQ) request_q(a, c0, stage, ks);
+        });
+        quadrant(c1, c1, c1, [&](auto ks) {
+          read_q(other, c0, next, ks);
+          if constexpr (decltype(ks)::value < JP) request_p(a, c0, stage, ks);
+        });
+        meet(std::integral_constant<int, 3 * JP>{});
+        quadrant(c1, c0, now, [&](auto ks) {
+          read_p(other, c0, ks);
+          if constexpr (decltype(ks)::value < JQ) request_q(a, c1, stage, ks);
+        });
+      };
+      for (int kt = kt_lo;;) {
+        tile(kt, c0, c1, c0, c2);
+        if (++kt == kt_hi) break;
+        tile(kt, c1, c0, c2, c0);
+        if (++kt == kt_hi) break;
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may still be on its way into LDS when the workgroup ends
     }
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    Step f0, f1;
-    if (kt_lo < kt_hi) read_step(0, 0, f0);
-    for (int kt = kt_lo; kt < kt_hi; ++kt) {
-      const int stage = (kt - kt_lo) & 1;
-      read_step(stage, 1, f1);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(f0, no_job);
-      __builtin_amdgcn_sched_barrier(0);
-      read_step(stage, 2, f0);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(f1, no_job);
-      __builtin_amdgcn_sched_barrier(0);
-      read_step(stage, 3, f1);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(f0, no_job);
-      __builtin_amdgcn_sched_barrier(0);
-      // the next tile has landed, and this one has been read, for every wavefront
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      // (behind the last tile but one, the last again, which nobody reads: a branch here would cost registers)
-      const int ahead = min(kt + 2, kt_hi - 1);
-      if (kt + 2 < kt_hi) renew_list(ahead);
-      look_up(ahead);
-      const Ask a = prepare(ahead, stage);
-      read_step(stage ^ 1, 0, f0);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(f1, [&](auto i) {
-        constexpr int I = decltype(i)::value;
-        __builtin_amdgcn_sched_barrier(0);
-        ffn_for<I * EACH, (I + 1) * EACH < JOBS ? (I + 1) * EACH : JOBS>([&](auto j) { request_one(a, j); });
-        __builtin_amdgcn_sched_barrier(0);
-      });
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may still be on its way into LDS when the workgroup ends
   } else {
     if (kt_lo < kt_hi) {
       renew_list(kt_lo);
@@ -373,12 +438,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
         renew_list(kt + 1);
         hold(kt + 1);
       }
-#pragma unroll
-      for (int ks = 0; ks < L::STEPS; ++ks) {
-        Step f;
-        read_step(0, ks, f);
-        multiply(f, no_job);
-      }
+      ffn_for<0, L::STEPS>([&](auto ks) { read_p(c0, c0, ks); read_q(c0, c0, c0, ks); read_q(c0, c1, c1, ks); });
+      quadrant(c0, c0, c0, [](auto) {});
+      quadrant(c0, c1, c1, [](auto) {});
+      ffn_for<0, L::STEPS>([&](auto ks) { read_p(c0, c1, ks); });
+      quadrant(c1, c1, c1, [](auto) {});
+      quadrant(c1, c0, c0, [](auto) {});
     }
   }
 
@@ -405,27 +470,27 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     }
   };
 #pragma unroll
-  for (int mi = 0; mi < MI; ++mi) {
-    const int i = m0 + (wm * MI + mi) * 32 + l32;
+  for (int mi = 0; mi < 2 * MB; ++mi) {
+    const int i = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
     const int row = i < m ? i : -1;
     int out_row = row;
     if (row >= 0 && p.c_rows) out_row = p.c_rows[row];
 #pragma unroll
-    for (int ni = 0; ni < HALF; ++ni) {
-      const int col = n0 + (wn * HALF + ni) * 32 + 16 * h;
+    for (int ni = 0; ni < (GATED ? NB : 2 * NB); ++ni) {
+      const int col = n0 + ni / NB * PN + (wn * NB + ni % NB) * 32 + 16 * h;
       if constexpr (WHAT == kFfnUp) {
         floatx16 hidden;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float a, da;
           ffn_act(p.activation, acc[mi][ni][e], a, da);
-          hidden[e] = a * acc[mi][ni + HALF][e];
+          hidden[e] = a * acc[mi][ni + NB][e];
         }
         store(static_cast<T*>(p.c[0]), p.ldc, row, col, hidden);
         if (p.saved) {
           T* g = static_cast<T*>(p.saved);
           store(g, p.ldc, row, col, acc[mi][ni]);
-          store(g + (int64_t)m * n, p.ldc, row, col, acc[mi][ni + HALF]);
+          store(g + (int64_t)m * n, p.ldc, row, col, acc[mi][ni + NB]);
         }
       } else if constexpr (WHAT == kFfnGateGrad) {
         float g[16], u[16];
@@ -466,9 +531,9 @@ hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
   g.n_tiles = (g.n + cols - 1) / cols;
   g.group = 8;
   const bool listed = WHAT == kFfnWGrad && (g.p_rows || g.q_rows);
-  const int lds = (BM + BN) * 128 * (ALIGNED ? 2 : 1) + (listed ? kFfnList * 4 : 0);
+  const int lds = (BM + BN) * 256 + (listed ? kFfnList * 4 : 0);
   static std::atomic<uint64_t> told{0};
-  const hipError_t e = ffn_allow_lds(reinterpret_cast<const void*>(kernel), (BM + BN) * 128 * (ALIGNED ? 2 : 1) + kFfnList * 4, told);
+  const hipError_t e = ffn_allow_lds(reinterpret_cast<const void*>(kernel), (BM + BN) * 256 + kFfnList * 4, told);
   if (e != hipSuccess) return e;
   const int64_t total = (int64_t)g.m_tiles * g.n_tiles * g.batch * g.splits;
   kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WAVES_M * WAVES_N), lds, s>>>(g);
