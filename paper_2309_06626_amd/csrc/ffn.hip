@@ -10,6 +10,7 @@
 #include "ffn_params.hpp"
 #include "rows.hpp"
 
+#include <algorithm>
 #include <initializer_list>
 
 namespace sc {
@@ -31,80 +32,120 @@ static sc_status check_ffn(const sc_ffn_desc* d, int64_t kept) {
   return SC_OK;
 }
 
-static hipError_t launch(int dtype, FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
+static hipError_t launch(int dtype, FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s) {
   switch (dtype) {
-    case SC_BF16: return ffn_launch_bf16(what, g, tile, aligned, s);
-    case SC_F16: return ffn_launch_f16(what, g, tile, aligned, s);
-    default: return ffn_launch_f32(what, g, tile, aligned, s);
+    case SC_BF16: return ffn_launch_bf16(what, g, tile, rows, s);
+    case SC_F16: return ffn_launch_f16(what, g, tile, rows, s);
+    default: return ffn_launch_f32(what, g, tile, rows, s);
   }
 }
 
 constexpr int64_t kFewRows = 64;
 
-static hipError_t launch_forward(int dtype, FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
-  if (g.m > kFewRows) return launch(dtype, what, g, tile, aligned, s);
-  switch (dtype) {
-    case SC_BF16: return ffn_few_bf16(what == kFfnUp, g, aligned, s);
-    case SC_F16: return ffn_few_f16(what == kFfnUp, g, aligned, s);
-    default: return ffn_few_f32(what == kFfnUp, g, aligned, s);
+static int row_kind(const sc_ffn_desc& d) {
+  const int all = (d.d_in | d.d_hidden | d.d_out) * elem_bytes(d.dtype);
+  return all % 16 == 0 ? kFfnWholeRows : all % 4 == 0 ? kFfnWordRows : kFfnAnyRows;
+}
+
+// Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`.
+// Priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other: 256 workgroups of 256 x
+// 256 take 1.6 (128 or fewer 1.05, since the clock is higher), 512 of 128 x 128, two a compute unit, 1.06 (256 or fewer 0.42); across k on
+// both sides 1.75, 1.15, 1.2 and 0.62.  Floats take 4.1 and 2.05 in tiles of 128 and no less in tiles of 256, which have no float form.  A launch
+// and a tile's beginning and end take 8.  A contraction in parts leaves sums in float, written and read once at 4 TB/s, and another launch.
+constexpr int kMostSplits = 32, kLeastTiles = 4;
+static int64_t k_tiles_of(int64_t k, int segments, int dtype) { return segments * ((k + (dtype == SC_F32 ? 31 : 63)) / (dtype == SC_F32 ? 32 : 64)); }
+
+struct Tiling {
+  int tile, splits;
+  double us;
+};
+
+static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, int segments, int batch, int dtype, int layout) {
+  const bool across = what == kFfnWGrad, f32 = dtype == SC_F32, splittable = what != kFfnUp && what != kFfnGateGrad;
+  const int64_t k_tiles = k_tiles_of(k, segments, dtype);
+  Tiling best = {0, 1, 1e30};
+  for (int tile = 0; tile < 2; ++tile) {
+    if (tile == 1 && (f32 || layout != kFfnWholeRows)) break;
+    const int64_t edge = tile ? 256 : 128, room = tile ? 256 : 512;
+    const double half = f32 ? 2.05 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42);
+    const double full = f32 ? 4.1 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06);
+    const int64_t tiles = ((m + edge - 1) / edge) * ((cols + edge - 1) / edge) * batch;
+    for (int splits = 1; splits <= kMostSplits; ++splits) {
+      if (splits > 1 && (!splittable || k_tiles / splits < kLeastTiles)) break;
+      const int64_t count = tiles * splits, rest = count % room;
+      if (splits > 1 && ((splits - 1) * tiles > room * (tile ? 1 : 2) || count > 2 * room)) break;
+      const double rounds = (double)(count / room), left = rest == 0 ? 0.0 : rest <= room / 2 ? half : full;
+      const double per = (double)((k_tiles + splits - 1) / splits);
+      double us = 3.0 + (rounds * full + left) * per + (rounds + (rest ? 1.0 : 0.0)) * 5.0;
+      if (splits > 1) us += 4.0 + (double)splits * batch * m * cols * 8.0 / 4e6;
+      if (us < best.us) best = {tile, splits, us};
+    }
+  }
+  return best;
+}
+
+// What a workspace must hold of a result's parts, whatever the number of rows up to this one: a part has four K tiles or more, and there are
+// at most kMostSplits, and at most 1 024 tiles of 128 x 128 (256 of 256 x 256) besides a result that is no larger than that itself.
+static size_t most_parts(int64_t m, int64_t n, int64_t k, int segments, int batch, int dtype) {
+  const int64_t parts = std::min<int64_t>(kMostSplits, k_tiles_of(k, segments, dtype) / kLeastTiles);
+  return parts < 2 ? 0 : up256(std::min((size_t)parts * batch * m * n * 4, (size_t)128 << 20));
+}
+static size_t most_parts(const sc_ffn_desc& d, int64_t kept, bool training) {
+  size_t most = most_parts(kept, d.d_out, d.d_hidden, 1, 1, d.dtype);
+  if (training)
+    most = std::max({most, most_parts(kept, d.d_in, d.d_hidden, 2, 1, d.dtype), most_parts(d.d_hidden, d.d_in, kept, 1, 2, d.dtype),
+                     most_parts(d.d_out, d.d_hidden, kept, 1, 1, d.dtype)});
+  return most;
+}
+
+// sums of the parts, in order, into the rows of c; a row of a result a workgroup, blockIdx.y the result
+template <typename T, int WIDTH>
+__global__ __launch_bounds__(256) void ffn_sum_parts_kernel(const float* __restrict__ partial, T* c0, T* c1, int64_t ldc,
+                                                            const int32_t* __restrict__ c_rows, int m, int n, int splits) {
+  typedef float vec __attribute__((ext_vector_type(WIDTH)));
+  const int z = blockIdx.y, row = blockIdx.x;
+  const float* p = partial + ((int64_t)z * splits * m + row) * n;
+  T* c = (z ? c1 : c0) + (c_rows ? (int64_t)c_rows[row] : row) * ldc;
+  for (int i = threadIdx.x * WIDTH; i < n; i += 256 * WIDTH) {
+    vec v = *reinterpret_cast<const vec*>(p + i);
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const vec*>(p + (int64_t)s * m * n + i);
+    T out[WIDTH];
+#pragma unroll
+    for (int u = 0; u < WIDTH; ++u) out[u] = (T)v[u];
+    __builtin_memcpy(c + i, out, sizeof(out));
   }
 }
 
-static bool whole_groups(const sc_ffn_desc& d) {
-  const int v = 16 / elem_bytes(d.dtype);
-  return d.d_in % v == 0 && d.d_hidden % v == 0 && d.d_out % v == 0;
-}
-
-// Tiles of 256 x 256 where they fill the chip, 128 x 128 otherwise.
-static int pick_tile(int64_t m, int64_t cols, int batch) {
-  const int64_t big = ((m + 255) / 256) * ((cols + 255) / 256) * batch;
-  return big >= 192 ? 1 : 0;
-}
-
-// Parts of the contraction over rows: a weight gradient has few tiles and many rows.  Every part leaves its sums in float.
-static int pick_splits(int64_t m, int64_t n, int batch, int tile, int64_t kept, int dtype) {
-  const int edge = tile == 1 ? 256 : 128, bk = dtype == SC_F32 ? 32 : 64;
-  const int64_t tiles = ((m + edge - 1) / edge) * ((n + edge - 1) / edge) * batch;
-  const int64_t wanted = (tile == 1 ? 256 : 512) / tiles, most = ((kept + bk - 1) / bk) / 8;
-  const int64_t splits = wanted < most ? wanted : most;
-  return splits < 1 ? 1 : splits > 64 ? 64 : (int)splits;
-}
-
-static size_t partial_bytes(const sc_ffn_desc& d, int64_t kept) {
-  size_t most = 0;
-  const int tile_in = pick_tile(d.d_hidden, d.d_in, 2), tile_out = pick_tile(d.d_out, d.d_hidden, 1);
-  const int s_in = pick_splits(d.d_hidden, d.d_in, 2, tile_in, kept, d.dtype);
-  const int s_out = pick_splits(d.d_out, d.d_hidden, 1, tile_out, kept, d.dtype);
-  if (s_in > 1) most = (size_t)2 * s_in * d.d_hidden * d.d_in * 4;
-  if (s_out > 1 && (size_t)s_out * d.d_out * d.d_hidden * 4 > most) most = (size_t)s_out * d.d_out * d.d_hidden * 4;
-  return up256(most);
-}
-
-// sums of the parts, in order; batch results of `count` values each
-template <typename T>
-__global__ __launch_bounds__(256) void ffn_sum_parts_kernel(const float* __restrict__ partial, T* c0, T* c1, int64_t count,
-                                                            int splits) {
-  const int z = blockIdx.y;
-  T* c = z ? c1 : c0;
-  const float* p = partial + (int64_t)z * splits * count;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
-    float v = 0.0f;
-    for (int s = 0; s < splits; ++s) v += p[(int64_t)s * count + i];
-    c[i] = (T)v;
-  }
-}
-
-static hipError_t sum_parts(int dtype, const FfnGemm& g, hipStream_t s) {
-  const int64_t count = (int64_t)g.m * g.n;
-  const int64_t want = (count + 255) / 256;
-  const dim3 grid((unsigned)(want < 4096 ? want : 4096), g.batch);
-  if (dtype == SC_BF16)
-    ffn_sum_parts_kernel<__bf16><<<grid, dim3(256), 0, s>>>(g.partial, (__bf16*)g.c[0], (__bf16*)g.c[1], count, g.splits);
-  else if (dtype == SC_F16)
-    ffn_sum_parts_kernel<_Float16><<<grid, dim3(256), 0, s>>>(g.partial, (_Float16*)g.c[0], (_Float16*)g.c[1], count, g.splits);
-  else
-    ffn_sum_parts_kernel<float><<<grid, dim3(256), 0, s>>>(g.partial, (float*)g.c[0], (float*)g.c[1], count, g.splits);
+template <typename T> static hipError_t sum_parts_type(const FfnGemm& g, hipStream_t s) {
+  const dim3 grid((unsigned)g.m, g.batch);
+  T *c0 = static_cast<T*>(g.c[0]), *c1 = static_cast<T*>(g.c[1]);
+  if (g.n % 4 == 0) ffn_sum_parts_kernel<T, 4><<<grid, dim3(256), 0, s>>>(g.partial, c0, c1, g.ldc, g.c_rows, g.m, g.n, g.splits);
+  else ffn_sum_parts_kernel<T, 1><<<grid, dim3(256), 0, s>>>(g.partial, c0, c1, g.ldc, g.c_rows, g.m, g.n, g.splits);
   return hipGetLastError();
+}
+static hipError_t sum_parts(int dtype, const FfnGemm& g, hipStream_t s) {
+  if (dtype == SC_BF16) return sum_parts_type<__bf16>(g, s);
+  if (dtype == SC_F16) return sum_parts_type<_Float16>(g, s);
+  return sum_parts_type<float>(g, s);
+}
+
+// a product in the tiles and parts that its sizes ask for
+static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, int layout, float* parts, hipStream_t s) {
+  const Tiling t = pick_tiling(what, g.m, what == kFfnUp ? 2 * (int64_t)g.n : g.n, g.k, g.segments, g.batch, dtype, layout);
+  g.splits = t.splits;
+  g.partial = parts;
+  const hipError_t e = launch(dtype, what, g, t.tile, layout, s);
+  return e == hipSuccess && g.splits > 1 ? sum_parts(dtype, g, s) : e;
+}
+// kFfnUp and kFfnDown
+static hipError_t multiply_forward(int dtype, FfnProduct what, FfnGemm& g, int layout, float* parts, hipStream_t s) {
+  if (g.m > kFewRows) return multiply(dtype, what, g, layout, parts, s);
+  const bool whole = layout == kFfnWholeRows;
+  switch (dtype) {
+    case SC_BF16: return ffn_few_bf16(what == kFfnUp, g, whole, s);
+    case SC_F16: return ffn_few_f16(what == kFfnUp, g, whole, s);
+    default: return ffn_few_f32(what == kFfnUp, g, whole, s);
+  }
 }
 
 __global__ __launch_bounds__(256) void ffn_zero_kernel(uint16_t* out, int64_t count) {
@@ -163,7 +204,7 @@ sc_status sparse_ffn_workspace_bytes(const sc_ffn_desc* desc, int64_t kept, int3
   const sc_status st = sc::check_ffn(desc, kept);
   if (st != SC_OK) return st;
   const size_t hidden = sc::up256((size_t)kept * desc->d_hidden * sc::elem_bytes(desc->dtype));
-  *bytes = 256 + (training ? 2 * hidden + sc::partial_bytes(*desc, kept) : hidden);
+  *bytes = 256 + (training ? 2 * hidden : hidden) + sc::most_parts(*desc, kept, training != 0);
   return SC_OK;
 }
 
@@ -178,16 +219,18 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
     return SC_ERR_NULL;
   size_t need = 0;
   sparse_ffn_workspace_bytes(desc, kept, 0, &need);
-  if (!saved_dev && workspace_bytes < need) return SC_ERR_WORKSPACE;
+  if (workspace_bytes < need) return SC_ERR_WORKSPACE;
   if (sc::misaligned({x_dev, w_gate_dev, w_up_dev, w_down_dev, y_dev, saved_dev, workspace_dev})) return SC_ERR_ALIGN;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int eb = sc::elem_bytes(desc->dtype);
-  const bool aligned = sc::whole_groups(*desc);
+  const int layout = sc::row_kind(*desc);
   hipError_t e = hipSuccess;
   if (y_rows == SC_ROWS_DENSE) e = sc::rows_zero_dropped(rows, (int64_t)desc->d_out * eb, y_dev, s);
   if (e != hipSuccess) return sc::failed(e);
   if (kept == 0) return SC_OK;
-  void* hidden = saved_dev ? static_cast<char*>(saved_dev) + (size_t)2 * kept * desc->d_hidden * eb : workspace_dev;
+  const size_t hidden_bytes = (size_t)kept * desc->d_hidden * eb;
+  void* const hidden = saved_dev ? static_cast<char*>(saved_dev) + 2 * hidden_bytes : workspace_dev;
+  float* const parts = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + sc::up256(hidden_bytes));
 
   sc::FfnGemm up = sc::gemm_of(kept, desc->d_hidden, desc->d_in);
   up.p[0] = x_dev;
@@ -199,7 +242,7 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
   up.ldc = desc->d_hidden;
   up.saved = saved_dev;
   up.activation = desc->activation;
-  e = sc::launch_forward(desc->dtype, sc::kFfnUp, up, sc::pick_tile(kept, 2 * (int64_t)desc->d_hidden, 1), aligned, s);
+  e = sc::multiply_forward(desc->dtype, sc::kFfnUp, up, layout, parts, s);
   if (e != hipSuccess) return sc::failed(e);
 
   sc::FfnGemm down = sc::gemm_of(kept, desc->d_out, desc->d_hidden);
@@ -209,7 +252,7 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
   down.c[0] = y_dev;
   down.ldc = desc->d_out;
   down.c_rows = sc::map_of(rows, y_rows);
-  e = sc::launch_forward(desc->dtype, sc::kFfnDown, down, sc::pick_tile(kept, desc->d_out, 1), aligned, s);
+  e = sc::multiply_forward(desc->dtype, sc::kFfnDown, down, layout, parts, s);
   return e == hipSuccess ? SC_OK : sc::failed(e);
 }
 
@@ -232,7 +275,7 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int eb = sc::elem_bytes(desc->dtype);
   const int64_t d_in = desc->d_in, d_hidden = desc->d_hidden, d_out = desc->d_out;
-  const bool aligned = sc::whole_groups(*desc);
+  const int layout = sc::row_kind(*desc);
   hipError_t e = hipSuccess;
   if (dx_dev && x_rows == SC_ROWS_DENSE) e = sc::rows_zero_dropped(rows, d_in * eb, dx_dev, s);
   if (e != hipSuccess) return sc::failed(e);
@@ -259,7 +302,7 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
   gate.c[1] = du;
   gate.ldc = d_hidden;
   gate.activation = desc->activation;
-  e = sc::launch(desc->dtype, sc::kFfnGateGrad, gate, sc::pick_tile(kept, d_hidden, 1), aligned, s);
+  e = sc::multiply(desc->dtype, sc::kFfnGateGrad, gate, layout, partial, s);
   if (e != hipSuccess) return sc::failed(e);
 
   if (dx_dev) {
@@ -274,7 +317,7 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
     in.c[0] = dx_dev;
     in.ldc = d_in;
     in.c_rows = sc::map_of(rows, x_rows);
-    e = sc::launch(desc->dtype, sc::kFfnInGrad, in, sc::pick_tile(kept, d_in, 1), aligned, s);
+    e = sc::multiply(desc->dtype, sc::kFfnInGrad, in, layout, partial, s);
     if (e != hipSuccess) return sc::failed(e);
   }
   if (weights) {
@@ -289,11 +332,7 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
     in.c[0] = dw_gate_dev;
     in.c[1] = dw_up_dev;
     in.ldc = d_in;
-    in.partial = partial;
-    const int tile_in = sc::pick_tile(d_hidden, d_in, 2);
-    in.splits = sc::pick_splits(d_hidden, d_in, 2, tile_in, kept, desc->dtype);
-    e = sc::launch(desc->dtype, sc::kFfnWGrad, in, tile_in, aligned, s);
-    if (e == hipSuccess && in.splits > 1) e = sc::sum_parts(desc->dtype, in, s);
+    e = sc::multiply(desc->dtype, sc::kFfnWGrad, in, layout, partial, s);
     if (e != hipSuccess) return sc::failed(e);
 
     sc::FfnGemm out = sc::gemm_of(d_out, d_hidden, kept);      // dWd = dY' hidden
@@ -304,11 +343,7 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
     out.ldq = d_hidden;
     out.c[0] = dw_down_dev;
     out.ldc = d_hidden;
-    out.partial = partial;
-    const int tile_out = sc::pick_tile(d_out, d_hidden, 1);
-    out.splits = sc::pick_splits(d_out, d_hidden, 1, tile_out, kept, desc->dtype);
-    e = sc::launch(desc->dtype, sc::kFfnWGrad, out, tile_out, aligned, s);
-    if (e == hipSuccess && out.splits > 1) e = sc::sum_parts(desc->dtype, out, s);
+    e = sc::multiply(desc->dtype, sc::kFfnWGrad, out, layout, partial, s);
     if (e != hipSuccess) return sc::failed(e);
   }
   return SC_OK;

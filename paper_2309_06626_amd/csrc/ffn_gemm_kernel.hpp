@@ -29,10 +29,14 @@ __device__ __forceinline__ int ffn_q_order(int r) { return ((r >> 2) & 1) * 16 +
 constexpr int kFfnList = 4096;      // rows of the contraction whose list entries lie in LDS
 static __device__ __align__(16) v4i ffn_zeros = {0, 0, 0, 0};      // what is read beyond an operand's end
 
-// 16 bytes a lane from memory into LDS at base + 16 lane.  Written out, because the compiler would let every later LDS read wait
+// 16 (or 4) bytes a lane from memory into LDS at base + 16 (4) lane.  Written out, because the compiler would let every later LDS read wait
 // for all transfers in flight; their arrival is waited for at the barriers below.
 __device__ __forceinline__ void ffn_dma16(const void* src, unsigned lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src));
+}
+
+__device__ __forceinline__ void ffn_dma4(const void* src, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_base), "v"(src));
 }
 
 template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f) {
@@ -42,7 +46,7 @@ template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f
   }
 }
 
-template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int ROWS>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const FfnGemm p) {
   using E = Elem<DT>;
   using T = typename E::T;
@@ -53,14 +57,17 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   // a tile is two halves of P's rows by two halves of Q's; a wavefront has MB x NB blocks of 32 x 32 in each quadrant
   constexpr int PM = BM / 2, PN = BN / 2;
   constexpr int MB = PM / WAVES_M / 32, NB = PN / WAVES_N / 32;
-  constexpr int JP = PM * 8 / NT, JQ = PN * 8 / NT;            // transfers a lane and half tile
+  constexpr bool DMA = ROWS != kFfnAnyRows;
+  constexpr int UNIT = ROWS == kFfnWordRows ? 4 / EB : V;      // entries a lane and transfer
+  constexpr int JP = PM * 128 / (UNIT * EB) / NT, JQ = PN * 128 / (UNIT * EB) / NT;      // transfers a lane and half tile
+  constexpr int UNITS = V / UNIT, PAR = UNITS > 1 ? 2 : 1;     // units a 16-byte group; transfers whose rows have different keys
   constexpr int P_PIECE = PM * 128, Q_PIECE = PN * 128, STAGE = 2 * (P_PIECE + Q_PIECE);
   // half h of stage s in LDS, the halves of an operand within 64 KB of each other: one address a lane, the rest is in the instructions
   auto at_p = [](int h, int s) constexpr { return (2 * h + s) * P_PIECE; };
   auto at_q = [](int h, int s) constexpr { return 4 * P_PIECE + (2 * h + s) * Q_PIECE; };
   constexpr bool GATED = WHAT == kFfnUp;                       // the halves of Q: gate and up weights of the same columns
   constexpr int COLS = GATED ? PN : BN;                        // result columns of a tile
-  static_assert(JP == JQ && JP * 6 <= 63, "the counts of transfers below");
+  static_assert(JP == JQ && JP * 5 <= 63, "the counts of transfers below");
   extern __shared__ __align__(16) unsigned char smem[];
 
   constexpr std::integral_constant<int, 0> c0{};
@@ -88,10 +95,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   const int kt_lo = (int)((int64_t)all_tiles * split / p.splits), kt_hi = (int)((int64_t)all_tiles * (split + 1) / p.splits);
 
   // ---- loads ----
-  // slot s of a half of an operand's tile (16 bytes): along k, row s / 8, group s % 8; across k, row s / CPR of k, group s % CPR
-  constexpr int P_CPR = P_ALONG ? 8 : PM / V, Q_CPR = Q_ALONG ? 8 : PN / V;
-  const int p_row = wave * (64 / P_CPR) + lane / P_CPR, q_row = wave * (64 / Q_CPR) + lane / Q_CPR;      // of transfer 0
-  constexpr int P_NEXT = W * (64 / P_CPR), Q_NEXT = W * (64 / Q_CPR);                                    // rows from transfer to transfer
+  // unit s of a half of an operand's tile: along k, row s / PPR, across k, row s / PPR of k
+  constexpr int P_PPR = (P_ALONG ? 128 : PM * EB) / (UNIT * EB), Q_PPR = (Q_ALONG ? 128 : PN * EB) / (UNIT * EB);
+  const int p_row = t / P_PPR, q_row = t / Q_PPR;              // of transfer 0
+  constexpr int P_NEXT = NT / P_PPR, Q_NEXT = NT / Q_PPR;      // rows from transfer to transfer
+  // first entry, within the row, of what belongs at unit u of row r of the tile: 16-byte groups are exchanged by the row's key
+  auto entry = [](auto along, auto ppr, int u, int r) -> int {
+    const int key = decltype(along)::value ? L::key_along(r) : L::template key_across<decltype(ppr)::value / UNITS>(r);
+    return ((u / UNITS) ^ key) * V + u % UNITS * UNIT;
+  };
   // held in scalar registers: a load of a kernel argument between the products would have to wait for the operands on their way
   const T *p0 = static_cast<const T*>(p.p[P_ALONG ? 0 : z]), *p1 = static_cast<const T*>(p.p[p.segments > 1]);
   const T *q0 = static_cast<const T*>(p.q[0]), *q1 = static_cast<const T*>(p.q[p.segments > 1 || GATED]);
@@ -101,28 +113,34 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   asm volatile("" : "+s"(p0), "+s"(p1), "+s"(q0), "+s"(q1), "+s"(ldp), "+s"(ldq), "+s"(k_end), "+s"(zeros));
   // along: k of the lane's group, and its rows from the start of the operand; rows beyond the end: results that are not stored.
   // across: result row / column of the group in either half (beyond the end: any that exists)
-  int p_at[2], q_at[2];
+  int p_at[2][PAR], q_at[2][PAR];
   int64_t p_off[2][P_ALONG ? JP : 1], q_off[2][Q_ALONG ? JQ : 1];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int u = 0; u < PAR; ++u) {
+      p_at[h][u] = entry(std::bool_constant<P_ALONG>{}, std::integral_constant<int, P_PPR>{}, t % P_PPR, p_row + u * P_NEXT);
+      q_at[h][u] = entry(std::bool_constant<Q_ALONG>{}, std::integral_constant<int, Q_PPR>{}, t % Q_PPR, q_row + u * Q_NEXT);
+      if constexpr (!P_ALONG) {
+        p_at[h][u] += m0 + h * PM;
+        if constexpr (DMA) p_at[h][u] = min(p_at[h][u], p.m - UNIT);
+      }
+      if constexpr (!Q_ALONG) {
+        q_at[h][u] += n0 + h * PN;
+        if constexpr (DMA) q_at[h][u] = min(q_at[h][u], p.n - UNIT);
+      }
+    }
     if constexpr (P_ALONG) {
-      p_at[h] = ((lane & 7) ^ L::key_along(p_row)) * V;
 #pragma unroll
       for (int j = 0; j < JP; ++j) {
         const int i = min(m0 + h * PM + p_row + j * P_NEXT, p.m - 1);
-        p_off[h][j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_at[h];
+        p_off[h][j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_at[h][j % PAR];
       }
-    } else {
-      p_at[h] = m0 + h * PM + ((lane % P_CPR) ^ L::template key_across<P_CPR>(p_row)) * V;
-      if constexpr (ALIGNED) p_at[h] = min(p_at[h], p.m - V);
     }
     if constexpr (Q_ALONG) {
-      q_at[h] = ((lane & 7) ^ L::key_along(q_row)) * V;
 #pragma unroll
-      for (int j = 0; j < JQ; ++j) q_off[h][j] = min(n0 + (GATED ? 0 : h * PN) + q_row + j * Q_NEXT, n_last) * ldq + q_at[h];
-    } else {
-      q_at[h] = n0 + h * PN + ((lane % Q_CPR) ^ L::template key_across<Q_CPR>(q_row)) * V;
-      if constexpr (ALIGNED) q_at[h] = min(q_at[h], p.n - V);
+      for (int j = 0; j < JQ; ++j)
+        q_off[h][j] = min(n0 + (GATED ? 0 : h * PN) + q_row + j * Q_NEXT, n_last) * ldq + q_at[h][j % PAR];
     }
   }
   // rows of the contraction that stand for others: a stretch of the list at a time in LDS (a look-up in memory would have to wait
@@ -159,20 +177,24 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     a.q[1] = GATED ? q1 + k0 : a.q[0];
     return a;
   };
-  const unsigned to = lds0 + wave * 1024;
+  const unsigned to = lds0 + wave * (64 * UNIT * EB);
+  auto dma = [](const void* src, unsigned at) {
+    if constexpr (UNIT * EB == 16) ffn_dma16(src, at);
+    else ffn_dma4(src, at);
+  };
   auto request_p = [&](const Ask& a, auto half, auto stage, auto which) {
     constexpr int h = decltype(half)::value, j = decltype(which)::value;
     const T* src;
     bool in;
     if constexpr (P_ALONG) {
       src = a.p + p_off[h][j];
-      in = a.k0 + p_at[0] < k_end;
+      in = a.k0 + p_at[0][j % PAR] < k_end;
     } else {
       const int k = a.k0 + p_row + j * P_NEXT;
       in = k < k_end;
-      src = a.p + p_at[h] + (LISTED && list && !q_listed ? listed_row[j] : k) * ldp;
+      src = a.p + p_at[h][j % PAR] + (LISTED && list && !q_listed ? listed_row[j] : k) * ldp;
     }
-    ffn_dma16(in ? (const void*)src : zeros, to + at_p(h, decltype(stage)::value) + j * NT * 16);
+    dma(in ? (const void*)src : zeros, to + at_p(h, decltype(stage)::value) + j * NT * UNIT * EB);
   };
   auto request_q = [&](const Ask& a, auto half, auto stage, auto which) {
     constexpr int h = decltype(half)::value, j = decltype(which)::value;
@@ -180,37 +202,37 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
     bool in;
     if constexpr (Q_ALONG) {
       src = a.q[h] + q_off[h][j];
-      in = a.k0 + q_at[0] < k_end;
+      in = a.k0 + q_at[0][j % PAR] < k_end;
     } else {
       const int k = a.k0 + q_row + j * Q_NEXT;
       in = k < k_end;
-      src = a.q[h] + q_at[h] + (LISTED && q_listed ? listed_row[j] : k) * ldq;
+      src = a.q[h] + q_at[h][j % PAR] + (LISTED && q_listed ? listed_row[j] : k) * ldq;
     }
-    ffn_dma16(in ? (const void*)src : zeros, to + at_q(h, decltype(stage)::value) + j * NT * 16);
+    dma(in ? (const void*)src : zeros, to + at_q(h, decltype(stage)::value) + j * NT * UNIT * EB);
   };
   // rows of any length: through registers.  The source of a group of K tile kt, and how many of its entries there are
   auto p_src = [&](int kt, int h, int j, int& have) -> const T* {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     const T* const base = seg ? p1 : p0;
     if constexpr (P_ALONG) {
-      have = min(V, p.k - (k0 + p_at[h]));
+      have = min(V, p.k - (k0 + p_at[h][0]));
       return base + p_off[h][j] + k0;
     } else {
       const int k = k0 + p_row + j * P_NEXT;
-      have = k < p.k ? min(V, p.m - p_at[h]) : 0;
-      return base + (have > 0 ? p_k(k) * ldp + p_at[h] : 0);
+      have = k < p.k ? min(V, p.m - p_at[h][0]) : 0;
+      return base + (have > 0 ? p_k(k) * ldp + p_at[h][0] : 0);
     }
   };
   auto q_src = [&](int kt, int h, int j, int& have) -> const T* {
     const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
     const T* const base = (GATED ? h : seg) ? q1 : q0;
     if constexpr (Q_ALONG) {
-      have = min(V, p.k - (k0 + q_at[h]));
+      have = min(V, p.k - (k0 + q_at[h][0]));
       return base + q_off[h][j] + k0;
     } else {
       const int k = k0 + q_row + j * Q_NEXT;
-      have = k < p.k ? min(V, p.n - q_at[h]) : 0;
-      return base + (have > 0 ? q_k(k) * ldq + q_at[h] : 0);
+      have = k < p.k ? min(V, p.n - q_at[h][0]) : 0;
+      return base + (have > 0 ? q_k(k) * ldq + q_at[h][0] : 0);
     }
   };
   v4i held[2 * (JP + JQ)];
@@ -361,7 +383,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
       }
     }
   };
-  if constexpr (ALIGNED) {
+  if constexpr (DMA) {
     // Two K tiles in LDS, each in four halves.  The quadrants of a tile are multiplied in the order (P0, Q0), (P0, Q1), (P1, Q1),
     // (P1, Q0).  The operands of a quadrant are read from LDS one or two quadrants before, into registers that are free by then, and a
     // half's place in LDS is taken by the same half of the tile after next as soon as it is in everybody's registers: wavefronts meet
@@ -390,12 +412,17 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
       meet(std::integral_constant<int, 5 * JP>{});
       ffn_for<0, L::STEPS>([&](auto ks) { read_q(c0, c0, c0, ks); read_p(c0, c0, ks); });
       meet(std::integral_constant<int, 4 * JP>{});
+      constexpr int EACH = (JP + L::STEPS - 1) / L::STEPS;     // transfers behind a step
+      auto some = [&](auto ks, auto&& request) {
+        constexpr int lo = decltype(ks)::value * EACH, hi = lo + EACH < JP ? lo + EACH : JP;
+        ffn_for<lo, hi>(request);
+      };
       // tile kt in `stage`, its first half of Q in registers `now`, that of the next tile goes into `next`
       auto tile = [&](int kt, auto stage, auto other, auto now, auto next) {
         // a: the next tile's
         quadrant(c0, c0, now, [&](auto ks) {
           read_q(stage, c1, c1, ks);
-          if constexpr (decltype(ks)::value < JP) request_p(a, c1, other, ks);
+          some(ks, [&](auto j) { request_p(a, c1, other, j); });
         });
         meet(std::integral_constant<int, 3 * JP>{});
         // (behind the last tiles the last one again, which nobody reads: the counts stay, and a branch would cost registers)
@@ -405,16 +432,16 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
         a = prepare(ahead);
         quadrant(c0, c1, c1, [&](auto ks) {
           read_p(stage, c1, ks);
-          if constexpr (decltype(ks)::value < JQ) request_q(a, c0, stage, ks);
+          some(ks, [&](auto j) { request_q(a, c0, stage, j); });
         });
         quadrant(c1, c1, c1, [&](auto ks) {
           read_q(other, c0, next, ks);
-          if constexpr (decltype(ks)::value < JP) request_p(a, c0, stage, ks);
+          some(ks, [&](auto j) { request_p(a, c0, stage, j); });
         });
         meet(std::integral_constant<int, 3 * JP>{});
         quadrant(c1, c0, now, [&](auto ks) {
           read_p(other, c0, ks);
-          if constexpr (decltype(ks)::value < JQ) request_q(a, c1, stage, ks);
+          some(ks, [&](auto j) { request_q(a, c1, stage, j); });
         });
       };
       for (int kt = kt_lo;;) {
@@ -450,12 +477,20 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   // ---- results: the lane has row l32 of a block, its columns 16 h .. 16 h + 15 ----
   const int n = p.n, m = p.m;
   auto store = [&](T* c, int64_t ldc, int row, int col, const floatx16& v) {      // row < 0: none
-    if constexpr (ALIGNED) {
+    if constexpr (ROWS == kFfnWholeRows) {
       store_block_pairs<DT, false>(v, row, false, col, c, nullptr, 0, (int)ldc);
     } else if (row >= 0) {
+      T out[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (col + e < n) c[(int64_t)row * ldc + col + e] = E::from_float(v[e]);
+      for (int e = 0; e < 16; ++e) out[e] = E::from_float(v[e]);
+      T* const dst = c + (int64_t)row * ldc + col;
+      if (col + 16 <= n) {
+        __builtin_memcpy(dst, out, sizeof(out));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (col + e < n) dst[e] = out[e];
+      }
     }
   };
   auto load16 = [&](const T* c, int64_t ldc, int row, int col, float (&out)[16]) {
@@ -508,7 +543,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
         store(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
         store(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
       } else {
-        if (WHAT == kFfnWGrad && p.splits > 1) {
+        if (p.splits > 1) {
           if (row >= 0) {
             float* dst = p.partial + (((int64_t)z * p.splits + split) * m + row) * n + col;
 #pragma unroll
@@ -523,9 +558,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
   }
 }
 
-template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int ROWS>
 hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
-  auto kernel = ffn_gemm_kernel<DT, P_ALONG, Q_ALONG, WHAT, BM, BN, WAVES_M, WAVES_N, ALIGNED>;
+  auto kernel = ffn_gemm_kernel<DT, P_ALONG, Q_ALONG, WHAT, BM, BN, WAVES_M, WAVES_N, ROWS>;
   constexpr int cols = WHAT == kFfnUp ? BN / 2 : BN;
   g.m_tiles = (g.m + BM - 1) / BM;
   g.n_tiles = (g.n + cols - 1) / cols;
@@ -541,19 +576,22 @@ hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
 }
 
 template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT>
-hipError_t ffn_launch_what(const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
-  if (!aligned) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, false>(g, s);
-  if (tile == 1) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 256, 2, 4, true>(g, s);
-  return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, true>(g, s);
+hipError_t ffn_launch_what(const FfnGemm& g, int tile, int rows, hipStream_t s) {
+  if constexpr (DT != kF32)
+    if (rows == kFfnAnyRows) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, kFfnAnyRows>(g, s);
+  if (rows != kFfnWholeRows) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, kFfnWordRows>(g, s);
+  if constexpr (DT != kF32)
+    if (tile == 1) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 256, 2, 4, kFfnWholeRows>(g, s);
+  return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, kFfnWholeRows>(g, s);
 }
 
-template <int DT> hipError_t ffn_launch_type(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s) {
+template <int DT> hipError_t ffn_launch_type(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s) {
   switch (what) {
-    case kFfnUp: return ffn_launch_what<DT, true, true, kFfnUp>(g, tile, aligned, s);
-    case kFfnDown: return ffn_launch_what<DT, true, true, kFfnDown>(g, tile, aligned, s);
-    case kFfnGateGrad: return ffn_launch_what<DT, true, false, kFfnGateGrad>(g, tile, aligned, s);
-    case kFfnInGrad: return ffn_launch_what<DT, true, false, kFfnInGrad>(g, tile, aligned, s);
-    case kFfnWGrad: return ffn_launch_what<DT, false, false, kFfnWGrad>(g, tile, aligned, s);
+    case kFfnUp: return ffn_launch_what<DT, true, true, kFfnUp>(g, tile, rows, s);
+    case kFfnDown: return ffn_launch_what<DT, true, true, kFfnDown>(g, tile, rows, s);
+    case kFfnGateGrad: return ffn_launch_what<DT, true, false, kFfnGateGrad>(g, tile, rows, s);
+    case kFfnInGrad: return ffn_launch_what<DT, true, false, kFfnInGrad>(g, tile, rows, s);
+    case kFfnWGrad: return ffn_launch_what<DT, false, false, kFfnWGrad>(g, tile, rows, s);
     default: return hipErrorInvalidValue;
   }
 }

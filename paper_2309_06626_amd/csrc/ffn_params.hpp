@@ -18,6 +18,10 @@ enum FfnProduct : int32_t {
   kFfnProducts = 5
 };
 
+// How the rows of the operands lie: whole 16-byte groups; whole words (of floats any row, of 16-bit entries an even number); any number of
+// 16-bit entries, which pass through registers.
+enum FfnRows : int { kFfnWholeRows = 0, kFfnWordRows = 1, kFfnAnyRows = 2 };
+
 struct FfnGemm {
   const void* p[2];
   const void* q[2];
@@ -32,16 +36,16 @@ struct FfnGemm {
   const int32_t* c_rows;       // row of c that receives result row i; null: i
   void* saved;                 // kFfnUp: [3][m][n] or null, c[0] is then its third matrix.  kFfnGateGrad: read
   int32_t activation;
-  int32_t splits;              // kFfnWGrad: parts of the contraction, each with partial sums in `partial`
+  int32_t splits;              // not kFfnUp, kFfnGateGrad: parts of the contraction, each with its sums in `partial`
   float* partial;              // [batch][splits][m][n]
   // set by the launcher
   int32_t m_tiles, n_tiles, group;
 };
 
-// tile: index into the launcher's list of tile shapes; aligned: rows of all operands are whole 16-byte groups
-hipError_t ffn_launch_bf16(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
-hipError_t ffn_launch_f16(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
-hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, bool aligned, hipStream_t s);
+// tile: index into the launcher's list of tile shapes; rows: FfnRows
+hipError_t ffn_launch_bf16(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s);
+hipError_t ffn_launch_f16(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s);
+hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s);
 
 // kFfnUp (gated) and kFfnDown for a few rows
 hipError_t ffn_few_bf16(bool gated, const FfnGemm& g, bool whole, hipStream_t s);
