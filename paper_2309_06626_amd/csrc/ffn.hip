@@ -7,6 +7,7 @@
 // hidden, dg and du are rounded to the operands' type between the launches (they are operands of the next product); everything
 // else stays in float until it is stored.
 #include "../../include/sparse_block.h"
+#include "ffn_act.hpp"
 #include "ffn_params.hpp"
 #include "rows.hpp"
 
@@ -50,8 +51,8 @@ static int row_kind(const sc_ffn_desc& d) {
 // Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`.
 // Priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other: 256 workgroups of 256 x
 // 256 take 1.6 (128 or fewer 1.05, since the clock is higher), 512 of 128 x 128, two a compute unit, 1.06 (256 or fewer 0.42); across k on
-// both sides 1.75, 1.15, 1.2 and 0.62.  Floats take 4.1 and 2.05 in tiles of 128 and no less in tiles of 256, which have no float form.  A launch
-// and a tile's beginning and end take 8.  A contraction in parts leaves sums in float, written and read once at 4 TB/s, and another launch.
+// both sides 1.75, 1.15, 1.2 and 0.62.  Floats take 4.1 and 2.05 in tiles of 128 and no less in tiles of 256, which have no float form; rows
+// that are no 16-byte groups a third more.  A launch and a tile's beginning and end take 8.  A contraction in parts leaves sums in float, written and read once at 4 TB/s, and another launch.
 constexpr int kMostSplits = 32, kLeastTiles = 4;
 static int64_t k_tiles_of(int64_t k, int segments, int dtype) { return segments * ((k + (dtype == SC_F32 ? 31 : 63)) / (dtype == SC_F32 ? 32 : 64)); }
 
@@ -61,17 +62,18 @@ struct Tiling {
 };
 
 static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, int segments, int batch, int dtype, int layout) {
-  const bool across = what == kFfnWGrad, f32 = dtype == SC_F32, splittable = what != kFfnUp && what != kFfnGateGrad;
+  const bool across = what == kFfnWGrad, f32 = dtype == SC_F32;
   const int64_t k_tiles = k_tiles_of(k, segments, dtype);
   Tiling best = {0, 1, 1e30};
   for (int tile = 0; tile < 2; ++tile) {
     if (tile == 1 && (f32 || layout != kFfnWholeRows)) break;
     const int64_t edge = tile ? 256 : 128, room = tile ? 256 : 512;
-    const double half = f32 ? 2.05 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42);
-    const double full = f32 ? 4.1 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06);
+    const double words = layout == kFfnWholeRows ? 1.0 : 1.35;
+    const double half = words * (f32 ? 2.05 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42));
+    const double full = words * (f32 ? 4.1 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06));
     const int64_t tiles = ((m + edge - 1) / edge) * ((cols + edge - 1) / edge) * batch;
     for (int splits = 1; splits <= kMostSplits; ++splits) {
-      if (splits > 1 && (!splittable || k_tiles / splits < kLeastTiles)) break;
+      if (splits > 1 && k_tiles / splits < kLeastTiles) break;
       const int64_t count = tiles * splits, rest = count % room;
       if (splits > 1 && ((splits - 1) * tiles > room * (tile ? 1 : 2) || count > 2 * room)) break;
       const double rounds = (double)(count / room), left = rest == 0 ? 0.0 : rest <= room / 2 ? half : full;
@@ -91,42 +93,82 @@ static size_t most_parts(int64_t m, int64_t n, int64_t k, int segments, int batc
   return parts < 2 ? 0 : up256(std::min((size_t)parts * batch * m * n * 4, (size_t)128 << 20));
 }
 static size_t most_parts(const sc_ffn_desc& d, int64_t kept, bool training) {
-  size_t most = most_parts(kept, d.d_out, d.d_hidden, 1, 1, d.dtype);
+  size_t most = std::max(most_parts(kept, d.d_hidden, d.d_in, 1, 2, d.dtype), most_parts(kept, d.d_out, d.d_hidden, 1, 1, d.dtype));
   if (training)
-    most = std::max({most, most_parts(kept, d.d_in, d.d_hidden, 2, 1, d.dtype), most_parts(d.d_hidden, d.d_in, kept, 1, 2, d.dtype),
+    most = std::max({most, most_parts(kept, d.d_hidden, d.d_out, 1, 1, d.dtype), most_parts(kept, d.d_in, d.d_hidden, 2, 1, d.dtype), most_parts(d.d_hidden, d.d_in, kept, 1, 2, d.dtype),
                      most_parts(d.d_out, d.d_hidden, kept, 1, 1, d.dtype)});
   return most;
 }
 
-// sums of the parts, in order, into the rows of c; a row of a result a workgroup, blockIdx.y the result
-template <typename T, int WIDTH>
-__global__ __launch_bounds__(256) void ffn_sum_parts_kernel(const float* __restrict__ partial, T* c0, T* c1, int64_t ldc,
-                                                            const int32_t* __restrict__ c_rows, int m, int n, int splits) {
+// The parts added up, in order, and what the product's own epilogue would have done; a row of a result a workgroup, blockIdx.y the result.
+template <typename T, int WIDTH, int WHAT> __global__ __launch_bounds__(256) void ffn_finish_kernel(const FfnGemm g) {
   typedef float vec __attribute__((ext_vector_type(WIDTH)));
-  const int z = blockIdx.y, row = blockIdx.x;
-  const float* p = partial + ((int64_t)z * splits * m + row) * n;
-  T* c = (z ? c1 : c0) + (c_rows ? (int64_t)c_rows[row] : row) * ldc;
-  for (int i = threadIdx.x * WIDTH; i < n; i += 256 * WIDTH) {
-    vec v = *reinterpret_cast<const vec*>(p + i);
-    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const vec*>(p + (int64_t)s * m * n + i);
+  const int row = blockIdx.x, n = g.n;
+  const int64_t whole = (int64_t)g.m * n;
+  auto sum = [&](int z, int i) -> vec {
+    const float* p = g.partial + (int64_t)z * g.splits * whole + (int64_t)row * n + i;
+    vec v = *reinterpret_cast<const vec*>(p);
+    for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const vec*>(p + s * whole);
+    return v;
+  };
+  auto store = [&](void* c, int64_t at, vec v) {
     T out[WIDTH];
 #pragma unroll
     for (int u = 0; u < WIDTH; ++u) out[u] = (T)v[u];
-    __builtin_memcpy(c + i, out, sizeof(out));
+    __builtin_memcpy(static_cast<T*>(c) + at, out, sizeof(out));
+  };
+  for (int i = threadIdx.x * WIDTH; i < n; i += 256 * WIDTH) {
+    const int64_t at = (int64_t)row * n + i;
+    if constexpr (WHAT == kFfnUp) {
+      const vec gate = sum(0, i), up = sum(1, i);
+      vec hidden;
+#pragma unroll
+      for (int u = 0; u < WIDTH; ++u) {
+        float a, da;
+        ffn_act(g.activation, gate[u], a, da);
+        hidden[u] = a * up[u];
+      }
+      store(g.c[0], at, hidden);
+      if (g.saved) {
+        store(g.saved, at, gate);
+        store(static_cast<T*>(g.saved) + whole, at, up);
+      }
+    } else if constexpr (WHAT == kFfnGateGrad) {
+      const vec dh = sum(0, i);
+      T gate[WIDTH], up[WIDTH];
+      __builtin_memcpy(gate, static_cast<const T*>(g.saved) + at, sizeof(gate));
+      __builtin_memcpy(up, static_cast<const T*>(g.saved) + whole + at, sizeof(up));
+      vec dg, du;
+#pragma unroll
+      for (int u = 0; u < WIDTH; ++u) {
+        float a, da;
+        ffn_act(g.activation, (float)gate[u], a, da);
+        dg[u] = dh[u] * (float)up[u] * da;
+        du[u] = dh[u] * a;
+      }
+      store(g.c[0], at, dg);
+      store(g.c[1], at, du);
+    } else {
+      store(g.c[blockIdx.y], (g.c_rows ? (int64_t)g.c_rows[row] : row) * g.ldc + i, sum(blockIdx.y, i));
+    }
   }
 }
 
-template <typename T> static hipError_t sum_parts_type(const FfnGemm& g, hipStream_t s) {
-  const dim3 grid((unsigned)g.m, g.batch);
-  T *c0 = static_cast<T*>(g.c[0]), *c1 = static_cast<T*>(g.c[1]);
-  if (g.n % 4 == 0) ffn_sum_parts_kernel<T, 4><<<grid, dim3(256), 0, s>>>(g.partial, c0, c1, g.ldc, g.c_rows, g.m, g.n, g.splits);
-  else ffn_sum_parts_kernel<T, 1><<<grid, dim3(256), 0, s>>>(g.partial, c0, c1, g.ldc, g.c_rows, g.m, g.n, g.splits);
-  return hipGetLastError();
+template <typename T, int WIDTH> static void finish_width(FfnProduct what, const FfnGemm& g, hipStream_t s) {
+  const dim3 grid((unsigned)g.m, g.batch), block(256);
+  if (what == kFfnUp) ffn_finish_kernel<T, WIDTH, kFfnUp><<<grid, block, 0, s>>>(g);
+  else if (what == kFfnGateGrad) ffn_finish_kernel<T, WIDTH, kFfnGateGrad><<<grid, block, 0, s>>>(g);
+  else ffn_finish_kernel<T, WIDTH, kFfnDown><<<grid, block, 0, s>>>(g);
 }
-static hipError_t sum_parts(int dtype, const FfnGemm& g, hipStream_t s) {
-  if (dtype == SC_BF16) return sum_parts_type<__bf16>(g, s);
-  if (dtype == SC_F16) return sum_parts_type<_Float16>(g, s);
-  return sum_parts_type<float>(g, s);
+template <typename T> static void finish_type(FfnProduct what, const FfnGemm& g, hipStream_t s) {
+  if (g.n % 4 == 0) finish_width<T, 4>(what, g, s);
+  else finish_width<T, 1>(what, g, s);
+}
+static hipError_t finish(int dtype, FfnProduct what, const FfnGemm& g, hipStream_t s) {
+  if (dtype == SC_BF16) finish_type<__bf16>(what, g, s);
+  else if (dtype == SC_F16) finish_type<_Float16>(what, g, s);
+  else finish_type<float>(what, g, s);
+  return hipGetLastError();
 }
 
 // a product in the tiles and parts that its sizes ask for
@@ -135,7 +177,7 @@ static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, int layout, f
   g.splits = t.splits;
   g.partial = parts;
   const hipError_t e = launch(dtype, what, g, t.tile, layout, s);
-  return e == hipSuccess && g.splits > 1 ? sum_parts(dtype, g, s) : e;
+  return e == hipSuccess && g.splits > 1 ? finish(dtype, what, g, s) : e;
 }
 // kFfnUp and kFfnDown
 static hipError_t multiply_forward(int dtype, FfnProduct what, FfnGemm& g, int layout, float* parts, hipStream_t s) {

@@ -504,6 +504,25 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
       for (int i = 0; i < V; ++i) out[g * V + i] = (float)e[i];
     }
   };
+  if (p.splits > 1) {                                          // sums of this part: [batch, or gate and up][splits][m][n]
+#pragma unroll
+    for (int mi = 0; mi < 2 * MB; ++mi) {
+      const int row = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
+#pragma unroll
+      for (int ni = 0; ni < 2 * NB; ++ni) {
+        const int col = n0 + (GATED ? 0 : ni / NB * PN) + (wn * NB + ni % NB) * 32 + 16 * h;
+        float* const dst = p.partial + (((int64_t)(GATED ? ni / NB : z) * p.splits + split) * m + row) * n + col;
+        if (row < m && col + 16 <= n) {
+          __builtin_memcpy(dst, &acc[mi][ni], 64);
+        } else if (row < m) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (col + e < n) dst[e] = acc[mi][ni][e];
+        }
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int mi = 0; mi < 2 * MB; ++mi) {
     const int i = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
@@ -543,16 +562,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
         store(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
         store(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
       } else {
-        if (p.splits > 1) {
-          if (row >= 0) {
-            float* dst = p.partial + (((int64_t)z * p.splits + split) * m + row) * n + col;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (col + e < n) dst[e] = acc[mi][ni][e];
-          }
-        } else {
-          store(static_cast<T*>(p.c[z]), p.ldc, out_row, col, acc[mi][ni]);
-        }
+        store(static_cast<T*>(p.c[z]), p.ldc, out_row, col, acc[mi][ni]);
       }
     }
   }

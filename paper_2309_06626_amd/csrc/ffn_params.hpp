@@ -36,8 +36,8 @@ struct FfnGemm {
   const int32_t* c_rows;       // row of c that receives result row i; null: i
   void* saved;                 // kFfnUp: [3][m][n] or null, c[0] is then its third matrix.  kFfnGateGrad: read
   int32_t activation;
-  int32_t splits;              // not kFfnUp, kFfnGateGrad: parts of the contraction, each with its sums in `partial`
-  float* partial;              // [batch][splits][m][n]
+  int32_t splits;              // parts of the contraction, each with its sums in `partial`
+  float* partial;              // [batch, or gate and up][splits][m][n]
   // set by the launcher
   int32_t m_tiles, n_tiles, group;
 };
