@@ -14,6 +14,7 @@
 #include "mma_common.hpp"
 #include "rows.hpp"
 
+#include <algorithm>
 #include <initializer_list>
 
 namespace sc {
@@ -34,9 +35,9 @@ struct NormParams {
   const void *dx_new, *dh;
   void *dx, *df, *dgate;
   float *dw[4];                        // w_post, b_post, w_pre, b_pre; null: not wanted
-  float* parts;                        // [blocks][4][d]
-  float* gate_parts;                   // [blocks][2][d]: a block's first gate group, its last one
-  int64_t rows_per_block;
+  float* parts;                        // [workgroups][4][d]
+  float* gate_parts;                   // [teams][2][d]: the gate that a team's rows begin with, the one they end with
+  int64_t rows_per_block;              // of a team
 };
 
 template <int CTRL, int ROWS> __device__ __forceinline__ float norm_dpp(float v) {
@@ -93,24 +94,31 @@ template <int NT> struct NormSums {
 // any address, and the row's last one, if it is not whole, channel by channel.
 template <typename T, int NT, int E, bool VEC> struct NormLane {
   static constexpr int V = 16 / (int)sizeof(T);
-  int d;
-  __device__ __forceinline__ int col(int e) const { return ((int)threadIdx.x + NT * (e / V)) * V + e % V; }
+  int d, lane;
+  struct Raw { T u[E]; };
+  __device__ __forceinline__ int col(int e) const { return (lane + NT * (e / V)) * V + e % V; }
   __device__ __forceinline__ bool in(int e) const { return col(e) < d; }
   __device__ __forceinline__ bool whole(int q) const { return VEC ? in(q * V) : col(q * V) + V <= d; }
-  __device__ __forceinline__ void load(const T* row, float (&v)[E]) const {
-    T u[E];
+  __device__ __forceinline__ void fetch(const T* row, Raw& r) const {
 #pragma unroll
     for (int q = 0; q < E / V; ++q) {
       if (whole(q)) {
-        if constexpr (VEC) *reinterpret_cast<v4i*>(u + q * V) = *reinterpret_cast<const v4i*>(row + col(q * V));
-        else __builtin_memcpy(u + q * V, row + col(q * V), 16);
+        if constexpr (VEC) *reinterpret_cast<v4i*>(r.u + q * V) = *reinterpret_cast<const v4i*>(row + col(q * V));
+        else __builtin_memcpy(r.u + q * V, row + col(q * V), 16);
       } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) u[q * V + i] = !VEC && in(q * V + i) ? row[col(q * V + i)] : T(0);
+        for (int i = 0; i < V; ++i) r.u[q * V + i] = !VEC && in(q * V + i) ? row[col(q * V + i)] : T(0);
       }
     }
+  }
+  static __device__ __forceinline__ void widen(const Raw& r, float (&v)[E]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = (float)u[e];
+    for (int e = 0; e < E; ++e) v[e] = (float)r.u[e];
+  }
+  __device__ __forceinline__ void load(const T* row, float (&v)[E]) const {
+    Raw r;
+    fetch(row, r);
+    widen(r, v);
   }
   __device__ __forceinline__ void store(T* row, const float (&v)[E]) const {
 #pragma unroll
@@ -136,7 +144,9 @@ template <typename T, int NT, int E, bool VEC> struct NormLane {
   __device__ __forceinline__ void load_param(const float* p, float otherwise, float (&v)[E]) const {
 #pragma unroll
     for (int e = 0; e < E; e += 4) {
-      v4f g = {otherwise, otherwise, otherwise, otherwise};
+      v4f g;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = in(e + i) ? otherwise : 0.0f;
       if (p && (VEC ? in(e) : in(e + 3))) {
         g = *reinterpret_cast<const v4f*>(p + col(e));      // (the parameters themselves are aligned)
       } else if (!VEC && p) {
@@ -177,7 +187,8 @@ __device__ __forceinline__ void norm_row(int kind, float eps, const Lane& lane, 
 template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) void norm_kernel(const NormParams p) {
   __shared__ float slots[2][2][8];
   NormSums<NT> sums{slots};
-  const NormLane<T, NT, E, VEC> lane{p.d};
+  using Lane = NormLane<T, NT, E, VEC>;
+  const Lane lane{p.d, (int)threadIdx.x};
   float w_post[E], b_post[E], w_pre[E], b_pre[E], gate[E];
   lane.load_param(p.w_post, 1.0f, w_post);
   lane.load_param(p.b_post, 0.0f, b_post);
@@ -190,18 +201,16 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
     const int64_t fr = !p.f ? -1 : p.f_slot ? p.f_slot[r] : r, hr = !p.h ? -1 : p.h_slot ? p.h_slot[r] : r;
     float x[E], v[E];
     lane.load(static_cast<const T*>(p.x) + r * p.d, x);
+    if (fr >= 0) lane.load(static_cast<const T*>(p.f) + fr * p.d, v);
     float mean1 = 0.0f, rstd1 = 0.0f, mean2 = 0.0f, rstd2 = 0.0f;
-    if (fr >= 0) {
-      lane.load(static_cast<const T*>(p.f) + fr * p.d, v);
-      if (p.gate && (uint32_t)r / p.rows_per_gate != group) {
-        group = (uint32_t)r / p.rows_per_gate;
-        lane.load(static_cast<const T*>(p.gate) + group * p.d, gate);
-      }
+    if (fr >= 0 && p.gate && (uint32_t)r / p.rows_per_gate != group) {
+      group = (uint32_t)r / p.rows_per_gate;
+      lane.load(static_cast<const T*>(p.gate) + (int64_t)group * p.d, gate);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= p.a;
     if (fr >= 0) {
-      norm_row<decltype(lane), NT, E>(p.post, p.eps, lane, sums, v, mean1, rstd1);
+      norm_row<Lane, NT, E>(p.post, p.eps, lane, sums, v, mean1, rstd1);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] += p.b * gate[e] * (v[e] * w_post[e] + b_post[e]);
     }
@@ -209,7 +218,7 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
     if (hr >= 0) {
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = lane.in(e) ? x[e] : 0.0f;
-      norm_row<decltype(lane), NT, E>(p.pre, p.eps, lane, sums, x, mean2, rstd2);
+      norm_row<Lane, NT, E>(p.pre, p.eps, lane, sums, x, mean2, rstd2);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = x[e] * w_pre[e] + b_pre[e];
       lane.store(static_cast<T*>(p.h) + hr * p.d, x);
@@ -222,7 +231,7 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
 template <int NT, int E, bool IN_LDS> struct NormAcc {
   float v[IN_LDS ? 1 : E];
   float* at;
-  __device__ __forceinline__ explicit NormAcc(float* lds) : at(lds + threadIdx.x) { clear(); }
+  __device__ __forceinline__ explicit NormAcc(float* lds) : at(lds + threadIdx.x % NT) { clear(); }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -239,16 +248,23 @@ template <int NT, int E, bool IN_LDS> struct NormAcc {
     else return v[e];
   }
 };
-template <int NT, int E> constexpr int norm_acc_bytes() { return NT * E > 4096 ? 4 * NT * E * 4 : 0; }
+// Rows of up to 512 channels are a wavefront's: eight of them make a workgroup, each with rows of its own, and leave one part together.
+template <int NT> constexpr int norm_teams() { return NT == 64 ? 8 : 1; }
+template <int NT, int E> constexpr int norm_acc_bytes() { return NT * E > 4096 ? 4 * NT * E * 4 : norm_teams<NT>() > 1 ? norm_teams<NT>() * NT * E * 4 : 0; }
 
-template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) void norm_backward_kernel(const NormParams p) {
+// PLAIN: two RMS norms and no biases, as decoders have them; the other forms keep means and gradients of biases too
+template <typename T, int NT, int E, bool VEC, bool PLAIN>
+__global__ __launch_bounds__(NT * norm_teams<NT>()) void norm_backward_kernel(const NormParams p) {
   __shared__ float slots[2][2][8];
   NormSums<NT> sums{slots};
-  const NormLane<T, NT, E, VEC> lane{p.d};
+  constexpr int TEAMS = norm_teams<NT>();
+  using Lane = NormLane<T, NT, E, VEC>;
+  Lane lane{p.d, (int)threadIdx.x % NT};
+  const int64_t team = TEAMS > 1 ? (int64_t)blockIdx.x * TEAMS + __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : blockIdx.x;
   float w_post[E], b_post[E], w_pre[E], gate[E];
   auto load_params = [&]() {
     lane.load_param(p.w_post, 1.0f, w_post);
-    lane.load_param(p.b_post, 0.0f, b_post);
+    if constexpr (!PLAIN) lane.load_param(p.b_post, 0.0f, b_post);
   };
   constexpr bool KEPT = NT * E <= 4096;      // otherwise there are no registers for the parameters: from the caches for every row
   if constexpr (KEPT) {
@@ -257,11 +273,12 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
   }
   extern __shared__ float acc_lds[];
   NormAcc<NT, E, false> dw_post(acc_lds);
-  NormAcc<NT, E, !KEPT> db_post(acc_lds), dw_pre(acc_lds + NT * E), db_pre(acc_lds + 2 * NT * E), dgate(acc_lds + 3 * NT * E);
+  NormAcc<NT, E, !KEPT> dw_pre(acc_lds + NT * E), dgate(acc_lds + 3 * NT * E);
+  NormAcc<NT, PLAIN ? 1 : E, !KEPT && !PLAIN> db_post(acc_lds), db_pre(acc_lds + 2 * NT * E);
 #pragma unroll
   for (int e = 0; e < E; ++e) gate[e] = 1.0f;
   const float inv = 1.0f / (float)p.d;
-  const int64_t r0 = blockIdx.x * p.rows_per_block, r1 = r0 + p.rows_per_block < p.rows ? r0 + p.rows_per_block : p.rows;
+  const int64_t r0 = team * p.rows_per_block, r1 = r0 + p.rows_per_block < p.rows ? r0 + p.rows_per_block : p.rows;
   const int64_t first_group = p.gate ? r0 / p.rows_per_gate : 0;
   int64_t group = -1, group_end = r0;
   // the gate's rows [begin, end) end, or this block's do: its gradient is complete if all of them were here
@@ -274,7 +291,7 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
         for (int e = 0; e < E; ++e) v[e] = dgate.get(e);
         lane.store(static_cast<T*>(p.dgate) + group * p.d, v);
       } else {
-        float* part = p.gate_parts + ((int64_t)blockIdx.x * 2 + (group != first_group)) * p.d;
+        float* part = p.gate_parts + (team * 2 + (group != first_group)) * p.d;
 #pragma unroll
         for (int e = 0; e < E; ++e)
           if (lane.in(e)) part[lane.col(e)] = dgate.get(e);
@@ -282,13 +299,33 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
     }
     dgate.clear();
   };
+  // the next row is on its way while this one is summed, where there are registers for it
+  typename Lane::Raw next_x, next_f, next_t, next_dh;
+  int64_t next_fr = -1, next_hr = -1;
+  auto fetch = [&](int64_t r) {
+    next_fr = !p.f ? -1 : p.f_slot ? p.f_slot[r] : r;
+    next_hr = !p.dh ? -1 : p.h_slot ? p.h_slot[r] : r;
+    lane.fetch(static_cast<const T*>(p.x) + r * p.d, next_x);
+    if (next_fr >= 0) lane.fetch(static_cast<const T*>(p.f) + next_fr * p.d, next_f);
+    if constexpr (KEPT) {
+      if (p.dx_new) lane.fetch(static_cast<const T*>(p.dx_new) + r * p.d, next_t);
+      if (next_hr >= 0) lane.fetch(static_cast<const T*>(p.dh) + next_hr * p.d, next_dh);
+    }
+  };
+  if (KEPT && r0 < r1) fetch(r0);
   for (int64_t r = r0; r < r1; ++r) {
-    const int64_t fr = !p.f ? -1 : p.f_slot ? p.f_slot[r] : r, hr = !p.dh ? -1 : p.h_slot ? p.h_slot[r] : r;
     float x[E], f[E], t[E], dh[E];
-    lane.load(static_cast<const T*>(p.x) + r * p.d, x);
-    if (KEPT && p.dx_new) lane.load(static_cast<const T*>(p.dx_new) + r * p.d, t);
-    if (fr >= 0) lane.load(static_cast<const T*>(p.f) + fr * p.d, f);
-    if (KEPT && hr >= 0) lane.load(static_cast<const T*>(p.dh) + hr * p.d, dh);
+    if constexpr (!KEPT) {
+      __builtin_amdgcn_sched_barrier(0);      // (nothing of this row before the last one's end, and no addresses kept: registers)
+      asm volatile("" : "+v"(lane.lane));
+      fetch(r);
+    }
+    const int64_t fr = next_fr, hr = next_hr;
+    Lane::widen(next_x, x);
+    if (fr >= 0) Lane::widen(next_f, f);
+    if (KEPT && p.dx_new) Lane::widen(next_t, t);
+    if (KEPT && hr >= 0) Lane::widen(next_dh, dh);
+    if (KEPT && r + 1 < r1) fetch(r + 1);
     const v4f st = *reinterpret_cast<const v4f*>(p.stats + 4 * r);
     if constexpr (!KEPT) load_params();
     if (p.gate && r == group_end) {
@@ -301,17 +338,18 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
 #pragma unroll
       for (int e = 0; e < E; ++e) t[e] = 0.0f;
     }
-    if (fr >= 0 && p.post != SC_NORM_NONE) {
+    if (fr >= 0 && (PLAIN || p.post != SC_NORM_NONE)) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) f[e] = lane.in(e) ? (f[e] - st[0]) * st[1] : 0.0f;
+      for (int e = 0; e < E; ++e) f[e] = (PLAIN ? f[e] : f[e] - st[0]) * st[1];
     }
     if (hr >= 0) {
       // x becomes the normalised row of x'
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         x[e] *= p.a;
-        if (fr >= 0) x[e] += p.b * gate[e] * (f[e] * w_post[e] + b_post[e]);
-        if (p.pre != SC_NORM_NONE) x[e] = (x[e] - st[2]) * st[3];
+        if (fr >= 0) x[e] += p.b * gate[e] * (PLAIN ? f[e] * w_post[e] : f[e] * w_post[e] + b_post[e]);
+        if constexpr (PLAIN) x[e] *= st[3];
+        else if (p.pre != SC_NORM_NONE) x[e] = (x[e] - st[2]) * st[3];
       }
       if constexpr (!KEPT) {
         __builtin_amdgcn_sched_barrier(0);
@@ -321,19 +359,19 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
       float s = 0.0f, u = 0.0f;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        if (!lane.in(e)) x[e] = 0.0f;
-        dw_pre.add(e, dh[e] * x[e]);
-        db_pre.add(e, dh[e]);
+        dw_pre.add(e, dh[e] * x[e]);      // (beyond the row's end dh and the weights are 0, and so is what follows)
+        if constexpr (!PLAIN) db_pre.add(e, dh[e]);
         dh[e] *= w_pre[e];
         s += dh[e] * x[e];
-        u += dh[e];
+        if constexpr (!PLAIN) u += dh[e];
       }
-      if (p.pre != SC_NORM_NONE) {
-        sums(s, u);
+      if (PLAIN || p.pre != SC_NORM_NONE) {
+        if constexpr (PLAIN) s = sums.one(s);
+        else sums(s, u);
         s *= inv;
-        u = p.pre == SC_NORM_LAYER ? u * inv : 0.0f;
+        u = !PLAIN && p.pre == SC_NORM_LAYER ? u * inv : 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) dh[e] = st[3] * (dh[e] - x[e] * s - u);
+        for (int e = 0; e < E; ++e) dh[e] = st[3] * (PLAIN ? dh[e] - x[e] * s : dh[e] - x[e] * s - u);
       }
     }
     if (!KEPT && p.dx_new) {
@@ -350,26 +388,31 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
       for (int e = 0; e < E; ++e) dx[e] = p.a * t[e];
       lane.store(static_cast<T*>(p.dx) + r * p.d, dx);
     }
+    if constexpr (!KEPT) {
+      __builtin_amdgcn_sched_barrier(0);
+      load_params();
+    }
     if (fr >= 0) {
       float s = 0.0f, u = 0.0f;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float q = lane.in(e) ? p.b * t[e] : 0.0f;
-        dgate.add(e, q * (f[e] * w_post[e] + b_post[e]));
+        const float q = p.b * t[e], n = PLAIN ? f[e] * w_post[e] : f[e] * w_post[e] + b_post[e];
+        dgate.add(e, q * n);
         const float g = q * gate[e];
         dw_post.add(e, g * f[e]);
-        db_post.add(e, g);
+        if constexpr (!PLAIN) db_post.add(e, g);
         t[e] = g * w_post[e];
         s += t[e] * f[e];
-        u += t[e];
+        if constexpr (!PLAIN) u += t[e];
       }
       if (p.df) {
-        if (p.post != SC_NORM_NONE) {
-          sums(s, u);
+        if (PLAIN || p.post != SC_NORM_NONE) {
+          if constexpr (PLAIN) s = sums.one(s);
+          else sums(s, u);
           s *= inv;
-          u = p.post == SC_NORM_LAYER ? u * inv : 0.0f;
+          u = !PLAIN && p.post == SC_NORM_LAYER ? u * inv : 0.0f;
 #pragma unroll
-          for (int e = 0; e < E; ++e) t[e] = st[1] * (t[e] - f[e] * s - u);
+          for (int e = 0; e < E; ++e) t[e] = st[1] * (PLAIN ? t[e] - f[e] * s : t[e] - f[e] * s - u);
         }
         lane.store(static_cast<T*>(p.df) + fr * p.d, t);
       }
@@ -379,52 +422,72 @@ template <typename T, int NT, int E, bool VEC> __global__ __launch_bounds__(NT) 
   auto leave = [&](int k, const auto& acc) {
     if (!p.dw[k]) return;
     float* part = p.parts + ((int64_t)blockIdx.x * 4 + k) * p.d;
+    if constexpr (TEAMS == 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (lane.in(e)) part[lane.col(e)] = acc.get(e);
+      for (int e = 0; e < E; ++e)
+        if (lane.in(e)) part[lane.col(e)] = acc.get(e);
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc_lds[threadIdx.x / NT * (NT * E) + lane.col(e)] = acc.get(e);
+      __syncthreads();
+      for (int c = threadIdx.x; c < p.d; c += TEAMS * NT) {
+        float v = 0.0f;
+#pragma unroll
+        for (int u = 0; u < TEAMS; ++u) v += acc_lds[u * (NT * E) + c];
+        part[c] = v;
+      }
+    }
   };
   leave(0, dw_post);
-  leave(1, db_post);
   leave(2, dw_pre);
-  leave(3, db_pre);
+  if constexpr (!PLAIN) {
+    leave(1, db_post);
+    leave(3, db_pre);
+  }
 }
 
-// Sums of the blocks' parts, in order: 32 columns a workgroup, eight lanes of blocks a column.  blockIdx.y: which parameter.
-__global__ __launch_bounds__(256) void norm_param_kernel(const NormParams p, int blocks) {
+// The parts added up, in order, 32 columns a workgroup and eight lanes of parts a column: the parameters wanted, then the gates (whose rows
+// lie in more than one team's stretch of p.rows_per_block; in all of these but the first the gate is the one that the stretch begins with).
+template <typename T> __global__ __launch_bounds__(256) void norm_finish_kernel(const NormParams p, int blocks, int params) {
   __shared__ float s[8][32];
-  float* out = p.dw[blockIdx.y];
-  if (!out) return;
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
-  const int per = (blocks + 7) / 8, lo = share * per, hi = lo + per < blocks ? lo + per : blocks;
+  const int col_blocks = (p.d + 31) / 32;
+  const int what = blockIdx.x / col_blocks, c = (blockIdx.x - what * col_blocks) * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
   float v = 0.0f;
-  if (c < p.d) {
-    const float* part = p.parts + (int64_t)blockIdx.y * p.d + c;
+  float* out = nullptr;
+  const int64_t group = what - params;
+  if (what < params) {
+    int k = 0;      // the what-th parameter that is wanted
+    for (int seen = 0; k < 4; ++k)
+      if (p.dw[k] && seen++ == what) break;
+    out = p.dw[k];
+    const int per = (blocks + 7) / 8, lo = share * per, hi = lo + per < blocks ? lo + per : blocks;
+    if (c < p.d) {
+      const float* part = p.parts + (int64_t)k * p.d + c;
 #pragma unroll 8
-    for (int b = lo; b < hi; ++b) v += part[(int64_t)b * 4 * p.d];
+      for (int b = lo; b < hi; ++b) v += part[(int64_t)b * 4 * p.d];
+    }
+  } else {
+    const int64_t begin = group * p.rows_per_gate, end = begin + p.rows_per_gate < p.rows ? begin + p.rows_per_gate : p.rows;
+    const int64_t lo = begin / p.rows_per_block, hi = (end - 1) / p.rows_per_block + 1;
+    if (lo + 1 == hi) return;      // finished there
+    const int64_t per = (hi - lo + 7) / 8, b0 = lo + share * per, b1 = b0 + per < hi ? b0 + per : hi;
+    if (c < p.d) {
+      const float* part = p.gate_parts + c;
+      int64_t b = b0;
+      if (b == lo && b < b1) v = part[(b++ * 2 + (begin > lo * p.rows_per_block)) * p.d];
+#pragma unroll 8
+      for (; b < b1; ++b) v += part[b * 2 * p.d];
+    }
   }
   s[share][threadIdx.x & 31] = v;
   __syncthreads();
   if (share == 0 && c < p.d) {
 #pragma unroll
     for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
-    out[c] = v;
+    if (out) out[c] = v;
+    else static_cast<T*>(p.dgate)[group * p.d + c] = (T)v;
   }
-}
-
-// The same for the gates whose rows lie in more than one block.
-template <typename T> __global__ __launch_bounds__(256) void norm_gate_kernel(const NormParams p) {
-  const int64_t group = blockIdx.x;
-  const int64_t begin = group * p.rows_per_gate, end = begin + p.rows_per_gate < p.rows ? begin + p.rows_per_gate : p.rows;
-  const int64_t lo = begin / p.rows_per_block, hi = (end - 1) / p.rows_per_block;
-  if (lo == hi) return;      // finished there
-  const int c = blockIdx.y * 256 + threadIdx.x;
-  if (c >= p.d) return;
-  float v = 0.0f;
-  for (int64_t b = lo; b <= hi; ++b) {
-    const int64_t first = b * p.rows_per_block / p.rows_per_gate;
-    v += p.gate_parts[(b * 2 + (group != first)) * p.d + c];
-  }
-  static_cast<T*>(p.dgate)[group * p.d + c] = (T)v;
 }
 
 constexpr int32_t kNormMost = 8192;      // channels: 512 lanes of 16
@@ -432,20 +495,33 @@ constexpr int32_t kNormMost = 8192;      // channels: 512 lanes of 16
 // ---- host ---------------------------------------------------------------------------------------------------------------------
 static size_t norm_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// blocks of the backward pass: one a compute unit, since each leaves parts as large as a few rows
-constexpr int64_t kNormBlocks = 512;
-static int64_t rows_per_block(int64_t rows) { return (rows + kNormBlocks - 1) / kNormBlocks; }
+// Teams of the backward pass: every workgroup leaves parts as large as a few rows, so there is one of eight wavefronts a compute unit, or
+// as many lanes in smaller ones.
+static int norm_team_size(int d) { return d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : 512; }
+static int64_t norm_most_teams(int d) { return 256 * 512 / norm_team_size(d); }
+static int norm_teams_together(int d) { return d <= 512 ? 8 : 1; }
+static int64_t norm_rows_per_team(int64_t rows, int d) {
+  const int64_t most = norm_most_teams(d);
+  return rows > 0 ? (rows + most - 1) / most : 1;
+}
+static int64_t norm_team_count(int64_t rows, int d) {
+  const int64_t per = norm_rows_per_team(rows, d);
+  return (rows + per - 1) / per;
+}
+static int64_t norm_block_count(int64_t rows, int d) {
+  return (norm_team_count(rows, d) + norm_teams_together(d) - 1) / norm_teams_together(d);
+}
 
 template <typename T, int NT, int E, bool VEC> static hipError_t norm_launch(const NormParams& p, bool backward, hipStream_t s) {
   if (backward) {
-    const int64_t blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
     constexpr int lds = norm_acc_bytes<NT, E>();
-    auto kernel = norm_backward_kernel<T, NT, E, VEC>;
-    if constexpr (lds > 0) {
+    const bool plain = p.post == SC_NORM_RMS && p.pre == SC_NORM_RMS && !p.b_post && !p.dw[1] && !p.dw[3];
+    auto kernel = plain ? norm_backward_kernel<T, NT, E, VEC, true> : norm_backward_kernel<T, NT, E, VEC, false>;
+    if constexpr (lds > 65536) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       if (e != hipSuccess) return e;
     }
-    kernel<<<dim3((unsigned)blocks), dim3(NT), lds, s>>>(p);
+    kernel<<<dim3((unsigned)norm_block_count(p.rows, p.d)), dim3(NT * norm_teams<NT>()), lds, s>>>(p);
   } else {
     const int64_t most = 262144 / NT;
     norm_kernel<T, NT, E, VEC><<<dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(NT), 0, s>>>(p);
@@ -540,8 +616,9 @@ sc_status sparse_norm_workspace_bytes(const sc_norm_desc* desc, int64_t rows, si
   *bytes = 0;
   const sc_status st = sc::check_norm(desc, rows);
   if (st != SC_OK) return st;
-  const int64_t blocks = rows < sc::kNormBlocks ? rows : sc::kNormBlocks;
-  *bytes = 256 + sc::norm_up((size_t)blocks * 4 * desc->d * 4) + sc::norm_up((size_t)blocks * 2 * desc->d * 4);
+  // (as many as there can be for up to this many rows)
+  const int64_t teams = std::min(rows, sc::norm_most_teams(desc->d)), together = sc::norm_teams_together(desc->d);
+  *bytes = 256 + sc::norm_up((size_t)((teams + together - 1) / together) * 4 * desc->d * 4) + sc::norm_up((size_t)teams * 2 * desc->d * 4);
   return SC_OK;
 }
 
@@ -581,27 +658,24 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
   p.df = df_dev;
   p.dgate = dgate_dev;
   float* const grads[4] = {dw_post_dev, db_post_dev, dw_pre_dev, db_pre_dev};
-  bool any = false;
+  int params = 0;
   for (int k = 0; k < 4; ++k) {
     p.dw[k] = grads[k];
-    any = any || grads[k];
+    params += grads[k] != nullptr;
   }
-  p.rows_per_block = rows > 0 ? sc::rows_per_block(rows) : 1;
-  const int64_t blocks = (rows + p.rows_per_block - 1) / p.rows_per_block;
+  p.rows_per_block = sc::norm_rows_per_team(rows, desc->d);
+  const int64_t blocks = sc::norm_block_count(rows, desc->d);
   p.parts = static_cast<float*>(workspace_dev);
   p.gate_parts = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + sc::norm_up((size_t)blocks * 4 * desc->d * 4));
   hipError_t e = hipSuccess;
   if (rows > 0) e = sc::norm_dispatch(desc->dtype, p, true, s);
-  if (e == hipSuccess && any) {
-    sc::norm_param_kernel<<<dim3((unsigned)((desc->d + 31) / 32), 4), dim3(256), 0, s>>>(p, (int)blocks);
-    e = hipGetLastError();
-  }
-  if (e == hipSuccess && rows > 0 && dgate_dev && blocks > 1 && p.rows_per_gate > 1) {
-    const int64_t groups = (rows + p.rows_per_gate - 1) / p.rows_per_gate;
-    const dim3 grid((unsigned)groups, (unsigned)((desc->d + 255) / 256));
-    if (desc->dtype == SC_BF16) sc::norm_gate_kernel<__bf16><<<grid, dim3(256), 0, s>>>(p);
-    else if (desc->dtype == SC_F16) sc::norm_gate_kernel<_Float16><<<grid, dim3(256), 0, s>>>(p);
-    else sc::norm_gate_kernel<float><<<grid, dim3(256), 0, s>>>(p);
+  const bool gates = rows > 0 && dgate_dev && sc::norm_team_count(rows, desc->d) > 1 && p.rows_per_gate > 1;
+  const int64_t units = (params + (gates ? (rows + p.rows_per_gate - 1) / p.rows_per_gate : 0)) * ((desc->d + 31) / 32);
+  if (e == hipSuccess && units > 0) {
+    const dim3 grid((unsigned)units);
+    if (desc->dtype == SC_BF16) sc::norm_finish_kernel<__bf16><<<grid, dim3(256), 0, s>>>(p, (int)blocks, params);
+    else if (desc->dtype == SC_F16) sc::norm_finish_kernel<_Float16><<<grid, dim3(256), 0, s>>>(p, (int)blocks, params);
+    else sc::norm_finish_kernel<float><<<grid, dim3(256), 0, s>>>(p, (int)blocks, params);
     e = hipGetLastError();
   }
   if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
