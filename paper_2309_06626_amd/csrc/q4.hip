@@ -9,7 +9,7 @@
 //   * scales act on a group's sums, four outputs a lane, and not on the codes;
 //   * the plan lays codes out in the order in which lanes take them: 16 outputs x 128 columns are 1 KB, read by one wavefront at once,
 //     its dword j the columns 32 j + 8 (lane / 16) .. + 7, in the nibble order that one AND-OR a pair undoes;
-//   * a workgroup has 16 outputs and eight wavefronts, which share the columns; their sums meet in LDS, in order.
+//   * a workgroup has 16 outputs and eight or sixteen wavefronts, which share the columns; their sums meet in LDS, in order.
 #include "../../include/sparse_block.h"
 #include "ffn_act.hpp"
 #include "mma_common.hpp"
@@ -28,7 +28,6 @@ namespace sc {
 
 void note_hip_error(int32_t code);
 
-constexpr int kQ4Waves = 8;
 constexpr int kQ4MostRows = 64;      // of a workgroup; more rows take more workgroups, which read the weights again
 
 template <int DT> struct Q4Elem;
@@ -92,12 +91,13 @@ struct Q4Params {
   int32_t k, n, blocks, groups, activation;
 };
 
-// GROUP columns share a scale; MT tiles of 16 rows; MATS 2: act(x gate') (x up')
-template <int DT, int GROUP, int MT, int MATS> __global__ __launch_bounds__(64 * kQ4Waves) void q4_kernel(const Q4Params p) {
+// GROUP columns share a scale; MT tiles of 16 rows; MATS 2: act(x gate') (x up'); AHEAD blocks of 128 columns asked for at once
+template <int DT, int GROUP, int MT, int MATS, int WAVES, int AHEAD>
+__global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Q4Params p) {
   using Q = Q4Elem<DT>;
   using T = typename Elem<DT>::T;
   constexpr int PER = GROUP / 32, GPB = 4 / PER;      // matrix instructions a group, groups a block of 128 columns
-  __shared__ float s_sum[kQ4Waves][MATS][MT][64][4];
+  extern __shared__ float q4_sum[];                   // [WAVES][MATS][MT][64][4]
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 15, kg = lane >> 4;
   const int64_t row0 = (int64_t)blockIdx.y * kQ4MostRows;
@@ -111,12 +111,10 @@ template <int DT, int GROUP, int MT, int MATS> __global__ __launch_bounds__(64 *
     scales[m] = static_cast<const v4i*>(p.scales[m]) + (int64_t)tile * p.groups * 4 + kg;
   }
   const T* x[MT];
-  bool here[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int64_t r = row0 + 16 * i + col;
-    here[i] = r < p.rows;
-    x[i] = static_cast<const T*>(p.x) + (here[i] ? r : 0) * p.k + 8 * kg;
+    const int64_t r = row0 + 16 * i + col;            // a row that is not there: the first one again, whose results are not stored
+    x[i] = static_cast<const T*>(p.x) + (r < p.rows ? r : 0) * p.k + 8 * kg;
   }
   const v4i ones = {(int)Q::ONES, (int)Q::ONES, (int)Q::ONES, (int)Q::ONES};
 
@@ -126,29 +124,38 @@ template <int DT, int GROUP, int MT, int MATS> __global__ __launch_bounds__(64 *
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[m][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
-  for (int b = wave; b < p.blocks; b += kQ4Waves) {
-    v4i w[MATS], sz[MATS][GPB], xf[MT][4];
+  struct Block { v4i w[MATS], sz[MATS][GPB], x[MT][4]; };
+  auto ask = [&](int b, Block& k) {
 #pragma unroll
     for (int m = 0; m < MATS; ++m) {
-      w[m] = codes[m][(int64_t)b * 64];
+      k.w[m] = codes[m][(int64_t)b * 64];
 #pragma unroll
-      for (int g = 0; g < GPB; ++g) sz[m][g] = scales[m][((int64_t)b * GPB + g) * 4];
+      for (int g = 0; g < GPB; ++g) k.sz[m][g] = scales[m][((int64_t)b * GPB + g) * 4];
     }
+    if ((b + 1) * 128 <= p.k) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int c = b * 128 + 32 * j, left = p.k - c - 8 * kg;
-        xf[i][j] = v4i{0, 0, 0, 0};
-        if (here[i] && left >= 8) {
-          __builtin_memcpy(&xf[i][j], x[i] + c, 16);
-        } else if (here[i] && left > 0) {      // the row ends in the middle of a group of eight
-          T e[8];
+        for (int j = 0; j < 4; ++j) __builtin_memcpy(&k.x[i][j], x[i] + b * 128 + 32 * j, 16);
+    } else {                                          // the rows end within this block
 #pragma unroll
-          for (int u = 0; u < 8; ++u) e[u] = u < left ? x[i][c + u] : T(0);
-          __builtin_memcpy(&xf[i][j], e, 16);
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = b * 128 + 32 * j, left = p.k - c - 8 * kg;
+          k.x[i][j] = v4i{0, 0, 0, 0};
+          if (left >= 8) {
+            __builtin_memcpy(&k.x[i][j], x[i] + c, 16);
+          } else if (left > 0) {
+            T e[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) e[u] = u < left ? x[i][c + u] : T(0);
+            __builtin_memcpy(&k.x[i][j], e, 16);
+          }
         }
-      }
+    }
+  };
+  auto add = [&](const Block& k) {
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
       v4f sum[MATS][MT], xs[MT];
@@ -161,21 +168,21 @@ template <int DT, int GROUP, int MT, int MATS> __global__ __launch_bounds__(64 *
 #pragma unroll
       for (int j = g * PER; j < (g + 1) * PER; ++j) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xs[i] = Q::mma(ones, xf[i][j], xs[i]);
+        for (int i = 0; i < MT; ++i) xs[i] = Q::mma(ones, k.x[i][j], xs[i]);
 #pragma unroll
         for (int m = 0; m < MATS; ++m) {
-          const unsigned c = (unsigned)w[m][j];
+          const unsigned c = (unsigned)k.w[m][j];
           v4i a;
 #pragma unroll
           for (int e = 0; e < 4; ++e) a[e] = (int)((c >> (4 * e) & 0x000f000fu) | Q::BIAS);
 #pragma unroll
-          for (int i = 0; i < MT; ++i) sum[m][i] = Q::mma(a, xf[i][j], sum[m][i]);
+          for (int i = 0; i < MT; ++i) sum[m][i] = Q::mma(a, k.x[i][j], sum[m][i]);
         }
       }
 #pragma unroll
       for (int m = 0; m < MATS; ++m) {
         T e[8];
-        __builtin_memcpy(e, &sz[m][g], 16);
+        __builtin_memcpy(e, &k.sz[m][g], 16);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float s = (float)e[q], z = Q::B + (float)e[4 + q];
@@ -184,22 +191,38 @@ template <int DT, int GROUP, int MT, int MATS> __global__ __launch_bounds__(64 *
         }
       }
     }
+  };
+  int b = wave;
+  for (; b + (AHEAD - 1) * WAVES < p.blocks; b += AHEAD * WAVES) {
+    Block k[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) ask(b + u * WAVES, k[u]);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) add(k[u]);
   }
+  if constexpr (AHEAD > 1) {
+    for (; b < p.blocks; b += WAVES) {
+      Block k;
+      ask(b, k);
+      add(k);
+    }
+  }
+  v4f* const mine = reinterpret_cast<v4f*>(q4_sum) + wave * (MATS * MT * 64) + lane;
 #pragma unroll
   for (int m = 0; m < MATS; ++m)
 #pragma unroll
-    for (int i = 0; i < MT; ++i) *reinterpret_cast<v4f*>(s_sum[wave][m][i][lane]) = acc[m][i];
+    for (int i = 0; i < MT; ++i) mine[(m * MT + i) * 64] = acc[m][i];
   __syncthreads();
   // value v of a tile: lane v / 4 of the accumulators, output 4 (lane / 16) + v % 4, row lane % 16
-  for (int at = t; at < MT * 256; at += 64 * kQ4Waves) {
+  for (int at = t; at < MT * 256; at += 64 * WAVES) {
     const int n16 = at & 15, r = at >> 4;      // outputs of one row next to each other
-    const int i = r >> 4, l = (n16 >> 2) * 16 + (r & 15), q = n16 & 3;
+    const int word = ((r >> 4) * 64 + (n16 >> 2) * 16 + (r & 15)) * 4 + (n16 & 3);
     float v[MATS];
 #pragma unroll
     for (int m = 0; m < MATS; ++m) {
       v[m] = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kQ4Waves; ++w) v[m] += s_sum[w][m][i][l][q];
+      for (int w = 0; w < WAVES; ++w) v[m] += q4_sum[(w * MATS + m) * (MT * 256) + word];
     }
     const int n = tile * 16 + n16;
     const int64_t row = row0 + r;
@@ -215,11 +238,23 @@ template <int DT, int GROUP, int MT, int MATS> __global__ __launch_bounds__(64 *
   }
 }
 
+template <int DT, int GROUP, int MT, int MATS, int WAVES, int AHEAD> static void q4_launch(const Q4Params& p, hipStream_t s) {
+  constexpr int lds = WAVES * MATS * MT * 1024;
+  static_assert(lds <= 65536, "no more than any kernel may have");
+  const dim3 grid((unsigned)((p.n + 15) / 16), (unsigned)((p.rows + kQ4MostRows - 1) / kQ4MostRows));
+  q4_kernel<DT, GROUP, MT, MATS, WAVES, AHEAD><<<grid, dim3(64 * WAVES), lds, s>>>(p);
+}
+// Sixteen wavefronts where there are no more than two workgroups a compute unit: they ask for as much at once as twice as many workgroups.
 template <int DT, int GROUP, int MATS> static void q4_launch_rows(const Q4Params& p, hipStream_t s) {
-  const dim3 grid((unsigned)((p.n + 15) / 16), (unsigned)((p.rows + kQ4MostRows - 1) / kQ4MostRows)), block(64 * kQ4Waves);
-  if (p.rows <= 16) q4_kernel<DT, GROUP, 1, MATS><<<grid, block, 0, s>>>(p);
-  else if (p.rows <= 32) q4_kernel<DT, GROUP, 2, MATS><<<grid, block, 0, s>>>(p);
-  else q4_kernel<DT, GROUP, 4, MATS><<<grid, block, 0, s>>>(p);
+  constexpr int AHEAD = GROUP == 32 && MATS == 2 ? 1 : 2;      // (registers)
+  if (p.rows <= 16) {
+    if (p.n <= 512 * 16) q4_launch<DT, GROUP, 1, MATS, 16, AHEAD>(p, s);
+    else q4_launch<DT, GROUP, 1, MATS, 8, 2>(p, s);
+  } else if (p.rows <= 32) {
+    q4_launch<DT, GROUP, 2, MATS, 8, 1>(p, s);
+  } else {
+    q4_launch<DT, GROUP, 4, MATS, 8, 1>(p, s);
+  }
 }
 template <int DT, int MATS> static void q4_launch_group(int group, const Q4Params& p, hipStream_t s) {
   if (group == 32) q4_launch_rows<DT, 32, MATS>(p, s);
