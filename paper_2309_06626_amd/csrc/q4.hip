@@ -246,7 +246,7 @@ template <int DT, int GROUP, int MT, int MATS, int WAVES, int AHEAD> static void
 }
 // Sixteen wavefronts where there are no more than two workgroups a compute unit: they ask for as much at once as twice as many workgroups.
 template <int DT, int GROUP, int MATS> static void q4_launch_rows(const Q4Params& p, hipStream_t s) {
-  constexpr int AHEAD = GROUP == 32 && MATS == 2 ? 1 : 2;      // (registers)
+  constexpr int AHEAD = MATS == 2 ? 1 : 2;      // of sixteen wavefronts: registers
   if (p.rows <= 16) {
     if (p.n <= 512 * 16) q4_launch<DT, GROUP, 1, MATS, 16, AHEAD>(p, s);
     else q4_launch<DT, GROUP, 1, MATS, 8, 2>(p, s);
