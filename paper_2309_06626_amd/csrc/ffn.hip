@@ -51,8 +51,8 @@ static int row_kind(const sc_ffn_desc& d) {
 // Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`.
 // Priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other: 256 workgroups of 256 x
 // 256 take 1.6 (128 or fewer 1.05, since the clock is higher), 512 of 128 x 128, two a compute unit, 1.06 (256 or fewer 0.42); across k on
-// both sides 1.75, 1.15, 1.2 and 0.62.  Floats take 4.1 and 2.05 in tiles of 128 and no less in tiles of 256, which have no float form; rows
-// that are no 16-byte groups a third more.  A launch and a tile's beginning and end take 8.  A contraction in parts leaves sums in float, written and read once at 4 TB/s, and another launch.
+// both sides 1.75, 1.15, 1.2 and 0.62.  Floats, in tiles of 128 alone, take 2.75 and 1.55; rows that are no
+// 16-byte groups a third more.  A launch and a tile's beginning and end take 8.  A contraction in parts leaves sums in float, written and read once at 4 TB/s, and another launch.
 constexpr int kMostSplits = 32, kLeastTiles = 4;
 static int64_t k_tiles_of(int64_t k, int segments, int dtype) { return segments * ((k + (dtype == SC_F32 ? 31 : 63)) / (dtype == SC_F32 ? 32 : 64)); }
 
@@ -69,8 +69,8 @@ static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, i
     if (tile == 1 && (f32 || layout != kFfnWholeRows)) break;
     const int64_t edge = tile ? 256 : 128, room = tile ? 256 : 512;
     const double words = layout == kFfnWholeRows ? 1.0 : 1.35;
-    const double half = words * (f32 ? 2.05 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42));
-    const double full = words * (f32 ? 4.1 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06));
+    const double half = words * (f32 ? 1.55 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42));
+    const double full = words * (f32 ? 2.75 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06));
     const int64_t tiles = ((m + edge - 1) / edge) * ((cols + edge - 1) / edge) * batch;
     for (int splits = 1; splits <= kMostSplits; ++splits) {
       if (splits > 1 && k_tiles / splits < kLeastTiles) break;

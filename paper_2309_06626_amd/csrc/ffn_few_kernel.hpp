@@ -35,7 +35,7 @@ template <> struct FewMma<kF32> {      // entry e of the four groups of a row: a
 template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FfnGemm p) {
   using T = typename Elem<DT>::T;
   constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V, MATS = GATED ? 2 : 1;
-  constexpr int AHEAD = MT == 1 ? 8 : 4;      // k steps whose operands a wavefront asks for at once
+  constexpr int AHEAD = 4;                    // k steps whose operands a wavefront asks for at once (gated, 1 x 2048 -> 5632: 11.5 us, 8: 13.5)
   extern __shared__ float few_sum[];          // [WAVES][MATS][MT][64][4]
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
@@ -45,12 +45,10 @@ template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch
 #pragma unroll
   for (int a = 0; a < MATS; ++a) w[a] = static_cast<const T*>(p.q[a]) + (int64_t)min(n0 + l16, p.n - 1) * p.ldq + kg * V;
   const T* x[MT];
-  bool here[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int r = row0 + 16 * i + l16;
-    here[i] = r < p.m;
-    x[i] = static_cast<const T*>(p.p[0]) + (here[i] ? p.p_rows ? (int64_t)p.p_rows[r] : r : 0) * p.ldp + kg * V;
+    const int r = min(row0 + 16 * i + l16, p.m - 1);      // a row that is not there: the last one again, whose results are not stored
+    x[i] = static_cast<const T*>(p.p[0]) + (p.p_rows ? (int64_t)p.p_rows[r] : r) * p.ldp + kg * V;
   }
   auto group = [=](const T* s, int left) -> v4i {      // `left` entries of a row from here on
     v4i g = {0, 0, 0, 0};
@@ -84,7 +82,7 @@ template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch
     for (int s = 0; s < AHEAD; ++s) {
       const int k = k0 + s * STEP, left = p.k - k - kg * V;
 #pragma unroll
-      for (int i = 0; i < MT; ++i) xf[i][s] = group(x[i] + k, here[i] ? left : 0);
+      for (int i = 0; i < MT; ++i) xf[i][s] = group(x[i] + k, left);
     }
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s)

@@ -39,6 +39,37 @@ __device__ __forceinline__ void ffn_dma4(const void* src, unsigned lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_base), "v"(src));
 }
 
+// Eight floats of a row in bf16 parts.  Cutting off keeps 8 bits a part, and what is left over is exact: hi + mid + lo is the float.
+struct FfnParts { v4i part[3]; };
+__device__ __forceinline__ FfnParts ffn_parts(v4i first, v4i second) {
+  unsigned bits[3][8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float left = __builtin_bit_cast(float, e < 4 ? first[e] : second[e - 4]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      bits[k][e] = __builtin_bit_cast(unsigned, left);
+      if (k < 2) left -= __builtin_bit_cast(float, bits[k][e] & 0xffff0000u);
+    }
+  }
+  FfnParts p;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.part[k][i] = (int)__builtin_amdgcn_perm(bits[k][2 * i + 1], bits[k][2 * i], 0x07060302u);
+  return p;
+}
+template <class E> __device__ __forceinline__ void ffn_mma(floatx16& acc, const v4i& q, const v4i& p) { E::mma(acc, q, p); }
+template <class E> __device__ __forceinline__ void ffn_mma(floatx16& acc, const FfnParts& q, const FfnParts& p) {
+  using B = Elem<kBF16>;      // the smallest products first
+  B::mma(acc, q.part[2], p.part[0]);
+  B::mma(acc, q.part[0], p.part[2]);
+  B::mma(acc, q.part[1], p.part[1]);
+  B::mma(acc, q.part[1], p.part[0]);
+  B::mma(acc, q.part[0], p.part[1]);
+  B::mma(acc, q.part[0], p.part[0]);
+}
+
 template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f) {
   if constexpr (I < N) {
     f(std::integral_constant<int, I>{});
@@ -47,7 +78,7 @@ template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f
 }
 
 template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int ROWS>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const FfnGemm p) {
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(const FfnGemm p) {
   using E = Elem<DT>;
   using T = typename E::T;
   constexpr int EB = sizeof(T);
@@ -337,33 +368,68 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[mi][ni][v] = 0.0f;
 
-  // operands: one half of P, both of Q, and the first half of Q of the next tile (the first and the third change places from tile to tile)
-  v4i pf[L::STEPS][MB], qf[3][L::STEPS][NB];
+  // operands: one half of P, both of Q, and the first half of Q of the next tile (the first and the third change places from tile to tile).
+  // Floats are multiplied in three bf16 parts (x = hi + mid + lo, exactly: 3 x 8 bits) on the 16-bit instruction, six of the nine products; the
+  // other three are below 2^-21 of the whole.  What is read waits as it is until it is taken apart, once for all its products.
+  constexpr bool PARTS = DT == kF32;
+  constexpr int GROUPS = PARTS ? 2 : L::STEPS;                 // groups of instructions over a tile's k
+  using Operand = std::conditional_t<PARTS, FfnParts, v4i>;
+  Operand pf[GROUPS][MB], qf[3][GROUPS][NB];
+  v4i p_raw[PARTS ? L::STEPS : 1][MB], q_raw[PARTS ? L::STEPS : 1][NB];
   auto read_p = [&](auto stage, auto half, auto step) {
+    constexpr int ks = decltype(step)::value;
 #pragma unroll
-    for (int b = 0; b < MB; ++b)
-      pf[decltype(step)::value][b] = fragment(std::bool_constant<P_ALONG>{}, std::integral_constant<int, PM>{}, step, p_addr, b,
-                                              at_p(decltype(half)::value, decltype(stage)::value));
+    for (int b = 0; b < MB; ++b) {
+      const v4i f = fragment(std::bool_constant<P_ALONG>{}, std::integral_constant<int, PM>{}, step, p_addr, b,
+                             at_p(decltype(half)::value, decltype(stage)::value));
+      if constexpr (PARTS) p_raw[ks][b] = f;
+      else pf[ks][b] = f;
+    }
   };
   auto read_q = [&](auto stage, auto half, auto into, auto step) {
+    constexpr int ks = decltype(step)::value;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-      qf[decltype(into)::value][decltype(step)::value][b] =
-          fragment(std::bool_constant<Q_ALONG>{}, std::integral_constant<int, PN>{}, step, q_addr, b,
-                   at_q(decltype(half)::value, decltype(stage)::value) - at_q(0, 0));
+    for (int b = 0; b < NB; ++b) {
+      const v4i f = fragment(std::bool_constant<Q_ALONG>{}, std::integral_constant<int, PN>{}, step, q_addr, b,
+                             at_q(decltype(half)::value, decltype(stage)::value) - at_q(0, 0));
+      if constexpr (PARTS) q_raw[ks][b] = f;
+      else qf[decltype(into)::value][ks][b] = f;
+    }
+  };
+  auto settle_p = [&]() {
+    if constexpr (PARTS) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) pf[g][b] = ffn_parts(p_raw[2 * g][b], p_raw[2 * g + 1][b]);
+    }
+  };
+  auto settle_q = [&](auto into) {
+    if constexpr (PARTS) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) qf[decltype(into)::value][g][b] = ffn_parts(q_raw[2 * g][b], q_raw[2 * g + 1][b]);
+    }
   };
   // the products of a quadrant with Q in registers `set`; then(ks) behind those of a step of k
   auto quadrant = [&](auto half_p, auto half_q, auto set, auto&& then) {
     constexpr int hp = decltype(half_p)::value, hq = decltype(half_q)::value;
-    ffn_for<0, L::STEPS>([&](auto step) {
-      constexpr int ks = decltype(step)::value;
+    ffn_for<0, GROUPS>([&](auto group) {
+      constexpr int g = decltype(group)::value;
 #pragma unroll
       for (int b = 0; b < MB; ++b)
 #pragma unroll
-        for (int c = 0; c < NB; ++c) E::mma(acc[hp * MB + b][hq * NB + c], qf[decltype(set)::value][ks][c], pf[ks][b]);
-      __builtin_amdgcn_sched_barrier(0);
-      then(step);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int c = 0; c < NB; ++c) ffn_mma<E>(acc[hp * MB + b][hq * NB + c], qf[decltype(set)::value][g][c], pf[g][b]);
+      if constexpr (!PARTS) {
+        __builtin_amdgcn_sched_barrier(0);
+        then(group);
+        __builtin_amdgcn_sched_barrier(0);
+      } else if constexpr (g == 0) {                           // all reads behind the first half, which hides them
+        __builtin_amdgcn_sched_barrier(0);
+        ffn_for<0, L::STEPS>(then);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     });
   };
   // all transfers but the youngest N have landed, for every wavefront, and all have come this far
@@ -411,6 +477,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
       all_q(a, c1, c1);
       meet(std::integral_constant<int, 5 * JP>{});
       ffn_for<0, L::STEPS>([&](auto ks) { read_q(c0, c0, c0, ks); read_p(c0, c0, ks); });
+      settle_q(c0);
+      settle_p();
       meet(std::integral_constant<int, 4 * JP>{});
       constexpr int EACH = (JP + L::STEPS - 1) / L::STEPS;     // transfers behind a step
       auto some = [&](auto ks, auto&& request) {
@@ -424,6 +492,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
           read_q(stage, c1, c1, ks);
           some(ks, [&](auto j) { request_p(a, c1, other, j); });
         });
+        settle_q(c1);
         meet(std::integral_constant<int, 3 * JP>{});
         // (behind the last tiles the last one again, which nobody reads: the counts stay, and a branch would cost registers)
         const int ahead = min(kt + 2, last);
@@ -434,15 +503,18 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
           read_p(stage, c1, ks);
           some(ks, [&](auto j) { request_q(a, c0, stage, j); });
         });
+        settle_p();
         quadrant(c1, c1, c1, [&](auto ks) {
           read_q(other, c0, next, ks);
           some(ks, [&](auto j) { request_p(a, c0, stage, j); });
         });
+        settle_q(next);
         meet(std::integral_constant<int, 3 * JP>{});
         quadrant(c1, c0, now, [&](auto ks) {
           read_p(other, c0, ks);
           some(ks, [&](auto j) { request_q(a, c1, stage, j); });
         });
+        settle_p();
       };
       for (int kt = kt_lo;;) {
         tile(kt, c0, c1, c0, c2);
@@ -465,6 +537,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void ffn_gemm_kernel(const 
         renew_list(kt + 1);
         hold(kt + 1);
       }
+      static_assert(DMA || !PARTS, "floats always go straight into LDS");
       ffn_for<0, L::STEPS>([&](auto ks) { read_p(c0, c0, ks); read_q(c0, c0, c0, ks); read_q(c0, c1, c1, ks); });
       quadrant(c0, c0, c0, [](auto) {});
       quadrant(c0, c1, c1, [](auto) {});
