@@ -124,7 +124,7 @@ class RowSet:
     def __init__(self, handle: int, workspace: torch.Tensor):
         self.handle = handle
         self.workspace = workspace
-        self.rows, self.kept = sparse_rows_info(self)[:2]
+        self.rows, self.kept = _row_counts(handle)
 
     def close(self):
         if self.handle:
@@ -136,6 +136,12 @@ class RowSet:
             self.close()
         except Exception:
             pass
+
+
+def _row_counts(handle: int) -> Tuple[int, int]:
+    m, kept = ctypes.c_int64(), ctypes.c_int64()
+    B._check(lib().sparse_rows_info(handle, ctypes.byref(m), ctypes.byref(kept), None, None), "sparse_rows_info")
+    return m.value, kept.value
 
 
 def _handle(rows: Optional[RowSet]) -> Optional[int]:
@@ -166,7 +172,7 @@ def sparse_rows_set_mask(rows: RowSet, mask: torch.Tensor, stream=None) -> RowSe
     """A new mask of as many rows (synchronises the stream); the number of kept rows may change."""
     B._check(lib().sparse_rows_set_mask(rows.handle, _tensor(mask, "mask", rows.rows, torch.uint8), _stream_handle(stream)),
              "sparse_rows_set_mask")
-    rows.kept = sparse_rows_info(rows)[1]
+    rows.kept = _row_counts(rows.handle)[1]
     return rows
 
 

@@ -18,8 +18,6 @@ namespace sc {
 
 void note_hip_error(int32_t code);
 
-enum : int32_t { kTypeF32 = SC_F32, kTypeF16 = SC_F16, kTypeBF16 = SC_BF16 };
-
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 static int elem_bytes(int dtype) { return dtype == SC_F32 ? 4 : 2; }
 
@@ -48,13 +46,18 @@ static int row_kind(const sc_ffn_desc& d) {
   return all % 16 == 0 ? kFfnWholeRows : all % 4 == 0 ? kFfnWordRows : kFfnAnyRows;
 }
 
-// Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`.
-// Priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other: 256 workgroups of 256 x
-// 256 take 1.6 (128 or fewer 1.05, since the clock is higher), 512 of 128 x 128, two a compute unit, 1.06 (256 or fewer 0.42); across k on
-// both sides 1.75, 1.15, 1.2 and 0.62.  Floats, in tiles of 128 alone, take 2.75 and 1.55; rows that are no
-// 16-byte groups a third more.  A launch and a tile's beginning and end take 8.  A contraction in parts leaves sums in float, written and read once at 4 TB/s, and another launch.
+// Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`,
+// priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other:
+//   256 workgroups of 256 x 256                         1.6 (128 or fewer 1.05: the clock is higher); across k on both sides 1.75 and 1.15
+//   512 workgroups of 128 x 128, two a compute unit     1.06 (256 or fewer 0.42); across k on both sides 1.2 and 0.62
+//   the same for floats, which have these tiles alone   2.75 (256 or fewer 1.55)
+// Rows that are no 16-byte groups take a third more, a launch and a tile's beginning and end 8 us.  A contraction in parts leaves sums in
+// float, written and read once at 4 TB/s, and another launch.
 constexpr int kMostSplits = 32, kLeastTiles = 4;
-static int64_t k_tiles_of(int64_t k, int segments, int dtype) { return segments * ((k + (dtype == SC_F32 ? 31 : 63)) / (dtype == SC_F32 ? 32 : 64)); }
+static int64_t k_tiles_of(int64_t k, int segments, int dtype) {
+  const int64_t entries = 128 / elem_bytes(dtype);
+  return segments * ((k + entries - 1) / entries);
+}
 
 struct Tiling {
   int tile, splits;
@@ -95,8 +98,8 @@ static size_t most_parts(int64_t m, int64_t n, int64_t k, int segments, int batc
 static size_t most_parts(const sc_ffn_desc& d, int64_t kept, bool training) {
   size_t most = std::max(most_parts(kept, d.d_hidden, d.d_in, 1, 2, d.dtype), most_parts(kept, d.d_out, d.d_hidden, 1, 1, d.dtype));
   if (training)
-    most = std::max({most, most_parts(kept, d.d_hidden, d.d_out, 1, 1, d.dtype), most_parts(kept, d.d_in, d.d_hidden, 2, 1, d.dtype), most_parts(d.d_hidden, d.d_in, kept, 1, 2, d.dtype),
-                     most_parts(d.d_out, d.d_hidden, kept, 1, 1, d.dtype)});
+    most = std::max({most, most_parts(kept, d.d_hidden, d.d_out, 1, 1, d.dtype), most_parts(kept, d.d_in, d.d_hidden, 2, 1, d.dtype),
+                     most_parts(d.d_hidden, d.d_in, kept, 1, 2, d.dtype), most_parts(d.d_out, d.d_hidden, kept, 1, 1, d.dtype)});
   return most;
 }
 
