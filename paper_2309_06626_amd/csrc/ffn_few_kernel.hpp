@@ -4,6 +4,8 @@
 // and add their sums up in LDS, in order.  The weights go from memory straight into the left operand of 16 x 16 matrix instructions (16
 // rows x 64 bytes an instruction: the four lanes of a row take 16 bytes each), the rows of P into the right one, so that 1 and 16 rows
 // cost the same.
+// Up to 4 (8) rows: the 16 rows of an operand are 4 (8) outputs or rows in 4 (2) neighbouring stretches of k.  The diagonal blocks of
+// the products are the sums of a stretch each, the rest is not looked at.  4 (2) times as many workgroups, and 256 (128) bytes in a row.
 #pragma once
 #include "ffn_act.hpp"
 #include "ffn_params.hpp"
@@ -31,24 +33,26 @@ template <> struct FewMma<kF32> {      // entry e of the four groups of a row: a
   }
 };
 
-// MT tiles of 16 rows; GATED: q[0] gate, q[1] up; WHOLE: rows are whole 16-byte groups
-template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FfnGemm p) {
+// MT tiles of 16 rows; S stretches of k a tile; GATED: q[0] gate, q[1] up; WHOLE: rows are whole 16-byte groups
+template <int DT, int MT, int S, bool GATED, bool WHOLE, int WAVES> __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FfnGemm p) {
   using T = typename Elem<DT>::T;
-  constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V, MATS = GATED ? 2 : 1;
-  constexpr int AHEAD = 4;                    // k steps whose operands a wavefront asks for at once (gated, 1 x 2048 -> 5632: 11.5 us, 8: 13.5)
+  constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V * S, MATS = GATED ? 2 : 1, O = 16 / S;
+  static_assert(S == 1 || MT == 1, "rows and stretches share the 16 columns");
+    constexpr int AHEAD = S == 4 ? 2 : 4;       // k steps whose operands a wavefront asks for at once
   extern __shared__ float few_sum[];          // [WAVES][MATS][MT][64][4]
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
-  const int n0 = blockIdx.x * 16, row0 = blockIdx.y * (16 * MT);
+  const int n0 = blockIdx.x * O, row0 = blockIdx.y * (16 * MT);
+  const int own = (l16 / O) * (4 * V) + kg * V;      // first of the lane's entries of a step
 
   const T* w[MATS];
 #pragma unroll
-  for (int a = 0; a < MATS; ++a) w[a] = static_cast<const T*>(p.q[a]) + (int64_t)min(n0 + l16, p.n - 1) * p.ldq + kg * V;
+  for (int a = 0; a < MATS; ++a) w[a] = static_cast<const T*>(p.q[a]) + (int64_t)min(n0 + l16 % O, p.n - 1) * p.ldq + own;
   const T* x[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int r = min(row0 + 16 * i + l16, p.m - 1);      // a row that is not there: the last one again, whose results are not stored
-    x[i] = static_cast<const T*>(p.p[0]) + (p.p_rows ? (int64_t)p.p_rows[r] : r) * p.ldp + kg * V;
+    const int r = min(row0 + 16 * i + l16 % O, p.m - 1);      // a row that is not there: the last one again, whose results are not stored
+    x[i] = static_cast<const T*>(p.p[0]) + (p.p_rows ? (int64_t)p.p_rows[r] : r) * p.ldp + own;
   }
   auto group = [=](const T* s, int left) -> v4i {      // `left` entries of a row from here on
     v4i g = {0, 0, 0, 0};
@@ -74,13 +78,13 @@ template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch
     v4i wf[MATS][AHEAD], xf[MT][AHEAD];
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s) {
-      const int k = k0 + s * STEP, left = p.k - k - kg * V;
+      const int k = k0 + s * STEP, left = p.k - k - own;
 #pragma unroll
       for (int a = 0; a < MATS; ++a) wf[a][s] = group(w[a] + k, left);
     }
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s) {
-      const int k = k0 + s * STEP, left = p.k - k - kg * V;
+      const int k = k0 + s * STEP, left = p.k - k - own;
 #pragma unroll
       for (int i = 0; i < MT; ++i) xf[i][s] = group(x[i] + k, left);
     }
@@ -97,16 +101,19 @@ template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch
 #pragma unroll
     for (int i = 0; i < MT; ++i) mine[(a * MT + i) * 64] = acc[a][i];
   __syncthreads();
-  // output 4 (lane / 16) + e of row lane % 16 lies in entry e of a lane
-  for (int at = t; at < MT * 256; at += 64 * WAVES) {
-    const int n16 = at & 15, r = at >> 4, n = n0 + n16, row = row0 + r;
-    const int word = (((r >> 4) * 64) + (n16 >> 2) * 16 + (r & 15)) * 4 + (n16 & 3);
+  // value (output q of 16, row c of 16) lies in entry q % 4 of lane 16 (q / 4) + c; stretch s: outputs and rows from s O on
+  for (int at = t; at < MT * O * O; at += 64 * WAVES) {
+    const int q = at % O, r = at / O, n = n0 + q, row = row0 + r;
     float v[MATS];
 #pragma unroll
     for (int a = 0; a < MATS; ++a) {
       v[a] = 0.0f;
 #pragma unroll
-      for (int u = 0; u < WAVES; ++u) v[a] += few_sum[(u * MATS + a) * (MT * 256) + word];
+      for (int s = 0; s < S; ++s) {
+        const int qs = q + s * O, word = ((r >> 4) * 64 + (qs >> 2) * 16 + (r & 15) + s * O) * 4 + (qs & 3);
+#pragma unroll
+        for (int u = 0; u < WAVES; ++u) v[a] += few_sum[(u * MATS + a) * (MT * 256) + word];
+      }
     }
     if (n >= p.n || row >= p.m) continue;
     if constexpr (GATED) {
@@ -124,21 +131,26 @@ template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> __global__ __launch
   }
 }
 
-template <int DT, int MT, bool GATED, bool WHOLE, int WAVES> hipError_t ffn_few_launch(const FfnGemm& g, hipStream_t s) {
-  auto kernel = ffn_few_kernel<DT, MT, GATED, WHOLE, WAVES>;
+template <int DT, int MT, int S, bool GATED, bool WHOLE, int WAVES> hipError_t ffn_few_launch(const FfnGemm& g, hipStream_t s) {
+  auto kernel = ffn_few_kernel<DT, MT, S, GATED, WHOLE, WAVES>;
   constexpr int lds = WAVES * (GATED ? 2 : 1) * MT * 1024;
   static std::atomic<uint64_t> told{0};
   const hipError_t e = ffn_allow_lds(reinterpret_cast<const void*>(kernel), lds, told);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)((g.n + 15) / 16), (unsigned)((g.m + 16 * MT - 1) / (16 * MT))), dim3(64 * WAVES), lds, s>>>(g);
+  constexpr int outputs = 16 / S;
+  kernel<<<dim3((unsigned)((g.n + outputs - 1) / outputs), (unsigned)((g.m + 16 * MT - 1) / (16 * MT))), dim3(64 * WAVES), lds, s>>>(g);
   return hipGetLastError();
 }
-// Sixteen wavefronts where there are fewer workgroups than compute units: each has half as many steps.
+// Stretches: up to 4 rows and up to 8.  1 row, weights from memory, bf16: gated 2048 -> 5632 9.0 us (5.1 TB/s), in 2 stretches 9.2, in one 11.5;
+// 5632 -> 2048 5.6 (4.1 TB/s), 5.5 and 8.1; gated 4096 -> 8192 25 (5.4 TB/s), 27.6 and 27.  Without: sixteen wavefronts where there are
+// fewer workgroups than compute units, each with half as many steps.
 template <int DT, bool GATED, bool WHOLE> hipError_t ffn_few_rows(const FfnGemm& g, hipStream_t s) {
+  if (g.m <= 4) return ffn_few_launch<DT, 1, 4, GATED, WHOLE, 8>(g, s);
+  if (g.m <= 8) return ffn_few_launch<DT, 1, 2, GATED, WHOLE, 8>(g, s);
   const bool more = (g.n + 15) / 16 < 256;
-  if (g.m <= 16) return more ? ffn_few_launch<DT, 1, GATED, WHOLE, 16>(g, s) : ffn_few_launch<DT, 1, GATED, WHOLE, 8>(g, s);
-  if (g.m <= 32) return ffn_few_launch<DT, 2, GATED, WHOLE, 8>(g, s);
-  return ffn_few_launch<DT, 4, GATED, WHOLE, 8>(g, s);
+  if (g.m <= 16) return more ? ffn_few_launch<DT, 1, 1, GATED, WHOLE, 16>(g, s) : ffn_few_launch<DT, 1, 1, GATED, WHOLE, 8>(g, s);
+  if (g.m <= 32) return ffn_few_launch<DT, 2, 1, GATED, WHOLE, 8>(g, s);
+  return ffn_few_launch<DT, 4, 1, GATED, WHOLE, 8>(g, s);
 }
 template <int DT> hipError_t ffn_few_type(bool gated, const FfnGemm& g, bool whole, hipStream_t s) {
   if (gated) return whole ? ffn_few_rows<DT, true, true>(g, s) : ffn_few_rows<DT, true, false>(g, s);

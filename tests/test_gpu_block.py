@@ -291,6 +291,38 @@ def test_ffn_forward_and_gradients(c):
         inside(v, w, b, name)
 
 
+FEW = [(rows, di, dh, do, dtype, "silu", mask, 0, 0)
+       for dtype, di, dh, do in (("bf16", 520, 1037, 264), ("f16", 1048, 264, 5), ("f32", 333, 68, 130), ("f16", 77, 1030, 1031))
+       for rows, mask in ((3, "all"), (4, "all"), (8, "half"), (8, "all"), (9, "all"), (15, "half"))]
+
+
+@pytest.mark.parametrize("c", FEW, ids=lambda c: "-".join(map(str, c)))
+def test_ffn_of_a_few_rows(c):
+    rows, di, dh, do, dtype, kind, mask, _, _ = c
+    m, keep, full = ffn_case(c, 11 * rows + di)
+    got = ffn_call(c, m, keep, full, backward=False)
+    x = full["x"][keep]
+    want = O.ffn_forward(x, full["wg"], full["wu"], full["wd"], kind)
+    assert (got[~keep.to(DEV)] == 0).all()
+    inside(got[keep.to(DEV)], want, O.ffn_bounds(x, full["wg"], full["wu"], full["wd"], kind, dtype), "y")
+
+
+@pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** 40])
+def test_float_rows_of_any_size(size):
+    # parts of 16 bits have a float's range: rows far from 1, weights that bring them back
+    c = (150, 96, 72, 80, "f32", "gelu_tanh", "half", 0, 0)
+    m, keep, full = ffn_case(c, 31)
+    full["x"], full["wg"], full["wu"] = full["x"] * size, full["wg"] / size, full["wu"] / size
+    got = ffn_call(c, m, keep, full)
+    x, dy = full["x"][keep], full["dy"][keep]
+    leaves = [v.clone().requires_grad_(True) for v in (x, full["wg"], full["wu"], full["wd"])]
+    y = O.ffn_forward(*leaves, "gelu_tanh")
+    want = [y.detach(), *torch.autograd.grad(y, leaves, dy)]
+    bounds = O.ffn_bounds(x, full["wg"], full["wu"], full["wd"], "gelu_tanh", "f32", dy)
+    for name, v, w, b in zip(("y", "dx", "dw_gate", "dw_up", "dw_down"), got, want, bounds):
+        inside(v[keep.to(DEV)] if name in ("y", "dx") else v, w, b, name)
+
+
 @pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
 def test_ffn_gradient_against_differences(kind):
     c = (9, 12, 20, 8, "f32", kind, "half", 0, 0)
