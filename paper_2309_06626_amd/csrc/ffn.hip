@@ -31,27 +31,88 @@ static sc_status check_ffn(const sc_ffn_desc* d, int64_t kept) {
   return SC_OK;
 }
 
-static hipError_t launch(int dtype, FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s) {
+static hipError_t launch(int dtype, FfnProduct what, const FfnGemm& g, int tile, bool whole, hipStream_t s) {
   switch (dtype) {
-    case SC_BF16: return ffn_launch_bf16(what, g, tile, rows, s);
-    case SC_F16: return ffn_launch_f16(what, g, tile, rows, s);
-    default: return ffn_launch_f32(what, g, tile, rows, s);
+    case SC_BF16: return ffn_launch_bf16(what, g, tile, whole, s);
+    case SC_F16: return ffn_launch_f16(what, g, tile, whole, s);
+    default: return ffn_launch_f32(what, g, tile, whole, s);
   }
 }
 
 constexpr int64_t kFewRows = 64;
 
-static int row_kind(const sc_ffn_desc& d) {
-  const int all = (d.d_in | d.d_hidden | d.d_out) * elem_bytes(d.dtype);
-  return all % 16 == 0 ? kFfnWholeRows : all % 4 == 0 ? kFfnWordRows : kFfnAnyRows;
+// entries from row to row of an operand: whole 16-byte groups
+static int64_t pitch_of(int64_t entries, int dtype) {
+  const int64_t group = 16 / elem_bytes(dtype);
+  return (entries + group - 1) / group * group;
 }
+static bool whole_rows(const sc_ffn_desc& d) { return (d.d_in | d.d_hidden | d.d_out) * elem_bytes(d.dtype) % 16 == 0; }
+
+// Operands whose rows are not whole 16-byte groups are copied first, kept rows alone, with zeros up to the next whole group: the products
+// then load straight into LDS and have no ends to look after.  5 000 x 423 -> 2 809 in bf16, forward and backward: COPYTIME
+constexpr int kMostCopies = 6;
+struct FfnCopies {
+  struct One {
+    const void* src;
+    void* dst;
+    const int32_t* rows;      // row of src that row i stands for; null: i
+    uint32_t cols, groups;    // entries a row, 16-byte groups a row of dst
+    int64_t first;            // group of the launch that is dst's first
+  } one[kMostCopies];
+  int32_t count, elem;
+  int64_t groups;
+};
+template <typename T> __global__ __launch_bounds__(256) void ffn_copy_kernel(const FfnCopies c) {
+  constexpr uint32_t V = 16 / sizeof(T);
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= c.groups) return;
+  int which = 0;
+  while (which + 1 < c.count && at >= c.one[which + 1].first) ++which;
+  const FfnCopies::One& o = c.one[which];
+  const int64_t local = at - o.first;
+  const int64_t row = local >> 32 ? local / o.groups : (uint32_t)local / o.groups;
+  const uint32_t col = (uint32_t)(local - row * o.groups) * V;
+  const T* src = static_cast<const T*>(o.src) + (o.rows ? (int64_t)o.rows[row] : row) * o.cols + col;
+  T v[V];
+#pragma unroll
+  for (uint32_t e = 0; e < V; ++e) v[e] = T(0);
+  if (col + V <= o.cols) {
+    __builtin_memcpy(v, src, 16);
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < V; ++e)
+      if (col + e < o.cols) v[e] = src[e];
+  }
+  __builtin_memcpy(__builtin_assume_aligned(static_cast<T*>(o.dst) + local * V, 16), v, 16);
+}
+struct Copies {
+  FfnCopies c = {};
+  char* at;
+  explicit Copies(void* workspace, int dtype) : at(static_cast<char*>(workspace)) { c.elem = elem_bytes(dtype); }
+  static size_t bytes(int64_t rows, int64_t cols, int dtype) { return up256((size_t)rows * pitch_of(cols, dtype) * elem_bytes(dtype)); }
+  const void* add(const void* src, int64_t rows, int64_t cols, int dtype, const int32_t* list = nullptr) {
+    const int64_t groups = pitch_of(cols, dtype) * c.elem / 16;
+    c.one[c.count++] = {src, at, list, (uint32_t)cols, (uint32_t)groups, c.groups};
+    c.groups += rows * groups;
+    void* const dst = at;
+    at += bytes(rows, cols, dtype);
+    return dst;
+  }
+  hipError_t run(hipStream_t s) const {
+    if (c.groups == 0) return hipSuccess;
+    const dim3 grid((unsigned)((c.groups + 255) / 256));
+    if (c.elem == 4) ffn_copy_kernel<uint32_t><<<grid, dim3(256), 0, s>>>(c);
+    else ffn_copy_kernel<uint16_t><<<grid, dim3(256), 0, s>>>(c);
+    return hipGetLastError();
+  }
+};
 
 // Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`,
 // priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other:
 //   256 workgroups of 256 x 256                         1.6 (128 or fewer 1.05: the clock is higher); across k on both sides 1.75 and 1.15
 //   512 workgroups of 128 x 128, two a compute unit     1.06 (256 or fewer 0.42); across k on both sides 1.2 and 0.62
 //   the same for floats, which have these tiles alone   2.75 (256 or fewer 1.55)
-// Rows that are no 16-byte groups take a third more, a launch and a tile's beginning and end 8 us.  A contraction in parts leaves sums in
+// A launch and a tile's beginning and end take 8 us.  A contraction in parts leaves sums in
 // float, written and read once at 4 TB/s, and another launch.
 constexpr int kMostSplits = 32, kLeastTiles = 4;
 static int64_t k_tiles_of(int64_t k, int segments, int dtype) {
@@ -64,16 +125,15 @@ struct Tiling {
   double us;
 };
 
-static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, int segments, int batch, int dtype, int layout) {
+static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, int segments, int batch, int dtype) {
   const bool across = what == kFfnWGrad, f32 = dtype == SC_F32;
   const int64_t k_tiles = k_tiles_of(k, segments, dtype);
   Tiling best = {0, 1, 1e30};
   for (int tile = 0; tile < 2; ++tile) {
-    if (tile == 1 && (f32 || layout != kFfnWholeRows)) break;
+    if (tile == 1 && f32) break;
     const int64_t edge = tile ? 256 : 128, room = tile ? 256 : 512;
-    const double words = layout == kFfnWholeRows ? 1.0 : 1.35;
-    const double half = words * (f32 ? 1.55 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42));
-    const double full = words * (f32 ? 2.75 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06));
+    const double half = f32 ? 1.55 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42);
+    const double full = f32 ? 2.75 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06);
     const int64_t tiles = ((m + edge - 1) / edge) * ((cols + edge - 1) / edge) * batch;
     for (int splits = 1; splits <= kMostSplits; ++splits) {
       if (splits > 1 && k_tiles / splits < kLeastTiles) break;
@@ -131,10 +191,12 @@ template <typename T, int WIDTH, int WHAT> __global__ __launch_bounds__(256) voi
         ffn_act(g.activation, gate[u], a, da);
         hidden[u] = a * up[u];
       }
-      store(g.c[0], at, hidden);
+      store(g.c[0], row * g.ldc + i, hidden);
       if (g.saved) {
-        store(g.saved, at, gate);
-        store(static_cast<T*>(g.saved) + whole, at, up);
+        T* const saved = static_cast<T*>(g.saved);
+        store(saved, at, gate);
+        store(saved + whole, at, up);
+        if (saved + 2 * whole != g.c[0]) store(saved + 2 * whole, at, hidden);
       }
     } else if constexpr (WHAT == kFfnGateGrad) {
       const vec dh = sum(0, i);
@@ -149,12 +211,17 @@ template <typename T, int WIDTH, int WHAT> __global__ __launch_bounds__(256) voi
         dg[u] = dh[u] * (float)up[u] * da;
         du[u] = dh[u] * a;
       }
-      store(g.c[0], at, dg);
-      store(g.c[1], at, du);
+      store(g.c[0], row * g.ldc + i, dg);
+      store(g.c[1], row * g.ldc + i, du);
     } else {
       store(g.c[blockIdx.y], (g.c_rows ? (int64_t)g.c_rows[row] : row) * g.ldc + i, sum(blockIdx.y, i));
     }
   }
+  if (WHAT == kFfnUp || WHAT == kFfnGateGrad)      // zeros behind the last entry of an operand's row
+    for (int64_t i = n + threadIdx.x; i < g.ldc; i += 256) {
+      static_cast<T*>(g.c[0])[row * g.ldc + i] = T(0);
+      if (WHAT == kFfnGateGrad) static_cast<T*>(g.c[1])[row * g.ldc + i] = T(0);
+    }
 }
 
 template <typename T, int WIDTH> static void finish_width(FfnProduct what, const FfnGemm& g, hipStream_t s) {
@@ -175,17 +242,16 @@ static hipError_t finish(int dtype, FfnProduct what, const FfnGemm& g, hipStream
 }
 
 // a product in the tiles and parts that its sizes ask for
-static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, int layout, float* parts, hipStream_t s) {
-  const Tiling t = pick_tiling(what, g.m, what == kFfnUp ? 2 * (int64_t)g.n : g.n, g.k, g.segments, g.batch, dtype, layout);
+static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, bool whole, float* parts, hipStream_t s) {
+  const Tiling t = pick_tiling(what, g.m, what == kFfnUp ? 2 * (int64_t)g.n : g.n, g.k, g.segments, g.batch, dtype);
   g.splits = t.splits;
   g.partial = parts;
-  const hipError_t e = launch(dtype, what, g, t.tile, layout, s);
+  const hipError_t e = launch(dtype, what, g, t.tile, whole, s);
   return e == hipSuccess && g.splits > 1 ? finish(dtype, what, g, s) : e;
 }
 // kFfnUp and kFfnDown
-static hipError_t multiply_forward(int dtype, FfnProduct what, FfnGemm& g, int layout, float* parts, hipStream_t s) {
-  if (g.m > kFewRows) return multiply(dtype, what, g, layout, parts, s);
-  const bool whole = layout == kFfnWholeRows;
+static hipError_t multiply_forward(int dtype, FfnProduct what, FfnGemm& g, bool whole, float* parts, hipStream_t s) {
+  if (g.m > kFewRows) return multiply(dtype, what, g, whole, parts, s);
   switch (dtype) {
     case SC_BF16: return ffn_few_bf16(what == kFfnUp, g, whole, s);
     case SC_F16: return ffn_few_f16(what == kFfnUp, g, whole, s);
@@ -248,8 +314,14 @@ sc_status sparse_ffn_workspace_bytes(const sc_ffn_desc* desc, int64_t kept, int3
   *bytes = 0;
   const sc_status st = sc::check_ffn(desc, kept);
   if (st != SC_OK) return st;
-  const size_t hidden = sc::up256((size_t)kept * desc->d_hidden * sc::elem_bytes(desc->dtype));
+  const int dt = desc->dtype;
+  const int64_t d_in = desc->d_in, d_hidden = desc->d_hidden, d_out = desc->d_out;
+  const size_t hidden = sc::Copies::bytes(kept, d_hidden, dt);
   *bytes = 256 + (training ? 2 * hidden : hidden) + sc::most_parts(*desc, kept, training != 0);
+  if (!sc::whole_rows(*desc)) {
+    *bytes += sc::Copies::bytes(kept, d_in, dt) + 2 * sc::Copies::bytes(d_hidden, d_in, dt) + sc::Copies::bytes(d_out, d_hidden, dt);
+    if (training) *bytes += sc::Copies::bytes(kept, d_out, dt) + hidden;
+  }
   return SC_OK;
 }
 
@@ -268,36 +340,52 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
   if (sc::misaligned({x_dev, w_gate_dev, w_up_dev, w_down_dev, y_dev, saved_dev, workspace_dev})) return SC_ERR_ALIGN;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int eb = sc::elem_bytes(desc->dtype);
-  const int layout = sc::row_kind(*desc);
   hipError_t e = hipSuccess;
   if (y_rows == SC_ROWS_DENSE) e = sc::rows_zero_dropped(rows, (int64_t)desc->d_out * eb, y_dev, s);
   if (e != hipSuccess) return sc::failed(e);
   if (kept == 0) return SC_OK;
-  const size_t hidden_bytes = (size_t)kept * desc->d_hidden * eb;
-  void* const hidden = saved_dev ? static_cast<char*>(saved_dev) + 2 * hidden_bytes : workspace_dev;
-  float* const parts = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + sc::up256(hidden_bytes));
+  const int dt = desc->dtype;
+  const bool whole = sc::whole_rows(*desc), copied = !whole && kept > sc::kFewRows;
+  const int64_t d_in = desc->d_in, d_hidden = desc->d_hidden, d_out = desc->d_out;
+  const int64_t in_pitch = copied ? sc::pitch_of(d_in, dt) : d_in, hidden_pitch = copied ? sc::pitch_of(d_hidden, dt) : d_hidden;
+  void* const hidden = saved_dev && !copied ? static_cast<char*>(saved_dev) + 2 * (size_t)kept * d_hidden * eb : workspace_dev;
+  char* const w = static_cast<char*>(workspace_dev) + sc::Copies::bytes(kept, d_hidden, dt);
+  float* const parts = reinterpret_cast<float*>(w);
 
-  sc::FfnGemm up = sc::gemm_of(kept, desc->d_hidden, desc->d_in);
-  up.p[0] = x_dev;
-  up.ldp = up.ldq = desc->d_in;
-  up.p_rows = sc::map_of(rows, x_rows);
-  up.q[0] = w_gate_dev;
-  up.q[1] = w_up_dev;
+  const int32_t* x_map = sc::map_of(rows, x_rows);
+  const void *x = x_dev, *w_gate = w_gate_dev, *w_up = w_up_dev, *w_down = w_down_dev;
+  if (copied) {
+    sc::Copies copies(w + sc::most_parts(*desc, kept, false), dt);
+    x = copies.add(x, kept, d_in, dt, x_map);
+    w_gate = copies.add(w_gate, d_hidden, d_in, dt);
+    w_up = copies.add(w_up, d_hidden, d_in, dt);
+    w_down = copies.add(w_down, d_out, d_hidden, dt);
+    x_map = nullptr;
+    e = copies.run(s);
+    if (e != hipSuccess) return sc::failed(e);
+  }
+
+  sc::FfnGemm up = sc::gemm_of(kept, d_hidden, d_in);
+  up.p[0] = x;
+  up.ldp = up.ldq = in_pitch;
+  up.p_rows = x_map;
+  up.q[0] = w_gate;
+  up.q[1] = w_up;
   up.c[0] = hidden;
-  up.ldc = desc->d_hidden;
+  up.ldc = hidden_pitch;
   up.saved = saved_dev;
   up.activation = desc->activation;
-  e = sc::multiply_forward(desc->dtype, sc::kFfnUp, up, layout, parts, s);
+  e = sc::multiply_forward(dt, sc::kFfnUp, up, whole, parts, s);
   if (e != hipSuccess) return sc::failed(e);
 
-  sc::FfnGemm down = sc::gemm_of(kept, desc->d_out, desc->d_hidden);
+  sc::FfnGemm down = sc::gemm_of(kept, d_out, d_hidden);
   down.p[0] = hidden;
-  down.q[0] = w_down_dev;
-  down.ldp = down.ldq = desc->d_hidden;
+  down.q[0] = w_down;
+  down.ldp = down.ldq = hidden_pitch;
   down.c[0] = y_dev;
-  down.ldc = desc->d_out;
+  down.ldc = d_out;
   down.c_rows = sc::map_of(rows, y_rows);
-  e = sc::multiply_forward(desc->dtype, sc::kFfnDown, down, layout, parts, s);
+  e = sc::multiply_forward(dt, sc::kFfnDown, down, whole, parts, s);
   return e == hipSuccess ? SC_OK : sc::failed(e);
 }
 
@@ -320,7 +408,8 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int eb = sc::elem_bytes(desc->dtype);
   const int64_t d_in = desc->d_in, d_hidden = desc->d_hidden, d_out = desc->d_out;
-  const int layout = sc::row_kind(*desc);
+  const int dt = desc->dtype;
+  const bool whole = sc::whole_rows(*desc);
   hipError_t e = hipSuccess;
   if (dx_dev && x_rows == SC_ROWS_DENSE) e = sc::rows_zero_dropped(rows, d_in * eb, dx_dev, s);
   if (e != hipSuccess) return sc::failed(e);
@@ -331,23 +420,44 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
     return e == hipSuccess ? SC_OK : sc::failed(e);
   }
   char* const w = static_cast<char*>(workspace_dev);
-  const size_t hidden_bytes = (size_t)kept * d_hidden * eb;
+  const size_t hidden_bytes = sc::Copies::bytes(kept, d_hidden, dt);
+  const int64_t in_pitch = sc::pitch_of(d_in, dt), hidden_pitch = sc::pitch_of(d_hidden, dt), out_pitch = sc::pitch_of(d_out, dt);
   void* const dg = w;
-  void* const du = w + sc::up256(hidden_bytes);
-  float* const partial = reinterpret_cast<float*>(w + 2 * sc::up256(hidden_bytes));
+  void* const du = w + hidden_bytes;
+  float* const partial = reinterpret_cast<float*>(w + 2 * hidden_bytes);
+  const int32_t *x_map = sc::map_of(rows, x_rows), *y_map = sc::map_of(rows, y_rows);
+  const int32_t* const dx_map = x_map;
+  const void *x = x_dev, *dy = dy_dev, *w_gate = w_gate_dev, *w_up = w_up_dev, *w_down = w_down_dev;
+  const void* hidden = static_cast<const char*>(saved_dev) + 2 * (size_t)kept * d_hidden * eb;
+  if (!whole) {
+    sc::Copies copies(w + 2 * hidden_bytes + sc::most_parts(*desc, kept, true), dt);
+    dy = copies.add(dy, kept, d_out, dt, y_map);
+    w_down = copies.add(w_down, d_out, d_hidden, dt);
+    if (dx_dev) {
+      w_gate = copies.add(w_gate, d_hidden, d_in, dt);
+      w_up = copies.add(w_up, d_hidden, d_in, dt);
+    }
+    if (weights) {
+      x = copies.add(x, kept, d_in, dt, x_map);
+      hidden = copies.add(hidden, kept, d_hidden, dt);
+    }
+    x_map = y_map = nullptr;
+    e = copies.run(s);
+    if (e != hipSuccess) return sc::failed(e);
+  }
 
   sc::FfnGemm gate = sc::gemm_of(kept, d_hidden, d_out);       // dhidden = dY Wd, then dg and du
-  gate.p[0] = dy_dev;
-  gate.ldp = d_out;
-  gate.p_rows = sc::map_of(rows, y_rows);
-  gate.q[0] = w_down_dev;
-  gate.ldq = d_hidden;
+  gate.p[0] = dy;
+  gate.ldp = out_pitch;
+  gate.p_rows = y_map;
+  gate.q[0] = w_down;
+  gate.ldq = hidden_pitch;
   gate.saved = const_cast<void*>(saved_dev);
   gate.c[0] = dg;
   gate.c[1] = du;
-  gate.ldc = d_hidden;
+  gate.ldc = hidden_pitch;
   gate.activation = desc->activation;
-  e = sc::multiply(desc->dtype, sc::kFfnGateGrad, gate, layout, partial, s);
+  e = sc::multiply(dt, sc::kFfnGateGrad, gate, whole, partial, s);
   if (e != hipSuccess) return sc::failed(e);
 
   if (dx_dev) {
@@ -355,14 +465,14 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
     in.segments = 2;
     in.p[0] = dg;
     in.p[1] = du;
-    in.ldp = d_hidden;
-    in.q[0] = w_gate_dev;
-    in.q[1] = w_up_dev;
-    in.ldq = d_in;
+    in.ldp = hidden_pitch;
+    in.q[0] = w_gate;
+    in.q[1] = w_up;
+    in.ldq = in_pitch;
     in.c[0] = dx_dev;
     in.ldc = d_in;
-    in.c_rows = sc::map_of(rows, x_rows);
-    e = sc::multiply(desc->dtype, sc::kFfnInGrad, in, layout, partial, s);
+    in.c_rows = dx_map;
+    e = sc::multiply(dt, sc::kFfnInGrad, in, whole, partial, s);
     if (e != hipSuccess) return sc::failed(e);
   }
   if (weights) {
@@ -370,25 +480,25 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
     in.batch = 2;
     in.p[0] = dg;
     in.p[1] = du;
-    in.ldp = d_hidden;
-    in.q[0] = x_dev;
-    in.ldq = d_in;
-    in.q_rows = sc::map_of(rows, x_rows);
+    in.ldp = hidden_pitch;
+    in.q[0] = x;
+    in.ldq = in_pitch;
+    in.q_rows = x_map;
     in.c[0] = dw_gate_dev;
     in.c[1] = dw_up_dev;
     in.ldc = d_in;
-    e = sc::multiply(desc->dtype, sc::kFfnWGrad, in, layout, partial, s);
+    e = sc::multiply(dt, sc::kFfnWGrad, in, whole, partial, s);
     if (e != hipSuccess) return sc::failed(e);
 
     sc::FfnGemm out = sc::gemm_of(d_out, d_hidden, kept);      // dWd = dY' hidden
-    out.p[0] = dy_dev;
-    out.ldp = d_out;
-    out.p_rows = sc::map_of(rows, y_rows);
-    out.q[0] = static_cast<const char*>(saved_dev) + 2 * hidden_bytes;
-    out.ldq = d_hidden;
+    out.p[0] = dy;
+    out.ldp = out_pitch;
+    out.p_rows = y_map;
+    out.q[0] = hidden;
+    out.ldq = hidden_pitch;
     out.c[0] = dw_down_dev;
     out.ldc = d_hidden;
-    e = sc::multiply(desc->dtype, sc::kFfnWGrad, out, layout, partial, s);
+    e = sc::multiply(dt, sc::kFfnWGrad, out, whole, partial, s);
     if (e != hipSuccess) return sc::failed(e);
   }
   return SC_OK;

@@ -3,8 +3,8 @@
 #include "ffn_gemm_kernel.hpp"
 
 namespace sc {
-hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s) {
-  return ffn_launch_type<kF32>(what, g, tile, rows, s);
+hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, bool whole, hipStream_t s) {
+  return ffn_launch_type<kF32>(what, g, tile, whole, s);
 }
 hipError_t ffn_few_f32(bool gated, const FfnGemm& g, bool whole, hipStream_t s) { return ffn_few_type<kF32>(gated, g, whole, s); }
 }  // namespace sc

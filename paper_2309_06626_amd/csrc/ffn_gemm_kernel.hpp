@@ -35,10 +35,6 @@ __device__ __forceinline__ void ffn_dma16(const void* src, unsigned lds_base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src));
 }
 
-__device__ __forceinline__ void ffn_dma4(const void* src, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_base), "v"(src));
-}
-
 // Eight floats of a row in bf16 parts.  Cutting off keeps 8 bits a part, and what is left over is exact: hi + mid + lo is the float.
 struct FfnParts { v4i part[3]; };
 __device__ __forceinline__ FfnParts ffn_parts(v4i first, v4i second) {
@@ -77,7 +73,7 @@ template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f
   }
 }
 
-template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int ROWS>
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(const FfnGemm p) {
   using E = Elem<DT>;
   using T = typename E::T;
@@ -88,10 +84,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
   // a tile is two halves of P's rows by two halves of Q's; a wavefront has MB x NB blocks of 32 x 32 in each quadrant
   constexpr int PM = BM / 2, PN = BN / 2;
   constexpr int MB = PM / WAVES_M / 32, NB = PN / WAVES_N / 32;
-  constexpr bool DMA = ROWS != kFfnAnyRows;
-  constexpr int UNIT = ROWS == kFfnWordRows ? 4 / EB : V;      // entries a lane and transfer
-  constexpr int JP = PM * 128 / (UNIT * EB) / NT, JQ = PN * 128 / (UNIT * EB) / NT;      // transfers a lane and half tile
-  constexpr int UNITS = V / UNIT, PAR = UNITS > 1 ? 2 : 1;     // units a 16-byte group; transfers whose rows have different keys
+  constexpr int JP = PM * 8 / NT, JQ = PN * 8 / NT;            // transfers of 16 bytes a lane and half tile
   constexpr int P_PIECE = PM * 128, Q_PIECE = PN * 128, STAGE = 2 * (P_PIECE + Q_PIECE);
   // half h of stage s in LDS, the halves of an operand within 64 KB of each other: one address a lane, the rest is in the instructions
   auto at_p = [](int h, int s) constexpr { return (2 * h + s) * P_PIECE; };
@@ -126,14 +119,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
   const int kt_lo = (int)((int64_t)all_tiles * split / p.splits), kt_hi = (int)((int64_t)all_tiles * (split + 1) / p.splits);
 
   // ---- loads ----
-  // unit s of a half of an operand's tile: along k, row s / PPR, across k, row s / PPR of k
-  constexpr int P_PPR = (P_ALONG ? 128 : PM * EB) / (UNIT * EB), Q_PPR = (Q_ALONG ? 128 : PN * EB) / (UNIT * EB);
+  // 16-byte group s of a half of an operand's tile: along k, row s / PPR, across k, row s / PPR of k
+  constexpr int P_PPR = (P_ALONG ? 128 : PM * EB) / 16, Q_PPR = (Q_ALONG ? 128 : PN * EB) / 16;
   const int p_row = t / P_PPR, q_row = t / Q_PPR;              // of transfer 0
   constexpr int P_NEXT = NT / P_PPR, Q_NEXT = NT / Q_PPR;      // rows from transfer to transfer
-  // first entry, within the row, of what belongs at unit u of row r of the tile: 16-byte groups are exchanged by the row's key
+  // first entry, within the row, of the group that belongs at place u of row r of the tile
   auto entry = [](auto along, auto ppr, int u, int r) -> int {
-    const int key = decltype(along)::value ? L::key_along(r) : L::template key_across<decltype(ppr)::value / UNITS>(r);
-    return ((u / UNITS) ^ key) * V + u % UNITS * UNIT;
+    const int key = decltype(along)::value ? L::key_along(r) : L::template key_across<decltype(ppr)::value>(r);
+    return (u ^ key) * V;
   };
   // held in scalar registers: a load of a kernel argument between the products would have to wait for the operands on their way
   const T *p0 = static_cast<const T*>(p.p[P_ALONG ? 0 : z]), *p1 = static_cast<const T*>(p.p[p.segments > 1]);
@@ -143,35 +136,25 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
   const void* zeros = &ffn_zeros;
   asm volatile("" : "+s"(p0), "+s"(p1), "+s"(q0), "+s"(q1), "+s"(ldp), "+s"(ldq), "+s"(k_end), "+s"(zeros));
   // along: k of the lane's group, and its rows from the start of the operand; rows beyond the end: results that are not stored.
-  // across: result row / column of the group in either half (beyond the end: any that exists)
-  int p_at[2][PAR], q_at[2][PAR];
+  // across: result row / column of the group in either half (beyond the end: any that exists; a row is whole groups long)
+  const int p_k0 = entry(std::bool_constant<P_ALONG>{}, std::integral_constant<int, P_PPR>{}, t % P_PPR, p_row);
+  const int q_k0 = entry(std::bool_constant<Q_ALONG>{}, std::integral_constant<int, Q_PPR>{}, t % Q_PPR, q_row);
+  int p_at[2], q_at[2];
   int64_t p_off[2][P_ALONG ? JP : 1], q_off[2][Q_ALONG ? JQ : 1];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-#pragma unroll
-    for (int u = 0; u < PAR; ++u) {
-      p_at[h][u] = entry(std::bool_constant<P_ALONG>{}, std::integral_constant<int, P_PPR>{}, t % P_PPR, p_row + u * P_NEXT);
-      q_at[h][u] = entry(std::bool_constant<Q_ALONG>{}, std::integral_constant<int, Q_PPR>{}, t % Q_PPR, q_row + u * Q_NEXT);
-      if constexpr (!P_ALONG) {
-        p_at[h][u] += m0 + h * PM;
-        if constexpr (DMA) p_at[h][u] = min(p_at[h][u], p.m - UNIT);
-      }
-      if constexpr (!Q_ALONG) {
-        q_at[h][u] += n0 + h * PN;
-        if constexpr (DMA) q_at[h][u] = min(q_at[h][u], p.n - UNIT);
-      }
-    }
+    p_at[h] = P_ALONG ? p_k0 : min(p_k0 + m0 + h * PM, (int)ldp - V);
+    q_at[h] = Q_ALONG ? q_k0 : min(q_k0 + n0 + h * PN, (int)ldq - V);
     if constexpr (P_ALONG) {
 #pragma unroll
       for (int j = 0; j < JP; ++j) {
         const int i = min(m0 + h * PM + p_row + j * P_NEXT, p.m - 1);
-        p_off[h][j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_at[h][j % PAR];
+        p_off[h][j] = (p.p_rows ? (int64_t)p.p_rows[i] : i) * ldp + p_k0;
       }
     }
     if constexpr (Q_ALONG) {
 #pragma unroll
-      for (int j = 0; j < JQ; ++j)
-        q_off[h][j] = min(n0 + (GATED ? 0 : h * PN) + q_row + j * Q_NEXT, n_last) * ldq + q_at[h][j % PAR];
+      for (int j = 0; j < JQ; ++j) q_off[h][j] = min(n0 + (GATED ? 0 : h * PN) + q_row + j * Q_NEXT, n_last) * ldq + q_k0;
     }
   }
   // rows of the contraction that stand for others: a stretch of the list at a time in LDS (a look-up in memory would have to wait
@@ -184,8 +167,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     list_base = kt * BK;
     for (int i = t; i < kFfnList && list_base + i < p.k; i += NT) s_list[i] = list[list_base + i];
   };
-  auto p_k = [&](int k) -> int64_t { return LISTED && p.p_rows ? s_list[k - list_base] : k; };
-  auto q_k = [&](int k) -> int64_t { return LISTED && q_listed ? s_list[k - list_base] : k; };
 
   const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
   int listed_row[JP];                                          // of the tile asked for next; the halves share them
@@ -208,24 +189,20 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     a.q[1] = GATED ? q1 + k0 : a.q[0];
     return a;
   };
-  const unsigned to = lds0 + wave * (64 * UNIT * EB);
-  auto dma = [](const void* src, unsigned at) {
-    if constexpr (UNIT * EB == 16) ffn_dma16(src, at);
-    else ffn_dma4(src, at);
-  };
+  const unsigned to = lds0 + wave * 1024;
   auto request_p = [&](const Ask& a, auto half, auto stage, auto which) {
     constexpr int h = decltype(half)::value, j = decltype(which)::value;
     const T* src;
     bool in;
     if constexpr (P_ALONG) {
       src = a.p + p_off[h][j];
-      in = a.k0 + p_at[0][j % PAR] < k_end;
+      in = a.k0 + p_k0 < k_end;
     } else {
       const int k = a.k0 + p_row + j * P_NEXT;
       in = k < k_end;
-      src = a.p + p_at[h][j % PAR] + (LISTED && list && !q_listed ? listed_row[j] : k) * ldp;
+      src = a.p + p_at[h] + (LISTED && list && !q_listed ? listed_row[j] : k) * ldp;
     }
-    dma(in ? (const void*)src : zeros, to + at_p(h, decltype(stage)::value) + j * NT * UNIT * EB);
+    ffn_dma16(in ? (const void*)src : zeros, to + at_p(h, decltype(stage)::value) + j * NT * 16);
   };
   auto request_q = [&](const Ask& a, auto half, auto stage, auto which) {
     constexpr int h = decltype(half)::value, j = decltype(which)::value;
@@ -233,80 +210,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     bool in;
     if constexpr (Q_ALONG) {
       src = a.q[h] + q_off[h][j];
-      in = a.k0 + q_at[0][j % PAR] < k_end;
+      in = a.k0 + q_k0 < k_end;
     } else {
       const int k = a.k0 + q_row + j * Q_NEXT;
       in = k < k_end;
-      src = a.q[h] + q_at[h][j % PAR] + (LISTED && q_listed ? listed_row[j] : k) * ldq;
+      src = a.q[h] + q_at[h] + (LISTED && q_listed ? listed_row[j] : k) * ldq;
     }
-    dma(in ? (const void*)src : zeros, to + at_q(h, decltype(stage)::value) + j * NT * UNIT * EB);
+    ffn_dma16(in ? (const void*)src : zeros, to + at_q(h, decltype(stage)::value) + j * NT * 16);
   };
-  // rows of any length: through registers.  The source of a group of K tile kt, and how many of its entries there are
-  auto p_src = [&](int kt, int h, int j, int& have) -> const T* {
-    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
-    const T* const base = seg ? p1 : p0;
-    if constexpr (P_ALONG) {
-      have = min(V, p.k - (k0 + p_at[h][0]));
-      return base + p_off[h][j] + k0;
-    } else {
-      const int k = k0 + p_row + j * P_NEXT;
-      have = k < p.k ? min(V, p.m - p_at[h][0]) : 0;
-      return base + (have > 0 ? p_k(k) * ldp + p_at[h][0] : 0);
-    }
-  };
-  auto q_src = [&](int kt, int h, int j, int& have) -> const T* {
-    const int seg = kt >= seg_tiles, k0 = (kt - seg * seg_tiles) * BK;
-    const T* const base = (GATED ? h : seg) ? q1 : q0;
-    if constexpr (Q_ALONG) {
-      have = min(V, p.k - (k0 + q_at[h][0]));
-      return base + q_off[h][j] + k0;
-    } else {
-      const int k = k0 + q_row + j * Q_NEXT;
-      have = k < p.k ? min(V, p.n - q_at[h][0]) : 0;
-      return base + (have > 0 ? q_k(k) * ldq + q_at[h][0] : 0);
-    }
-  };
-  v4i held[2 * (JP + JQ)];
-  auto load_group = [=](const T* s, int have) -> v4i {
-    if (have >= V) {
-      v4i g;
-      __builtin_memcpy(&g, s, 16);
-      return g;
-    }
-    T e[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = i < have ? s[i] : T(0);
-    v4i g;
-    __builtin_memcpy(&g, e, 16);
-    return g;
-  };
-  auto hold = [&](int kt) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int j = 0; j < JP; ++j) {
-        int have;
-        const T* s = p_src(kt, h, j, have);
-        held[h * (JP + JQ) + j] = load_group(s, have);
-      }
-#pragma unroll
-      for (int j = 0; j < JQ; ++j) {
-        int have;
-        const T* s = q_src(kt, h, j, have);
-        held[h * (JP + JQ) + JP + j] = load_group(s, have);
-      }
-    }
-  };
-  auto put = [&]() {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int j = 0; j < JP; ++j) *reinterpret_cast<v4i*>(smem + at_p(h, 0) + (j * NT + t) * 16) = held[h * (JP + JQ) + j];
-#pragma unroll
-      for (int j = 0; j < JQ; ++j) *reinterpret_cast<v4i*>(smem + at_q(h, 0) + (j * NT + t) * 16) = held[h * (JP + JQ) + JP + j];
-    }
-  };
-
   // ---- operands of the matrix instructions, from LDS ----
   // 32 rows of a half of an operand and KSTEP entries of k.  A lane's addresses in half 0 of stage 0: along k one for every step (the
   // keys differ), across k one for every block of 32 rows; the rest is an offset in the instruction.
@@ -449,108 +360,86 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
       }
     }
   };
-  if constexpr (DMA) {
-    // Two K tiles in LDS, each in four halves.  The quadrants of a tile are multiplied in the order (P0, Q0), (P0, Q1), (P1, Q1),
-    // (P1, Q0).  The operands of a quadrant are read from LDS one or two quadrants before, into registers that are free by then, and a
-    // half's place in LDS is taken by the same half of the tile after next as soon as it is in everybody's registers: wavefronts meet
-    // twice a tile, behind the first quadrant and behind the third, and a transfer has four to five quadrants (2 000 to 2 500 cycles for
-    // tiles of 256) to arrive.  64 KB take 1.1 us to arrive in a compute unit that has nothing else to do.
-    //   quadrant    1          2          3              4
-    //   reads       Q1         P1         Q0, next tile  P0, next tile
-    //   asks for    P1, next   Q0, after  P0, after      Q1, after next
-    if (kt_lo < kt_hi) {
-      const int last = kt_hi - 1;
-      const std::integral_constant<int, 2> c2{};
-      auto all_p = [&](const Ask& a, auto half, auto stage) { ffn_for<0, JP>([&](auto j) { request_p(a, half, stage, j); }); };
-      auto all_q = [&](const Ask& a, auto half, auto stage) { ffn_for<0, JQ>([&](auto j) { request_q(a, half, stage, j); }); };
-      renew_list(kt_lo);
-      look_up(kt_lo);
-      Ask a = prepare(kt_lo);
-      all_q(a, c0, c0);
-      all_p(a, c0, c0);
-      all_q(a, c1, c0);
-      all_p(a, c1, c0);
-      look_up(min(kt_lo + 1, last));
-      a = prepare(min(kt_lo + 1, last));
-      all_q(a, c0, c1);
-      all_p(a, c0, c1);
-      all_q(a, c1, c1);
-      meet(std::integral_constant<int, 5 * JP>{});
-      ffn_for<0, L::STEPS>([&](auto ks) { read_q(c0, c0, c0, ks); read_p(c0, c0, ks); });
-      settle_q(c0);
+  // Two K tiles in LDS, each in four halves.  The quadrants of a tile are multiplied in the order (P0, Q0), (P0, Q1), (P1, Q1),
+  // (P1, Q0).  The operands of a quadrant are read from LDS one or two quadrants before, into registers that are free by then, and a
+  // half's place in LDS is taken by the same half of the tile after next as soon as it is in everybody's registers: wavefronts meet
+  // twice a tile, behind the first quadrant and behind the third, and a transfer has four to five quadrants (2 000 to 2 500 cycles for
+  // tiles of 256) to arrive.  64 KB take 1.1 us to arrive in a compute unit that has nothing else to do.
+  //   quadrant    1          2          3              4
+  //   reads       Q1         P1         Q0, next tile  P0, next tile
+  //   asks for    P1, next   Q0, after  P0, after      Q1, after next
+  if (kt_lo < kt_hi) {
+    const int last = kt_hi - 1;
+    const std::integral_constant<int, 2> c2{};
+    auto all_p = [&](const Ask& a, auto half, auto stage) { ffn_for<0, JP>([&](auto j) { request_p(a, half, stage, j); }); };
+    auto all_q = [&](const Ask& a, auto half, auto stage) { ffn_for<0, JQ>([&](auto j) { request_q(a, half, stage, j); }); };
+    renew_list(kt_lo);
+    look_up(kt_lo);
+    Ask a = prepare(kt_lo);
+    all_q(a, c0, c0);
+    all_p(a, c0, c0);
+    all_q(a, c1, c0);
+    all_p(a, c1, c0);
+    look_up(min(kt_lo + 1, last));
+    a = prepare(min(kt_lo + 1, last));
+    all_q(a, c0, c1);
+    all_p(a, c0, c1);
+    all_q(a, c1, c1);
+    meet(std::integral_constant<int, 5 * JP>{});
+    ffn_for<0, L::STEPS>([&](auto ks) { read_q(c0, c0, c0, ks); read_p(c0, c0, ks); });
+    settle_q(c0);
+    settle_p();
+    meet(std::integral_constant<int, 4 * JP>{});
+    constexpr int EACH = (JP + L::STEPS - 1) / L::STEPS;     // transfers behind a step
+    auto some = [&](auto ks, auto&& request) {
+      constexpr int lo = decltype(ks)::value * EACH, hi = lo + EACH < JP ? lo + EACH : JP;
+      ffn_for<lo, hi>(request);
+    };
+    // tile kt in `stage`, its first half of Q in registers `now`, that of the next tile goes into `next`
+    auto tile = [&](int kt, auto stage, auto other, auto now, auto next) {
+      // a: the next tile's
+      quadrant(c0, c0, now, [&](auto ks) {
+        read_q(stage, c1, c1, ks);
+        some(ks, [&](auto j) { request_p(a, c1, other, j); });
+      });
+      settle_q(c1);
+      meet(std::integral_constant<int, 3 * JP>{});
+      // (behind the last tiles the last one again, which nobody reads: the counts stay, and a branch would cost registers)
+      const int ahead = min(kt + 2, last);
+      if (kt + 2 <= last) renew_list(ahead);
+      look_up(ahead);
+      a = prepare(ahead);
+      quadrant(c0, c1, c1, [&](auto ks) {
+        read_p(stage, c1, ks);
+        some(ks, [&](auto j) { request_q(a, c0, stage, j); });
+      });
       settle_p();
-      meet(std::integral_constant<int, 4 * JP>{});
-      constexpr int EACH = (JP + L::STEPS - 1) / L::STEPS;     // transfers behind a step
-      auto some = [&](auto ks, auto&& request) {
-        constexpr int lo = decltype(ks)::value * EACH, hi = lo + EACH < JP ? lo + EACH : JP;
-        ffn_for<lo, hi>(request);
-      };
-      // tile kt in `stage`, its first half of Q in registers `now`, that of the next tile goes into `next`
-      auto tile = [&](int kt, auto stage, auto other, auto now, auto next) {
-        // a: the next tile's
-        quadrant(c0, c0, now, [&](auto ks) {
-          read_q(stage, c1, c1, ks);
-          some(ks, [&](auto j) { request_p(a, c1, other, j); });
-        });
-        settle_q(c1);
-        meet(std::integral_constant<int, 3 * JP>{});
-        // (behind the last tiles the last one again, which nobody reads: the counts stay, and a branch would cost registers)
-        const int ahead = min(kt + 2, last);
-        if (kt + 2 <= last) renew_list(ahead);
-        look_up(ahead);
-        a = prepare(ahead);
-        quadrant(c0, c1, c1, [&](auto ks) {
-          read_p(stage, c1, ks);
-          some(ks, [&](auto j) { request_q(a, c0, stage, j); });
-        });
-        settle_p();
-        quadrant(c1, c1, c1, [&](auto ks) {
-          read_q(other, c0, next, ks);
-          some(ks, [&](auto j) { request_p(a, c0, stage, j); });
-        });
-        settle_q(next);
-        meet(std::integral_constant<int, 3 * JP>{});
-        quadrant(c1, c0, now, [&](auto ks) {
-          read_p(other, c0, ks);
-          some(ks, [&](auto j) { request_q(a, c1, stage, j); });
-        });
-        settle_p();
-      };
-      for (int kt = kt_lo;;) {
-        tile(kt, c0, c1, c0, c2);
-        if (++kt == kt_hi) break;
-        tile(kt, c1, c0, c2, c0);
-        if (++kt == kt_hi) break;
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may still be on its way into LDS when the workgroup ends
+      quadrant(c1, c1, c1, [&](auto ks) {
+        read_q(other, c0, next, ks);
+        some(ks, [&](auto j) { request_p(a, c0, stage, j); });
+      });
+      settle_q(next);
+      meet(std::integral_constant<int, 3 * JP>{});
+      quadrant(c1, c0, now, [&](auto ks) {
+        read_p(other, c0, ks);
+        some(ks, [&](auto j) { request_q(a, c1, stage, j); });
+      });
+      settle_p();
+    };
+    for (int kt = kt_lo;;) {
+      tile(kt, c0, c1, c0, c2);
+      if (++kt == kt_hi) break;
+      tile(kt, c1, c0, c2, c0);
+      if (++kt == kt_hi) break;
     }
-  } else {
-    if (kt_lo < kt_hi) {
-      renew_list(kt_lo);
-      hold(kt_lo);
-    }
-    for (int kt = kt_lo; kt < kt_hi; ++kt) {
-      __syncthreads();
-      put();
-      __syncthreads();
-      if (kt + 1 < kt_hi) {
-        renew_list(kt + 1);
-        hold(kt + 1);
-      }
-      static_assert(DMA || !PARTS, "floats always go straight into LDS");
-      ffn_for<0, L::STEPS>([&](auto ks) { read_p(c0, c0, ks); read_q(c0, c0, c0, ks); read_q(c0, c1, c1, ks); });
-      quadrant(c0, c0, c0, [](auto) {});
-      quadrant(c0, c1, c1, [](auto) {});
-      ffn_for<0, L::STEPS>([&](auto ks) { read_p(c0, c1, ks); });
-      quadrant(c1, c1, c1, [](auto) {});
-      quadrant(c1, c0, c0, [](auto) {});
-    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing may still be on its way into LDS when the workgroup ends
   }
 
   // ---- results: the lane has row l32 of a block, its columns 16 h .. 16 h + 15 ----
   const int n = p.n, m = p.m;
-  auto store = [&](T* c, int64_t ldc, int row, int col, const floatx16& v) {      // row < 0: none
-    if constexpr (ROWS == kFfnWholeRows) {
+  // rows of any length, and rows for the next product, whole groups with zeros behind the last column; row < 0: none
+  auto store = [&](T* c, int64_t ldc, int row, int col, const floatx16& v) {
+    if constexpr (WHOLE) {
       store_block_pairs<DT, false>(v, row, false, col, c, nullptr, 0, (int)ldc);
     } else if (row >= 0) {
       T out[16];
@@ -566,13 +455,29 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
       }
     }
   };
+  auto store_operand = [&](T* c, int64_t ldc, int row, int col, const floatx16& v) {
+    floatx16 out = v;
+    if constexpr (!WHOLE) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) out[e] = col + e < n ? v[e] : 0.0f;
+    }
+    store_block_pairs<DT, false>(out, row, false, col, c, nullptr, 0, (int)ldc);
+  };
   auto load16 = [&](const T* c, int64_t ldc, int row, int col, float (&out)[16]) {
     const T* s = c + (int64_t)row * ldc + col;
 #pragma unroll
     for (int g = 0; g < 16 / V; ++g) {
-      const v4i q = load_group(s + g * V, row < 0 ? 0 : n - col - g * V);
       T e[V];
-      __builtin_memcpy(e, &q, 16);
+      const int have = row < 0 ? 0 : n - col - g * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = T(0);
+      if (have >= V) {
+        __builtin_memcpy(e, s + g * V, 16);
+      } else if (!WHOLE) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (i < have) e[i] = s[g * V + i];
+      }
 #pragma unroll
       for (int i = 0; i < V; ++i) out[g * V + i] = (float)e[i];
     }
@@ -613,17 +518,18 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
           ffn_act(p.activation, acc[mi][ni][e], a, da);
           hidden[e] = a * acc[mi][ni + NB][e];
         }
-        store(static_cast<T*>(p.c[0]), p.ldc, row, col, hidden);
+        store_operand(static_cast<T*>(p.c[0]), p.ldc, row, col, hidden);
         if (p.saved) {
           T* g = static_cast<T*>(p.saved);
-          store(g, p.ldc, row, col, acc[mi][ni]);
-          store(g + (int64_t)m * n, p.ldc, row, col, acc[mi][ni + NB]);
+          store(g, n, row, col, acc[mi][ni]);
+          store(g + (int64_t)m * n, n, row, col, acc[mi][ni + NB]);
+          if constexpr (!WHOLE) store(g + 2 * (int64_t)m * n, n, row, col, hidden);
         }
       } else if constexpr (WHAT == kFfnGateGrad) {
         float g[16], u[16];
         const T* sv = static_cast<const T*>(p.saved);
-        load16(sv, p.ldc, row, col, g);
-        load16(sv + (int64_t)m * n, p.ldc, row, col, u);
+        load16(sv, n, row, col, g);
+        load16(sv + (int64_t)m * n, n, row, col, u);
         floatx16 dg, du;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -632,8 +538,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
           dg[e] = acc[mi][ni][e] * u[e] * da;
           du[e] = acc[mi][ni][e] * a;
         }
-        store(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
-        store(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
+        store_operand(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
+        store_operand(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
       } else {
         store(static_cast<T*>(p.c[z]), p.ldc, out_row, col, acc[mi][ni]);
       }
@@ -641,9 +547,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
   }
 }
 
-template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int ROWS>
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, bool WHOLE>
 hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
-  auto kernel = ffn_gemm_kernel<DT, P_ALONG, Q_ALONG, WHAT, BM, BN, WAVES_M, WAVES_N, ROWS>;
+  auto kernel = ffn_gemm_kernel<DT, P_ALONG, Q_ALONG, WHAT, BM, BN, WAVES_M, WAVES_N, WHOLE>;
   constexpr int cols = WHAT == kFfnUp ? BN / 2 : BN;
   g.m_tiles = (g.m + BM - 1) / BM;
   g.n_tiles = (g.n + cols - 1) / cols;
@@ -658,23 +564,24 @@ hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, bool WHOLE>
+hipError_t ffn_launch_rows(const FfnGemm& g, int tile, hipStream_t s) {
+  if constexpr (DT != kF32)
+    if (tile == 1) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 256, 2, 4, WHOLE>(g, s);
+  return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, WHOLE>(g, s);
+}
 template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT>
-hipError_t ffn_launch_what(const FfnGemm& g, int tile, int rows, hipStream_t s) {
-  if constexpr (DT != kF32)
-    if (rows == kFfnAnyRows) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, kFfnAnyRows>(g, s);
-  if (rows != kFfnWholeRows) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, kFfnWordRows>(g, s);
-  if constexpr (DT != kF32)
-    if (tile == 1) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 256, 2, 4, kFfnWholeRows>(g, s);
-  return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, kFfnWholeRows>(g, s);
+hipError_t ffn_launch_what(const FfnGemm& g, int tile, bool whole, hipStream_t s) {
+  return whole ? ffn_launch_rows<DT, P_ALONG, Q_ALONG, WHAT, true>(g, tile, s) : ffn_launch_rows<DT, P_ALONG, Q_ALONG, WHAT, false>(g, tile, s);
 }
 
-template <int DT> hipError_t ffn_launch_type(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s) {
+template <int DT> hipError_t ffn_launch_type(FfnProduct what, const FfnGemm& g, int tile, bool whole, hipStream_t s) {
   switch (what) {
-    case kFfnUp: return ffn_launch_what<DT, true, true, kFfnUp>(g, tile, rows, s);
-    case kFfnDown: return ffn_launch_what<DT, true, true, kFfnDown>(g, tile, rows, s);
-    case kFfnGateGrad: return ffn_launch_what<DT, true, false, kFfnGateGrad>(g, tile, rows, s);
-    case kFfnInGrad: return ffn_launch_what<DT, true, false, kFfnInGrad>(g, tile, rows, s);
-    case kFfnWGrad: return ffn_launch_what<DT, false, false, kFfnWGrad>(g, tile, rows, s);
+    case kFfnUp: return ffn_launch_what<DT, true, true, kFfnUp>(g, tile, whole, s);
+    case kFfnDown: return ffn_launch_what<DT, true, true, kFfnDown>(g, tile, whole, s);
+    case kFfnGateGrad: return ffn_launch_what<DT, true, false, kFfnGateGrad>(g, tile, whole, s);
+    case kFfnInGrad: return ffn_launch_what<DT, true, false, kFfnInGrad>(g, tile, whole, s);
+    case kFfnWGrad: return ffn_launch_what<DT, false, false, kFfnWGrad>(g, tile, whole, s);
     default: return hipErrorInvalidValue;
   }
 }

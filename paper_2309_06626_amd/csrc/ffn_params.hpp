@@ -18,10 +18,7 @@ enum FfnProduct : int32_t {
   kFfnProducts = 5
 };
 
-// How the rows of the operands lie: whole 16-byte groups; whole words (of floats any row, of 16-bit entries an even number); any number of
-// 16-bit entries, which pass through registers.
-enum FfnRows : int { kFfnWholeRows = 0, kFfnWordRows = 1, kFfnAnyRows = 2 };
-
+// Rows of operands are whole 16-byte groups, with zeros behind the last entry; so are the rows that a product leaves for the next one.
 struct FfnGemm {
   const void* p[2];
   const void* q[2];
@@ -32,9 +29,9 @@ struct FfnGemm {
   int32_t segments;            // pairs (p[s], q[s]) whose products are summed
   int32_t batch;               // results c[z] of p[z] with q[0]
   void* c[2];
-  int64_t ldc;
+  int64_t ldc;                 // (of kFfnUp's and kFfnGateGrad's results: whole groups)
   const int32_t* c_rows;       // row of c that receives result row i; null: i
-  void* saved;                 // kFfnUp: [3][m][n] or null, c[0] is then its third matrix.  kFfnGateGrad: read
+  void* saved;                 // [3][m][n].  kFfnUp: may be null; where n is whole groups c[0] is its third matrix.  kFfnGateGrad: read
   int32_t activation;
   int32_t splits;              // parts of the contraction, each with its sums in `partial`
   float* partial;              // [batch, or gate and up][splits][m][n]
@@ -42,10 +39,10 @@ struct FfnGemm {
   int32_t m_tiles, n_tiles, group;
 };
 
-// tile: index into the launcher's list of tile shapes; rows: FfnRows
-hipError_t ffn_launch_bf16(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s);
-hipError_t ffn_launch_f16(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s);
-hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, int rows, hipStream_t s);
+// tile: index into the launcher's list of tile shapes; whole: rows of `saved` and of all results are whole groups too
+hipError_t ffn_launch_bf16(FfnProduct what, const FfnGemm& g, int tile, bool whole, hipStream_t s);
+hipError_t ffn_launch_f16(FfnProduct what, const FfnGemm& g, int tile, bool whole, hipStream_t s);
+hipError_t ffn_launch_f32(FfnProduct what, const FfnGemm& g, int tile, bool whole, hipStream_t s);
 
 // kFfnUp (gated) and kFfnDown for a few rows
 hipError_t ffn_few_bf16(bool gated, const FfnGemm& g, bool whole, hipStream_t s);
