@@ -9,6 +9,7 @@
 #include "../../include/sparse_block.h"
 #include "ffn_act.hpp"
 #include "ffn_params.hpp"
+#include "mma_common.hpp"
 #include "rows.hpp"
 
 #include <algorithm>
@@ -112,7 +113,7 @@ struct Copies {
 //   256 workgroups of 256 x 256                         1.6 (128 or fewer 1.05: the clock is higher); across k on both sides 1.75 and 1.15
 //   512 workgroups of 128 x 128, two a compute unit     1.06 (256 or fewer 0.42); across k on both sides 1.2 and 0.62
 //   the same for floats, which have these tiles alone   2.75 (256 or fewer 1.55)
-// A launch and a tile's beginning and end take 8 us.  A contraction in parts leaves sums in
+// A launch takes 3 us, a tile's beginning and end 5, in proportion to its rows.  A contraction in parts leaves sums in
 // float, written and read once at 4 TB/s, and another launch.
 constexpr int kMostSplits = 32, kLeastTiles = 4;
 static int64_t k_tiles_of(int64_t k, int segments, int dtype) {
@@ -141,7 +142,7 @@ static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, i
       if (splits > 1 && ((splits - 1) * tiles > room * (tile ? 1 : 2) || count > 2 * room)) break;
       const double rounds = (double)(count / room), left = rest == 0 ? 0.0 : rest <= room / 2 ? half : full;
       const double per = (double)((k_tiles + splits - 1) / splits);
-      double us = 3.0 + (rounds * full + left) * per + (rounds + (rest ? 1.0 : 0.0)) * 5.0;
+      double us = 3.0 + (rounds * full + left) * per + (rounds + (rest ? 1.0 : 0.0)) * 5.0 * std::min(1.0, (double)m / edge);
       if (splits > 1) us += 4.0 + (double)splits * batch * m * cols * 8.0 / 4e6;
       if (us < best.us) best = {tile, splits, us};
     }
@@ -153,7 +154,7 @@ static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, i
 // at most kMostSplits, and at most 1 024 tiles of 128 x 128 (256 of 256 x 256) besides a result that is no larger than that itself.
 static size_t most_parts(int64_t m, int64_t n, int64_t k, int segments, int batch, int dtype) {
   const int64_t parts = std::min<int64_t>(kMostSplits, k_tiles_of(k, segments, dtype) / kLeastTiles);
-  return parts < 2 ? 0 : up256(std::min((size_t)parts * batch * m * n * 4, (size_t)128 << 20));
+  return parts < 2 ? 0 : up256(std::min((size_t)parts * batch * m * ((n + 3) & ~(int64_t)3) * 4, (size_t)128 << 20));
 }
 static size_t most_parts(const sc_ffn_desc& d, int64_t kept, bool training) {
   size_t most = std::max(most_parts(kept, d.d_hidden, d.d_in, 1, 2, d.dtype), most_parts(kept, d.d_out, d.d_hidden, 1, 1, d.dtype));
@@ -163,95 +164,134 @@ static size_t most_parts(const sc_ffn_desc& d, int64_t kept, bool training) {
   return most;
 }
 
-// The parts added up, in order, and what the product's own epilogue would have done; a row of a result a workgroup, blockIdx.y the result.
-template <typename T, int WIDTH, int WHAT> __global__ __launch_bounds__(256) void ffn_finish_kernel(const FfnGemm g) {
-  typedef float vec __attribute__((ext_vector_type(WIDTH)));
-  const int row = blockIdx.x, n = g.n;
-  const int64_t whole = (int64_t)g.m * n;
-  auto sum = [&](int z, int i) -> vec {
-    const float* p = g.partial + (int64_t)z * g.splits * whole + (int64_t)row * n + i;
-    vec v = *reinterpret_cast<const vec*>(p);
-    for (int s = 1; s < g.splits; ++s) v += *reinterpret_cast<const vec*>(p + s * whole);
+// The parts added up, in order, and what the product's own epilogue would have done; 1 024 columns of a row a workgroup, blockIdx.y the result.
+// Four columns a lane; rows of any length end within four (WHOLE: they do not).
+template <typename T, int WHAT, bool WHOLE> __global__ __launch_bounds__(256) void ffn_finish_kernel(const FfnGemm g) {
+  const int row = blockIdx.x, n = g.n, pitch = (n + 3) & ~3;
+  const int64_t whole = (int64_t)g.m * n, part = (int64_t)g.m * pitch;
+  auto sum = [&](int z, int i) -> v4f {
+    const float* p = g.partial + z * g.splits * part + (int64_t)row * pitch + i;
+    v4f v = *reinterpret_cast<const v4f*>(p);
+    int s = 1;
+    for (; s + 8 <= g.splits; s += 8) {      // eight on their way at once
+      v4f next[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) next[u] = *reinterpret_cast<const v4f*>(p + (s + u) * part);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v += next[u];
+    }
+    for (; s + 2 <= g.splits; s += 2) {
+      const v4f a = *reinterpret_cast<const v4f*>(p + s * part), b = *reinterpret_cast<const v4f*>(p + (s + 1) * part);
+      v += a;
+      v += b;
+    }
+    if (s < g.splits) v += *reinterpret_cast<const v4f*>(p + s * part);
     return v;
   };
-  auto store = [&](void* c, int64_t at, vec v) {
-    T out[WIDTH];
+  auto store = [&](T* c, int64_t at, int have, v4f v) {
+    T out[4];
 #pragma unroll
-    for (int u = 0; u < WIDTH; ++u) out[u] = (T)v[u];
-    __builtin_memcpy(static_cast<T*>(c) + at, out, sizeof(out));
+    for (int u = 0; u < 4; ++u) out[u] = (T)v[u];
+    if (WHOLE || have >= 4) {
+      __builtin_memcpy(c + at, out, sizeof(out));
+    } else {
+#pragma unroll
+      for (int u = 0; u < 3; ++u)
+        if (u < have) c[at + u] = out[u];
+    }
   };
-  for (int i = threadIdx.x * WIDTH; i < n; i += 256 * WIDTH) {
-    const int64_t at = (int64_t)row * n + i;
-    if constexpr (WHAT == kFfnUp) {
-      const vec gate = sum(0, i), up = sum(1, i);
-      vec hidden;
+  auto load = [&](const T* c, int64_t at, int have, T (&v)[4]) {
+    if (WHOLE || have >= 4) {
+      __builtin_memcpy(v, c + at, sizeof(v));
+    } else {
 #pragma unroll
-      for (int u = 0; u < WIDTH; ++u) {
+      for (int u = 0; u < 4; ++u) v[u] = u < have ? c[at + u] : T(0);
+    }
+  };
+  T* const saved = static_cast<T*>(g.saved);
+  const int i = (blockIdx.z * 256 + threadIdx.x) * 4;
+  if (i < n) {
+    const int64_t at = (int64_t)row * n + i, to = row * g.ldc + i;
+    const int have = n - i;
+    if constexpr (WHAT == kFfnUp) {
+      const v4f gate = sum(0, i), up = sum(1, i);
+      v4f hidden;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
         float a, da;
         ffn_act(g.activation, gate[u], a, da);
         hidden[u] = a * up[u];
       }
-      store(g.c[0], row * g.ldc + i, hidden);
-      if (g.saved) {
-        T* const saved = static_cast<T*>(g.saved);
-        store(saved, at, gate);
-        store(saved + whole, at, up);
-        if (saved + 2 * whole != g.c[0]) store(saved + 2 * whole, at, hidden);
+      store(static_cast<T*>(g.c[0]), to, have, hidden);
+      if (saved) {
+        store(saved, at, have, gate);
+        store(saved + whole, at, have, up);
+        if (saved + 2 * whole != g.c[0]) store(saved + 2 * whole, at, have, hidden);
       }
     } else if constexpr (WHAT == kFfnGateGrad) {
-      const vec dh = sum(0, i);
-      T gate[WIDTH], up[WIDTH];
-      __builtin_memcpy(gate, static_cast<const T*>(g.saved) + at, sizeof(gate));
-      __builtin_memcpy(up, static_cast<const T*>(g.saved) + whole + at, sizeof(up));
-      vec dg, du;
+      const v4f dh = sum(0, i);
+      T gate[4], up[4];
+      load(saved, at, have, gate);
+      load(saved + whole, at, have, up);
+      v4f dg, du;
 #pragma unroll
-      for (int u = 0; u < WIDTH; ++u) {
+      for (int u = 0; u < 4; ++u) {
         float a, da;
         ffn_act(g.activation, (float)gate[u], a, da);
         dg[u] = dh[u] * (float)up[u] * da;
         du[u] = dh[u] * a;
       }
-      store(g.c[0], row * g.ldc + i, dg);
-      store(g.c[1], row * g.ldc + i, du);
+      store(static_cast<T*>(g.c[0]), to, have, dg);
+      store(static_cast<T*>(g.c[1]), to, have, du);
     } else {
-      store(g.c[blockIdx.y], (g.c_rows ? (int64_t)g.c_rows[row] : row) * g.ldc + i, sum(blockIdx.y, i));
+      store(static_cast<T*>(g.c[blockIdx.y]), g.c_rows ? g.c_rows[row] * g.ldc + i : to, have, sum(blockIdx.y, i));
     }
   }
-  if (WHAT == kFfnUp || WHAT == kFfnGateGrad)      // zeros behind the last entry of an operand's row
-    for (int64_t i = n + threadIdx.x; i < g.ldc; i += 256) {
-      static_cast<T*>(g.c[0])[row * g.ldc + i] = T(0);
-      if (WHAT == kFfnGateGrad) static_cast<T*>(g.c[1])[row * g.ldc + i] = T(0);
+  if (!WHOLE && (WHAT == kFfnUp || WHAT == kFfnGateGrad))      // zeros behind the last entry of an operand's row
+    if (blockIdx.z == 0 && n + (int)threadIdx.x < g.ldc) {
+      static_cast<T*>(g.c[0])[row * g.ldc + n + threadIdx.x] = T(0);
+      if (WHAT == kFfnGateGrad) static_cast<T*>(g.c[1])[row * g.ldc + n + threadIdx.x] = T(0);
     }
 }
 
-template <typename T, int WIDTH> static void finish_width(FfnProduct what, const FfnGemm& g, hipStream_t s) {
-  const dim3 grid((unsigned)g.m, g.batch), block(256);
-  if (what == kFfnUp) ffn_finish_kernel<T, WIDTH, kFfnUp><<<grid, block, 0, s>>>(g);
-  else if (what == kFfnGateGrad) ffn_finish_kernel<T, WIDTH, kFfnGateGrad><<<grid, block, 0, s>>>(g);
-  else ffn_finish_kernel<T, WIDTH, kFfnDown><<<grid, block, 0, s>>>(g);
+template <typename T, bool WHOLE> static void finish_rows(FfnProduct what, const FfnGemm& g, hipStream_t s) {
+  const dim3 grid((unsigned)g.m, g.batch, (unsigned)((g.n + 1023) / 1024)), block(256);
+  if (what == kFfnUp) ffn_finish_kernel<T, kFfnUp, WHOLE><<<grid, block, 0, s>>>(g);
+  else if (what == kFfnGateGrad) ffn_finish_kernel<T, kFfnGateGrad, WHOLE><<<grid, block, 0, s>>>(g);
+  else ffn_finish_kernel<T, kFfnDown, WHOLE><<<grid, block, 0, s>>>(g);
 }
-template <typename T> static void finish_type(FfnProduct what, const FfnGemm& g, hipStream_t s) {
-  if (g.n % 4 == 0) finish_width<T, 4>(what, g, s);
-  else finish_width<T, 1>(what, g, s);
+template <typename T> static void finish_type(FfnProduct what, const FfnGemm& g, bool whole, hipStream_t s) {
+  if (whole) finish_rows<T, true>(what, g, s);
+  else finish_rows<T, false>(what, g, s);
 }
-static hipError_t finish(int dtype, FfnProduct what, const FfnGemm& g, hipStream_t s) {
-  if (dtype == SC_BF16) finish_type<__bf16>(what, g, s);
-  else if (dtype == SC_F16) finish_type<_Float16>(what, g, s);
-  else finish_type<float>(what, g, s);
+static hipError_t finish(int dtype, FfnProduct what, const FfnGemm& g, bool whole, hipStream_t s) {
+  if (dtype == SC_BF16) finish_type<__bf16>(what, g, whole, s);
+  else if (dtype == SC_F16) finish_type<_Float16>(what, g, whole, s);
+  else finish_type<float>(what, g, whole, s);
   return hipGetLastError();
 }
 
-// a product in the tiles and parts that its sizes ask for
-static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, bool whole, float* parts, hipStream_t s) {
-  const Tiling t = pick_tiling(what, g.m, what == kFfnUp ? 2 * (int64_t)g.n : g.n, g.k, g.segments, g.batch, dtype);
+static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, const Tiling& t, bool whole, float* parts, hipStream_t s) {
   g.splits = t.splits;
   g.partial = parts;
   const hipError_t e = launch(dtype, what, g, t.tile, whole, s);
-  return e == hipSuccess && g.splits > 1 ? finish(dtype, what, g, s) : e;
+  return e == hipSuccess && g.splits > 1 ? finish(dtype, what, g, whole, s) : e;
 }
-// kFfnUp and kFfnDown
+// a product in the tiles and parts that its sizes ask for
+static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, bool whole, float* parts, hipStream_t s) {
+  return multiply(dtype, what, g, pick_tiling(what, g.m, what == kFfnUp ? 2 * (int64_t)g.n : g.n, g.k, g.segments, g.batch, dtype), whole, parts, s);
+}
+// kFfnUp and kFfnDown.  A few rows: the kernel for them reads all of P in every workgroup, at 4.2 TB/s in all, where the tiles' workgroups
+// have eight (gated: four) times the outputs.  bf16, gated 2 048 -> 5 632 and back: 8 rows 18 us, in tiles 22; 16 rows 26 and 23; 64 rows 58
+// and 28.  512 -> 1 408 and back: 64 rows 15 and 17.  Rows that are not whole groups would have to be copied for tiles, weights too.
 static hipError_t multiply_forward(int dtype, FfnProduct what, FfnGemm& g, bool whole, float* parts, hipStream_t s) {
-  if (g.m > kFewRows) return multiply(dtype, what, g, whole, parts, s);
+  const int64_t cols = what == kFfnUp ? 2 * (int64_t)g.n : g.n;
+  const Tiling t = pick_tiling(what, g.m, cols, g.k, g.segments, g.batch, dtype);
+  if (g.m > kFewRows) return multiply(dtype, what, g, t, whole, parts, s);
+  if (whole) {
+    const double row = (double)g.k * elem_bytes(dtype), rows = g.m <= 8 ? g.m : (g.m + 15) / 16 * 16;
+    if (3.0 + cols * row / 6e6 + (g.n + 15) / 16 * rows * row / 4.2e6 > t.us) return multiply(dtype, what, g, t, whole, parts, s);
+  }
   switch (dtype) {
     case SC_BF16: return ffn_few_bf16(what == kFfnUp, g, whole, s);
     case SC_F16: return ffn_few_f16(what == kFfnUp, g, whole, s);

@@ -482,20 +482,21 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
       for (int i = 0; i < V; ++i) out[g * V + i] = (float)e[i];
     }
   };
-  if (p.splits > 1) {                                          // sums of this part: [batch, or gate and up][splits][m][n]
+  if (p.splits > 1) {                                          // sums of this part: [batch, or gate and up][splits][m][pitch]
+    const int pitch = (n + 3) & ~3;
 #pragma unroll
     for (int mi = 0; mi < 2 * MB; ++mi) {
       const int row = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
 #pragma unroll
       for (int ni = 0; ni < 2 * NB; ++ni) {
         const int col = n0 + (GATED ? 0 : ni / NB * PN) + (wn * NB + ni % NB) * 32 + 16 * h;
-        float* const dst = p.partial + (((int64_t)(GATED ? ni / NB : z) * p.splits + split) * m + row) * n + col;
-        if (row < m && col + 16 <= n) {
+        float* const dst = p.partial + (((int64_t)(GATED ? ni / NB : z) * p.splits + split) * m + row) * pitch + col;
+        if (row < m && col + 16 <= pitch) {
           __builtin_memcpy(dst, &acc[mi][ni], 64);
         } else if (row < m) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (col + e < n) dst[e] = acc[mi][ni][e];
+            if (col + e < pitch) dst[e] = acc[mi][ni][e];
         }
       }
     }

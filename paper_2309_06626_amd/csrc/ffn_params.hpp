@@ -34,7 +34,7 @@ struct FfnGemm {
   void* saved;                 // [3][m][n].  kFfnUp: may be null; where n is whole groups c[0] is its third matrix.  kFfnGateGrad: read
   int32_t activation;
   int32_t splits;              // parts of the contraction, each with its sums in `partial`
-  float* partial;              // [batch, or gate and up][splits][m][n]
+  float* partial;              // [batch, or gate and up][splits][m][n up to a multiple of 4]
   // set by the launcher
   int32_t m_tiles, n_tiles, group;
 };

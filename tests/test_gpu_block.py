@@ -294,6 +294,8 @@ def test_ffn_forward_and_gradients(c):
 FEW = [(rows, di, dh, do, dtype, "silu", mask, 0, 0)
        for dtype, di, dh, do in (("bf16", 520, 1037, 264), ("f16", 1048, 264, 5), ("f32", 333, 68, 130), ("f16", 77, 1030, 1031))
        for rows, mask in ((3, "all"), (4, "all"), (8, "half"), (8, "all"), (9, "all"), (15, "half"))]
+FEW += [(64, 1024, 5632, 1024, "bf16", "gelu", "all", 0, 0), (70, 2048, 5632, 1024, "f16", "silu", "half", 0, 0),
+        (40, 1024, 4096, 2048, "f32", "silu", "half", 0, 0)]
 
 
 @pytest.mark.parametrize("c", FEW, ids=lambda c: "-".join(map(str, c)))
