@@ -513,12 +513,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
       const int col = n0 + ni / NB * PN + (wn * NB + ni % NB) * 32 + 16 * h;
       if constexpr (WHAT == kFfnUp) {
         floatx16 hidden;
+        ffn_act_kind(p.activation, [&](auto kind) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float a, da;
-          ffn_act(p.activation, acc[mi][ni][e], a, da);
-          hidden[e] = a * acc[mi][ni + NB][e];
-        }
+          for (int e = 0; e < 16; ++e) {
+            float a, da;
+            ffn_act_of<decltype(kind)::value>(acc[mi][ni][e], a, da);
+            hidden[e] = a * acc[mi][ni + NB][e];
+          }
+        });
         store_operand(static_cast<T*>(p.c[0]), p.ldc, row, col, hidden);
         if (p.saved) {
           T* g = static_cast<T*>(p.saved);
@@ -532,13 +534,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
         load16(sv, n, row, col, g);
         load16(sv + (int64_t)m * n, n, row, col, u);
         floatx16 dg, du;
+        ffn_act_kind(p.activation, [&](auto kind) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float a, da;
-          ffn_act(p.activation, g[e], a, da);
-          dg[e] = acc[mi][ni][e] * u[e] * da;
-          du[e] = acc[mi][ni][e] * a;
-        }
+          for (int e = 0; e < 16; ++e) {
+            float a, da;
+            ffn_act_of<decltype(kind)::value>(g[e], a, da);
+            dg[e] = acc[mi][ni][e] * u[e] * da;
+            du[e] = acc[mi][ni][e] * a;
+          }
+        });
         store_operand(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
         store_operand(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
       } else {
