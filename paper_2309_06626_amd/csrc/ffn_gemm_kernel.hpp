@@ -463,24 +463,25 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     }
     store_block_pairs<DT, false>(out, row, false, col, c, nullptr, 0, (int)ldc);
   };
-  auto load16 = [&](const T* c, int64_t ldc, int row, int col, float (&out)[16]) {
-    const T* s = c + (int64_t)row * ldc + col;
+  // 16 columns of a row of `saved`, as they lie
+  struct Raw { v4i g[16 / V]; };
+  auto load16 = [&](const T* c, int row, int col) {
+    Raw raw;
+    const T* s = c + (int64_t)row * n + col;
 #pragma unroll
     for (int g = 0; g < 16 / V; ++g) {
-      T e[V];
       const int have = row < 0 ? 0 : n - col - g * V;
-#pragma unroll
-      for (int i = 0; i < V; ++i) e[i] = T(0);
+      raw.g[g] = v4i{0, 0, 0, 0};
       if (have >= V) {
-        __builtin_memcpy(e, s + g * V, 16);
+        __builtin_memcpy(&raw.g[g], s + g * V, 16);
       } else if (!WHOLE) {
+        T e[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < have) e[i] = s[g * V + i];
+        for (int i = 0; i < V; ++i) e[i] = i < have ? s[g * V + i] : T(0);
+        __builtin_memcpy(&raw.g[g], e, 16);
       }
-#pragma unroll
-      for (int i = 0; i < V; ++i) out[g * V + i] = (float)e[i];
     }
+    return raw;
   };
   if (p.splits > 1) {                                          // sums of this part: [batch, or gate and up][splits][m][pitch]
     const int pitch = (n + 3) & ~3;
@@ -502,15 +503,49 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     }
     return;
   }
+  auto row_of = [&](int mi) {
+    const int i = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
+    return i < m ? i : -1;
+  };
+  auto col_of = [&](int ni) { return n0 + ni / NB * PN + (wn * NB + ni % NB) * 32 + 16 * h; };
+  if constexpr (WHAT == kFfnGateGrad) {
+    // a block's rows of gate and up are asked for a block ahead
+    const T* const gate = static_cast<const T*>(p.saved);
+    const T* const up = gate + (int64_t)m * n;
+    Raw next_g = load16(gate, row_of(0), col_of(0)), next_u = load16(up, row_of(0), col_of(0));
+    ffn_for<0, 4 * MB * NB>([&](auto block) {
+      constexpr int b = decltype(block)::value, mi = b / (2 * NB), ni = b % (2 * NB), after = b + 1 < 4 * MB * NB ? b + 1 : b;
+      const Raw raw_g = next_g, raw_u = next_u;
+      if constexpr (after != b) {
+        next_g = load16(gate, row_of(after / (2 * NB)), col_of(after % (2 * NB)));
+        next_u = load16(up, row_of(after / (2 * NB)), col_of(after % (2 * NB)));
+      }
+      T g[16], u[16];
+      __builtin_memcpy(g, &raw_g, sizeof(g));
+      __builtin_memcpy(u, &raw_u, sizeof(u));
+      floatx16 dg, du;
+      ffn_act_kind(p.activation, [&](auto kind) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float a, da;
+          ffn_act_of<decltype(kind)::value>((float)g[e], a, da);
+          dg[e] = acc[mi][ni][e] * (float)u[e] * da;
+          du[e] = acc[mi][ni][e] * a;
+        }
+      });
+      store_operand(static_cast<T*>(p.c[0]), p.ldc, row_of(mi), col_of(ni), dg);
+      store_operand(static_cast<T*>(p.c[1]), p.ldc, row_of(mi), col_of(ni), du);
+    });
+    return;
+  }
 #pragma unroll
   for (int mi = 0; mi < 2 * MB; ++mi) {
-    const int i = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
-    const int row = i < m ? i : -1;
+    const int row = row_of(mi);
     int out_row = row;
     if (row >= 0 && p.c_rows) out_row = p.c_rows[row];
 #pragma unroll
     for (int ni = 0; ni < (GATED ? NB : 2 * NB); ++ni) {
-      const int col = n0 + ni / NB * PN + (wn * NB + ni % NB) * 32 + 16 * h;
+      const int col = col_of(ni);
       if constexpr (WHAT == kFfnUp) {
         floatx16 hidden;
         ffn_act_kind(p.activation, [&](auto kind) {
@@ -528,23 +563,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
           store(g + (int64_t)m * n, n, row, col, acc[mi][ni + NB]);
           if constexpr (!WHOLE) store(g + 2 * (int64_t)m * n, n, row, col, hidden);
         }
-      } else if constexpr (WHAT == kFfnGateGrad) {
-        float g[16], u[16];
-        const T* sv = static_cast<const T*>(p.saved);
-        load16(sv, n, row, col, g);
-        load16(sv + (int64_t)m * n, n, row, col, u);
-        floatx16 dg, du;
-        ffn_act_kind(p.activation, [&](auto kind) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float a, da;
-            ffn_act_of<decltype(kind)::value>(g[e], a, da);
-            dg[e] = acc[mi][ni][e] * u[e] * da;
-            du[e] = acc[mi][ni][e] * a;
-          }
-        });
-        store_operand(static_cast<T*>(p.c[0]), p.ldc, row, col, dg);
-        store_operand(static_cast<T*>(p.c[1]), p.ldc, row, col, du);
       } else {
         store(static_cast<T*>(p.c[z]), p.ldc, out_row, col, acc[mi][ni]);
       }
