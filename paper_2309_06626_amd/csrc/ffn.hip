@@ -50,7 +50,8 @@ static int64_t pitch_of(int64_t entries, int dtype) {
 static bool whole_rows(const sc_ffn_desc& d) { return (d.d_in | d.d_hidden | d.d_out) * elem_bytes(d.dtype) % 16 == 0; }
 
 // Operands whose rows are not whole 16-byte groups are copied first, kept rows alone, with zeros up to the next whole group: the products
-// then load straight into LDS and have no ends to look after.  5 000 x 423 -> 2 809 in bf16, forward and backward: COPYTIME
+// then load straight into LDS and have no ends to look after.  5 000 x 423 -> 2 809 in bf16, forward and backward, takes
+// 310 us (424 -> 2 808: 248), 699 where rows went through registers into LDS.
 constexpr int kMostCopies = 6;
 struct FfnCopies {
   struct One {
@@ -108,13 +109,21 @@ struct Copies {
   }
 };
 
-// Tile shape (0: 128 x 128, 1: 256 x 256) and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`,
-// priced with what was measured, in us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other:
-//   256 workgroups of 256 x 256                         1.6 (128 or fewer 1.05: the clock is higher); across k on both sides 1.75 and 1.15
-//   512 workgroups of 128 x 128, two a compute unit     1.06 (256 or fewer 0.42); across k on both sides 1.2 and 0.62
-//   the same for floats, which have these tiles alone   2.75 (256 or fewer 1.55)
-// A launch takes 3 us, a tile's beginning and end 5, in proportion to its rows.  A contraction in parts leaves sums in
-// float, written and read once at 4 TB/s, and another launch.
+// Tile shape and parts of the contraction for a product of m x cols results (cols: rows of Q) and `k`, priced with what was measured, in
+// us a K tile of 128 bytes of k, launches of 2 048 x 16-bit k behind each other.  `half`: half as many workgroups as there is room for, or
+// fewer (the clock is higher); `full`: as many; across k on both sides the second pair.
+//   128 x 128, two a compute unit   0.42, 1.06   0.62, 1.2     floats, which have these tiles alone: 1.55, 2.75
+//   256 x 256                       1.05, 1.6    1.15, 1.75
+//   256 x 128                       0.58, 0.8    0.72, 0.95
+// A launch takes 3 us, a tile's beginning and end 5, in proportion to its rows.  A contraction in parts leaves sums in float, written and
+// read once at 4 TB/s, and another launch.  6 272 x 2 048 -> 768 in bf16: 30.5, 40.9 and 26.9 us in these tiles; 8 192 x 2 048 -> 4 096:
+// 113 in the second, 128 in the third.
+struct FfnTileShape {
+  int rows, cols, room;
+  double half[2], full[2];
+};
+constexpr FfnTileShape kTiles[] = {{128, 128, 512, {0.42, 0.62}, {1.06, 1.2}}, {256, 256, 256, {1.05, 1.15}, {1.6, 1.75}},
+                                {256, 128, 256, {0.58, 0.72}, {0.8, 0.95}}};
 constexpr int kMostSplits = 32, kLeastTiles = 4;
 static int64_t k_tiles_of(int64_t k, int segments, int dtype) {
   const int64_t entries = 128 / elem_bytes(dtype);
@@ -130,19 +139,20 @@ static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, i
   const bool across = what == kFfnWGrad, f32 = dtype == SC_F32;
   const int64_t k_tiles = k_tiles_of(k, segments, dtype);
   Tiling best = {0, 1, 1e30};
-  for (int tile = 0; tile < 2; ++tile) {
-    if (tile == 1 && f32) break;
-    const int64_t edge = tile ? 256 : 128, room = tile ? 256 : 512;
-    const double half = f32 ? 1.55 : tile ? (across ? 1.15 : 1.05) : (across ? 0.62 : 0.42);
-    const double full = f32 ? 2.75 : tile ? (across ? 1.75 : 1.6) : (across ? 1.2 : 1.06);
-    const int64_t tiles = ((m + edge - 1) / edge) * ((cols + edge - 1) / edge) * batch;
+  for (int tile = 0; tile < (f32 ? 1 : 3); ++tile) {
+    const FfnTileShape& shape = kTiles[tile];
+    const int64_t room = shape.room;
+    const double half = f32 ? 1.55 : shape.half[across], full = f32 ? 2.75 : shape.full[across];
+    const int64_t tiles = ((m + shape.rows - 1) / shape.rows) * ((cols + shape.cols - 1) / shape.cols) * batch;
     for (int splits = 1; splits <= kMostSplits; ++splits) {
       if (splits > 1 && k_tiles / splits < kLeastTiles) break;
       const int64_t count = tiles * splits, rest = count % room;
-      if (splits > 1 && ((splits - 1) * tiles > room * (tile ? 1 : 2) || count > 2 * room)) break;
-      const double rounds = (double)(count / room), left = rest == 0 ? 0.0 : rest <= room / 2 ? half : full;
+      if (splits > 1 && ((splits - 1) * tiles > (tile ? 256 : 1024) || count > 2 * room)) break;
+      const double rounds = (double)(count / room), over = 2.0 * rest / room - 1.0;
+      // beyond half the room, tiles of 128 share some compute units, and the slower ones count
+      const double left = rest == 0 ? 0.0 : over <= 0.0 ? half : half + (full - half) * (tile == 0 ? 0.4 + 0.6 * over : over);
       const double per = (double)((k_tiles + splits - 1) / splits);
-      double us = 3.0 + (rounds * full + left) * per + (rounds + (rest ? 1.0 : 0.0)) * 5.0 * std::min(1.0, (double)m / edge);
+      double us = 3.0 + (rounds * full + left) * per + (rounds + (rest ? 1.0 : 0.0)) * 5.0 * std::min(1.0, (double)m / shape.rows);
       if (splits > 1) us += 4.0 + (double)splits * batch * m * cols * 8.0 / 4e6;
       if (us < best.us) best = {tile, splits, us};
     }
@@ -151,7 +161,7 @@ static Tiling pick_tiling(FfnProduct what, int64_t m, int64_t cols, int64_t k, i
 }
 
 // What a workspace must hold of a result's parts, whatever the number of rows up to this one: a part has four K tiles or more, and there are
-// at most kMostSplits, and at most 1 024 tiles of 128 x 128 (256 of 256 x 256) besides a result that is no larger than that itself.
+// at most kMostSplits, and at most 1 024 tiles of 128 x 128 (256 of the larger ones) besides a result that is no larger than that itself.
 static size_t most_parts(int64_t m, int64_t n, int64_t k, int segments, int batch, int dtype) {
   const int64_t parts = std::min<int64_t>(kMostSplits, k_tiles_of(k, segments, dtype) / kLeastTiles);
   return parts < 2 ? 0 : up256(std::min((size_t)parts * batch * m * ((n + 3) & ~(int64_t)3) * 4, (size_t)128 << 20));
@@ -219,7 +229,7 @@ template <typename T, int WHAT, bool WHOLE> __global__ __launch_bounds__(256) vo
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         float a, da;
-        ffn_act(g.activation, gate[u], a, da);
+        ffn_act<T>(g.activation, gate[u], a, da);
         hidden[u] = a * up[u];
       }
       store(static_cast<T*>(g.c[0]), to, have, hidden);
@@ -237,7 +247,7 @@ template <typename T, int WHAT, bool WHOLE> __global__ __launch_bounds__(256) vo
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         float a, da;
-        ffn_act(g.activation, (float)gate[u], a, da);
+        ffn_act<T>(g.activation, (float)gate[u], a, da);
         dg[u] = dh[u] * (float)up[u] * da;
         du[u] = dh[u] * a;
       }

@@ -118,7 +118,7 @@ template <int DT, int MT, int S, bool GATED, bool WHOLE, int WAVES> __global__ _
     if (n >= p.n || row >= p.m) continue;
     if constexpr (GATED) {
       float act, slope;
-      ffn_act(p.activation, v[0], act, slope);
+      ffn_act<T>(p.activation, v[0], act, slope);
       static_cast<T*>(p.c[0])[(int64_t)row * p.ldc + n] = (T)(act * v[1]);
       if (p.saved) {
         T* g = static_cast<T*>(p.saved);

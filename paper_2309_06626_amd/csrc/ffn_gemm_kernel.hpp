@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
   auto at_q = [](int h, int s) constexpr { return 4 * P_PIECE + (2 * h + s) * Q_PIECE; };
   constexpr bool GATED = WHAT == kFfnUp;                       // the halves of Q: gate and up weights of the same columns
   constexpr int COLS = GATED ? PN : BN;                        // result columns of a tile
-  static_assert(JP == JQ && JP * 5 <= 63, "the counts of transfers below");
+  static_assert(2 * JP + 3 * JQ <= 63, "the counts of transfers below");
   extern __shared__ __align__(16) unsigned char smem[];
 
   constexpr std::integral_constant<int, 0> c0{};
@@ -169,13 +169,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
   };
 
   const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char*)smem;
-  int listed_row[JP];                                          // of the tile asked for next; the halves share them
+  int listed_row[JP > JQ ? JP : JQ];                           // of the tile asked for next; the halves share them
   auto look_up = [&](int kt) {
     if constexpr (LISTED) {
       if (!list) return;
       const int first = kt * BK + (q_listed ? q_row : p_row), next = q_listed ? Q_NEXT : P_NEXT;
 #pragma unroll
-      for (int j = 0; j < JP; ++j) listed_row[j] = s_list[min(first + j * next, p.k - 1) - list_base];
+      for (int j = 0; j < (JP > JQ ? JP : JQ); ++j)
+        if ((j < JP && j < JQ) || j < (q_listed ? JQ : JP)) listed_row[j] = s_list[min(first + j * next, p.k - 1) - list_base];
     }
   };
   // What the transfers of a K tile share, worked out once: whole groups go straight into LDS, zeros beyond the end of k.
@@ -385,25 +386,26 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     all_q(a, c0, c1);
     all_p(a, c0, c1);
     all_q(a, c1, c1);
-    meet(std::integral_constant<int, 5 * JP>{});
+    meet(std::integral_constant<int, 2 * JP + 3 * JQ>{});
     ffn_for<0, L::STEPS>([&](auto ks) { read_q(c0, c0, c0, ks); read_p(c0, c0, ks); });
     settle_q(c0);
     settle_p();
-    meet(std::integral_constant<int, 4 * JP>{});
-    constexpr int EACH = (JP + L::STEPS - 1) / L::STEPS;     // transfers behind a step
-    auto some = [&](auto ks, auto&& request) {
-      constexpr int lo = decltype(ks)::value * EACH, hi = lo + EACH < JP ? lo + EACH : JP;
-      ffn_for<lo, hi>(request);
+    meet(std::integral_constant<int, 2 * JP + 2 * JQ>{});
+    auto some = [&](auto ks, auto all, auto&& request) {       // transfers behind a step
+      constexpr int n = decltype(all)::value, each = (n + L::STEPS - 1) / L::STEPS, lo = decltype(ks)::value * each;
+      ffn_for<(lo < n ? lo : n), (lo + each < n ? lo + each : n)>(request);
     };
+    constexpr std::integral_constant<int, JP> all_of_p{};
+    constexpr std::integral_constant<int, JQ> all_of_q{};
     // tile kt in `stage`, its first half of Q in registers `now`, that of the next tile goes into `next`
     auto tile = [&](int kt, auto stage, auto other, auto now, auto next) {
       // a: the next tile's
       quadrant(c0, c0, now, [&](auto ks) {
         read_q(stage, c1, c1, ks);
-        some(ks, [&](auto j) { request_p(a, c1, other, j); });
+        some(ks, all_of_p, [&](auto j) { request_p(a, c1, other, j); });
       });
       settle_q(c1);
-      meet(std::integral_constant<int, 3 * JP>{});
+      meet(std::integral_constant<int, 2 * JP + JQ>{});
       // (behind the last tiles the last one again, which nobody reads: the counts stay, and a branch would cost registers)
       const int ahead = min(kt + 2, last);
       if (kt + 2 <= last) renew_list(ahead);
@@ -411,18 +413,18 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
       a = prepare(ahead);
       quadrant(c0, c1, c1, [&](auto ks) {
         read_p(stage, c1, ks);
-        some(ks, [&](auto j) { request_q(a, c0, stage, j); });
+        some(ks, all_of_q, [&](auto j) { request_q(a, c0, stage, j); });
       });
       settle_p();
       quadrant(c1, c1, c1, [&](auto ks) {
         read_q(other, c0, next, ks);
-        some(ks, [&](auto j) { request_p(a, c0, stage, j); });
+        some(ks, all_of_p, [&](auto j) { request_p(a, c0, stage, j); });
       });
       settle_q(next);
-      meet(std::integral_constant<int, 3 * JP>{});
+      meet(std::integral_constant<int, 2 * JP + JQ>{});
       quadrant(c1, c0, now, [&](auto ks) {
         read_p(other, c0, ks);
-        some(ks, [&](auto j) { request_q(a, c1, stage, j); });
+        some(ks, all_of_q, [&](auto j) { request_q(a, c1, stage, j); });
       });
       settle_p();
     };
@@ -528,7 +530,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float a, da;
-          ffn_act_of<decltype(kind)::value>((float)g[e], a, da);
+          ffn_act_of<decltype(kind)::value, T>((float)g[e], a, da);
           dg[e] = acc[mi][ni][e] * (float)u[e] * da;
           du[e] = acc[mi][ni][e] * a;
         }
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             float a, da;
-            ffn_act_of<decltype(kind)::value>(acc[mi][ni][e], a, da);
+            ffn_act_of<decltype(kind)::value, T>(acc[mi][ni][e], a, da);
             hidden[e] = a * acc[mi][ni + NB][e];
           }
         });
@@ -589,8 +591,10 @@ hipError_t ffn_launch_tile(FfnGemm g, hipStream_t s) {
 
 template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT, bool WHOLE>
 hipError_t ffn_launch_rows(const FfnGemm& g, int tile, hipStream_t s) {
-  if constexpr (DT != kF32)
+  if constexpr (DT != kF32) {
     if (tile == 1) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 256, 2, 4, WHOLE>(g, s);
+    if (tile == 2) return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 256, 128, 4, 2, WHOLE>(g, s);
+  }
   return ffn_launch_tile<DT, P_ALONG, Q_ALONG, WHAT, 128, 128, 2, 2, WHOLE>(g, s);
 }
 template <int DT, bool P_ALONG, bool Q_ALONG, int WHAT>

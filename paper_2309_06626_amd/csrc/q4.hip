@@ -230,7 +230,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_kernel(const Q4Params p) {
       float out = v[0];
       if constexpr (MATS == 2) {
         float a, da;
-        ffn_act(p.activation, v[0], a, da);
+        ffn_act<T>(p.activation, v[0], a, da);
         out = a * v[1];
       }
       static_cast<T*>(p.y)[row * p.n + n] = (T)out;
