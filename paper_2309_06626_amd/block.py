@@ -17,6 +17,7 @@ SC_NORM_NONE, SC_NORM_RMS, SC_NORM_LAYER = 0, 1, 2
 SC_ACT_SILU, SC_ACT_GELU, SC_ACT_GELU_TANH = 0, 1, 2
 NORM_CODE = {"none": SC_NORM_NONE, "rms": SC_NORM_RMS, "layer": SC_NORM_LAYER}
 ACT_CODE = {"silu": SC_ACT_SILU, "gelu": SC_ACT_GELU, "gelu_tanh": SC_ACT_GELU_TANH}
+_F32 = torch.float32
 _TORCH_OF_CODE = {code: TORCH_DTYPE[name] for name, code in DTYPE_CODE.items()}
 
 
@@ -40,7 +41,7 @@ _declared = None
 def lib() -> ctypes.CDLL:
     """The library, with the signatures of the block operators."""
     global _declared
-    L = B.lib()
+    L = B._lib or B.lib()
     if _declared is not L:
         vp, i32, i64, size = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         out = ctypes.POINTER
@@ -106,7 +107,7 @@ def _stream_handle(stream) -> int:
 
 
 def _rows_of(t: torch.Tensor, d: int, what: str) -> int:
-    if t.dim() < 1 or t.size(-1) != d:
+    if not t.dim() or t.shape[-1] != d:
         raise ValueError(f"the last extent of {what} must be {d}")
     return t.numel() // d
 
@@ -202,30 +203,39 @@ def sparse_norm_workspace_bytes(desc: sc_norm_desc, rows: int) -> int:
 
 def _norm_shapes(desc, x, f_rows, h_rows):
     rows = _rows_of(x, desc.d, "x")
-    for r in (f_rows, h_rows):
-        if r is not None and r.rows != rows:
-            raise ValueError(f"the row set is of {r.rows} rows, x has {rows}")
-    per = desc.rows_per_gate or max(rows, 1)
-    return rows, (rows if f_rows is None else f_rows.kept), (rows if h_rows is None else h_rows.kept), -(-rows // per)
+    f_kept = h_kept = rows
+    if f_rows is not None or h_rows is not None:
+        for r in (f_rows, h_rows):
+            if r is not None and r.rows != rows:
+                raise ValueError(f"the row set is of {r.rows} rows, x has {rows}")
+        f_kept, h_kept = (rows if r is None else r.kept for r in (f_rows, h_rows))
+    per = desc.rows_per_gate
+    return rows, f_kept, h_kept, -(-rows // per) if per else min(rows, 1)
 
 
 def _elem(desc) -> torch.dtype:
-    if desc.dtype not in _TORCH_OF_CODE:
+    t = _TORCH_OF_CODE.get(desc.dtype)
+    if t is None:
         raise ScError(B.SC_ERR_UNSUPPORTED, "descriptor")
-    return _TORCH_OF_CODE[desc.dtype]
+    return t
 
 
 def sparse_norm_run(desc: sc_norm_desc, x, f, gate, w_post, b_post, w_pre, b_pre, x_new, h, f_rows: Optional[RowSet] = None,
                     h_rows: Optional[RowSet] = None, stats=None, stream=None):
     """(x_new, h): x_new = a x + b gate post(f), h = pre(x_new); tensors may be None where the C entry point allows NULL."""
-    t, f32, d = _elem(desc), torch.float32, desc.d
+    t, d, tensor = _elem(desc), desc.d, _tensor
     rows, f_kept, h_kept, gates = _norm_shapes(desc, x, f_rows, h_rows)
-    B._check(lib().sparse_norm_run(
-        ctypes.byref(desc), rows, _tensor(x, "x", rows * d, t), _tensor(f, "f", f_kept * d, t), _handle(f_rows),
-        _tensor(gate, "gate", gates * d, t), _tensor(w_post, "w_post", d, f32), _tensor(b_post, "b_post", d, f32),
-        _tensor(w_pre, "w_pre", d, f32), _tensor(b_pre, "b_pre", d, f32), _tensor(x_new, "x_new", rows * d, t),
-        _tensor(h, "h", h_kept * d, t), _handle(h_rows), _tensor(stats, "stats", rows * 4, f32), _stream_handle(stream)),
-        "sparse_norm_run")
+    all_of_x = rows * d
+    status = lib().sparse_norm_run(
+        ctypes.byref(desc), rows, tensor(x, "x", all_of_x, t), None if f is None else tensor(f, "f", f_kept * d, t),
+        None if f_rows is None else f_rows.handle, None if gate is None else tensor(gate, "gate", gates * d, t),
+        None if w_post is None else tensor(w_post, "w_post", d, _F32), None if b_post is None else tensor(b_post, "b_post", d, _F32),
+        None if w_pre is None else tensor(w_pre, "w_pre", d, _F32), None if b_pre is None else tensor(b_pre, "b_pre", d, _F32),
+        None if x_new is None else tensor(x_new, "x_new", all_of_x, t), None if h is None else tensor(h, "h", h_kept * d, t),
+        None if h_rows is None else h_rows.handle, None if stats is None else tensor(stats, "stats", rows * 4, _F32),
+        _stream_handle(stream))
+    if status:
+        raise ScError(status, "sparse_norm_run")
     return x_new, h
 
 
@@ -306,6 +316,7 @@ class Q4Plan:
         self.handle = handle
         self.desc = desc
         self.workspace = workspace
+        self.type, self.k, self.n = _elem(desc), desc.k, desc.n
 
     def close(self):
         if self.handle:
@@ -359,8 +370,14 @@ def sparse_q4_plan_gated(desc: sc_q4_desc, gate: Dict[str, torch.Tensor], up: Di
 
 
 def sparse_q4_run(plan: Q4Plan, x, y, stream=None):
-    t, d = _elem(plan.desc), plan.desc
-    rows = _rows_of(x, d.k, "x")
-    B._check(lib().sparse_q4_run(plan.handle, rows, _tensor(x, "x", rows * d.k, t), _tensor(y, "y", rows * d.n, t),
-                                 _stream_handle(stream)), "sparse_q4_run")
+    t, k = plan.type, plan.k
+    rows = x.numel() // k
+    # (one condition for the call of a single token; what is wrong with it is said by the checks below)
+    if not (x.dtype is t and y.dtype is t and x.dim() and x.shape[-1] == k and y.numel() == rows * plan.n and x.is_cuda and y.is_cuda
+            and x.is_contiguous() and y.is_contiguous()):
+        rows = _rows_of(x, k, "x")
+        _tensor(x, "x", rows * k, t), _tensor(y, "y", rows * plan.n, t)
+    status = lib().sparse_q4_run(plan.handle, rows, x.data_ptr(), y.data_ptr(), _stream_handle(stream))
+    if status:
+        raise ScError(status, "sparse_q4_run")
     return y
