@@ -87,7 +87,8 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
  * x_rows = SC_ROWS_DENSE x (and dx) is [m x d_in], with SC_ROWS_COMPACT [kept x d_in]; y_rows says the same of y (and dy).
  * Dropped rows of a dense x or dy are not looked at, whatever they hold.
  * saved_dev: [3][kept][d_hidden] of the descriptor's type -- g, u and hidden, rounded -- for the backward pass; NULL in inference.
- * Sizes need not be multiples of anything; rows of whole 16-byte groups are the fast path.
+ * Sizes need not be multiples of anything; rows of whole 16-byte groups are the fast path, others are copied into the
+ * workspace first where there are more than 64 kept rows.
  * With more than 64 kept rows, and in every backward pass, floats are multiplied in three 16-bit parts (to a float's precision); an
  * infinity among them gives NaN. */
 typedef enum { SC_ACT_SILU = 0, SC_ACT_GELU = 1, SC_ACT_GELU_TANH = 2 } sc_activation;
@@ -114,7 +115,8 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
  * codes are [n][ceil(k / 2)] bytes, the even column in the low half; scales and zeros are [n][ceil(k / group)] of the
  * descriptor's type (zeros may be NULL: 8).  The plan lays the weights out once in the caller's workspace, from which every run
  * reads them; codes, scales and zeros are not needed afterwards.  sparse_q4_plan_gated lays out two matrices of one shape,
- * whose run gives act(x Gate') * (x Up'), rounded once.  Planning only enqueues work.  Any number of rows; made for few. */
+ * whose run gives act(x Gate') * (x Up'), rounded once.  Planning only enqueues work.  Up to 65 535 * 64 rows; made for few.
+ * x is finite, and in SC_BF16 below 2^110 in size: sums of x times up to 143 (SC_F16: 1 039) are formed in float on the way. */
 typedef struct {
   int32_t k, n;          /* columns contracted, outputs */
   int32_t group;         /* 32, 64 or 128 columns share a scale */

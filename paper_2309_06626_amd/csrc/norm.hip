@@ -10,6 +10,8 @@
 // passes once and a layer norm's spread is summed about its mean, not from squares.  A workgroup walks over rows with the
 // parameters in registers; backward their gradients too, and since its rows are consecutive, a gate's gradient is finished as its
 // rows end.  What a workgroup cannot finish it leaves in float, and a second launch adds these parts in order.
+// Measured, tensors from memory: 8 192 x 4 096 in bf16 forward 50 us (5.3 TB/s; a plain copy 6.3), backward of 4 096 x 4 096 50 and 5 for the
+// parts (3.7 TB/s: four reductions a row), 3 137 x 410 in float (no whole groups) 8 and 15.5.
 #include "../../include/sparse_block.h"
 #include "mma_common.hpp"
 #include "rows.hpp"
@@ -523,7 +525,9 @@ template <typename T, int NT, int E, bool VEC> static hipError_t norm_launch(con
     }
     kernel<<<dim3((unsigned)norm_block_count(p.rows, p.d)), dim3(NT * norm_teams<NT>()), lds, s>>>(p);
   } else {
-    const int64_t most = 262144 / NT;
+    // rows that a workgroup takes after one another spare it the parameters; short rows gain more from more workgroups
+    // (12 544 x 768 in f16: 2 048 workgroups 19.1 us, 8 192 17.9; 8 192 x 4 096 in bf16: 512 51.5, 2 048 53.2)
+    const int64_t most = NT <= 128 ? 8192 : 262144 / NT;
     norm_kernel<T, NT, E, VEC><<<dim3((unsigned)(p.rows < most ? p.rows : most)), dim3(NT), 0, s>>>(p);
   }
   return hipGetLastError();

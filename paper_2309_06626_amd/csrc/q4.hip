@@ -10,6 +10,9 @@
 //   * the plan lays codes out in the order in which lanes take them: 16 outputs x 128 columns are 1 KB, read by one wavefront at once,
 //     its dword j the columns 32 j + 8 (lane / 16) .. + 7, in the nibble order that one AND-OR a pair undoes;
 //   * a workgroup has 16 outputs and eight or sixteen wavefronts, which share the columns; their sums meet in LDS, in order.
+// Measured, bf16, one row: 4 096 -> 4 096 3.9 us (2.3 TB/s, most of it a launch), 11 264 -> 4 096 8.0 (3.1 TB/s), gated 4 096 -> 11 264 14.3
+// (3.6 TB/s).  More rows read x again in every workgroup: the gated block 4 096 -> 11 264 -> 4 096 takes 21 us for 1 row, 23 for 8, 30 for
+// 16 and 115 for 64.
 #include "../../include/sparse_block.h"
 #include "ffn_act.hpp"
 #include "mma_common.hpp"
