@@ -88,9 +88,9 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
  * Dropped rows of a dense x or dy are not looked at, whatever they hold.
  * saved_dev: [3][kept][d_hidden] of the descriptor's type -- g, u and hidden, rounded -- for the backward pass; NULL in inference.
  * Sizes need not be multiples of anything; rows of whole 16-byte groups are the fast path, others are copied into the
- * workspace first where there are more than 64 kept rows.
- * With more than 64 kept rows, and in every backward pass, floats are multiplied in three 16-bit parts (to a float's precision); an
- * infinity among them gives NaN. */
+ * workspace first, in a run with more than 64 kept rows and in every backward pass.
+ * Floats of more than a few rows, and of every backward pass, are multiplied in three 16-bit parts (to a float's precision); an infinity
+ * among them gives NaN. */
 typedef enum { SC_ACT_SILU = 0, SC_ACT_GELU = 1, SC_ACT_GELU_TANH = 2 } sc_activation;
 
 typedef struct {
