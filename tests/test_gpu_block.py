@@ -291,6 +291,14 @@ def test_ffn_forward_and_gradients(c):
         inside(v, w, b, name)
 
 
+@pytest.mark.parametrize("c", [(6000, 768, 384, 768, "bf16", "gelu", "all", 0, 0), (8192, 256, 520, 776, "f16", "silu", "half", 1, 0),
+                               (9000, 505, 771, 258, "bf16", "gelu_tanh", "half", 0, 1),
+                               (8200, 1040, 2072, 1032, "bf16", "gelu", "half", 0, 0), (8200, 1037, 2071, 1030, "f16", "silu", "half", 0, 0),
+                               (5200, 1288, 3080, 1544, "f16", "gelu", "half", 0, 1)], ids=lambda c: "-".join(map(str, c)))
+def test_ffn_in_larger_tiles(c):
+    test_ffn_forward_and_gradients(c)
+
+
 FEW = [(rows, di, dh, do, dtype, "silu", mask, 0, 0)
        for dtype, di, dh, do in (("bf16", 520, 1037, 264), ("f16", 1048, 264, 5), ("f32", 333, 68, 130), ("f16", 77, 1030, 1031))
        for rows, mask in ((3, "all"), (4, "all"), (8, "half"), (8, "all"), (9, "all"), (15, "half"))]
