@@ -292,8 +292,8 @@ static hipError_t multiply(int dtype, FfnProduct what, FfnGemm& g, bool whole, f
   return multiply(dtype, what, g, pick_tiling(what, g.m, what == kFfnUp ? 2 * (int64_t)g.n : g.n, g.k, g.segments, g.batch, dtype), whole, parts, s);
 }
 // kFfnUp and kFfnDown.  A few rows: the kernel for them reads all of P in every workgroup, at 4.2 TB/s in all, where the tiles' workgroups
-// have eight (gated: four) times the outputs.  bf16, gated 2 048 -> 5 632 and back: 8 rows 18 us, in tiles 22; 16 rows 26 and 23; 64 rows 58
-// and 28.  512 -> 1 408 and back: 64 rows 15 and 17.  Rows that are not whole groups would have to be copied for tiles, weights too.
+// have eight (gated: four) times the outputs.  bf16, gated 2 048 -> 5 632 and back: 8 rows 18 us, in tiles 22; 16 rows 26 and 24; 64 rows 58
+// and 30.  512 -> 1 408 and back: 64 rows 15 and 17.  Rows that are not whole groups would have to be copied for tiles, weights too.
 static hipError_t multiply_forward(int dtype, FfnProduct what, FfnGemm& g, bool whole, float* parts, hipStream_t s) {
   const int64_t cols = what == kFfnUp ? 2 * (int64_t)g.n : g.n;
   const Tiling t = pick_tiling(what, g.m, cols, g.k, g.segments, g.batch, dtype);
