@@ -635,7 +635,8 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
   const sc_status st = sc::check_norm(desc, rows);
   if (st != SC_OK) return st;
   if ((f_rows && f_rows->rows != rows) || (h_rows && h_rows->rows != rows)) return SC_ERR_BAD_SHAPE;
-  if ((rows > 0 && (!x_dev || !stats_dev || (!dx_new_dev && !dh_dev))) || !workspace_dev) return SC_ERR_NULL;
+  // (a matrix of no rows may have no address)
+  if ((rows > 0 && (!x_dev || !stats_dev || (!dx_new_dev && !dh_dev && !(h_rows && h_rows->kept == 0)))) || !workspace_dev) return SC_ERR_NULL;
   if (rows > 0 && !f_dev && (!f_rows || f_rows->kept > 0) && (df_dev || dgate_dev || dw_post_dev || db_post_dev)) return SC_ERR_NULL;
   if (dgate_dev && !gate_dev) return SC_ERR_NULL;
   if (rows > 0 && !dh_dev && (!h_rows || h_rows->kept > 0) && (dw_pre_dev || db_pre_dev)) return SC_ERR_NULL;

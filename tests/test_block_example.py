@@ -103,3 +103,15 @@ def test_training_reduces_the_loss(dtype):
         losses.append(error.square().sum(1).mean().item())
         stack.step(*stack.backward((error * (2 / rows.kept)).to(stack.type))[1:], rate=0.05)
     assert all(b < a for a, b in zip(losses, losses[1:]))
+
+
+@pytest.mark.gpu
+def test_a_mask_that_keeps_nothing_trains_nothing():
+    stack = X.FeedForwardStack(64, 128, 2, "bf16", seed=1)
+    x = torch.randn(50, 64, generator=torch.Generator().manual_seed(2)).to("cuda", stack.type)
+    rows = K.sparse_rows_plan(torch.zeros(50, dtype=torch.uint8, device="cuda"))
+    h = stack.forward(x, rows)
+    assert h.shape == (0, 64) and torch.equal(stack.x[-1], x)
+    dx, grads, first = stack.backward(torch.empty_like(h))
+    for t in (dx, first, *(t for g in grads for t in g.values())):
+        assert (t == 0).all()

@@ -211,6 +211,23 @@ def test_rows_that_the_mask_drops_are_not_looked_at():
     assert torch.equal(out["x_new"][hm.bool().to(DEV)], clean["x_new"][hm.bool().to(DEV)])
 
 
+def test_norm_gradients_where_no_row_is_kept_and_none_comes_from_elsewhere():
+    """dh is empty, and an empty tensor has no address: gradients are zero, the call is not refused."""
+    c = (40, 96, "bf16", "rms", "rms", 7, "nothing", "nothing", 1.0, 1.0)
+    g, t, fm, hm = norm_inputs(*c[:8], 4)
+    desc, dt, fr, hr, out = norm_call(c, t, fm, hm)
+    empty = torch.empty(0, 96, dtype=torch.bfloat16, device=DEV)
+    dx, dgate = nan_like(40, 96, dtype="bf16"), nan_like(6, 96, dtype="bf16")
+    dw = [nan_like(96) for _ in range(2)]
+    ws = torch.empty(K.sparse_norm_workspace_bytes(desc, 40), dtype=torch.uint8, device=DEV)
+    for gradient in (empty, None):
+        K.sparse_norm_backward(desc, dt["x"], dt["f"], dt["gate"], dt["w_post"], None, dt["w_pre"], out["stats"], None, gradient, dx, empty,
+                               dgate, dw[0], None, dw[1], None, ws, f_rows=fr, h_rows=hr)
+        for v in (dx, dgate, *dw):
+            assert (v == 0).all()
+            v.fill_(float("nan"))
+
+
 # ---- feed-forward block ------------------------------------------------------------------------------------------------
 
 FFNS = [  # rows, d_in, d_hidden, d_out, dtype, activation, mask, x_rows, y_rows
