@@ -451,9 +451,21 @@ __global__ __launch_bounds__(NT * norm_teams<NT>()) void norm_backward_kernel(co
 
 // The parts added up, in order, 32 columns a workgroup and eight lanes of parts a column: the parameters wanted, then the gates (whose rows
 // lie in more than one team's stretch of p.rows_per_block; in all of these but the first the gate is the one that the stretch begins with).
+// Gates of fewer rows than a stretch cross one border between stretches or none: a workgroup has 256 columns of a border then, since there may
+// be a gate for every row or two and there are no more borders than teams (4 096 x 4 096 in bf16, two rows a gate, forward and backward: 85 us;
+// 234 with workgroups for every gate, which beyond 2^32 lanes were no launch any more).
 template <typename T> __global__ __launch_bounds__(256) void norm_finish_kernel(const NormParams p, int blocks, int params) {
   __shared__ float s[8][32];
   const int col_blocks = (p.d + 31) / 32;
+  if (p.rows_per_gate < p.rows_per_block && (int)blockIdx.x >= params * col_blocks) {
+    const int wide = (p.d + 255) / 256, at = blockIdx.x - params * col_blocks, border = at / wide;
+    const int c = (at - border * wide) * 256 + threadIdx.x;
+    const int64_t row = (border + 1) * p.rows_per_block, group = row / p.rows_per_gate;
+    if (group * p.rows_per_gate == row || c >= p.d) return;      // (a gate begins there)
+    const float* part = p.gate_parts + c;
+    static_cast<T*>(p.dgate)[group * p.d + c] = (T)(part[((int64_t)border * 2 + 1) * p.d] + part[((int64_t)border + 1) * 2 * p.d]);
+    return;
+  }
   const int what = blockIdx.x / col_blocks, c = (blockIdx.x - what * col_blocks) * 32 + (threadIdx.x & 31), share = threadIdx.x >> 5;
   float v = 0.0f;
   float* out = nullptr;
@@ -674,8 +686,12 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
   p.gate_parts = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + sc::norm_up((size_t)blocks * 4 * desc->d * 4));
   hipError_t e = hipSuccess;
   if (rows > 0) e = sc::norm_dispatch(desc->dtype, p, true, s);
-  const bool gates = rows > 0 && dgate_dev && sc::norm_team_count(rows, desc->d) > 1 && p.rows_per_gate > 1;
-  const int64_t units = (params + (gates ? (rows + p.rows_per_gate - 1) / p.rows_per_gate : 0)) * ((desc->d + 31) / 32);
+  const int64_t teams = sc::norm_team_count(rows, desc->d), col_blocks = (desc->d + 31) / 32;
+  int64_t units = params * col_blocks;
+  if (rows > 0 && dgate_dev && teams > 1) {      // gates that no team finished: no more than there are borders between teams
+    if (p.rows_per_gate >= p.rows_per_block) units += (rows + p.rows_per_gate - 1) / p.rows_per_gate * col_blocks;
+    else if (p.rows_per_block % p.rows_per_gate) units += (teams - 1) * ((desc->d + 255) / 256);
+  }
   if (e == hipSuccess && units > 0) {
     const dim3 grid((unsigned)units);
     if (desc->dtype == SC_BF16) sc::norm_finish_kernel<__bf16><<<grid, dim3(256), 0, s>>>(p, (int)blocks, params);

@@ -211,6 +211,29 @@ def test_rows_that_the_mask_drops_are_not_looked_at():
     assert torch.equal(out["x_new"][hm.bool().to(DEV)], clean["x_new"][hm.bool().to(DEV)])
 
 
+@pytest.mark.parametrize("rows,d,per", [(6151, 64, 2), (6151, 64, 3), (6151, 64, 5), (20001, 40, 3), (20001, 40, 9), (20001, 40, 10),
+                                        (4100, 1000, 2), (4100, 1000, 3), (1300, 4104, 2), (1300, 4104, 5), (777, 2100, 2)])
+def test_norm_gradients_of_thousands_of_gates(rows, d, per):
+    # rows of a team: 4, 10, 5, 6 and 4; gates of fewer rows, that the teams' stretches hold whole or not, of as many, and of more
+    test_norm_forward_and_gradients((rows, d, "bf16", "layer", "rms", per, "half", "half", 0.5, 2.0))
+
+
+def test_norm_gradients_of_millions_of_gates():
+    """A gate for every two of 33 million rows, some across the borders of the teams' 16 385 rows: whole numbers, so sums are exact."""
+    rows, d = (1 << 25) + 7, 8
+    desc = K.make_norm_desc(d, B.SC_BF16, K.SC_NORM_NONE, K.SC_NORM_NONE, rows_per_gate=2)
+    whole = lambda n: torch.randint(-3, 4, (n, d), device=DEV, generator=torch.Generator(DEV).manual_seed(n)).to(torch.bfloat16)  # noqa: E731
+    x, f, dx_new, gate = whole(rows), whole(rows), whole(rows), whole((rows + 1) // 2)
+    stats = torch.empty(rows, 4, dtype=torch.float32, device=DEV)
+    K.sparse_norm_run(desc, x, f, gate, None, None, None, None, x, None, stats=stats)
+    dgate, df = torch.full_like(gate, float("nan")), torch.full_like(f, float("nan"))
+    ws = torch.empty(K.sparse_norm_workspace_bytes(desc, rows), dtype=torch.uint8, device=DEV)
+    K.sparse_norm_backward(desc, x, f, gate, None, None, None, stats, dx_new, None, None, df, dgate, None, None, None, None, ws)
+    terms = dx_new * f
+    assert torch.equal(dgate[:-1], terms[:-1].view(-1, 2, d).sum(1)) and torch.equal(dgate[-1], terms[-1])
+    assert torch.equal(df, dx_new * gate.repeat_interleave(2, 0)[:rows])
+
+
 def test_norm_gradients_where_no_row_is_kept_and_none_comes_from_elsewhere():
     """dh is empty, and an empty tensor has no address: gradients are zero, the call is not refused."""
     c = (40, 96, "bf16", "rms", "rms", 7, "nothing", "nothing", 1.0, 1.0)
