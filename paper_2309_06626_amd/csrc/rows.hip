@@ -80,21 +80,23 @@ __global__ __launch_bounds__(kRowsThreads) void rows_list_kernel(const uint8_t* 
 // zeros in the dropped rows of a dense output; one wavefront a row
 __global__ __launch_bounds__(256) void rows_zero_kernel(const int32_t* __restrict__ slot, int64_t rows, int64_t row_bytes,
                                                         unsigned char* __restrict__ out) {
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= rows || slot[r] >= 0) return;
-  unsigned char* row = out + r * row_bytes;
-  typedef int v4 __attribute__((ext_vector_type(4)));
-  if (row_bytes % 16 == 0) {
-    for (int64_t i = (threadIdx.x & 63) * 16; i < row_bytes; i += 1024) *reinterpret_cast<v4*>(row + i) = v4{0, 0, 0, 0};
-  } else {
-    for (int64_t i = (threadIdx.x & 63) * 2; i < row_bytes; i += 128) *reinterpret_cast<uint16_t*>(row + i) = 0;
+  for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4) {
+    if (slot[r] >= 0) continue;
+    unsigned char* row = out + r * row_bytes;
+    typedef int v4 __attribute__((ext_vector_type(4)));
+    if (row_bytes % 16 == 0) {
+      for (int64_t i = (threadIdx.x & 63) * 16; i < row_bytes; i += 1024) *reinterpret_cast<v4*>(row + i) = v4{0, 0, 0, 0};
+    } else {
+      for (int64_t i = (threadIdx.x & 63) * 2; i < row_bytes; i += 128) *reinterpret_cast<uint16_t*>(row + i) = 0;
+    }
   }
 }
 
 hipError_t rows_zero_dropped(const sc_rows* set, int64_t row_bytes, void* out, hipStream_t s) {
   if (!set || set->kept == set->rows || row_bytes == 0) return hipSuccess;
-  rows_zero_kernel<<<dim3((unsigned)((set->rows + 3) / 4)), dim3(256), 0, s>>>(set->slot, set->rows, row_bytes,
-                                                                             static_cast<unsigned char*>(out));
+  const int64_t want = (set->rows + 3) / 4, most = 1 << 22;      // a launch has fewer than 2^32 lanes
+  rows_zero_kernel<<<dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s>>>(set->slot, set->rows, row_bytes,
+                                                                                  static_cast<unsigned char*>(out));
   return hipGetLastError();
 }
 

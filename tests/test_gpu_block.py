@@ -429,6 +429,22 @@ def test_ffn_on_another_stream_and_in_a_graph():
         assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("rows,d_out", [((1 << 26) + 9, 8), ((1 << 26) + 9, 3)])
+def test_zeros_in_millions_of_dropped_rows(rows, d_out):
+    mask = torch.zeros(rows, dtype=torch.uint8, device=DEV)
+    at = torch.tensor([0, 12345, (1 << 24) + 3, rows - 2], device=DEV)
+    mask[at] = 1
+    rs = K.sparse_rows_plan(mask)
+    w = [torch.ones(*s, dtype=torch.bfloat16, device=DEV) for s in ((8, 8), (8, 8), (d_out, 8))]
+    desc = K.make_ffn_desc(8, 8, d_out)
+    ws = torch.empty(K.sparse_ffn_workspace_bytes(desc, 4), dtype=torch.uint8, device=DEV)
+    y = nan_like(rows, d_out, dtype="bf16")
+    K.sparse_ffn_run(desc, torch.ones(4, 8, dtype=torch.bfloat16, device=DEV), *w, y, ws, rows=rs, x_rows=B.SC_ROWS_COMPACT)
+    assert (y[at] > 400).all()                                  # 8 silu(8) 8 = 511.8
+    y[at] = 0
+    assert int(torch.count_nonzero(y.view(torch.int16))) == 0   # (NaN and -0.0 count)
+
+
 # ---- 4-bit weights -----------------------------------------------------------------------------------------------------
 
 Q4S = [  # rows, n, k, group, dtype, zeros
