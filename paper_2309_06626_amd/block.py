@@ -146,7 +146,12 @@ def _row_counts(handle: int) -> Tuple[int, int]:
 
 
 def _handle(rows: Optional[RowSet]) -> Optional[int]:
-    return None if rows is None else rows.handle
+    """None stands for all rows, so a closed set must not turn into it: its tensors may hold fewer."""
+    if rows is None:
+        return None
+    if not rows.handle:
+        raise ValueError("the row set is closed")
+    return rows.handle
 
 
 def sparse_rows_workspace_bytes(rows: int) -> int:
@@ -171,7 +176,7 @@ def sparse_rows_plan(mask: torch.Tensor, workspace: Optional[torch.Tensor] = Non
 
 def sparse_rows_set_mask(rows: RowSet, mask: torch.Tensor, stream=None) -> RowSet:
     """A new mask of as many rows (synchronises the stream); the number of kept rows may change."""
-    B._check(lib().sparse_rows_set_mask(rows.handle, _tensor(mask, "mask", rows.rows, torch.uint8), _stream_handle(stream)),
+    B._check(lib().sparse_rows_set_mask(_handle(rows), _tensor(mask, "mask", rows.rows, torch.uint8), _stream_handle(stream)),
              "sparse_rows_set_mask")
     rows.kept = _row_counts(rows.handle)[1]
     return rows
@@ -180,7 +185,7 @@ def sparse_rows_set_mask(rows: RowSet, mask: torch.Tensor, stream=None) -> RowSe
 def sparse_rows_info(rows: RowSet) -> Tuple[int, int, torch.Tensor, torch.Tensor]:
     """(rows, kept, ascending list of the kept rows, slot of every row or -1); the lists are copies."""
     m, kept, idx, slot = ctypes.c_int64(), ctypes.c_int64(), ctypes.c_void_p(), ctypes.c_void_p()
-    B._check(lib().sparse_rows_info(rows.handle, ctypes.byref(m), ctypes.byref(kept), ctypes.byref(idx), ctypes.byref(slot)),
+    B._check(lib().sparse_rows_info(_handle(rows), ctypes.byref(m), ctypes.byref(kept), ctypes.byref(idx), ctypes.byref(slot)),
              "sparse_rows_info")
     base = rows.workspace.data_ptr()
     flat = rows.workspace.view(torch.uint8).reshape(-1)
@@ -228,11 +233,11 @@ def sparse_norm_run(desc: sc_norm_desc, x, f, gate, w_post, b_post, w_pre, b_pre
     all_of_x = rows * d
     status = lib().sparse_norm_run(
         ctypes.byref(desc), rows, tensor(x, "x", all_of_x, t), None if f is None else tensor(f, "f", f_kept * d, t),
-        None if f_rows is None else f_rows.handle, None if gate is None else tensor(gate, "gate", gates * d, t),
+        None if f_rows is None else _handle(f_rows), None if gate is None else tensor(gate, "gate", gates * d, t),
         None if w_post is None else tensor(w_post, "w_post", d, _F32), None if b_post is None else tensor(b_post, "b_post", d, _F32),
         None if w_pre is None else tensor(w_pre, "w_pre", d, _F32), None if b_pre is None else tensor(b_pre, "b_pre", d, _F32),
         None if x_new is None else tensor(x_new, "x_new", all_of_x, t), None if h is None else tensor(h, "h", h_kept * d, t),
-        None if h_rows is None else h_rows.handle, None if stats is None else tensor(stats, "stats", rows * 4, _F32),
+        None if h_rows is None else _handle(h_rows), None if stats is None else tensor(stats, "stats", rows * 4, _F32),
         _stream_handle(stream))
     if status:
         raise ScError(status, "sparse_norm_run")

@@ -5,6 +5,7 @@ import os
 import re
 
 import pytest
+import torch
 
 from paper_2309_06626_amd import binding as B
 from paper_2309_06626_amd import block as K
@@ -176,3 +177,39 @@ def test_q4_calls_refuse():
     assert gated(0, FAKE, 2 * one - 1) == B.SC_ERR_WORKSPACE
     assert L.sparse_q4_run(None, 1, FAKE, FAKE, None) == B.SC_ERR_NULL
     L.sparse_q4_destroy(None)
+
+
+class Recorder:
+    """Stands in for the library: takes every call, notes its name, launches nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append(name) or 0
+
+
+def test_a_closed_row_set_is_not_all_rows(monkeypatch):
+    """The library takes NULL for all rows: with the kept rows alone in a tensor it would run over the end."""
+    t = torch.zeros(3, 64, dtype=torch.bfloat16)
+    x, w, stats = torch.zeros(8, 64, dtype=torch.bfloat16), torch.zeros(64, 64, dtype=torch.bfloat16), torch.zeros(8, 4)
+    closed = K.RowSet.__new__(K.RowSet)
+    closed.handle, closed.rows, closed.kept, closed.workspace = None, 8, 3, torch.zeros(512, dtype=torch.uint8)
+    fake = Recorder()
+    monkeypatch.setattr(K, "lib", lambda: fake)
+    monkeypatch.setattr(K, "_tensor", lambda t, *_: None if t is None else t.data_ptr())
+    monkeypatch.setattr(K, "_workspace", lambda t: (t.data_ptr(), t.numel()))
+    monkeypatch.setattr(K, "_stream_handle", lambda stream: 0)
+    norm, ffn, compact = K.make_norm_desc(64), K.make_ffn_desc(64, 64, 64), B.SC_ROWS_COMPACT
+    none = [None] * 5
+    for call in (lambda: K.sparse_ffn_run(ffn, t, w, w, w, t, x, closed, compact, compact),
+                 lambda: K.sparse_ffn_backward(ffn, t, w, w, w, t, t, t, w, w, w, x, closed, compact, compact),
+                 lambda: K.sparse_norm_run(norm, x, t, *none, x, x, f_rows=closed),
+                 lambda: K.sparse_norm_run(norm, x, None, *none, x, t, h_rows=closed),
+                 lambda: K.sparse_norm_backward(norm, x, t, None, None, None, None, stats, x, x, x, t, *none, x, f_rows=closed),
+                 lambda: K.sparse_norm_backward(norm, x, None, None, None, None, None, stats, x, t, x, None, *none, x, h_rows=closed),
+                 lambda: K.sparse_rows_set_mask(closed, torch.zeros(8, dtype=torch.uint8)),
+                 lambda: K.sparse_rows_info(closed)):
+        with pytest.raises(ValueError, match="closed"):
+            call()
+    assert not fake.calls
