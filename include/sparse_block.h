@@ -30,7 +30,8 @@ extern "C" {
 
 /* ---- kept rows of a mask ---------------------------------------------------------------------------------------------------
  * sparse_rows_plan builds the list in the caller's workspace and synchronises the stream once (the count is needed on the host).
- * sparse_rows_set_mask does the same again for a new mask of as many rows.  rows <= 2^31 - 1; 0 is allowed. */
+ * sparse_rows_set_mask does the same again for a new mask of as many rows; if it fails, the set keeps no row from then on.
+ * rows <= 2^31 - 1; 0 is allowed. */
 typedef struct sc_rows sc_rows;
 
 sc_status sparse_rows_workspace_bytes(int64_t rows, size_t* bytes);

@@ -176,9 +176,12 @@ def sparse_rows_plan(mask: torch.Tensor, workspace: Optional[torch.Tensor] = Non
 
 def sparse_rows_set_mask(rows: RowSet, mask: torch.Tensor, stream=None) -> RowSet:
     """A new mask of as many rows (synchronises the stream); the number of kept rows may change."""
-    B._check(lib().sparse_rows_set_mask(_handle(rows), _tensor(mask, "mask", rows.rows, torch.uint8), _stream_handle(stream)),
-             "sparse_rows_set_mask")
-    rows.kept = _row_counts(rows.handle)[1]
+    try:
+        B._check(lib().sparse_rows_set_mask(_handle(rows), _tensor(mask, "mask", rows.rows, torch.uint8), _stream_handle(stream)),
+                 "sparse_rows_set_mask")
+    finally:
+        if rows.handle:
+            rows.kept = _row_counts(rows.handle)[1]      # (after a failure the set keeps none)
     return rows
 
 

@@ -591,6 +591,8 @@ static NormParams norm_params(const sc_norm_desc* d, int64_t rows) {
   return p;
 }
 
+// a matrix of kept rows: nothing where none is kept
+template <typename P> static P* norm_kept(P* matrix, const sc_rows* set) { return set && set->kept == 0 ? nullptr : matrix; }
 // null where every row is kept
 static const int32_t* norm_slots(const sc_rows* set) { return set && set->kept != set->rows ? set->slot : nullptr; }
 
@@ -611,14 +613,14 @@ sc_status sparse_norm_run(const sc_norm_desc* desc, int64_t rows, const void* x_
   if (rows == 0) return SC_OK;
   sc::NormParams p = sc::norm_params(desc, rows);
   p.x = x_dev;
-  p.f = f_dev;
+  p.f = sc::norm_kept(f_dev, f_rows);
   p.gate = gate_dev;
   p.w_post = w_post_dev;
   p.b_post = b_post_dev;
   p.w_pre = w_pre_dev;
   p.b_pre = b_pre_dev;
   p.x_new = x_new_dev;
-  p.h = h_dev;
+  p.h = sc::norm_kept(h_dev, h_rows);
   p.stats = stats_dev;
   p.f_slot = sc::norm_slots(f_rows);
   p.h_slot = sc::norm_slots(h_rows);
@@ -661,7 +663,7 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   sc::NormParams p = sc::norm_params(desc, rows);
   p.x = x_dev;
-  p.f = f_dev;
+  p.f = sc::norm_kept(f_dev, f_rows);
   p.gate = gate_dev;
   p.w_post = w_post_dev;
   p.b_post = b_post_dev;
@@ -670,7 +672,7 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
   p.f_slot = sc::norm_slots(f_rows);
   p.h_slot = sc::norm_slots(h_rows);
   p.dx_new = dx_new_dev;
-  p.dh = dh_dev;
+  p.dh = sc::norm_kept(dh_dev, h_rows);
   p.dx = dx_dev;
   p.df = df_dev;
   p.dgate = dgate_dev;

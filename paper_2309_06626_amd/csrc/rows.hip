@@ -77,11 +77,11 @@ __global__ __launch_bounds__(kRowsThreads) void rows_list_kernel(const uint8_t* 
   if (blockIdx.x == gridDim.x - 1 && t == 0) counts[0] = at;
 }
 
-// zeros in the dropped rows of a dense output; one wavefront a row
+// zeros in the dropped rows of a dense output (no slots: all are); one wavefront a row
 __global__ __launch_bounds__(256) void rows_zero_kernel(const int32_t* __restrict__ slot, int64_t rows, int64_t row_bytes,
                                                         unsigned char* __restrict__ out) {
   for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4) {
-    if (slot[r] >= 0) continue;
+    if (slot && slot[r] >= 0) continue;
     unsigned char* row = out + r * row_bytes;
     typedef int v4 __attribute__((ext_vector_type(4)));
     if (row_bytes % 16 == 0) {
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void rows_zero_kernel(const int32_t* __restric
 hipError_t rows_zero_dropped(const sc_rows* set, int64_t row_bytes, void* out, hipStream_t s) {
   if (!set || set->kept == set->rows || row_bytes == 0) return hipSuccess;
   const int64_t want = (set->rows + 3) / 4, most = 1 << 22;      // a launch has fewer than 2^32 lanes
-  rows_zero_kernel<<<dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s>>>(set->slot, set->rows, row_bytes,
+  rows_zero_kernel<<<dim3((unsigned)(want < most ? want : most)), dim3(256), 0, s>>>(set->kept ? set->slot : nullptr, set->rows, row_bytes,
                                                                                   static_cast<unsigned char*>(out));
   return hipGetLastError();
 }
@@ -104,7 +104,7 @@ static size_t rows_up(size_t n) { return (n + 255) & ~(size_t)255; }
 static int64_t rows_parts(int64_t rows) { return (rows + kRowsPart - 1) / kRowsPart; }
 
 static sc_status build(sc_rows* set, const uint8_t* mask, hipStream_t s) {
-  set->kept = 0;
+  set->kept = 0;      // and nothing is kept if this fails, whatever became of the lists
   if (set->rows == 0) return SC_OK;
   const unsigned parts = (unsigned)rows_parts(set->rows);
   rows_count_kernel<<<dim3(parts), dim3(kRowsThreads), 0, s>>>(mask, set->rows, set->counts);

@@ -4,7 +4,7 @@
 #include <stdint.h>
 
 struct sc_rows {
-  int64_t rows, kept;
+  int64_t rows, kept;    // with kept = 0 the lists are not looked at
   int32_t* row_idx;      // [kept] ascending
   int32_t* slot;         // [rows] position in row_idx, or -1
   int32_t* counts;       // [0] kept, [1 ..] kept rows of each part

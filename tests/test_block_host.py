@@ -213,3 +213,28 @@ def test_a_closed_row_set_is_not_all_rows(monkeypatch):
         with pytest.raises(ValueError, match="closed"):
             call()
     assert not fake.calls
+
+
+def test_a_mask_that_could_not_be_set_leaves_no_stale_count(monkeypatch):
+    class Failing:
+        """The library's set keeps nothing after a failure."""
+        def sparse_rows_set_mask(self, *args):
+            return B.SC_ERR_HIP
+
+        def sparse_rows_info(self, handle, rows, kept, *lists):
+            rows._obj.value, kept._obj.value = 8, 0
+            return B.SC_OK
+
+        def sparse_rows_destroy(self, handle):
+            pass
+
+    fake = Failing()
+    rows = K.RowSet.__new__(K.RowSet)
+    rows.handle, rows.rows, rows.kept = FAKE, 8, 3
+    monkeypatch.setattr(K, "lib", lambda: fake)
+    monkeypatch.setattr(K, "_tensor", lambda t, *_: t.data_ptr())
+    monkeypatch.setattr(K, "_stream_handle", lambda stream: 0)
+    with pytest.raises(K.ScError):
+        K.sparse_rows_set_mask(rows, torch.zeros(8, dtype=torch.uint8))
+    assert rows.kept == 0
+    rows.handle = None      # (FAKE is no address to free)
