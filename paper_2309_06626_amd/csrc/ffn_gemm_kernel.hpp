@@ -35,10 +35,11 @@ __device__ __forceinline__ int ffn_q_order(int r) { return ((r >> 2) & 1) * 16 +
 constexpr int kFfnList = 4096;      // rows of the contraction whose list entries lie in LDS
 static __device__ __align__(16) v4i ffn_zeros = {0, 0, 0, 0};      // what is read beyond an operand's end
 
-// 16 (or 4) bytes a lane from memory into LDS at base + 16 (4) lane.  Written out, because the compiler would let every later LDS read wait
-// for all transfers in flight; their arrival is waited for at the barriers below.
+// 16 bytes a lane from memory into LDS at base + 16 lane.  Written out, because the compiler would let every later LDS read wait
+// for all transfers in flight; their arrival is waited for at the barriers below.  The base goes through m0, which the compiler writes (it
+// has to know what m0 holds), a wait state before the transfer.
 __device__ __forceinline__ void ffn_dma16(const void* src, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base), "v"(src));
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds_base), "v"(src));
 }
 
 // Eight floats of a row in bf16 parts.  Cutting off keeps 8 bits a part, and what is left over is exact: hi + mid + lo is the float.
