@@ -8,16 +8,18 @@ namespace sc {
 
 __device__ __forceinline__ float ffn_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 
-// Phi(v) = erfc(-v / sqrt 2) / 2 and e = exp(-v^2 / 2).  For 16-bit results Hastings' rational form (Abramowitz and Stegun 7.1.26), which
-// shares the exponential with the derivative: within 3e-7 of Phi, where erfcf takes some eighty operations (gated 6 272 x 768 -> 2 048 in
-// f16: 53 us, with erfcf 67)
+// Phi(v) = erfc(-v / sqrt 2) / 2 and e = exp(-v^2 / 2).  For 16-bit results Phi(-a) = e t P(t), t = 1 / (1 + 0.3 a), a rational form that
+// shares the exponential with the derivative; P of degree 5, fitted here to erfcx(a / sqrt 2) / 2 for a of 0 .. 14 so that its relative error
+// is evened out: below 1.2e-6 up to a = 1.5, 6e-6 up to 3 and 2.5e-5 beyond, where a form within so much of Phi alone would lose the small
+// results (half a unit is 5e-4 of an f16, 4e-3 of a bf16).  erfcf takes some eighty operations (gated
+// 6 272 x 768 -> 2 048 in f16 with a rational form of five terms 53 us, with erfcf 67; a sixth term costs 0.7)
 template <typename T> __device__ __forceinline__ float ffn_phi(float v, float& e) {
   e = __expf(-0.5f * v * v);
   if constexpr (sizeof(T) == 4) {
     return 0.5f * erfcf(-0.70710678118654752f * v);
   } else {
-    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678118654752f * fabsf(v));
-    const float q = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3f * fabsf(v));
+    const float q = e * t * (0.12010857f + t * (0.113153685f + t * (0.147376575f + t * (-0.024197675f + t * (0.22335236f + t * -0.079793915f)))));
     return v < 0.0f ? q : 1.0f - q;
   }
 }

@@ -402,6 +402,39 @@ def test_ffn_far_out_activations():
         assert y[1].abs().max() <= 1e-30 and torch.isfinite(got[1]).all()
 
 
+def activations(v, dtype, kind, rows):
+    """act(v) and act'(v) of the values v as the block has them: gate products v, up products and the rest 1; `rows` rows alike."""
+    n = len(v)
+    first = torch.zeros(n, 8, dtype=torch.float64)
+    gate = first.clone()
+    gate[:, 0], first[:, 0] = v, 1
+    full = dict(x=first[:1].repeat(rows, 1), wg=gate, wu=first, wd=torch.eye(n, dtype=torch.float64), dy=torch.zeros(rows, n).double())
+    full["dy"][-1] = 1      # one row's gradients alone, so that the weights' are the row's
+    y, _, dwg, _, _ = ffn_call((rows, 8, n, n, dtype, kind, "all", 0, 0), torch.ones(rows, dtype=torch.uint8),
+                               torch.ones(rows, dtype=torch.bool), full)
+    assert torch.equal(y, y[:1].expand_as(y))
+    return y[-1].double().cpu(), dwg[:, 0].double().cpu()
+
+
+def all_values(dtype, low, high):
+    v = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(O.TORCH[dtype]).double()
+    v = v[(v >= low) & (v <= high) & (v.abs() >= 1e-3)].unique()
+    return v[:: -(-len(v) // 1536)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 130])
+def test_gelu_keeps_its_small_results(dtype, rows):
+    """Far below zero v Phi(v) is small and still a number of 16 bits: it is rounded, not lost.  The products with 1 are exact, so the error
+    is half a unit and that of Phi and the exponential in float: below 2^-13 of the terms of v Phi(v), and of Phi(v) + v phi(v)."""
+    v = all_values(dtype, -12.5 if dtype == "bf16" else -5.5, 6.0)
+    y, slope = activations(v, dtype, "gelu", rows)
+    small = 0.0 if dtype == "bf16" else 2.0 ** -25      # half of f16's smallest
+    phi, density = 0.5 * torch.special.erfc(-v / math.sqrt(2)), torch.exp(-0.5 * v * v) / math.sqrt(2 * math.pi)
+    inside(y, v * phi, (O.U[dtype] + 2.0 ** -13) * (v * phi).abs() + small, "gelu")
+    inside(slope, phi + v * density, O.U[dtype] * (phi + v * density).abs() + 2.0 ** -13 * (phi + (v * density).abs()) + small, "its slope")
+
+
 def test_ffn_on_another_stream_and_in_a_graph():
     c = (96, 128, 256, 128, "bf16", "silu", "half", 0, 0)
     m, keep, full = ffn_case(c, 2)
