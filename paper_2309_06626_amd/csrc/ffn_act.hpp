@@ -6,7 +6,25 @@
 
 namespace sc {
 
-__device__ __forceinline__ float ffn_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+// T: what the results are rounded to.  The hardware's exponential of 1.44 v is off by |v| units of a float, its reciprocal by one: nothing to a
+// 16-bit result, up to 80 units of a float one.
+template <typename T> __device__ __forceinline__ float ffn_exp(float v) {
+  if constexpr (sizeof(T) == 4) return expf(v);
+  else return __expf(v);
+}
+// sigma(v), and 1 - sigma(v) in `rest` (of a float it keeps its digits where sigma(v) is close to 1)
+template <typename T> __device__ __forceinline__ float ffn_sigmoid(float v, float& rest) {
+  const float t = ffn_exp<T>(-v);
+  if constexpr (sizeof(T) == 4) {
+    const float s = 1.0f / (1.0f + t);
+    rest = v > 0.0f ? t * s : 1.0f - s;
+    return s;
+  } else {
+    const float s = __builtin_amdgcn_rcpf(1.0f + t);
+    rest = 1.0f - s;
+    return s;
+  }
+}
 
 // Phi(v) = erfc(-v / sqrt 2) / 2 and e = exp(-v^2 / 2).  For 16-bit results Phi(-a) = e t P(t), t = 1 / (1 + 0.3 a), a rational form that
 // shares the exponential with the derivative; P of degree 5, fitted here to erfcx(a / sqrt 2) / 2 for a of 0 .. 14 so that its relative error
@@ -14,7 +32,7 @@ __device__ __forceinline__ float ffn_sigmoid(float v) { return __builtin_amdgcn_
 // results (half a unit is 5e-4 of an f16, 4e-3 of a bf16).  erfcf takes some eighty operations (gated
 // 6 272 x 768 -> 2 048 in f16 with a rational form of five terms 53 us, with erfcf 67; a sixth term costs 0.7)
 template <typename T> __device__ __forceinline__ float ffn_phi(float v, float& e) {
-  e = __expf(-0.5f * v * v);
+  e = ffn_exp<T>(-0.5f * v * v);
   if constexpr (sizeof(T) == 4) {
     return 0.5f * erfcf(-0.70710678118654752f * v);
   } else {
@@ -26,9 +44,10 @@ template <typename T> __device__ __forceinline__ float ffn_phi(float v, float& e
 // a = act(v), da = its derivative; KIND: sc_activation; T: what the results are rounded to
 template <int KIND, typename T> __device__ __forceinline__ void ffn_act_of(float v, float& a, float& da) {
   if constexpr (KIND == 0) {                             // v sigma(v)
-    const float s = ffn_sigmoid(v);
+    float rest;
+    const float s = ffn_sigmoid<T>(v, rest);
     a = v * s;
-    da = s * (1.0f + v * (1.0f - s));
+    da = s * (1.0f + v * rest);
   } else if constexpr (KIND == 1) {                      // v Phi(v), Phi the normal distribution
     float e;
     const float p = ffn_phi<T>(v, e);
@@ -36,9 +55,10 @@ template <int KIND, typename T> __device__ __forceinline__ void ffn_act_of(float
     da = p + v * 0.39894228040143268f * e;
   } else {                                               // v sigma(2 t), t = sqrt(2 / pi) (v + 0.044715 v^3)
     const float c = 0.79788456080286536f, v2 = v * v;
-    const float s = ffn_sigmoid(2.0f * c * v * (1.0f + 0.044715f * v2));
+    float rest;
+    const float s = ffn_sigmoid<T>(2.0f * c * v * (1.0f + 0.044715f * v2), rest);
     a = v * s;
-    da = s + v * s * (1.0f - s) * 2.0f * c * (1.0f + 3.0f * 0.044715f * v2);
+    da = s + v * s * rest * 2.0f * c * (1.0f + 3.0f * 0.044715f * v2);
   }
 }
 // fn(kind) with the kind as a constant: one branch for as many values as fn takes

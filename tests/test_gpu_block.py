@@ -435,6 +435,16 @@ def test_gelu_keeps_its_small_results(dtype, rows):
     inside(slope, phi + v * density, O.U[dtype] * (phi + v * density).abs() + 2.0 ** -13 * (phi + (v * density).abs()) + small, "its slope")
 
 
+def test_silu_of_floats_has_a_floats_digits():
+    """v / (1 + exp(-v)): the exponential within 3 units of 2^-24, the sum, quotient and product within one each, as the slope's further
+    terms: no more than 16.  A row's products with 1 are exact."""
+    v = torch.linspace(-85.0, 20.0, 1401, dtype=torch.float32).double()
+    y, slope = activations(v, "f32", "silu", 1)
+    s = torch.sigmoid(v)
+    inside(y, v * s, 16 * O.E * (v * s).abs(), "silu")
+    inside(slope, s * (1 + v * (1 - s)), 16 * O.E * s * (1 + (v * (1 - s)).abs()) + O.TINY["f32"], "its slope")
+
+
 def test_ffn_on_another_stream_and_in_a_graph():
     c = (96, 128, 256, 128, "bf16", "silu", "half", 0, 0)
     m, keep, full = ffn_case(c, 2)
