@@ -54,7 +54,7 @@ template <int KIND, typename T> __device__ __forceinline__ void ffn_act_of(float
     a = v * p;
     da = p + v * 0.39894228040143268f * e;
   } else {                                               // v sigma(2 t), t = sqrt(2 / pi) (v + 0.044715 v^3)
-    const float c = 0.79788456080286536f, v2 = v * v;
+    const float c = 0.79788456080286536f, v2 = fminf(v * v, 1e4f);      // (beyond 100 sigma is 0 or 1; v^2 may be infinite)
     float rest;
     const float s = ffn_sigmoid<T>(2.0f * c * v * (1.0f + 0.044715f * v2), rest);
     a = v * s;

@@ -445,6 +445,16 @@ def test_silu_of_floats_has_a_floats_digits():
     inside(slope, s * (1 + v * (1 - s)), 16 * O.E * s * (1 + (v * (1 - s)).abs()) + O.TINY["f32"], "its slope")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 130])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+def test_activations_of_the_largest_numbers(dtype, rows, kind):
+    """v and 0 with slopes 1 and 0, exactly: the squares and cubes on the way are infinite."""
+    v = torch.tensor([1e10, 2e19, 1e30, 2e38, -1e10, -2e19, -1e30, -2e38]).to(O.TORCH[dtype]).double()
+    y, slope = activations(v, dtype, kind, rows)
+    assert torch.equal(y, v.clamp_min(0)) and torch.equal(slope, (v > 0).double())
+
+
 def test_ffn_on_another_stream_and_in_a_graph():
     c = (96, 128, 256, 128, "bf16", "silu", "half", 0, 0)
     m, keep, full = ffn_case(c, 2)
