@@ -42,7 +42,8 @@ __device__ __forceinline__ void ffn_dma16(const void* src, unsigned lds_base) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds_base), "v"(src));
 }
 
-// Eight floats of a row in bf16 parts.  Cutting off keeps 8 bits a part, and what is left over is exact: hi + mid + lo is the float.
+// Eight floats of a row in bf16 parts.  Cutting off keeps 8 bits a part, and what is left over is exact: hi + mid + lo is the float (of
+// numbers from 2^-102 on: what lies below 2^-126 is lost; infinities become infinity - infinity).
 struct FfnParts { v4i part[3]; };
 __device__ __forceinline__ FfnParts ffn_parts(v4i first, v4i second) {
   unsigned bits[3][8];

@@ -455,6 +455,41 @@ def test_activations_of_the_largest_numbers(dtype, rows, kind):
     assert torch.equal(y, v.clamp_min(0)) and torch.equal(slope, (v > 0).double())
 
 
+def test_floats_in_parts_lose_what_lies_below_the_smallest_normal_number():
+    """u of 2^-90 to 2^-124 in 130 rows: two of the three parts of u, and of the hidden row, may fall below 2^-126."""
+    small = torch.logspace(-90, -124, 700, base=2.0, dtype=torch.float32).double()
+    first, gate = torch.zeros(700, 8, dtype=torch.float64), torch.zeros(700, 8, dtype=torch.float64)
+    first[:, 0], gate[:, 0] = small, 20
+    full = dict(x=torch.tensor([1.0] + [0.0] * 7).double().repeat(130, 1), wg=gate, wu=first, wd=torch.eye(700).double(), dy=torch.zeros(130, 700))
+    y = ffn_call((130, 8, 700, 700, "f32", "silu", "all", 0, 0), torch.ones(130, dtype=torch.uint8), torch.ones(130, dtype=torch.bool), full,
+                 backward=False)
+    act = 20 / (1 + math.exp(-20))
+    inside(y, (act * small).expand(130, -1), (16 * O.E * act * small + (act + 1) * 2 * 2.0 ** -126).expand(130, -1), "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows", [4, 40, 200])
+def test_ffn_of_infinities_and_of_rows_too_large(dtype, rows):
+    """A row with an infinity, or with hidden values beyond f16, has no finite result; every other row is as it would be without."""
+    c = (rows, 96, 136, 80, dtype, "silu", "all", 0, 0)
+    m, keep, full = ffn_case(c, 13)
+    want = ffn_call(c, m, keep, full)
+    for lost, value in ((0, float("inf")), (rows // 2, -float("inf")), (rows - 1, float("nan")), (1, 3e4 if dtype == "f16" else float("inf"))):
+        bad = {n: v.clone() for n, v in full.items()}
+        bad["x"][lost, ::3] = value
+        t = {n: dev(v, dtype) for n, v in bad.items()}
+        desc = K.make_ffn_desc(96, 136, 80, K.DTYPE_CODE[dtype])
+        ws = torch.empty(K.sparse_ffn_workspace_bytes(desc, rows, True), dtype=torch.uint8, device=DEV)
+        y, saved = torch.empty_like(want[0]), nan_like(3, rows, 136, dtype=dtype)
+        K.sparse_ffn_run(desc, t["x"], t["wg"], t["wu"], t["wd"], y, ws, saved=saved)
+        grads = [torch.empty_like(v) for v in want[1:]]
+        K.sparse_ffn_backward(desc, t["x"], t["wg"], t["wu"], t["wd"], saved, t["dy"], *grads, ws)
+        others = torch.arange(rows) != lost
+        for have, clean in ((y, want[0]), (grads[0], want[1])):
+            assert torch.equal(have[others.to(DEV)], clean[others.to(DEV)])
+        assert not torch.isfinite(y[lost]).any()
+
+
 def test_ffn_on_another_stream_and_in_a_graph():
     c = (96, 128, 256, 128, "bf16", "silu", "half", 0, 0)
     m, keep, full = ffn_case(c, 2)
@@ -552,6 +587,18 @@ def test_q4_gated_products(rows, n, k, group, dtype, kind):
     bound = O.U[dtype] * want.abs() + 1.2 * ea * p.abs() + O.act(a, kind).abs() * ep + 1.2 * ea * ep + O.TINY[dtype]
     bound = bound + 64 * O.E * (1 + a.abs()) * a.abs().clamp_max(8) * p.abs()
     inside(y, want, bound, "y")
+
+
+@pytest.mark.parametrize("rows", [3, 40])
+def test_q4_rows_that_are_not_finite_stay_alone(rows):
+    g = gen(rows)
+    x = normal(g, rows, 300, dtype="bf16")
+    plan = K.sparse_q4_plan(K.make_q4_desc(300, 70, 64), *[v.to(DEV) for v in q4_matrix(g, 70, 300, 64, "bf16", True)])
+    want = K.sparse_q4_run(plan, dev(x, "bf16"), nan_like(rows, 70, dtype="bf16"))
+    x[1, 5] = float("inf")
+    y = K.sparse_q4_run(plan, dev(x, "bf16"), nan_like(rows, 70, dtype="bf16"))
+    others = torch.arange(rows, device=DEV) != 1
+    assert torch.equal(y[others], want[others]) and not torch.isfinite(y[1]).any()
 
 
 # ---- refusals of the binding -------------------------------------------------------------------------------------------
