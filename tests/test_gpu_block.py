@@ -339,6 +339,36 @@ def test_ffn_in_larger_tiles(c):
     test_ffn_forward_and_gradients(c)
 
 
+# Weight gradients of dense rows go through the list of kept rows, 4 096 entries at a time: kept rows beyond a stretch, or three, in one
+# piece (gate's and up's of the first, fourth and last, down's of the first) and in parts longer than a stretch (down's of the second, third
+# and last, gate's and up's of the third)
+@pytest.mark.parametrize("rows,di,dh,do,dtype", [(9200, 1040, 2072, 2056, "bf16"), (26000, 264, 1544, 1032, "f16"),
+                                                 (16800, 1032, 1672, 1032, "bf16"), (9000, 1928, 1288, 264, "f32"),
+                                                 (26000, 1544, 1800, 1160, "f32")])
+def test_ffn_weight_gradients_through_long_row_lists(rows, di, dh, do, dtype):
+    """The same sums in the same order as with the kept rows alone in memory; these against products in 64 bits."""
+    g, t = torch.Generator(DEV).manual_seed(rows), O.TORCH[dtype]
+    draw = lambda *s, std=1.0: (torch.randn(*s, generator=g, device=DEV) * std).to(t)  # noqa: E731
+    keep = torch.rand(rows, generator=g, device=DEV) < 0.5
+    rs = K.sparse_rows_plan(keep.to(torch.uint8))
+    x, dy, w = draw(rows, di), draw(rows, do), [draw(dh, di, std=di ** -0.5), draw(dh, di, std=di ** -0.5), draw(do, dh, std=dh ** -0.5)]
+    x[~keep], dy[~keep] = float("nan"), float("nan")
+    desc = K.make_ffn_desc(di, dh, do, K.DTYPE_CODE[dtype])
+    ws = torch.empty(K.sparse_ffn_workspace_bytes(desc, rs.kept, True), dtype=torch.uint8, device=DEV)
+    results = []
+    for a, b, fmt in ((x, dy, B.SC_ROWS_DENSE), (x[keep], dy[keep], B.SC_ROWS_COMPACT)):
+        y, saved = torch.empty_like(b), torch.empty(3, rs.kept, dh, dtype=t, device=DEV)
+        K.sparse_ffn_run(desc, a, *w, y, ws, rows=rs, x_rows=fmt, y_rows=fmt, saved=saved)
+        dw = [torch.full_like(v, float("nan")) for v in w]
+        K.sparse_ffn_backward(desc, a, *w, saved, b, None, *dw, ws, rows=rs, x_rows=fmt, y_rows=fmt)
+        results.append(dw + [saved])
+    assert all(torch.equal(p, q) for p, q in zip(*results))
+    hidden, left = results[0][3][2].double(), dy[keep].double()
+    want = left.t().contiguous() @ hidden
+    size = left.abs().t().contiguous() @ hidden.abs()
+    inside(results[0][2], want.cpu(), (O.U[dtype] * want.abs() + O.acc(rs.kept) * size).cpu() + O.TINY[dtype], "dw_down")
+
+
 FEW = [(rows, di, dh, do, dtype, "silu", mask, 0, 0)
        for dtype, di, dh, do in (("bf16", 520, 1037, 264), ("f16", 1048, 264, 5), ("f32", 333, 68, 130), ("f16", 77, 1030, 1031))
        for rows, mask in ((3, "all"), (4, "all"), (8, "half"), (8, "all"), (9, "all"), (15, "half"))]
@@ -533,6 +563,46 @@ def test_zeros_in_millions_of_dropped_rows(rows, d_out):
     assert int(torch.count_nonzero(y.view(torch.int16))) == 0   # (NaN and -0.0 count)
 
 
+def test_backward_passes_in_a_graph():
+    """Norm and block forward and backward: parts of gradients, copies of odd rows and zeros are launches of their own."""
+    rows, d, hidden = 700, 410, 300
+    g = torch.Generator(DEV).manual_seed(6)
+    draw = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    rs = K.sparse_rows_plan((draw(rows) < 0).to(torch.uint8))
+    nd, fd = K.make_norm_desc(d, B.SC_F32, rows_per_gate=3), K.make_ffn_desc(d, hidden, d, B.SC_F32)
+    x, f, gate, dx_new, dh = draw(rows, d), draw(rs.kept, d), draw(-(-rows // 3), d), draw(rows, d), draw(rs.kept, d)
+    w, wn = [draw(hidden, d) * d ** -0.5, draw(hidden, d) * d ** -0.5, draw(d, hidden) * hidden ** -0.5], [draw(d), draw(d)]
+    new = torch.empty_like
+    x_new, h, y, saved, stats = new(x), new(f), new(x), draw(3, rs.kept, hidden), draw(rows, 4)
+    out = [new(t) for t in (x, f, gate, wn[0], wn[1], f, *w)]
+    ws = torch.empty(max(K.sparse_norm_workspace_bytes(nd, rows), K.sparse_ffn_workspace_bytes(fd, rs.kept, True)), dtype=torch.uint8, device=DEV)
+
+    def run():
+        K.sparse_norm_run(nd, x, f, gate, wn[0], None, wn[1], None, x_new, h, f_rows=rs, h_rows=rs, stats=stats)
+        K.sparse_ffn_run(fd, h, *w, y, ws, rows=rs, x_rows=B.SC_ROWS_COMPACT, saved=saved)
+        K.sparse_ffn_backward(fd, h, *w, saved, dx_new, out[5], *out[6:], ws, rows=rs, x_rows=B.SC_ROWS_COMPACT)
+        K.sparse_norm_backward(nd, x, f, gate, wn[0], None, wn[1], stats, dx_new, out[5], *out[:4], None, out[4], None, ws, f_rows=rs, h_rows=rs)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    results = [x_new, h, y, *out]
+    for _ in range(3):
+        x.copy_(draw(rows, d))
+        for t in (*results, saved, stats, ws):
+            t.fill_(77)
+        run()
+        want = [t.clone() for t in results]
+        for t in (*results, saved, stats, ws):
+            t.fill_(99)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(results, want))
+
+
 # ---- 4-bit weights -----------------------------------------------------------------------------------------------------
 
 Q4S = [  # rows, n, k, group, dtype, zeros
@@ -587,6 +657,21 @@ def test_q4_gated_products(rows, n, k, group, dtype, kind):
     bound = O.U[dtype] * want.abs() + 1.2 * ea * p.abs() + O.act(a, kind).abs() * ep + 1.2 * ea * ep + O.TINY[dtype]
     bound = bound + 64 * O.E * (1 + a.abs()) * a.abs().clamp_max(8) * p.abs()
     inside(y, want, bound, "y")
+
+
+# columns beyond a round of the wavefronts, so that they take second and third blocks, and outputs beyond those that sixteen are used for
+@pytest.mark.parametrize("c", [(1, 40, 4100, 128, "bf16", True), (3, 24, 2177, 32, "f16", True), (16, 33, 6000, 64, "bf16", False),
+                               (2, 8209, 2200, 128, "bf16", True), (16, 8209, 2177, 32, "f16", True), (1, 8200, 130, 64, "bf16", True),
+                               (20, 8209, 1300, 64, "f16", True), (40, 20, 2300, 32, "bf16", True)], ids=lambda c: "-".join(map(str, c)))
+def test_q4_products_of_long_rows_and_many_outputs(c):
+    test_q4_products(c)
+
+
+@pytest.mark.parametrize("rows,n,k,group,dtype,kind", [(1, 40, 2200, 128, "bf16", "silu"), (16, 33, 4500, 32, "f16", "gelu"),
+                                                       (2, 8209, 2200, 64, "bf16", "silu"), (16, 8201, 2177, 128, "f16", "silu"),
+                                                       (40, 40, 1300, 64, "bf16", "gelu")])
+def test_q4_gated_products_of_long_rows_and_many_outputs(rows, n, k, group, dtype, kind):
+    test_q4_gated_products(rows, n, k, group, dtype, kind)
 
 
 @pytest.mark.parametrize("rows", [3, 40])
