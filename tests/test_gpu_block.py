@@ -603,6 +603,48 @@ def test_backward_passes_in_a_graph():
         assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(results, want))
 
 
+@pytest.mark.parametrize("d", [4096, 4098])
+def test_tensors_beyond_32_bits(d):
+    """1 100 000 rows, 4.5e9 entries, of which a few hundred at both ends and around 2^31 and 2^32 entries are kept."""
+    rows, hidden, t = 1_100_000, 40, torch.bfloat16
+    g = torch.Generator(DEV).manual_seed(d)
+    at = torch.cat([torch.arange(a, a + 70, device=DEV) for a in (0, (1 << 31) // d - 35, (1 << 32) // d - 35, rows - 70)])
+    mask = torch.zeros(rows, dtype=torch.uint8, device=DEV)
+    mask[at] = 1
+    rs = K.sparse_rows_plan(mask)
+    draw = lambda *s, std=1.0: (torch.randn(*s, generator=g, device=DEV) * std).to(t)  # noqa: E731
+    w = [draw(hidden, d, std=d ** -0.5), draw(hidden, d, std=d ** -0.5), draw(d, hidden, std=hidden ** -0.5)]
+    x, y = torch.zeros(rows, d, dtype=t, device=DEV), torch.empty(rows, d, dtype=t, device=DEV)
+    x[at] = draw(280, d)
+    fd, nd = K.make_ffn_desc(d, hidden, d), K.make_norm_desc(d, rows_per_gate=100)
+    ws = torch.empty(K.sparse_ffn_workspace_bytes(fd, 280, True) + K.sparse_norm_workspace_bytes(nd, rows), dtype=torch.uint8, device=DEV)
+
+    def block(x, y, rows, fmt):      # y of the block, then gradients for y = dy
+        saved, dx, dw = torch.empty(3, 280, hidden, dtype=t, device=DEV), torch.empty_like(x), [torch.empty_like(v) for v in w]
+        K.sparse_ffn_run(fd, x, *w, y, ws, rows=rows, x_rows=fmt, y_rows=fmt, saved=saved)
+        K.sparse_ffn_backward(fd, x, *w, saved, y, dx, *dw, ws, rows=rows, x_rows=fmt, y_rows=fmt)
+        return dx, dw
+
+    small_x, small_y = x[at], torch.empty(280, d, dtype=t, device=DEV)
+    dx, dw = block(x, y, rs, B.SC_ROWS_DENSE)
+    want_dx, want_dw = block(small_x, small_y, None, B.SC_ROWS_COMPACT)
+    assert torch.equal(y[at], small_y) and torch.equal(dx[at], want_dx) and all(torch.equal(p, q) for p, q in zip(dw, want_dw))
+    for v in (y, dx):      # (a sum over all would be in 16 bits)
+        v[at] = 0
+        assert not any(bool(piece.any()) for piece in v.split(1 << 17))
+
+    f, gate, ones, stats = draw(280, d), draw(rows // 100, d), torch.ones(d, device=DEV), torch.empty(rows, 4, device=DEV)
+    x_new, h, df = y, torch.empty_like(f), torch.empty_like(f)
+    K.sparse_norm_run(nd, x, f, gate, ones, None, ones, None, x_new, h, f_rows=rs, h_rows=rs, stats=stats)
+    K.sparse_norm_backward(nd, x, f, gate, ones, None, ones, stats, None, small_x, dx, df, None, None, None, None, None, ws, f_rows=rs, h_rows=rs)
+    one, small = K.make_norm_desc(d, rows_per_gate=1), (gate[at // 100], torch.empty_like(f), torch.empty_like(f), torch.empty(280, 4, device=DEV))
+    K.sparse_norm_run(one, x[at], f, small[0], ones, None, ones, None, small[1], small[2], stats=small[3])
+    assert torch.equal(x_new[at], small[1]) and torch.equal(h, small[2])
+    grads = torch.empty_like(f), torch.empty_like(f)
+    K.sparse_norm_backward(one, x[at], f, small[0], ones, None, ones, small[3], None, small_x, *grads, None, None, None, None, None, ws)
+    assert torch.equal(dx[at], grads[0]) and torch.equal(df, grads[1])
+
+
 # ---- 4-bit weights -----------------------------------------------------------------------------------------------------
 
 Q4S = [  # rows, n, k, group, dtype, zeros
