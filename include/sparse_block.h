@@ -92,7 +92,8 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
  * workspace first, in a run with more than 64 kept rows and in every backward pass.
  * SC_F16: hidden rows, g and u beyond 65 504 are infinite, although y need not be (their row is lost then, and no other).
  * Floats of up to 8 kept rows in a run are multiplied as they are.  Those of more than 64, and of every backward pass, are multiplied in
- * three 16-bit parts, others in either way: a float's precision, but a factor loses what of it lies below 2^-126, and an infinity gives NaN. */
+ * three 16-bit parts, others in either way: a float's precision, but a factor loses what of it lies below 2^-126, and an infinity
+ * gives NaN. */
 typedef enum { SC_ACT_SILU = 0, SC_ACT_GELU = 1, SC_ACT_GELU_TANH = 2 } sc_activation;
 
 typedef struct {
@@ -117,8 +118,8 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
  * codes are [n][ceil(k / 2)] bytes, the even column in the low half; scales and zeros are [n][ceil(k / group)] of the
  * descriptor's type (zeros may be NULL: 8).  The plan lays the weights out once in the caller's workspace, from which every run
  * reads them; codes, scales and zeros are not needed afterwards.  sparse_q4_plan_gated lays out two matrices of one shape,
- * whose run gives act(x Gate') * (x Up'), rounded once (SC_F16: beyond 65 504 to an infinity).  Planning only enqueues work.  Up to 65 535 * 64 rows; made for few.
- * x is finite, and in SC_BF16 below 2^110 in size: sums of x times up to 143 (SC_F16: 1 039) are formed in float on the way. */
+ * whose run gives act(x Gate') * (x Up'), rounded once (SC_F16: beyond 65 504 to an infinity).  Planning only enqueues work.
+ * Up to 65 535 * 64 rows; made for few.  x is finite (a row that is not is lost, and no other), and in SC_BF16 below 2^110 in size: sums of x times up to 143 (SC_F16: 1 039) are formed in float on the way. */
 typedef struct {
   int32_t k, n;          /* columns contracted, outputs */
   int32_t group;         /* 32, 64 or 128 columns share a scale */

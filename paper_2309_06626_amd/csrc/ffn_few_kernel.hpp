@@ -38,7 +38,7 @@ template <int DT, int MT, int S, bool GATED, bool WHOLE, int WAVES> __global__ _
   using T = typename Elem<DT>::T;
   constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V * S, MATS = GATED ? 2 : 1, O = 16 / S;
   static_assert(S == 1 || MT == 1, "rows and stretches share the 16 columns");
-    constexpr int AHEAD = S == 4 ? 2 : 4;       // k steps whose operands a wavefront asks for at once
+  constexpr int AHEAD = S == 4 ? 2 : 4;       // k steps whose operands a wavefront asks for at once
   extern __shared__ float few_sum[];          // [WAVES][MATS][MT][64][4]
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int l16 = lane & 15, kg = lane >> 4;

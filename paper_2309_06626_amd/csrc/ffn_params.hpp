@@ -14,8 +14,7 @@ enum FfnProduct : int32_t {
   kFfnDown = 1,     // P along, Q along
   kFfnGateGrad = 2, // P along, Q across: the product is the gradient of the hidden rows; leaves those of gate and up
   kFfnInGrad = 3,   // P along, Q across, two pairs of operands summed
-  kFfnWGrad = 4,    // P across, Q across, one or two P with results of their own
-  kFfnProducts = 5
+  kFfnWGrad = 4     // P across, Q across, one or two P with results of their own
 };
 
 // Rows of operands are whole 16-byte groups, with zeros behind the last entry; so are the rows that a product leaves for the next one.
