@@ -13,7 +13,7 @@
  *   - a mask byte != 0 keeps the row; a dropped row of a dense output holds +0.0 in every channel;
  *   - tensors are contiguous, row by row; *_dev is device memory of the caller, aligned to 16 bytes; the library allocates none;
  *   - sums, norm statistics and gradients of parameters are accumulated in float; every result is rounded once to its type, and
- *     so are the products between the two halves of the feed-forward block (hidden rows, and their gradients);
+ *     so are the operands of the feed-forward block's second products (hidden rows, and the gradients of g and u);
  *   - results do not depend on the order in which workgroups run: the same call gives the same bits;
  *   - status codes; argument checks come before the first HIP call; *_run and *_backward only enqueue work on hip_stream;
  *   - outputs must not overlap inputs, except where noted;
@@ -87,10 +87,12 @@ sc_status sparse_norm_backward(const sc_norm_desc* desc, int64_t rows, const voi
  * rows (sc_rows, may be NULL: all `m` rows are kept) says which rows of x count; m is the number of rows of the mask.  With
  * x_rows = SC_ROWS_DENSE x (and dx) is [m x d_in], with SC_ROWS_COMPACT [kept x d_in]; y_rows says the same of y (and dy).
  * Dropped rows of a dense x or dy are not looked at, whatever they hold.
- * saved_dev: [3][kept][d_hidden] of the descriptor's type -- g, u and hidden, rounded -- for the backward pass; NULL in inference.
+ * saved_dev: [3][kept][d_hidden] of the descriptor's type for the backward pass, as sparse_ffn_run leaves it: g and u in floats, or in
+ * 24 bits each of 16-bit types.  NULL in inference.
  * Sizes need not be multiples of anything; rows of whole 16-byte groups are the fast path, others are copied into the
  * workspace first, in a run with more than 64 kept rows and in every backward pass.
- * SC_F16: hidden rows, g and u beyond 65 504 are infinite, although y need not be (their row is lost then, and no other).
+ * SC_F16: hidden rows and gradients of g and u beyond 65 504 are infinite, although y and dx need not be (their row is lost then, and
+ * no other).
  * Floats of up to 8 kept rows in a run are multiplied as they are.  Those of more than 64, and of every backward pass, are multiplied in
  * three 16-bit parts, others in either way: a float's precision, but a factor loses what of it lies below 2^-126, and an infinity
  * gives NaN. */

@@ -287,7 +287,8 @@ def _ffn_shapes(desc, rows, x, x_rows, y, y_rows, y_name):
 
 def sparse_ffn_run(desc: sc_ffn_desc, x, w_gate, w_up, w_down, y, workspace, rows: Optional[RowSet] = None,
                    x_rows: int = SC_ROWS_DENSE, y_rows: int = SC_ROWS_DENSE, saved=None, stream=None):
-    """y = (act(x w_gate') * (x w_up')) w_down' over the kept rows; saved: [3, kept, d_hidden], for the backward pass."""
+    """y = (act(x w_gate') * (x w_up')) w_down' over the kept rows; saved: [3, kept, d_hidden], what the backward pass
+    needs of the two products (in its own layout)."""
     t = _elem(desc)
     m, kept = _ffn_shapes(desc, rows, x, x_rows, y, y_rows, "y")
     di, dh, do = desc.d_in, desc.d_hidden, desc.d_out

@@ -9,6 +9,7 @@
 #include "../../include/sparse_block.h"
 #include "ffn_act.hpp"
 #include "ffn_params.hpp"
+#include "ffn_saved.hpp"
 #include "mma_common.hpp"
 #include "rows.hpp"
 
@@ -52,7 +53,7 @@ static bool whole_rows(const sc_ffn_desc& d) { return (d.d_in | d.d_hidden | d.d
 // Operands whose rows are not whole 16-byte groups are copied first, kept rows alone, with zeros up to the next whole group: the products
 // then load straight into LDS and have no ends to look after.  5 000 x 423 -> 2 809 in bf16, forward and backward, takes
 // 310 us (424 -> 2 808: 248), 699 where rows went through registers into LDS.
-constexpr int kMostCopies = 6;
+constexpr int kMostCopies = 5;
 struct FfnCopies {
   struct One {
     const void* src;
@@ -210,15 +211,10 @@ template <typename T, int WHAT, bool WHOLE> __global__ __launch_bounds__(256) vo
         if (u < have) c[at + u] = out[u];
     }
   };
-  auto load = [&](const T* c, int64_t at, int have, T (&v)[4]) {
-    if (WHOLE || have >= 4) {
-      __builtin_memcpy(v, c + at, sizeof(v));
-    } else {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = u < have ? c[at + u] : T(0);
-    }
-  };
-  T* const saved = static_cast<T*>(g.saved);
+  using Saved = FfnSaved<T>;
+  using U = typename Saved::U;
+  constexpr int PLANES = Saved::PLANES;
+  U* const saved = static_cast<U*>(g.saved);
   const int i = (blockIdx.z * 256 + threadIdx.x) * 4;
   if (i < n) {
     const int64_t at = (int64_t)row * n + i, to = row * g.ldc + i;
@@ -234,25 +230,53 @@ template <typename T, int WHAT, bool WHOLE> __global__ __launch_bounds__(256) vo
       }
       store(static_cast<T*>(g.c[0]), to, have, hidden);
       if (saved) {
-        store(saved, at, have, gate);
-        store(saved + whole, at, have, up);
-        if (saved + 2 * whole != g.c[0]) store(saved + 2 * whole, at, have, hidden);
+        U kept[PLANES][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          U one[PLANES];
+          Saved::keep(gate[u], up[u], one);
+#pragma unroll
+          for (int plane = 0; plane < PLANES; ++plane) kept[plane][u] = one[plane];
+        }
+#pragma unroll
+        for (int plane = 0; plane < PLANES; ++plane) {
+          if (WHOLE || have >= 4) {
+            __builtin_memcpy(saved + plane * whole + at, kept[plane], sizeof(kept[plane]));
+          } else {
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+              if (u < have) saved[plane * whole + at + u] = kept[plane][u];
+          }
+        }
       }
     } else if constexpr (WHAT == kFfnGateGrad) {
       const v4f dh = sum(0, i);
-      T gate[4], up[4];
-      load(saved, at, have, gate);
-      load(saved + whole, at, have, up);
-      v4f dg, du;
+      U kept[PLANES][4];
+#pragma unroll
+      for (int plane = 0; plane < PLANES; ++plane) {
+        if (WHOLE || have >= 4) {
+          __builtin_memcpy(kept[plane], saved + plane * whole + at, sizeof(kept[plane]));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) kept[plane][u] = u < have ? saved[plane * whole + at + u] : U(0);
+        }
+      }
+      v4f dg, du, hidden;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        float a, da;
-        ffn_act<T>(g.activation, (float)gate[u], a, da);
-        dg[u] = dh[u] * (float)up[u] * da;
+        U one[PLANES];
+#pragma unroll
+        for (int plane = 0; plane < PLANES; ++plane) one[plane] = kept[plane][u];
+        float gate, up, a, da;
+        Saved::back(one, gate, up);
+        ffn_act<T>(g.activation, gate, a, da);
+        dg[u] = dh[u] * up * da;
         du[u] = dh[u] * a;
+        hidden[u] = a * up;
       }
       store(static_cast<T*>(g.c[0]), to, have, dg);
       store(static_cast<T*>(g.c[1]), to, have, du);
+      if (g.hidden) store(static_cast<T*>(g.hidden), to, have, hidden);
     } else {
       store(static_cast<T*>(g.c[blockIdx.y]), g.c_rows ? g.c_rows[row] * g.ldc + i : to, have, sum(blockIdx.y, i));
     }
@@ -260,7 +284,10 @@ template <typename T, int WHAT, bool WHOLE> __global__ __launch_bounds__(256) vo
   if (!WHOLE && (WHAT == kFfnUp || WHAT == kFfnGateGrad))      // zeros behind the last entry of an operand's row
     if (blockIdx.z == 0 && n + (int)threadIdx.x < g.ldc) {
       static_cast<T*>(g.c[0])[row * g.ldc + n + threadIdx.x] = T(0);
-      if (WHAT == kFfnGateGrad) static_cast<T*>(g.c[1])[row * g.ldc + n + threadIdx.x] = T(0);
+      if (WHAT == kFfnGateGrad) {
+        static_cast<T*>(g.c[1])[row * g.ldc + n + threadIdx.x] = T(0);
+        if (g.hidden) static_cast<T*>(g.hidden)[row * g.ldc + n + threadIdx.x] = T(0);
+      }
     }
 }
 
@@ -367,10 +394,10 @@ sc_status sparse_ffn_workspace_bytes(const sc_ffn_desc* desc, int64_t kept, int3
   const int dt = desc->dtype;
   const int64_t d_in = desc->d_in, d_hidden = desc->d_hidden, d_out = desc->d_out;
   const size_t hidden = sc::Copies::bytes(kept, d_hidden, dt);
-  *bytes = 256 + (training ? 2 * hidden : hidden) + sc::most_parts(*desc, kept, training != 0);
+  *bytes = 256 + (training ? 3 * hidden : hidden) + sc::most_parts(*desc, kept, training != 0);
   if (!sc::whole_rows(*desc)) {
     *bytes += sc::Copies::bytes(kept, d_in, dt) + 2 * sc::Copies::bytes(d_hidden, d_in, dt) + sc::Copies::bytes(d_out, d_hidden, dt);
-    if (training) *bytes += sc::Copies::bytes(kept, d_out, dt) + hidden;
+    if (training) *bytes += sc::Copies::bytes(kept, d_out, dt);
   }
   return SC_OK;
 }
@@ -398,7 +425,7 @@ sc_status sparse_ffn_run(const sc_ffn_desc* desc, int64_t m, const sc_rows* rows
   const bool whole = sc::whole_rows(*desc), copied = !whole && kept > sc::kFewRows;
   const int64_t d_in = desc->d_in, d_hidden = desc->d_hidden, d_out = desc->d_out;
   const int64_t in_pitch = copied ? sc::pitch_of(d_in, dt) : d_in, hidden_pitch = copied ? sc::pitch_of(d_hidden, dt) : d_hidden;
-  void* const hidden = saved_dev && !copied ? static_cast<char*>(saved_dev) + 2 * (size_t)kept * d_hidden * eb : workspace_dev;
+  void* const hidden = workspace_dev;
   char* const w = static_cast<char*>(workspace_dev) + sc::Copies::bytes(kept, d_hidden, dt);
   float* const parts = reinterpret_cast<float*>(w);
 
@@ -474,23 +501,20 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
   const int64_t in_pitch = sc::pitch_of(d_in, dt), hidden_pitch = sc::pitch_of(d_hidden, dt), out_pitch = sc::pitch_of(d_out, dt);
   void* const dg = w;
   void* const du = w + hidden_bytes;
-  float* const partial = reinterpret_cast<float*>(w + 2 * hidden_bytes);
+  void* const hidden = w + 2 * hidden_bytes;
+  float* const partial = reinterpret_cast<float*>(w + 3 * hidden_bytes);
   const int32_t *x_map = sc::map_of(rows, x_rows), *y_map = sc::map_of(rows, y_rows);
   const int32_t* const dx_map = x_map;
   const void *x = x_dev, *dy = dy_dev, *w_gate = w_gate_dev, *w_up = w_up_dev, *w_down = w_down_dev;
-  const void* hidden = static_cast<const char*>(saved_dev) + 2 * (size_t)kept * d_hidden * eb;
   if (!whole) {
-    sc::Copies copies(w + 2 * hidden_bytes + sc::most_parts(*desc, kept, true), dt);
+    sc::Copies copies(w + 3 * hidden_bytes + sc::most_parts(*desc, kept, true), dt);
     dy = copies.add(dy, kept, d_out, dt, y_map);
     w_down = copies.add(w_down, d_out, d_hidden, dt);
     if (dx_dev) {
       w_gate = copies.add(w_gate, d_hidden, d_in, dt);
       w_up = copies.add(w_up, d_hidden, d_in, dt);
     }
-    if (weights) {
-      x = copies.add(x, kept, d_in, dt, x_map);
-      hidden = copies.add(hidden, kept, d_hidden, dt);
-    }
+    if (weights) x = copies.add(x, kept, d_in, dt, x_map);
     x_map = y_map = nullptr;
     e = copies.run(s);
     if (e != hipSuccess) return sc::failed(e);
@@ -505,6 +529,7 @@ sc_status sparse_ffn_backward(const sc_ffn_desc* desc, int64_t m, const sc_rows*
   gate.saved = const_cast<void*>(saved_dev);
   gate.c[0] = dg;
   gate.c[1] = du;
+  gate.hidden = weights ? hidden : nullptr;
   gate.ldc = hidden_pitch;
   gate.activation = desc->activation;
   e = sc::multiply(dt, sc::kFfnGateGrad, gate, whole, partial, s);

@@ -9,6 +9,7 @@
 #pragma once
 #include "ffn_act.hpp"
 #include "ffn_params.hpp"
+#include "ffn_saved.hpp"
 #include "mma_common.hpp"
 
 namespace sc {
@@ -121,9 +122,12 @@ template <int DT, int MT, int S, bool GATED, bool WHOLE, int WAVES> __global__ _
       ffn_act<T>(p.activation, v[0], act, slope);
       static_cast<T*>(p.c[0])[(int64_t)row * p.ldc + n] = (T)(act * v[1]);
       if (p.saved) {
-        T* g = static_cast<T*>(p.saved);
-        g[(int64_t)row * p.ldc + n] = (T)v[0];
-        g[((int64_t)p.m + row) * p.ldc + n] = (T)v[1];
+        using Saved = FfnSaved<T>;
+        typename Saved::U kept[Saved::PLANES];
+        Saved::keep(v[0], v[1], kept);
+#pragma unroll
+        for (int s = 0; s < Saved::PLANES; ++s)
+          static_cast<typename Saved::U*>(p.saved)[((int64_t)s * p.m + row) * p.n + n] = kept[s];
       }
     } else {
       static_cast<T*>(p.c[0])[(p.c_rows ? (int64_t)p.c_rows[row] : row) * p.ldc + n] = (T)v[0];

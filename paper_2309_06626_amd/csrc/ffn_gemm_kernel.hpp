@@ -3,12 +3,13 @@
 //
 // Bound by the matrix cores, and under full load by power: 8 192 x 5 632 -> 2 048 in bf16 145 to 157 us (1 200 to 1 300 TFLOP/s, matrix
 // pipes busy 83 % of cycles at 1.6 to 1.9 GHz; the library's product 131, 89 %), gated 8 192 x 2 048 -> 2 x 5 632 with what backward needs
-// 340 to 360, hidden gradient 235 to 250, input gradient 280 to 300, weight gradients 380 to 425 (two) and 190 to 216.  Tiles of 256 x 256
+// 355 to 380, hidden gradient 283 to 300, input gradient 280 to 300, weight gradients 380 to 425 (two) and 190 to 216.  Tiles of 256 x 256
 // need the fewest bytes an operation from LDS and L2; the smaller ones fill the compute units where there are few tiles.
 // Floats: 8 192 x 512 -> 4 096 187 TFLOP/s, 132 on the float matrix instruction.
 #pragma once
 #include "ffn_act.hpp"
 #include "ffn_params.hpp"
+#include "ffn_saved.hpp"
 #include "mma_common.hpp"
 
 namespace sc {
@@ -78,6 +79,31 @@ template <int I, int N, class Fn> __device__ __forceinline__ void ffn_for(Fn&& f
   if constexpr (I < N) {
     f(std::integral_constant<int, I>{});
     ffn_for<I + 1, N>(f);
+  }
+}
+
+// As store_block_pairs, of 16 columns that lie as they are stored: two lanes trade pieces, so that they write 32 bytes of one row each time.
+template <typename T>
+__device__ __forceinline__ void ffn_store_pairs(const v4i (&pk)[sizeof(T)], int row, int c0, T* y, int c_out) {
+  constexpr int GC = 16 / (int)sizeof(T), PIECES = 16 / GC;
+  const bool odd = threadIdx.x & 1;
+  auto other = [](int v) { return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, false); };   // quad_perm [1, 0, 3, 2]
+  const int theirs = other(row);
+  const int row0 = odd ? theirs : row, row1 = odd ? row : theirs;
+  T* const y0 = y + ((int64_t)row0 * c_out + c0 + (odd ? GC : 0));
+  T* const y1 = y + ((int64_t)row1 * c_out + c0 + (odd ? GC : 0));
+#pragma unroll
+  for (int q = 0; q < PIECES; q += 2) {
+    v4i first, second;       // the pieces of the even and of the odd lane's row
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int got = other(odd ? pk[q][i] : pk[q + 1][i]);
+      first[i] = odd ? got : pk[q][i];
+      second[i] = odd ? pk[q + 1][i] : got;
+    }
+    const bool inside = c0 + q * GC + (odd ? GC : 0) < c_out;
+    if (inside && row0 >= 0) sc_store16(reinterpret_cast<v4i*>(y0 + q * GC), first);
+    if (inside && row1 >= 0) sc_store16(reinterpret_cast<v4i*>(y1 + q * GC), second);
   }
 }
 
@@ -474,24 +500,64 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     store_block_pairs<DT, false>(out, row, false, col, c, nullptr, 0, (int)ldc);
   };
   // 16 columns of a row of `saved`, as they lie
-  struct Raw { v4i g[16 / V]; };
-  auto load16 = [&](const T* c, int row, int col) {
+  using Saved = FfnSaved<T>;
+  using U = typename Saved::U;
+  constexpr int PLANES = Saved::PLANES, PER = Saved::PER;
+  struct Raw { v4i g[PLANES][16 / V]; };
+  auto load16 = [&](int row, int col) {
     Raw raw;
-    const T* s = c + (int64_t)row * n + col;
+    const int64_t at = (int64_t)row * n + col;
 #pragma unroll
-    for (int g = 0; g < 16 / V; ++g) {
-      const int have = row < 0 ? 0 : n - col - g * V;
-      raw.g[g] = v4i{0, 0, 0, 0};
-      if (have >= V) {
-        __builtin_memcpy(&raw.g[g], s + g * V, 16);
-      } else if (!WHOLE) {
-        T e[V];
+    for (int plane = 0; plane < PLANES; ++plane) {
+      const U* s = static_cast<const U*>(p.saved) + (int64_t)plane * m * n + at;
 #pragma unroll
-        for (int i = 0; i < V; ++i) e[i] = i < have ? s[g * V + i] : T(0);
-        __builtin_memcpy(&raw.g[g], e, 16);
+      for (int g = 0; g < 16 / V; ++g) {
+        const int have = row < 0 ? 0 : n - col - g * V;
+        raw.g[plane][g] = v4i{0, 0, 0, 0};
+        if (have >= V) {
+          __builtin_memcpy(&raw.g[plane][g], s + g * V, 16);
+        } else if (!WHOLE) {
+          U e[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) e[i] = i < have ? s[g * V + i] : U(0);
+          __builtin_memcpy(&raw.g[plane][g], e, 16);
+        }
       }
     }
     return raw;
+  };
+  auto save16 = [&](int row, int col, const floatx16& gate, const floatx16& up) {
+    unsigned words[PLANES][16 / PER];
+#pragma unroll
+    for (int w = 0; w < 16 / PER; ++w) {
+      float g[PER], u[PER];
+#pragma unroll
+      for (int e = 0; e < PER; ++e) g[e] = gate[w * PER + e], u[e] = up[w * PER + e];
+      unsigned one[PLANES];
+      Saved::keep_word(g, u, one);
+#pragma unroll
+      for (int plane = 0; plane < PLANES; ++plane) words[plane][w] = one[plane];
+    }
+#pragma unroll
+    for (int plane = 0; plane < PLANES; ++plane) {
+      U* const to = static_cast<U*>(p.saved) + (int64_t)plane * m * n;
+      if constexpr (WHOLE) {
+        v4i pieces[sizeof(U)];
+        __builtin_memcpy(pieces, words[plane], sizeof(pieces));
+        ffn_store_pairs<U>(pieces, row, col, to, n);
+      } else if (row >= 0) {
+        U* const dst = to + (int64_t)row * n + col;
+        if (col + 16 <= n) {
+          __builtin_memcpy(dst, words[plane], sizeof(words[plane]));
+        } else {
+          U one[16];
+          __builtin_memcpy(one, words[plane], sizeof(one));
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (col + e < n) dst[e] = one[e];
+        }
+      }
+    }
   };
   if (p.splits > 1) {                                          // sums of this part: [batch, or gate and up][splits][m][pitch]
     const int pitch = (n + 3) & ~3;
@@ -513,38 +579,51 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
     }
     return;
   }
+  int own_row = l32;
   auto row_of = [&](int mi) {
-    const int i = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + l32;
+    const int i = m0 + mi / MB * PM + (wm * MB + mi % MB) * 32 + own_row;
     return i < m ? i : -1;
   };
   auto col_of = [&](int ni) { return n0 + ni / NB * PN + (wn * NB + ni % NB) * 32 + 16 * h; };
   if constexpr (WHAT == kFfnGateGrad) {
     // a block's rows of gate and up are asked for a block ahead
-    const T* const gate = static_cast<const T*>(p.saved);
-    const T* const up = gate + (int64_t)m * n;
-    Raw next_g = load16(gate, row_of(0), col_of(0)), next_u = load16(up, row_of(0), col_of(0));
+    Raw next = load16(row_of(0), col_of(0));
     ffn_for<0, 4 * MB * NB>([&](auto block) {
       constexpr int b = decltype(block)::value, mi = b / (2 * NB), ni = b % (2 * NB), after = b + 1 < 4 * MB * NB ? b + 1 : b;
-      const Raw raw_g = next_g, raw_u = next_u;
-      if constexpr (after != b) {
-        next_g = load16(gate, row_of(after / (2 * NB)), col_of(after % (2 * NB)));
-        next_u = load16(up, row_of(after / (2 * NB)), col_of(after % (2 * NB)));
-      }
-      T g[16], u[16];
-      __builtin_memcpy(g, &raw_g, sizeof(g));
-      __builtin_memcpy(u, &raw_u, sizeof(u));
-      floatx16 dg, du;
+      const Raw raw = next;
+      asm volatile("" : "+v"(own_row));                        // (no addresses kept from block to block: registers)
+      if constexpr (after != b) next = load16(row_of(after / (2 * NB)), col_of(after % (2 * NB)));
+      unsigned words[PLANES][16 / PER];
+      __builtin_memcpy(words, &raw, sizeof(words));
+      T dg[16], du[16], hidden[16];                            // (converted at once: half as many registers)
       ffn_act_kind(p.activation, [&](auto kind) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float a, da;
-          ffn_act_of<decltype(kind)::value, T>((float)g[e], a, da);
-          dg[e] = acc[mi][ni][e] * (float)u[e] * da;
-          du[e] = acc[mi][ni][e] * a;
+        for (int w = 0; w < 16 / PER; ++w) {
+          unsigned one[PLANES];
+#pragma unroll
+          for (int plane = 0; plane < PLANES; ++plane) one[plane] = words[plane][w];
+          float g[PER], u[PER];
+          Saved::back_word(one, g, u);
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            const int e = w * PER + i;
+            float a, da;
+            ffn_act_of<decltype(kind)::value, T>(g[i], a, da);
+            const bool in = WHOLE || col_of(ni) + e < n;
+            dg[e] = E::from_float(in ? acc[mi][ni][e] * u[i] * da : 0.0f);
+            du[e] = E::from_float(in ? acc[mi][ni][e] * a : 0.0f);
+            hidden[e] = E::from_float(in ? a * u[i] : 0.0f);
+          }
         }
       });
-      store_operand(static_cast<T*>(p.c[0]), p.ldc, row_of(mi), col_of(ni), dg);
-      store_operand(static_cast<T*>(p.c[1]), p.ldc, row_of(mi), col_of(ni), du);
+      auto leave = [&](void* c, const T (&v)[16]) {
+        v4i pieces[sizeof(T)];
+        __builtin_memcpy(pieces, v, sizeof(pieces));
+        ffn_store_pairs<T>(pieces, row_of(mi), col_of(ni), static_cast<T*>(c), (int)p.ldc);
+      };
+      leave(p.c[0], dg);
+      leave(p.c[1], du);
+      if (p.hidden) leave(p.hidden, hidden);
     });
     return;
   }
@@ -567,12 +646,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void ffn_gemm_kernel(con
           }
         });
         store_operand(static_cast<T*>(p.c[0]), p.ldc, row, col, hidden);
-        if (p.saved) {
-          T* g = static_cast<T*>(p.saved);
-          store(g, n, row, col, acc[mi][ni]);
-          store(g + (int64_t)m * n, n, row, col, acc[mi][ni + NB]);
-          if constexpr (!WHOLE) store(g + 2 * (int64_t)m * n, n, row, col, hidden);
-        }
+        if (p.saved) save16(row, col, acc[mi][ni], acc[mi][ni + NB]);
       } else {
         store(static_cast<T*>(p.c[z]), p.ldc, out_row, col, acc[mi][ni]);
       }

@@ -10,9 +10,9 @@ namespace sc {
 // C[i][j] = sum_k P[i][k] Q[j][k].  An operand is "along k" (its rows are those of the result, k runs within them) or "across k"
 // (its rows are those of the contraction).
 enum FfnProduct : int32_t {
-  kFfnUp = 0,       // P along, Q = gate and up weights along: act(P Wg') * (P Wu'), and with `saved` the two products
+  kFfnUp = 0,       // P along, Q = gate and up weights along: hidden = act(P Wg') * (P Wu'), and with `saved` the two products
   kFfnDown = 1,     // P along, Q along
-  kFfnGateGrad = 2, // P along, Q across: the product is the gradient of the hidden rows; leaves those of gate and up
+  kFfnGateGrad = 2, // P along, Q across: the product is the gradient of the hidden rows; leaves those of gate and up, and hidden again
   kFfnInGrad = 3,   // P along, Q across, two pairs of operands summed
   kFfnWGrad = 4     // P across, Q across, one or two P with results of their own
 };
@@ -30,7 +30,8 @@ struct FfnGemm {
   void* c[2];
   int64_t ldc;                 // (of kFfnUp's and kFfnGateGrad's results: whole groups)
   const int32_t* c_rows;       // row of c that receives result row i; null: i
-  void* saved;                 // [3][m][n].  kFfnUp: may be null; where n is whole groups c[0] is its third matrix.  kFfnGateGrad: read
+  void* saved;                 // [3][m][n], see FfnSaved.  kFfnUp: written, may be null.  kFfnGateGrad: read
+  void* hidden;                // kFfnGateGrad: like c; null where it is not wanted
   int32_t activation;
   int32_t splits;              // parts of the contraction, each with its sums in `partial`
   float* partial;              // [batch, or gate and up][splits][m][n up to a multiple of 4]

@@ -361,12 +361,16 @@ def test_ffn_weight_gradients_through_long_row_lists(rows, di, dh, do, dtype):
         K.sparse_ffn_run(desc, a, *w, y, ws, rows=rs, x_rows=fmt, y_rows=fmt, saved=saved)
         dw = [torch.full_like(v, float("nan")) for v in w]
         K.sparse_ffn_backward(desc, a, *w, saved, b, None, *dw, ws, rows=rs, x_rows=fmt, y_rows=fmt)
-        results.append(dw + [saved])
+        results.append(dw)
     assert all(torch.equal(p, q) for p, q in zip(*results))
-    hidden, left = results[0][3][2].double(), dy[keep].double()
-    want = left.t().contiguous() @ hidden
-    size = left.abs().t().contiguous() @ hidden.abs()
-    inside(results[0][2], want.cpu(), (O.U[dtype] * want.abs() + O.acc(rs.kept) * size).cpu() + O.TINY[dtype], "dw_down")
+    gate, up = (x[keep].double() @ v.double().t().contiguous() for v in w[:2])
+    hidden, left = O.act(gate, "silu") * up, dy[keep].double()
+    want, size = left.t().contiguous() @ hidden, left.abs().t().contiguous() @ hidden.abs()
+    # of hidden: half a unit, and its float sums and activation, which are far below that of 16 bits and 16 acc(d_in) of a float's terms
+    rounding = O.U[dtype] if dtype != "f32" else 0.0
+    off = rounding * hidden.abs() + 16 * O.acc(di) * (1 + gate.abs()) * (1 + up.abs())
+    bound = O.U[dtype] * want.abs() + O.acc(rs.kept) * size + left.abs().t().contiguous() @ off
+    inside(results[0][2], want.cpu(), 1.05 * bound.cpu() + O.TINY[dtype], "dw_down")
 
 
 FEW = [(rows, di, dh, do, dtype, "silu", mask, 0, 0)
@@ -483,6 +487,43 @@ def test_activations_of_the_largest_numbers(dtype, rows, kind):
     v = torch.tensor([1e10, 2e19, 1e30, 2e38, -1e10, -2e19, -1e30, -2e38]).to(O.TORCH[dtype]).double()
     y, slope = activations(v, dtype, kind, rows)
     assert torch.equal(y, v.clamp_min(0)) and torch.equal(slope, (v > 0).double())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows,di,dh,do", [(3, 256, 512, 256), (60, 264, 520, 200), (900, 256, 512, 320), (900, 201, 403, 255)])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+def test_ffn_gradients_are_as_near_as_their_operands_allow(dtype, rows, di, dh, do, kind):
+    """hidden, dg and du are rounded once, as operands of products, and nothing else is on the way: a gradient is as far from the exact one as a
+    product in 64 bits of operands rounded once.  g and u in 24 bits turn the rounding of up to 6 % of the operands, which lie half way between
+    two numbers, to the other side: signs of errors change, not their size."""
+    c = (rows, di, dh, do, dtype, kind, "all", 0, 0)
+    m, keep, full = ffn_case(c, 17)
+    got = ffn_call(c, m, keep, full)
+    x, wg, wu, wd, dy = (full[n] for n in ("x", "wg", "wu", "wd", "dy"))
+    once = lambda v: v.to(O.TORCH[dtype]).double()  # noqa: E731
+    g, u, dhidden = x @ wg.T, x @ wu.T, dy @ wd
+    a = O.act(g, kind)
+    dg, du, hidden = once(dhidden * u * O.act_grad(g, kind)), once(dhidden * a), once(a * u)
+    leaves = [v.clone().requires_grad_(True) for v in (x, wg, wu, wd)]
+    exact = torch.autograd.grad(O.ffn_forward(*leaves, kind), leaves, dy)
+    for name, have, want, near in zip(("dx", "dw_gate", "dw_up", "dw_down"), got[1:], exact, (dg @ wg + du @ wu, dg.T @ x, du.T @ x, dy.T @ hidden)):
+        off, ideal = (have.double().cpu() - want).norm(), (once(near) - want).norm()
+        assert off <= 1.1 * ideal, f"{name}: {off / ideal:.3f}"
+
+
+@pytest.mark.parametrize("rows", [1, 130])
+def test_f16_products_beyond_its_range(rows):
+    """g of 90 000 with u of 0.01: hidden and every gradient are within f16, and so are the results."""
+    full = dict(x=torch.zeros(rows, 8).double(), wg=torch.zeros(16, 8).double(), wu=torch.zeros(16, 8).double(), wd=torch.eye(16).double(),
+                dy=torch.full((rows, 16), 0.0625).double())
+    full["x"][:, 0], full["x"][:, 1], full["wg"][:, 0], full["wu"][:, 1] = 300, 1, 300, 0.0078125
+    c = (rows, 8, 16, 16, "f16", "silu", "all", 0, 0)
+    y, dx, dwg, dwu, dwd = (v.double().cpu() for v in ffn_call(c, torch.ones(rows, dtype=torch.uint8), torch.ones(rows, dtype=torch.bool), full))
+    within = lambda have, want: ((have - want).abs() <= 2.0 ** -9 * abs(want)).all()  # noqa: E731
+    assert within(y, 90000 / 128)
+    assert within(dx[:, 0], 16 * 300 / 2048) and within(dx[:, 1], 16 * 5625 / 128) and (dx[:, 2:] == 0).all()
+    if rows == 1:      # (a sum over 130 rows of 5 625 is beyond f16)
+        assert within(dwg[:, 0], 300 / 2048) and within(dwu[:, 1], 5625) and within(dwd, 90000 / 2048)
 
 
 def test_floats_in_parts_lose_what_lies_below_the_smallest_normal_number():
