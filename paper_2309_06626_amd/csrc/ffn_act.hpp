@@ -30,7 +30,7 @@ template <typename T> __device__ __forceinline__ float ffn_sigmoid(float v, floa
 // shares the exponential with the derivative; P of degree 5, fitted here to erfcx(a / sqrt 2) / 2 for a of 0 .. 14 so that its relative error
 // is evened out: below 1.2e-6 up to a = 1.5, 6e-6 up to 3 and 2.5e-5 beyond, where a form within so much of Phi alone would lose the small
 // results (half a unit is 5e-4 of an f16, 4e-3 of a bf16).  erfcf takes some eighty operations (gated
-// 6 272 x 768 -> 2 048 in f16 with a rational form of five terms 53 us, with erfcf 67; a sixth term costs 0.7)
+// 6 272 x 768 -> 2 048 in f16: 54 us, with erfcf 67)
 template <typename T> __device__ __forceinline__ float ffn_phi(float v, float& e) {
   e = ffn_exp<T>(-0.5f * v * v);
   if constexpr (sizeof(T) == 4) {
