@@ -3,7 +3,7 @@
 //
 // Bound by the matrix cores, and under full load by power: 8 192 x 5 632 -> 2 048 in bf16 145 to 157 us (1 200 to 1 300 TFLOP/s, matrix
 // pipes busy 83 % of cycles at 1.6 to 1.9 GHz; the library's product 131, 89 %), gated 8 192 x 2 048 -> 2 x 5 632 with what backward needs
-// 345 to 380, hidden gradient 276 to 300, input gradient 280 to 300, weight gradients 372 to 440 (two) and 190 to 223.  Tiles of 256 x 256
+// 358 to 383, hidden gradient 278 to 300, input gradient 280 to 300, weight gradients 372 to 440 (two) and 190 to 223.  Tiles of 256 x 256
 // need the fewest bytes an operation from LDS and L2; the smaller ones fill the compute units where there are few tiles.
 // Floats: 8 192 x 512 -> 4 096 187 TFLOP/s, 132 on the float matrix instruction.
 #pragma once
