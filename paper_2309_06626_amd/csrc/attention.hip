@@ -1,0 +1,364 @@
+// Attention over packed sequences of kept rows: plans and calls (the kernels are in attn_kernel.hpp).
+//
+// A plan is a list of a workgroup's shares: tiles of packed rows (forward, and the queries' gradient) and of keys (their and the values'
+// gradient) of every sequence, those with the most to do first.
+#include "../../include/sparse_attention.h"
+
+#include "attn_params.hpp"
+#include "conv_params.hpp"
+#include "rows.hpp"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+struct sc_attn {
+  sc_attn_desc desc;
+  int64_t end, kept;               // rows of the sequences, and how many of them are kept
+  uint64_t version;                // of the row set; 0: none
+  int32_t waves;
+  const sc::AttnItem *row_items, *key_items;
+  int32_t n_row_items, n_key_items;
+};
+
+namespace sc {
+
+void note_hip_error(int32_t code);
+
+static hipError_t attn_dispatch(int dtype, int what, const AttnParams& p, int waves, bool vec, hipStream_t s) {
+  if (dtype == SC_BF16) return attn_launch<kBF16>(what, p, waves, vec, s);
+  if (dtype == SC_F16) return attn_launch<kF16>(what, p, waves, vec, s);
+  return attn_launch<kF32>(what, p, waves, vec, s);
+}
+
+// kept rows before each start
+__global__ __launch_bounds__(256) void attn_starts_kernel(const int32_t* __restrict__ starts, int n, const int32_t* __restrict__ row_idx,
+                                                          int32_t kept, int32_t* __restrict__ out) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  int lo = 0, hi = kept;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (row_idx[mid] < starts[i]) lo = mid + 1;
+    else hi = mid;
+  }
+  out[i] = lo;
+}
+
+// zeros in the dropped rows of up to three outputs; a wavefront a row
+struct AttnZeros {
+  void* out[3];
+  int64_t stride[3], width[3];      // bytes
+};
+template <typename T>
+__global__ __launch_bounds__(256) void attn_zero_kernel(const int32_t* __restrict__ slot, int64_t rows, AttnZeros z) {
+  for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4) {
+    if (slot && slot[r] >= 0) continue;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      T* row = reinterpret_cast<T*>(static_cast<unsigned char*>(z.out[k]) + r * z.stride[k]);
+      for (int64_t i = threadIdx.x & 63; i < z.width[k] / (int64_t)sizeof(T); i += 64) row[i] = T{};
+    }
+  }
+}
+
+static hipError_t attn_zero_dropped(const sc_rows* set, int64_t rows, const AttnZeros& z, hipStream_t s) {
+  if (!set || set->kept == set->rows || rows == 0) return hipSuccess;
+  uintptr_t all = 0;
+  for (int k = 0; k < 3; ++k) all |= (uintptr_t)z.out[k] | (uintptr_t)z.stride[k] | (uintptr_t)z.width[k];
+  const unsigned grid = (unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 22);
+  const int32_t* slot = set->kept ? set->slot : nullptr;
+  typedef int v4 __attribute__((ext_vector_type(4)));
+  if (all % 16 == 0) attn_zero_kernel<v4><<<dim3(grid), dim3(256), 0, s>>>(slot, rows, z);
+  else attn_zero_kernel<uint16_t><<<dim3(grid), dim3(256), 0, s>>>(slot, rows, z);
+  return hipGetLastError();
+}
+
+static size_t attn_up(size_t n) { return (n + 255) & ~(size_t)255; }
+static int64_t attn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int kAttnRowsLeast = 32;      // packed rows of the smallest tile
+
+sc_status check_attn(const sc_attn_desc* d) {
+  if (!d) return SC_ERR_NULL;
+  if (d->dtype != SC_F32 && d->dtype != SC_F16 && d->dtype != SC_BF16) return SC_ERR_UNSUPPORTED;
+  if (d->causal != 0 && d->causal != 1) return SC_ERR_UNSUPPORTED;
+  if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > 512 || d->heads > (1 << 20)) return SC_ERR_BAD_SHAPE;
+  if (d->d < 1 || d->window < 0 || !std::isfinite(d->scale) || !(d->scale > 0.0f)) return SC_ERR_BAD_SHAPE;
+  if (d->d > 128) return SC_ERR_UNSUPPORTED;
+  return SC_OK;
+}
+
+// (bytes of the starts twice, of the items of rows and of keys)
+struct AttnLayout { size_t starts, row_items, key_items; };
+static AttnLayout attn_layout(const sc_attn_desc* d, int64_t seqs, int64_t rows) {
+  const int64_t group = d->heads / d->kv_heads;
+  AttnLayout l;
+  l.starts = attn_up((size_t)(seqs + 1) * 4);
+  l.row_items = attn_up((size_t)(rows * group / kAttnRowsLeast + seqs) * sizeof(AttnItem));
+  l.key_items = attn_up((size_t)(rows / (32 * kAttnKeyWaves) + seqs) * sizeof(AttnItem));
+  return l;
+}
+
+// Tiles of `per` packed rows of every sequence, longest first.
+static void attn_items(const std::vector<int32_t>& starts, const sc_attn_desc& d, int64_t per, bool keys, std::vector<AttnItem>& items) {
+  const int64_t group = keys ? 1 : d.heads / d.kv_heads;
+  items.clear();
+  std::vector<int64_t> work;
+  for (size_t s = 0; s + 1 < starts.size(); ++s) {
+    const int64_t n = starts[s + 1] - starts[s], tiles = attn_ceil(n * group, per);
+    for (int64_t t = 0; t < tiles; ++t) {
+      const int64_t lo = t * per / group, hi = std::min((t * per + per - 1) / group, n - 1);      // rows (or keys) of the tile
+      int64_t first = 0, last = n - 1;                                                           // and what they see (or are seen by)
+      if (d.window) {
+        first = std::max<int64_t>(0, lo - d.window + 1);
+        last = std::min<int64_t>(last, hi + d.window - 1);
+      }
+      if (d.causal) (keys ? first : last) = keys ? lo : hi;
+      work.push_back(last - first + 1);
+      items.push_back({starts[s], (int32_t)n, (int32_t)t, 0});
+    }
+  }
+  std::vector<int32_t> order(items.size());
+  for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return work[a] > work[b]; });
+  std::vector<AttnItem> sorted(items.size());
+  for (size_t i = 0; i < order.size(); ++i) sorted[i] = items[order[i]];
+  items.swap(sorted);
+}
+
+static sc_status attn_plan(sc_attn* plan, int64_t seqs, const int64_t* starts, const sc_rows* set, unsigned char* w, hipStream_t s) {
+  const AttnLayout l = attn_layout(&plan->desc, seqs, plan->end);
+  std::vector<int32_t> at(seqs + 1);
+  for (int64_t i = 0; i <= seqs; ++i) at[i] = (int32_t)starts[i];
+  hipError_t e = hipSuccess;
+  if (set && set->kept != set->rows && plan->end > 0) {
+    int32_t *in = reinterpret_cast<int32_t*>(w), *out = reinterpret_cast<int32_t*>(w + l.starts);
+    e = hipMemcpyAsync(in, at.data(), at.size() * 4, hipMemcpyHostToDevice, s);
+    if (e == hipSuccess) {
+      attn_starts_kernel<<<dim3((unsigned)(at.size() + 255) / 256), dim3(256), 0, s>>>(in, (int)at.size(), set->row_idx, (int32_t)set->kept, out);
+      e = hipGetLastError();
+    }
+    std::vector<int32_t> kept(at.size());
+    if (e == hipSuccess) e = hipMemcpyAsync(kept.data(), out, kept.size() * 4, hipMemcpyDeviceToHost, s);
+    const hipError_t waited = hipStreamSynchronize(s);      // (also after an error: the copies read and write these vectors)
+    if (e == hipSuccess) e = waited;
+    at.swap(kept);
+  }
+  if (e != hipSuccess) { note_hip_error((int32_t)e); return SC_ERR_HIP; }
+  plan->kept = at.back();
+  std::vector<AttnItem> row_items, key_items;
+  attn_items(at, plan->desc, 32 * plan->waves, false, row_items);
+  attn_items(at, plan->desc, 32 * kAttnKeyWaves, true, key_items);
+  plan->n_row_items = (int32_t)row_items.size();
+  plan->n_key_items = (int32_t)key_items.size();
+  unsigned char* to = w + 2 * l.starts;
+  plan->row_items = reinterpret_cast<const AttnItem*>(to);
+  plan->key_items = reinterpret_cast<const AttnItem*>(to + l.row_items);
+  if (!row_items.empty()) {
+    e = hipMemcpyAsync(to, row_items.data(), row_items.size() * sizeof(AttnItem), hipMemcpyHostToDevice, s);
+    if (e == hipSuccess) e = hipMemcpyAsync(to + l.row_items, key_items.data(), key_items.size() * sizeof(AttnItem), hipMemcpyHostToDevice, s);
+    const hipError_t waited = hipStreamSynchronize(s);
+    if (e == hipSuccess) e = waited;
+  }
+  if (e != hipSuccess) { note_hip_error((int32_t)e); return SC_ERR_HIP; }
+  return SC_OK;
+}
+
+// what runs and backward passes check alike
+static sc_status attn_check_call(const sc_attn* plan, const sc_rows* rows, int32_t row_format) {
+  if (!plan) return SC_ERR_NULL;
+  if (row_format != SC_ROWS_DENSE && row_format != SC_ROWS_COMPACT) return SC_ERR_UNSUPPORTED;
+  if ((rows != nullptr) != (plan->version != 0)) return SC_ERR_BAD_SHAPE;
+  if (rows && rows->version != plan->version) return SC_ERR_MASK_COUNT;
+  return SC_OK;
+}
+
+struct AttnMatrix { const void* at; int64_t stride; int32_t heads; };      // [rows][heads][d]
+
+static sc_status attn_check_matrices(const sc_attn* plan, std::initializer_list<AttnMatrix> ms, bool* vec) {
+  const int eb = plan->desc.dtype == SC_F32 ? 4 : 2;
+  *vec = plan->desc.d * eb % 16 == 0;
+  for (const AttnMatrix& m : ms) {
+    if (plan->kept > 0 && !m.at) return SC_ERR_NULL;
+    if (m.stride < (int64_t)m.heads * plan->desc.d || m.stride > ((int64_t)1 << 40)) return SC_ERR_BAD_SHAPE;
+    if ((uintptr_t)m.at % eb) return SC_ERR_ALIGN;
+    if ((uintptr_t)m.at % 16 || m.stride * eb % 16) *vec = false;
+  }
+  return SC_OK;
+}
+
+static AttnParams attn_params(const sc_attn* plan, const sc_rows* rows, int32_t row_format) {
+  const sc_attn_desc& d = plan->desc;
+  AttnParams p = {};
+  p.map = row_format == SC_ROWS_DENSE && rows && rows->kept != rows->rows ? rows->row_idx : nullptr;
+  p.heads = d.heads;
+  p.kv_heads = d.kv_heads;
+  p.group = d.heads / d.kv_heads;
+  p.d = d.d;
+  p.causal = d.causal;
+  p.window = d.window;
+  p.magic = ((1u << 20) + p.group - 1) / p.group;
+  p.scale = d.scale;
+  return p;
+}
+
+}  // namespace sc
+
+extern "C" {
+
+sc_status sparse_attn_workspace_bytes(const sc_attn_desc* desc, int64_t seqs, int64_t rows, size_t* bytes) {
+  if (!bytes) return SC_ERR_NULL;
+  *bytes = 0;
+  const sc_status st = sc::check_attn(desc);
+  if (st != SC_OK) return st;
+  // packed rows and workgroups are counted in 32 bits, of which tiles need a few
+  if (seqs < 0 || rows < 0 || seqs > (1 << 24) || rows > 0x7fffffff || rows * desc->heads > ((int64_t)1 << 36) ||
+      rows * (desc->heads / desc->kv_heads) > (1 << 30) || (rows * (desc->heads / desc->kv_heads) / sc::kAttnRowsLeast + seqs) * desc->kv_heads > (1 << 23))
+    return SC_ERR_BAD_SHAPE;
+  const sc::AttnLayout l = sc::attn_layout(desc, seqs, rows);
+  *bytes = 2 * l.starts + l.row_items + l.key_items;
+  return SC_OK;
+}
+
+sc_status sparse_attn_plan(const sc_attn_desc* desc, int64_t seqs, const int64_t* starts, const sc_rows* rows, void* workspace_dev,
+                           size_t workspace_bytes, void* hip_stream, sc_attn** out) {
+  if (!out) return SC_ERR_NULL;
+  *out = nullptr;
+  sc_status st = sc::check_attn(desc);
+  if (st != SC_OK) return st;
+  if (!starts || !workspace_dev) return SC_ERR_NULL;
+  if (seqs < 0 || seqs > (1 << 24) || starts[0] != 0) return SC_ERR_BAD_SHAPE;
+  for (int64_t i = 0; i < seqs; ++i)
+    if (starts[i + 1] < starts[i]) return SC_ERR_BAD_SHAPE;
+  if (rows && starts[seqs] > rows->rows) return SC_ERR_BAD_SHAPE;
+  size_t need = 0;
+  st = sparse_attn_workspace_bytes(desc, seqs, starts[seqs], &need);
+  if (st != SC_OK) return st;
+  if (workspace_bytes < need) return SC_ERR_WORKSPACE;
+  if ((uintptr_t)workspace_dev & 15) return SC_ERR_ALIGN;
+  sc_attn* plan = nullptr;
+  try {      // the lists on the host
+    plan = new sc_attn;
+    plan->desc = *desc;
+    plan->end = starts[seqs];
+    plan->version = rows ? rows->version : 0;
+    plan->waves = 4;
+    st = sc::attn_plan(plan, seqs, starts, rows, static_cast<unsigned char*>(workspace_dev), static_cast<hipStream_t>(hip_stream));
+  } catch (const std::bad_alloc&) {
+    sc::note_hip_error((int32_t)hipErrorOutOfMemory);
+    st = SC_ERR_HIP;
+  }
+  if (st != SC_OK) {
+    delete plan;
+    return st;
+  }
+  *out = plan;
+  return SC_OK;
+}
+
+sc_status sparse_attn_info(const sc_attn* plan, int64_t* end, int64_t* kept) {
+  if (!plan) return SC_ERR_NULL;
+  if (end) *end = plan->end;
+  if (kept) *kept = plan->kept;
+  return SC_OK;
+}
+
+void sparse_attn_destroy(sc_attn* plan) { delete plan; }
+
+sc_status sparse_attn_run(const sc_attn* plan, const sc_rows* rows, int32_t row_format, const void* q_dev, int64_t q_stride,
+                          const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride, void* o_dev, float* lse_dev,
+                          void* hip_stream) {
+  sc_status st = sc::attn_check_call(plan, rows, row_format);
+  if (st != SC_OK) return st;
+  const sc_attn_desc& d = plan->desc;
+  bool vec;
+  st = sc::attn_check_matrices(plan, {{q_dev, q_stride, d.heads}, {k_dev, k_stride, d.kv_heads}, {v_dev, v_stride, d.kv_heads}}, &vec);
+  if (st != SC_OK) return st;
+  if (plan->end > 0 && !o_dev && (plan->kept > 0 || row_format == SC_ROWS_DENSE)) return SC_ERR_NULL;
+  if (((uintptr_t)o_dev | (uintptr_t)lse_dev) & 15) return SC_ERR_ALIGN;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  sc::AttnParams p = sc::attn_params(plan, rows, row_format);
+  p.q = q_dev;
+  p.k = k_dev;
+  p.v = v_dev;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.out = o_dev;
+  p.lse = lse_dev;
+  p.items = plan->row_items;
+  p.n_items = plan->n_row_items;
+  hipError_t e = hipSuccess;
+  if (p.n_items > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnForward, p, plan->waves, vec, s);
+  if (e == hipSuccess && row_format == SC_ROWS_DENSE) {
+    const int64_t width = (int64_t)d.heads * d.d * (d.dtype == SC_F32 ? 4 : 2);
+    e = sc::attn_zero_dropped(rows, plan->end, {{o_dev, nullptr, nullptr}, {width, 0, 0}, {width, 0, 0}}, s);
+  }
+  if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
+  return SC_OK;
+}
+
+sc_status sparse_attn_backward_workspace_bytes(const sc_attn* plan, size_t* bytes) {
+  if (!bytes) return SC_ERR_NULL;
+  *bytes = 0;
+  if (!plan) return SC_ERR_NULL;
+  *bytes = 256 + sc::attn_up((size_t)plan->kept * plan->desc.heads * 4);
+  return SC_OK;
+}
+
+sc_status sparse_attn_backward(const sc_attn* plan, const sc_rows* rows, int32_t row_format, const void* q_dev, int64_t q_stride,
+                               const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride, const void* o_dev,
+                               const float* lse_dev, const void* do_dev, void* dq_dev, int64_t dq_stride, void* dk_dev,
+                               int64_t dk_stride, void* dv_dev, int64_t dv_stride, void* workspace_dev, size_t workspace_bytes,
+                               void* hip_stream) {
+  sc_status st = sc::attn_check_call(plan, rows, row_format);
+  if (st != SC_OK) return st;
+  const sc_attn_desc& d = plan->desc;
+  bool vec;
+  st = sc::attn_check_matrices(plan, {{q_dev, q_stride, d.heads}, {k_dev, k_stride, d.kv_heads}, {v_dev, v_stride, d.kv_heads},
+                                      {dq_dev, dq_stride, d.heads}, {dk_dev, dk_stride, d.kv_heads}, {dv_dev, dv_stride, d.kv_heads}}, &vec);
+  if (st != SC_OK) return st;
+  if (plan->end > 0 && row_format == SC_ROWS_DENSE && (!dq_dev || !dk_dev || !dv_dev)) return SC_ERR_NULL;
+  if (plan->kept > 0 && (!o_dev || !lse_dev || !do_dev)) return SC_ERR_NULL;
+  if (!workspace_dev) return SC_ERR_NULL;
+  size_t need = 0;
+  sparse_attn_backward_workspace_bytes(plan, &need);
+  if (workspace_bytes < need) return SC_ERR_WORKSPACE;
+  if (((uintptr_t)o_dev | (uintptr_t)lse_dev | (uintptr_t)do_dev | (uintptr_t)workspace_dev) & 15) return SC_ERR_ALIGN;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  sc::AttnParams p = sc::attn_params(plan, rows, row_format);
+  p.q = q_dev;
+  p.k = k_dev;
+  p.v = v_dev;
+  p.o = o_dev;
+  p.d_o = do_dev;
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.dq = dq_dev;
+  p.dk = dk_dev;
+  p.dv = dv_dev;
+  p.dq_stride = dq_stride;
+  p.dk_stride = dk_stride;
+  p.dv_stride = dv_stride;
+  p.lse = const_cast<float*>(lse_dev);
+  p.delta = static_cast<float*>(workspace_dev);
+  hipError_t e = hipSuccess;
+  if (plan->n_row_items > 0) {
+    p.items = plan->row_items;
+    p.n_items = plan->n_row_items;
+    e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->waves, vec, s);      // (leaves delta for the keys)
+    p.items = plan->key_items;
+    p.n_items = plan->n_key_items;
+    if (e == hipSuccess) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardKV, p, plan->waves, vec, s);
+  }
+  if (e == hipSuccess && row_format == SC_ROWS_DENSE) {
+    const int64_t eb = d.dtype == SC_F32 ? 4 : 2, q = d.heads * eb * d.d, kv = d.kv_heads * eb * d.d;
+    e = sc::attn_zero_dropped(rows, plan->end, {{dq_dev, dk_dev, dv_dev}, {dq_stride * eb, dk_stride * eb, dv_stride * eb}, {q, kv, kv}}, s);
+  }
+  if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
+  return SC_OK;
+}
+
+}  // extern "C"

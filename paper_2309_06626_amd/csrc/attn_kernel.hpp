@@ -1,0 +1,371 @@
+// Attention over packed sequences of kept rows: forward pass and gradients.
+//
+//   s_ij = scale q_i . k_j of the keys that row i sees,  p = exp(s - lse_i),  o_i = sum_j p_ij v_j
+//   D_i = do_i . o_i,  ds = p (do_i . v_j - D_i),  dq_i = scale sum_j ds k_j,  dk_j = scale sum_i ds q_i,  dv_j = sum_i p do_i
+//
+// Query heads that share a key-value head are rows of one matrix: packed row r of a sequence is head r % group of its row r / group.
+#pragma once
+#include "attn_params.hpp"
+#include "attn_tile.hpp"
+
+#include <math.h>
+
+namespace sc {
+
+constexpr float kAttnLog2e = 1.4426950408889634f;
+// a row's lse, and what is taken off in the exponent of 2: in 64 bits, because the error of either is one of all the row's probabilities
+__device__ __forceinline__ float attn_lse(float m, float sum) { return (float)((double)m * 0.6931471805599453 + (double)__builtin_logf(sum)); }
+__device__ __forceinline__ float attn_lse2(float lse) { return (float)((double)lse * 1.4426950408889634); }
+
+// Consecutive workgroups go round the eight dies.  Where the key-value heads are a multiple of eight, each die takes heads of its own, whose
+// keys and values stay in its L2; otherwise heads are neighbours.  Items come with the longest first.
+struct AttnWork { AttnItem item; int head; };
+__device__ __forceinline__ AttnWork attn_work(const AttnParams& p) {
+  int item, head;
+  const int b = blockIdx.x;
+  if (p.kv_heads % 8 == 0) {
+    const int i = b >> 3;
+    head = (b & 7) + 8 * (i / p.n_items);
+    item = i % p.n_items;
+  } else {
+    head = b % p.kv_heads;
+    item = b / p.kv_heads;
+  }
+  return {p.items[item], head};
+}
+
+// Keys that row i of a sequence of n rows sees: lo .. hi.
+struct AttnSpan { int lo, hi; };
+__device__ __forceinline__ AttnSpan attn_keys(const AttnParams& p, int i, int n) {
+  AttnSpan s = {0, n - 1};
+  if (p.window) {
+    s.lo = i >= p.window ? i - p.window + 1 : 0;
+    if (p.window <= n - 1 - i) s.hi = i + p.window - 1;
+  }
+  if (p.causal) s.hi = i;
+  return s;
+}
+// Rows that see key j.
+__device__ __forceinline__ AttnSpan attn_rows(const AttnParams& p, int j, int n) {
+  AttnSpan s = {0, n - 1};
+  if (p.window) {
+    if (p.window <= n - 1 - j) s.hi = j + p.window - 1;
+    s.lo = j >= p.window ? j - p.window + 1 : 0;
+  }
+  if (p.causal) s.lo = j;
+  return s;
+}
+
+// ---- forward, and the gradient of the queries --------------------------------------------------------------------------------------
+// A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.
+template <int DT, int DP, int NW, bool VEC, bool BACKWARD>
+__global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
+  using A = AttnTile<DT, DP>;
+  using T = typename A::T;
+  constexpr int NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32, STAGES = 2;
+  constexpr int TILE = TK * A::RB, STAGE = 2 * TILE;
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
+
+  const AttnWork w = attn_work(p);
+  const int n = w.item.rows, first = w.item.first, packed = n * p.group;
+  const int r0 = w.item.tile * 32 * NW, r_wave = r0 + wave * 32, r = r_wave + l32;
+  const bool there = r < packed;
+  const int i = there ? r / p.group : 0, head = w.head * p.group + (there ? r - i * p.group : 0);
+  const int64_t row = p.map ? p.map[first + i] : first + i;
+  const AttnSpan mine = attn_keys(p, i, n);
+  // of the whole wavefront and workgroup: rows are in ascending order, and so are both ends of what they see
+  const bool any = r_wave < packed;
+  const AttnSpan from = attn_keys(p, any ? r_wave / p.group : 0, n), to = attn_keys(p, any ? (min(r_wave + 32, packed) - 1) / p.group : 0, n);
+  const int k_begin = attn_keys(p, r0 / p.group, n).lo / TK * TK;
+  const int k_end = attn_keys(p, (min(r0 + 32 * NW, packed) - 1) / p.group, n).hi + 1;
+  const int tiles = (k_end - k_begin + TK - 1) / TK;
+  // visible: key - lo <= span as unsigned; rows that do not exist see nothing
+  const int lo = there ? mine.lo : 0x40000000;
+  const unsigned span = there ? mine.hi - mine.lo : 0;
+
+  const T* const k_base = static_cast<const T*>(p.k) + (int64_t)w.head * p.d;
+  const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
+  const unsigned lds = attn_lds(smem);
+  auto request = [&](int tile) {
+    const int k0 = k_begin + tile * TK;
+    const unsigned at = lds + (tile % STAGES) * STAGE;
+    auto place = [&](const T* base, int64_t stride) {
+      return [=, &p](int r) -> const T* {
+        const int j = k0 + r;
+        if (j >= n) return nullptr;
+        return base + (p.map ? p.map[first + j] : first + j) * stride;
+      };
+    };
+    A::template request<TK, NT, VEC>(at, p.d, place(k_base, p.k_stride));
+    A::template request<TK, NT, VEC>(at + TILE, p.d, place(v_base, p.v_stride));
+  };
+
+  request(0);
+  v4i qf[A::KS], gf[BACKWARD ? A::KS : 1];
+  A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
+  const float c = p.scale * kAttnLog2e;
+  float lse2 = 0.0f, delta = 0.0f;
+  if constexpr (BACKWARD) {
+    const int64_t at = (row * p.heads + head) * p.d;
+    A::template read_row<VEC>(static_cast<const T*>(p.d_o) + at, p.d, h, there, gf);
+    v4i of[A::KS];
+    A::template read_row<VEC>(static_cast<const T*>(p.o) + at, p.d, h, there, of);
+#pragma unroll
+    for (int ks = 0; ks < A::KS; ++ks) {
+      T a[A::V], b[A::V];
+      __builtin_memcpy(a, &gf[ks], 16);
+      __builtin_memcpy(b, &of[ks], 16);
+#pragma unroll
+      for (int e = 0; e < A::V; ++e) delta += (float)a[e] * (float)b[e];
+    }
+    delta = attn_add_halves(delta);
+    const int64_t stat = (int64_t)(first + i) * p.heads + head;
+    if (there && h == 0) p.delta[stat] = delta;
+    lse2 = there ? attn_lse2(p.lse[stat]) : 0.0f;
+  }
+
+  const typename A::Along along = A::along(lane);
+  const typename A::Across across = A::across(lane);
+  floatx16 acc[A::DB];
+#pragma unroll
+  for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
+  float m = -INFINITY, sum = 0.0f;                     // m is a maximum times c, as it was rounded
+
+  for (int tile = 0; tile < tiles; ++tile) {
+    attn_meet<0>();                                   // this tile is here, and everybody is done with the one before
+    if (tile + 1 < tiles) request(tile + 1);
+    const int k0 = k_begin + tile * TK;
+    if (!any || k0 > to.hi || k0 + TK <= from.lo) continue;
+    const bool whole = k0 >= to.lo && k0 + TK - 1 <= from.hi && r_wave + 32 <= packed;
+    const unsigned at_k = lds + (tile % STAGES) * STAGE, at_v = at_k + TILE;
+    floatx16 s[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[b][v] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s[b], A::read_along(along, at_k, b, ks), qf[ks]);
+    }
+    auto visible = [&](int b, int v) { return (unsigned)(k0 + 4 * h - lo + (32 * b + 8 * (v >> 2) + (v & 3))) <= span; };
+    v4i pf[KB][A::SS];
+    if constexpr (!BACKWARD) {
+      if (!whole) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) s[b][v] = visible(b, v) ? s[b][v] : -INFINITY;
+      }
+      float most = s[0][0];
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) most = fmaxf(most, s[b][v]);
+      most = fmaxf(attn_max_halves(most) * c, m);
+      const float shift = most == -INFINITY ? 0.0f : most;      // (nothing seen so far: every term is 0)
+      if (attn_any(most > m)) {
+        const float less = attn_exp2(m - shift);
+        sum *= less;
+#pragma unroll
+        for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[db][v] *= less;
+        m = most;
+      }
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          s[b][v] = attn_exp2(__builtin_fmaf(s[b][v], c, -shift));
+          sum += s[b][v];
+        }
+        A::pack(s[b], pf[b]);
+      }
+    } else {
+      floatx16 g[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) g[b][v] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g[b], A::read_along(along, at_v, b, ks), gf[ks]);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const float e = attn_exp2(__builtin_fmaf(s[b][v], c, -lse2));
+          s[b][v] = (whole || visible(b, v) ? e : 0.0f) * (g[b][v] - delta);
+        }
+        A::pack(s[b], pf[b]);
+      }
+    }
+    // forward: values times probabilities; backward: keys times the gradients of the scores
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int ss = 0; ss < A::SS; ++ss)
+#pragma unroll
+        for (int db = 0; db < A::DB; ++db)
+          A::E::mma(acc[db], A::read_across(across, BACKWARD ? at_k : at_v, b, ss, db), pf[b][ss]);
+  }
+  if constexpr (!BACKWARD) {
+    sum = attn_add_halves(sum);
+    if (!there) return;
+    const float per = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;      // (NaN stays)
+    if (p.lse && h == 0) p.lse[(int64_t)(first + i) * p.heads + head] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
+    T* const out = static_cast<T*>(p.out) + (row * p.heads + head) * p.d;
+#pragma unroll
+    for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], per);
+  } else {
+    if (!there) return;
+    T* const out = static_cast<T*>(p.dq) + row * p.dq_stride + (int64_t)head * p.d;
+#pragma unroll
+    for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
+  }
+}
+
+// ---- gradients of keys and values ------------------------------------------------------------------------------------------------------
+// A wavefront has 32 keys, one a lane and half; packed rows of queries and of the result's gradient pass by in tiles.
+template <int DT, int DP, bool VEC>
+__global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys_kernel(const AttnParams p) {
+  using A = AttnTile<DT, DP>;
+  using T = typename A::T;
+  constexpr int NW = kAttnKeyWaves, NT = 64 * NW, TQ = 32, STAGES = 2;
+  constexpr int TILE = TQ * A::RB, STATS = 2 * TQ * 4, STAGE = 2 * TILE + STATS;
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
+
+  const AttnWork w = attn_work(p);
+  const int n = w.item.rows, first = w.item.first;
+  const int j0 = w.item.tile * 32 * NW, j_wave = j0 + wave * 32, j = j_wave + l32;
+  const bool there = j < n, any = j_wave < n;
+  const int64_t row = there ? (p.map ? p.map[first + j] : first + j) : 0;
+  const AttnSpan mine = attn_rows(p, there ? j : 0, n);
+  const AttnSpan from = attn_rows(p, any ? j_wave : 0, n), to = attn_rows(p, any ? min(j_wave + 32, n) - 1 : 0, n);
+  // packed rows
+  const int group = p.group;
+  const int r_begin = attn_rows(p, j0, n).lo * group / TQ * TQ, r_end = (attn_rows(p, min(j0 + 32 * NW, n) - 1, n).hi + 1) * group;
+  const int tiles = (r_end - r_begin + TQ - 1) / TQ;
+  const int lo = there ? mine.lo * group : 0x40000000;
+  const unsigned span = there ? (mine.hi - mine.lo + 1) * group - 1 : 0;
+  const int wave_lo = from.lo * group, wave_hi = (to.hi + 1) * group - 1;          // rows that see any key of the wavefront
+  const int all_lo = to.lo * group, all_hi = (from.hi + 1) * group - 1;            // rows that see all of them
+
+  const T* const q_base = static_cast<const T*>(p.q) + (int64_t)w.head * group * p.d;
+  const T* const g_base = static_cast<const T*>(p.d_o) + (int64_t)w.head * group * p.d;
+  const unsigned lds = attn_lds(smem);
+  const float c = p.scale * kAttnLog2e;
+  float stat = 0.0f;      // one of lse (lanes 0 .. 31) and delta (32 .. 63) of the next tile's rows
+  auto request = [&](int tile) {
+    const int r0 = r_begin + tile * TQ, i0 = r0 / group, rem = r0 - i0 * group;
+    const unsigned at = lds + (tile % STAGES) * STAGE;
+    auto place = [&](const T* base, int64_t stride) {
+      return [=, &p](int r) -> const T* {
+        const int past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
+        if (i >= n) return nullptr;
+        return base + (p.map ? p.map[first + i] : first + i) * stride + (rem + r - past * group) * p.d;
+      };
+    };
+    A::template request<TQ, NT, VEC>(at, p.d, place(q_base, p.q_stride));
+    A::template request<TQ, NT, VEC>(at + TILE, p.d, place(g_base, (int64_t)p.heads * p.d));
+    if (t < 64) {
+      const int past = (int)((unsigned)(rem + l32) * p.magic >> 20), i = i0 + past;
+      const int64_t of = (int64_t)(first + i) * p.heads + w.head * group + (rem + l32 - past * group);
+      stat = i < n ? (h ? p.delta[of] : attn_lse2(p.lse[of])) : 0.0f;
+      *(__attribute__((address_space(3))) float*)(uint64_t)(at + 2 * TILE + t * 4) = stat;
+    }
+  };
+  request(0);
+
+  v4i kf[A::KS], vf[A::KS];
+  A::template read_row<VEC>(static_cast<const T*>(p.k) + row * p.k_stride + (int64_t)w.head * p.d, p.d, h, there, kf);
+  A::template read_row<VEC>(static_cast<const T*>(p.v) + row * p.v_stride + (int64_t)w.head * p.d, p.d, h, there, vf);
+  const typename A::Along along = A::along(lane);
+  const typename A::Across across = A::across(lane);
+  floatx16 dk[A::DB], dv[A::DB];
+#pragma unroll
+  for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.0f;
+
+  typedef __attribute__((address_space(3))) const v4f lds_v4f;
+  for (int tile = 0; tile < tiles; ++tile) {
+    attn_meet<0>();
+    if (tile + 1 < tiles) request(tile + 1);
+    const int r0 = r_begin + tile * TQ;
+    if (!any || r0 > wave_hi || r0 + TQ <= wave_lo) continue;
+    const bool whole = r0 >= all_lo && r0 + TQ - 1 <= all_hi && j_wave + 32 <= n;
+    const unsigned at_q = lds + (tile % STAGES) * STAGE, at_g = at_q + TILE, at_s = at_g + TILE;
+    floatx16 s, g;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = g[v] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, at_q, 0, ks), kf[ks]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, at_g, 0, ks), vf[ks]);
+    v4i pf[A::SS], df[A::SS];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const v4f lse2 = *(lds_v4f*)(uint64_t)(at_s + (8 * a + 4 * h) * 4), delta = *(lds_v4f*)(uint64_t)(at_s + (TQ + 8 * a + 4 * h) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = 4 * a + e;
+        const bool seen = whole || (unsigned)(r0 + 4 * h - lo + (8 * a + e)) <= span;
+        const float pr = seen ? attn_exp2(__builtin_fmaf(s[v], c, -lse2[e])) : 0.0f;
+        s[v] = pr;
+        g[v] = pr * (g[v] - delta[e]);
+      }
+    }
+    A::pack(s, pf);
+    A::pack(g, df);
+#pragma unroll
+    for (int ss = 0; ss < A::SS; ++ss) {
+      __builtin_amdgcn_sched_barrier(0);      // (operands are read a product's worth ahead, not all at once into registers that are not there)
+#pragma unroll
+      for (int db = 0; db < A::DB; ++db) {
+        A::E::mma(dv[db], A::read_across(across, at_g, 0, ss, db), pf[ss]);
+        A::E::mma(dk[db], A::read_across(across, at_q, 0, ss, db), df[ss]);
+      }
+    }
+  }
+  if (!there) return;
+  T* const out_k = static_cast<T*>(p.dk) + row * p.dk_stride + (int64_t)w.head * p.d;
+  T* const out_v = static_cast<T*>(p.dv) + row * p.dv_stride + (int64_t)w.head * p.d;
+#pragma unroll
+  for (int db = 0; db < A::DB; ++db) {
+    A::template write_16<VEC>(out_k, 32 * db + 16 * h, p.d, dk[db], p.scale);
+    A::template write_16<VEC>(out_v, 32 * db + 16 * h, p.d, dv[db], 1.0f);
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------------------------
+template <class Kernel> static hipError_t attn_start(Kernel kernel, int threads, int lds, const AttnParams& p, hipStream_t s) {
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((unsigned)((int64_t)p.n_items * p.kv_heads)), dim3(threads), lds, s>>>(p);
+  return hipGetLastError();
+}
+
+template <int DT, int DP, int NW, bool VEC> static hipError_t attn_start_rows(int what, const AttnParams& p, hipStream_t s) {
+  constexpr int lds = 2 * 2 * (DT == kF32 ? 32 : 64) * AttnTile<DT, DP>::RB;
+  return what == kAttnForward ? attn_start(attn_rows_kernel<DT, DP, NW, VEC, false>, 64 * NW, lds, p, s)
+                              : attn_start(attn_rows_kernel<DT, DP, NW, VEC, true>, 64 * NW, lds, p, s);
+}
+
+template <int DT, int DP, bool VEC> static hipError_t attn_start_width(int what, const AttnParams& p, int waves, hipStream_t s) {
+  if (what == kAttnBackwardKV) {
+    constexpr int lds = 2 * (2 * 32 * AttnTile<DT, DP>::RB + 2 * 32 * 4);
+    return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, lds, p, s);
+  }
+  return attn_start_rows<DT, DP, 4, VEC>(what, p, s);
+}
+
+template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, bool vec, hipStream_t s) {
+  if (p.d <= 64) return vec ? attn_start_width<DT, 64, true>(what, p, waves, s) : attn_start_width<DT, 64, false>(what, p, waves, s);
+  return vec ? attn_start_width<DT, 128, true>(what, p, waves, s) : attn_start_width<DT, 128, false>(what, p, waves, s);
+}
+
+}  // namespace sc

@@ -1,0 +1,195 @@
+// Tiles of rows in LDS and the operands of the matrix instructions that the attention kernels take from them.
+//
+// A tile is a number of rows of DP channels (a head's channels, padded with zeros), as they lie in memory.  Every tile is read in one or
+// both of two ways, as the first operand of a 32 x 32 product:
+//   along    rows of the tile are rows of the operand, the contraction goes over the channels  (S' = K Q', dP' = V dO')
+//   across   channels are rows of the operand, the contraction goes over the tile's rows       (O' = V' P', dQ' = K' dS')
+// The results of a product along leave a lane one column and the rows 8 a + 4 h + i of 32 (h: half of the wavefront).  Across, a
+// lane's entries of the contraction are taken in that same order, so that results of the first product, rounded, are the second operand of
+// the next one without leaving their lane.
+#pragma once
+#include "mma_common.hpp"
+
+#include <type_traits>
+
+namespace sc {
+
+static __device__ __align__(16) v4i attn_zeros = {0, 0, 0, 0};      // what is read beyond a tile's end
+
+// 16 (4) bytes a lane from memory into LDS at base + 16 (4) lane.  Written out, because the compiler would let every later LDS read wait
+// for all transfers in flight; their arrival is waited for in attn_meet.  The base goes through m0, which the compiler writes (it has to
+// know what m0 holds), a wait state before the transfer.
+__device__ __forceinline__ void attn_dma16(const void* src, unsigned lds_base) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds_base), "v"(src) : "memory");
+}
+__device__ __forceinline__ void attn_dma4(const void* src, unsigned lds_base) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(lds_base), "v"(src) : "memory");
+}
+
+// All of this wavefront's transfers but the youngest N have landed and its LDS accesses are done; then the same holds for all.
+template <int N> __device__ __forceinline__ void attn_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+__device__ __forceinline__ unsigned attn_lds(const void* p) {
+  return (unsigned)(unsigned long long)(__attribute__((address_space(3))) const unsigned char*)p;
+}
+
+__device__ __forceinline__ float attn_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ bool attn_any(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
+// a value and that of the lane in the other half of the wavefront, in the same order in both
+__device__ __forceinline__ void attn_halves(float v, float& low, float& high) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  low = __builtin_bit_cast(float, (unsigned)r[0]);
+  high = __builtin_bit_cast(float, (unsigned)r[1]);
+}
+__device__ __forceinline__ float attn_max_halves(float v) { float a, b; attn_halves(v, a, b); return fmaxf(a, b); }
+__device__ __forceinline__ float attn_add_halves(float v) { float a, b; attn_halves(v, a, b); return a + b; }
+
+// A 32 x 32 block of results leaves 16 registers a lane: with the rows of the first operand read in this order, they are 16 consecutive
+// ones, from 16 h on.
+__device__ __forceinline__ int attn_order(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
+
+template <int DT, int DP> struct AttnTile {
+  using E = Elem<DT>;
+  using T = typename E::T;
+  static constexpr int EB = (int)sizeof(T), V = 16 / EB;
+  static constexpr int RB = DP * EB;            // bytes of a row
+  static constexpr int GROUPS = RB / 16;        // 16-byte groups of a row
+  static constexpr int KS = RB / 32;            // products of a contraction over the channels
+  static constexpr int SS = EB;                 // products of a contraction over 32 rows
+  static constexpr int DB = DP / 32;            // blocks of 32 channels
+
+  // A row's group g lies at g XOR key(row).  Along, the lanes that are served together (0-3, 12-15, 20-23, 24-27 and their like) read 16
+  // rows, whose keys differ in all of the low bits; across, four rows are read together whose keys differ in bits 2 and 3 (64 bytes apart).
+  static __device__ __forceinline__ int key(int row) {
+    if constexpr (EB == 2) return GROUPS >= 16 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    else return (((row >> 2) & 1) << 3) | ((row & 3) << 1) | ((row >> 3) & 1);
+  }
+
+  // Lane addresses within a tile, worked out once; what depends on the block of 32 rows is an offset.
+  struct Along { unsigned at[KS]; };
+  struct Across { unsigned at[EB == 2 ? 2 * DB : 16]; };
+
+  static __device__ __forceinline__ Along along(int lane) {
+    Along a;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) a.at[ks] = (lane & 31) * RB + (((2 * ks + (lane >> 5)) ^ key(lane & 31)) << 4);
+    return a;
+  }
+  static __device__ __forceinline__ Across across(int lane) {
+    Across a;
+    const int h = lane >> 5;
+    if constexpr (EB == 2) {
+      // within 16 lanes the transposing read gives lane j element t of source lane 4 t + j / 4, entry j % 4: source lane s points at
+      // row s / 4 of four, channels of the four lanes from 4 (s % 4) on
+      const int l16 = lane & 15;
+#pragma unroll
+      for (int i = 0; i < 2 * DB; ++i) {
+        const int row = 8 * (i & 1) + 4 * h + (l16 >> 2), c = 32 * (i >> 1) + attn_order(16 * ((lane >> 4) & 1) + 4 * (l16 & 3));
+        a.at[i] = row * RB + (((c >> 3) ^ key(row)) << 4) + (c & 7) * 2;
+      }
+    } else {
+      // channel 32 db + order of row 8 ss + 4 h + e; db and ss count by their low bits, the rest is an offset
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int e = i & 3, ss = (i >> 2) & 1, c = 32 * (i >> 3) + attn_order(lane & 31), row = 8 * ss + 4 * h + e;
+        a.at[i] = (4 * h + e) * RB + (((c >> 2) ^ key(row)) << 4) + (c & 3) * 4;
+      }
+    }
+    return a;
+  }
+
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) const v4i lds_v4i;
+  typedef __attribute__((address_space(3))) const int lds_int;
+
+  // rows 32 b .. of the tile at `tile`, channels of product ks
+  static __device__ __forceinline__ v4i read_along(const Along& a, unsigned tile, int b, int ks) {
+    return *(lds_v4i*)(uint64_t)(a.at[ks] + (tile + b * 32 * RB));
+  }
+  // channels 32 db .. as rows; the rows 32 b + ... of the tile of product ss
+  static __device__ __forceinline__ v4i read_across(const Across& a, unsigned tile, int b, int ss, int db) {
+    if constexpr (EB == 2) {
+      const unsigned at = tile + (b * 32 + ss * 16) * RB;
+      struct { s16x4 lo, hi; } both = {
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uint64_t)(a.at[2 * db] + at)),
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uint64_t)(a.at[2 * db + 1] + at))};
+      return __builtin_bit_cast(v4i, both);
+    } else {
+      v4i f;
+      const unsigned at = tile + (b * 32 + ss * 8) * RB + 256 * (db >> 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = *(lds_int*)(uint64_t)(a.at[8 * (db & 1) + 4 * (ss & 1) + e] + at);
+      return f;
+    }
+  }
+
+  // results of a block, rounded, as second operand of the SS products across
+  static __device__ __forceinline__ void pack(const floatx16& p, v4i (&f)[SS]) {
+    T r[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) r[v] = E::from_float(p[v]);
+    __builtin_memcpy(f, r, sizeof(r));
+  }
+
+  // a lane's share of a row in memory (channel groups 2 ks + h), as second operand of the products along; zeros beyond d
+  template <bool VEC> static __device__ __forceinline__ void read_row(const T* row, int d, int h, bool there, v4i (&f)[KS]) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) f[ks] = group<VEC>(row, (2 * ks + h) * V, d, there);
+  }
+  template <bool VEC> static __device__ __forceinline__ v4i group(const T* row, int c, int d, bool there) {
+    v4i g = {0, 0, 0, 0};
+    if constexpr (VEC) {
+      if (there && c < d) g = *reinterpret_cast<const v4i*>(row + c);
+    } else {
+      T e[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = there && c + i < d ? row[c + i] : T(0);
+      __builtin_memcpy(&g, e, 16);
+    }
+    return g;
+  }
+
+  // 16 channels from c0 on of a row, from a lane's results
+  template <bool VEC> static __device__ __forceinline__ void write_16(T* row, int c0, int d, const floatx16& o, float factor) {
+    T r[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) r[v] = E::from_float(o[v] * factor);
+    if constexpr (VEC) {
+      v4i g[EB];
+      __builtin_memcpy(g, r, sizeof(r));
+#pragma unroll
+      for (int i = 0; i < EB; ++i)
+        if (c0 + i * V < d) *reinterpret_cast<v4i*>(row + c0 + i * V) = g[i];
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (c0 + v < d) row[c0 + v] = r[v];
+    }
+  }
+
+  // Transfer of ROWS rows by NT lanes: `place(r)` is the row's address in memory, null for a row of zeros.
+  template <int ROWS, int NT> static constexpr int transfers() { return ROWS * GROUPS / NT; }
+  template <int ROWS, int NT, bool VEC, class Place>
+  static __device__ __forceinline__ void request(unsigned tile, int d, Place&& place) {
+    constexpr int J = ROWS * GROUPS / NT;
+    static_assert(J >= 1 && ROWS * GROUPS % NT == 0, "whole transfers");
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int at = j * NT + t, r = at / GROUPS, g = (at % GROUPS) ^ key(r);
+      const T* row = place(r);
+      if constexpr (VEC) {
+        attn_dma16(row && g * V < d ? (const void*)(row + g * V) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 16);
+      } else {
+        *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<false>(row, g * V, d, row != nullptr);
+      }
+    }
+  }
+};
+
+}  // namespace sc

@@ -1,0 +1,326 @@
+// Attention of single tokens over a paged cache of keys and values.
+//
+//   o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  s_j = scale q . k_j,  m = max s_j, over the first `length` rows of the sequence
+//
+// A workgroup takes the query heads of one key-value head (up to 32 of them) and a stretch of the sequence, of which its wavefronts take every
+// fourth tile of 32 keys each, on their own: keys by heads are one 32 x 32 product, whose results, rounded, are an operand of the next.
+// Maximum, sum and result of the wavefronts are joined in LDS, those of the stretches by a second launch, both in a fixed order.
+#pragma once
+#include "attn_tile.hpp"
+#include "decode_params.hpp"
+
+#include <math.h>
+
+namespace sc {
+
+// 8-bit codes as entries of the type: whole numbers up to 127 are exact in all of them.
+template <typename T> __device__ __forceinline__ void decode_widen(v4i codes, T (&out)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) out[i] = (T)(float)(int8_t)(codes[i >> 2] >> (8 * (i & 3)));
+}
+
+template <int DT, int DP, bool BITS8>
+__global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const DecodeParams p) {
+  using A = AttnTile<DT, DP>;
+  using T = typename A::T;
+  constexpr int TILE = 32 * A::RB, STAGES = BITS8 || A::RB > 256 ? 1 : 2, SCALES = 2 * 32 * 4;
+  constexpr int LDS_WAVE = 2 * TILE * STAGES;
+  constexpr int J = TILE / 1024;                               // transfers of 16 bytes a lane and tile
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
+  unsigned b = blockIdx.x;
+  const int split = b % p.splits;
+  b /= p.splits;
+  const int head = b % p.kv_heads;                             // key-value head
+  b /= p.kv_heads;
+  const int block = b % p.blocks;                              // 32 query heads of it
+  const int64_t row = b / p.blocks;
+
+  // the keys of this stretch
+  const int64_t most = (int64_t)p.table_width << p.shift;
+  const int64_t length = p.lengths[row] < most ? p.lengths[row] : most;
+  const int64_t begin = p.window && length > p.window ? length - p.window : 0;
+  const int64_t first_tile = begin / 32, all_tiles = length > begin ? (length + 31) / 32 - first_tile : 0;
+  int64_t per = (all_tiles + p.splits - 1) / p.splits;
+  per = per < kDecodeWaves ? kDecodeWaves : per;
+  const int64_t lo_tile = first_tile + split * per;
+  const int tiles = (int)(split * per >= all_tiles ? 0 : all_tiles - split * per < per ? all_tiles - split * per : per);
+  const int mine = tiles > wave ? (tiles - wave + kDecodeWaves - 1) / kDecodeWaves : 0;      // tiles of this wavefront
+
+  // pages of the stretch, in LDS
+  int32_t* const s_pages = reinterpret_cast<int32_t*>(smem + kDecodeWaves * (LDS_WAVE + SCALES));
+  const int64_t first_page = (lo_tile * 32) >> p.shift;
+  if (tiles) {
+    const int64_t end = (lo_tile + tiles) * 32 < length ? (lo_tile + tiles) * 32 : length;
+    const int count = min((int)(((end - 1) >> p.shift) - first_page) + 1, kDecodePages);      // (as many as there are, by the choice of splits)
+    for (int i = t; i < count; i += 64 * kDecodeWaves) s_pages[i] = p.table[row * p.table_width + first_page + i];
+  }
+  const int group = p.heads / p.kv_heads, col = block * 32 + l32, q_head = head * group + col;
+  const bool there = col < group;
+  v4i qf[A::KS];
+  if (p.vec) A::template read_row<true>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
+  else A::template read_row<false>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
+  __syncthreads();
+
+  const unsigned lds = attn_lds(smem) + wave * (LDS_WAVE + SCALES), at_scales = lds + LDS_WAVE;
+  // row of the cache that holds key l32 of a tile, or -1: beyond the length or the window, or on a page that is not there
+  auto cache_row = [&](int i) -> int {
+    const int64_t key = (lo_tile + wave + (int64_t)i * kDecodeWaves) * 32 + l32;
+    if (key < begin || key >= length) return -1;
+    const int page = s_pages[(key >> p.shift) - first_page];
+    if ((unsigned)page >= (unsigned)p.pages) return -1;
+    return (((unsigned)page * p.kv_heads + head) << p.shift) + (int)(key & ((1 << p.shift) - 1));
+  };
+  const unsigned char *const k_pages = static_cast<const unsigned char*>(p.k_pages), *const v_pages = static_cast<const unsigned char*>(p.v_pages);
+  // entries as they are: straight into LDS
+  auto request = [&](int i, int at_row) {
+    const unsigned at = lds + (i % STAGES) * 2 * TILE;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int place = j * 64 + lane, r = place / A::GROUPS, g = (place % A::GROUPS) ^ A::key(r);
+      const int64_t of = __shfl(at_row, r);
+      const bool in = of >= 0 && g * 16 < p.row_bytes;
+      attn_dma16(in ? (const void*)(k_pages + of * p.row_bytes + g * 16) : (const void*)&attn_zeros, at + j * 1024);
+      attn_dma16(in ? (const void*)(v_pages + of * p.row_bytes + g * 16) : (const void*)&attn_zeros, at + TILE + j * 1024);
+    }
+  };
+  // codes: into registers, widened on the way to LDS
+  constexpr int CG = DP / 16, CJ = BITS8 ? 32 * CG / 64 : 1;   // 16-byte groups of a row, and transfers of a tile
+  struct Codes { v4i k[CJ], v[CJ]; float k_scale, v_scale; };
+  auto fetch = [&](int at_row) -> Codes {
+    Codes c;
+#pragma unroll
+    for (int j = 0; j < CJ; ++j) {
+      const int place = j * 64 + lane, r = place / CG, g = place % CG;
+      const int64_t of = __shfl(at_row, r);
+      c.k[j] = c.v[j] = v4i{0, 0, 0, 0};
+      if (of >= 0 && g * 16 < p.row_bytes) {
+        c.k[j] = *reinterpret_cast<const v4i*>(k_pages + of * p.row_bytes + g * 16);
+        c.v[j] = *reinterpret_cast<const v4i*>(v_pages + of * p.row_bytes + g * 16);
+      }
+    }
+    c.k_scale = at_row >= 0 ? p.k_scales[at_row] : 0.0f;
+    c.v_scale = at_row >= 0 ? p.v_scales[at_row] : 0.0f;
+    return c;
+  };
+  auto widen = [&](const Codes& c) {
+#pragma unroll
+    for (int j = 0; j < CJ; ++j) {
+      const int place = j * 64 + lane, r = place / CG, g = place % CG;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        T e[16];
+        decode_widen(k ? c.v[j] : c.k[j], e);
+        v4i w[A::EB];
+        __builtin_memcpy(w, e, sizeof(e));
+#pragma unroll
+        for (int i = 0; i < A::EB; ++i)
+          *(__attribute__((address_space(3))) v4i*)(uint64_t)(lds + k * TILE + r * A::RB + (((g * A::EB + i) ^ A::key(r)) << 4)) = w[i];
+      }
+    }
+    *(__attribute__((address_space(3))) float*)(uint64_t)(at_scales + lane * 4) = h ? c.v_scale : c.k_scale;
+  };
+
+  const typename A::Along along = A::along(lane);
+  const typename A::Across across = A::across(lane);
+  floatx16 acc[A::DB];
+#pragma unroll
+  for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
+  const float c = p.scale * 1.4426950408889634f;
+  float m = -INFINITY, sum = 0.0f;                             // m is a maximum times c, as it was rounded
+  float unit = 0.0f;                                           // of SC_F16 and codes: acc is in units of it, see below
+
+  typedef __attribute__((address_space(3))) const v4f lds_v4f;
+  int row_now = mine > 0 ? cache_row(0) : -1, row_next = -1;
+  Codes codes;
+  if constexpr (BITS8) {
+    if (mine > 0) codes = fetch(row_now);
+  } else {
+    if (STAGES > 1 && mine > 0) request(0, row_now);
+  }
+  for (int i = 0; i < mine; ++i) {
+    if (i + 1 < mine) row_next = cache_row(i + 1);
+    const uint64_t seen = __ballot(row_now >= 0);
+    if constexpr (BITS8) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      widen(codes);
+      if (i + 1 < mine) codes = fetch(row_next);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    } else {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the tile before last is in registers)
+      if (STAGES == 1) request(i, row_now);
+      if (STAGES > 1 && i + 1 < mine) {
+        request(i + 1, row_next);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * J <= 63 ? 2 * J : 63) : "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+    }
+    row_now = row_next;
+    const unsigned at_k = lds + (i % STAGES) * 2 * TILE, at_v = at_k + TILE;
+    floatx16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, at_k, 0, ks), qf[ks]);
+    if constexpr (BITS8) {
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const v4f k_scale = *(lds_v4f*)(uint64_t)(at_scales + (8 * a + 4 * h) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * a + e] *= k_scale[e];
+      }
+    }
+    const unsigned keys = (unsigned)seen;                      // (both halves hold the same 32)
+    if (keys != 0xffffffffu) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = keys >> (8 * (v >> 2) + 4 * h + (v & 3)) & 1 ? s[v] : -INFINITY;
+    }
+    float top = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) top = fmaxf(top, s[v]);
+    top = fmaxf(attn_max_halves(top) * c, m);
+    const float shift = top == -INFINITY ? 0.0f : top;         // (nothing seen so far: every term is 0)
+    float less = attn_any(top > m) ? attn_exp2(m - shift) : 1.0f;
+    m = top;
+    sum *= less;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      s[v] = attn_exp2(__builtin_fmaf(s[v], c, -shift));
+      sum += s[v];
+    }
+    if constexpr (BITS8) {
+      // weights of the codes: p times the value's scale.  In f16 they are taken in units of a power of two near the largest scale so far,
+      // so that they keep their digits whatever the values' size.
+      float per_unit = 1.0f;
+      if constexpr (DT == kF16) {
+        float big = *(__attribute__((address_space(3))) const float*)(uint64_t)(at_scales + (32 + l32) * 4);
+        big = __builtin_isfinite(big) ? big : 0.0f;
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) big = fmaxf(big, __shfl_xor(big, x));
+        const float least = __builtin_bit_cast(float, (unsigned)(__builtin_bit_cast(unsigned, big) & 0x7f800000u));
+        if (least > unit) {
+          less *= unit / least;      // (powers of two; 0 at first)
+          unit = least;
+        }
+        per_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
+      }
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const v4f v_scale = *(lds_v4f*)(uint64_t)(at_scales + (32 + 8 * a + 4 * h) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[4 * a + e] *= DT == kF16 ? v_scale[e] * per_unit : v_scale[e];
+      }
+    }
+    if (attn_any(less != 1.0f)) {
+#pragma unroll
+      for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[db][v] *= less;
+    }
+    v4i pf[A::SS];
+    A::pack(s, pf);
+#pragma unroll
+    for (int ss = 0; ss < A::SS; ++ss)
+#pragma unroll
+      for (int db = 0; db < A::DB; ++db) A::E::mma(acc[db], A::read_across(across, at_v, 0, ss, db), pf[ss]);
+  }
+  if constexpr (BITS8 && DT == kF16) {
+#pragma unroll
+    for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] *= unit;
+  }
+  sum = attn_add_halves(sum);
+
+  // the wavefronts' shares: [wave][column][DP] results, [wave][column] maxima and sums
+  __syncthreads();
+  const int cols = group - block * 32 < 32 ? group - block * 32 : 32;
+  float* const s_acc = reinterpret_cast<float*>(smem);
+  float* const s_max = s_acc + kDecodeWaves * 32 * DP;
+  float* const s_sum = s_max + kDecodeWaves * 32;
+  if (there) {
+#pragma unroll
+    for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v4f part;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[e] = acc[db][4 * q + e];
+        *reinterpret_cast<v4f*>(s_acc + (wave * 32 + l32) * DP + 32 * db + 16 * h + 4 * q) = part;
+      }
+    if (h == 0) {
+      s_max[wave * 32 + l32] = m;
+      s_sum[wave * 32 + l32] = sum;
+    }
+  }
+  __syncthreads();
+  for (int at = t; at < cols * DP; at += 64 * kDecodeWaves) {
+    const int q = at / DP, ch = at % DP;
+    float top = s_max[q];
+#pragma unroll
+    for (int w = 1; w < kDecodeWaves; ++w) top = fmaxf(top, s_max[w * 32 + q]);
+    float all = 0.0f, out = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kDecodeWaves; ++w) {
+      const float sw = s_sum[w * 32 + q];
+      if (sw == 0.0f) continue;
+      const float f = attn_exp2(s_max[w * 32 + q] - top);
+      all += sw * f;
+      out += s_acc[(w * 32 + q) * DP + ch] * f;
+    }
+    const int64_t head_row = row * p.heads + head * group + block * 32 + q;
+    if (p.splits == 1) {
+      if (ch < p.d) static_cast<T*>(p.o)[head_row * p.d + ch] = A::E::from_float(all == 0.0f ? 0.0f : out / all);
+    } else {
+      p.part_o[(head_row * p.splits + split) * DP + ch] = out;
+      if (ch == 0) {
+        p.part_m[(head_row * p.splits + split) * 2] = top;
+        p.part_m[(head_row * p.splits + split) * 2 + 1] = all;
+      }
+    }
+  }
+}
+
+// the stretches' shares of a head, in order
+template <int DT, int DP> __global__ __launch_bounds__(DP) void decode_join_kernel(const DecodeParams p) {
+  using T = typename Elem<DT>::T;
+  const int64_t head_row = blockIdx.x;
+  const int ch = threadIdx.x;
+  const float* const stat = p.part_m + head_row * p.splits * 2;
+  float top = -INFINITY;
+  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, stat[2 * s]);
+  float all = 0.0f, out = 0.0f;
+  for (int s = 0; s < p.splits; ++s) {
+    const float sum = stat[2 * s + 1];
+    if (sum == 0.0f) continue;
+    const float f = attn_exp2(stat[2 * s] - top);
+    all += sum * f;
+    out += p.part_o[(head_row * p.splits + s) * DP + ch] * f;
+  }
+  if (ch < p.d) static_cast<T*>(p.o)[head_row * p.d + ch] = Elem<DT>::from_float(all == 0.0f ? 0.0f : out / all);
+}
+
+template <int DT, int DP, bool BITS8> static hipError_t decode_start(const DecodeParams& p, hipStream_t s) {
+  using A = AttnTile<DT, DP>;
+  constexpr int wave = 2 * 32 * A::RB * (BITS8 || A::RB > 256 ? 1 : 2) + 2 * 32 * 4, join = kDecodeWaves * 32 * (DP + 2) * 4;
+  constexpr int lds = (kDecodeWaves * wave + kDecodePages * 4) > join ? kDecodeWaves * wave + kDecodePages * 4 : join;
+  static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+  auto kernel = decode_kernel<DT, DP, BITS8>;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<dim3((unsigned)(p.rows * p.blocks * p.kv_heads * p.splits)), dim3(64 * kDecodeWaves), lds, s>>>(p);
+  if (p.splits > 1) decode_join_kernel<DT, DP><<<dim3((unsigned)(p.rows * p.heads)), dim3(DP), 0, s>>>(p);
+  return hipGetLastError();
+}
+
+template <int DT> hipError_t decode_launch(const DecodeParams& p, bool bits8, hipStream_t s) {
+  if (p.d <= 64) return bits8 ? decode_start<DT, 64, true>(p, s) : decode_start<DT, 64, false>(p, s);
+  return bits8 ? decode_start<DT, 128, true>(p, s) : decode_start<DT, 128, false>(p, s);
+}
+
+}  // namespace sc

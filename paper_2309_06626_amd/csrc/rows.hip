@@ -7,6 +7,7 @@
 
 #include "../../include/sparse_block.h"
 
+#include <atomic>
 #include <new>
 
 namespace sc {
@@ -104,6 +105,8 @@ static size_t rows_up(size_t n) { return (n + 255) & ~(size_t)255; }
 static int64_t rows_parts(int64_t rows) { return (rows + kRowsPart - 1) / kRowsPart; }
 
 static sc_status build(sc_rows* set, const uint8_t* mask, hipStream_t s) {
+  static std::atomic<uint64_t> versions{0};
+  set->version = ++versions;
   set->kept = 0;      // and nothing is kept if this fails, whatever became of the lists
   if (set->rows == 0) return SC_OK;
   const unsigned parts = (unsigned)rows_parts(set->rows);

@@ -8,6 +8,7 @@ struct sc_rows {
   int32_t* row_idx;      // [kept] ascending
   int32_t* slot;         // [rows] position in row_idx, or -1
   int32_t* counts;       // [0] kept, [1 ..] kept rows of each part
+  uint64_t version;      // another one for every mask of every set
 };
 
 namespace sc {
