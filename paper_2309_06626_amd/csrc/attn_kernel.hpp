@@ -17,6 +17,14 @@ constexpr float kAttnLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float attn_lse(float m, float sum) { return (float)((double)m * 0.6931471805599453 + (double)__builtin_logf(sum)); }
 __device__ __forceinline__ float attn_lse2(float lse) { return (float)((double)lse * 1.4426950408889634); }
 
+template <int N> constexpr std::integral_constant<int, N> attn_c{};
+template <int I, int N, class Fn> __device__ __forceinline__ void attn_for(Fn&& f) {
+  if constexpr (I < N) {
+    f(attn_c<I>);
+    attn_for<I + 1, N>(f);
+  }
+}
+
 // Consecutive workgroups go round the eight dies.  Where the key-value heads are a multiple of eight, each die takes heads of its own, whose
 // keys and values stay in its L2; otherwise heads are neighbours.  Items come with the longest first.
 struct AttnWork { AttnItem item; int head; };
@@ -56,9 +64,190 @@ __device__ __forceinline__ AttnSpan attn_rows(const AttnParams& p, int j, int n)
   return s;
 }
 
-// ---- forward, and the gradient of the queries --------------------------------------------------------------------------------------
+// ---- forward ---------------------------------------------------------------------------------------------------------------------------
+// A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.  While the matrix unit multiplies the keys of one tile, the
+// vector unit takes the exponentials of the tile before, and while it multiplies their values, the maximum of this one.
+template <int DT, int DP, int NW, bool VEC>
+__global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn_forward_kernel(const AttnParams p) {
+  using A = AttnTile<DT, DP>;
+  using T = typename A::T;
+  constexpr int NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32;
+  constexpr int TILE = TK * A::RB;                     // LDS: two tiles of keys, two of values
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
+
+  const AttnWork w = attn_work(p);
+  const int n = w.item.rows, first = w.item.first, packed = n * p.group;
+  const int r0 = w.item.tile * 32 * NW, r_wave = r0 + wave * 32, r = r_wave + l32;
+  const bool there = r < packed, any = r_wave < packed;
+  const int i = there ? r / p.group : 0, head = w.head * p.group + (there ? r - i * p.group : 0);
+  const int64_t row = p.map ? p.map[first + i] : first + i;
+  const AttnSpan mine = attn_keys(p, i, n);
+  // of the whole wavefront and workgroup: rows are in ascending order, and so are both ends of what they see
+  const AttnSpan from = attn_keys(p, any ? r_wave / p.group : 0, n), to = attn_keys(p, any ? (min(r_wave + 32, packed) - 1) / p.group : 0, n);
+  const int k_begin = attn_keys(p, r0 / p.group, n).lo / TK * TK;
+  const int k_end = attn_keys(p, (min(r0 + 32 * NW, packed) - 1) / p.group, n).hi + 1;
+  const int tiles = (k_end - k_begin + TK - 1) / TK;
+  // visible: key - lo <= span as unsigned; rows that do not exist see nothing
+  const int lo = there ? mine.lo : 0x40000000;
+  const unsigned span = there ? mine.hi - mine.lo : 0;
+
+  const T* const k_base = static_cast<const T*>(p.k) + (int64_t)w.head * p.d;
+  const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
+  const unsigned lds = attn_lds(smem);
+  auto request = [&](const T* base, int64_t stride, int tile, unsigned at) {
+    const int k0 = k_begin + tile * TK;
+    A::template request<TK, NT, VEC>(lds + at, p.d, [=, &p](int r) -> const T* {
+      const int j = k0 + r;
+      if (j >= n) return nullptr;
+      return base + (p.map ? p.map[first + j] : first + j) * stride;
+    });
+  };
+
+  request(k_base, p.k_stride, 0, 0);
+  v4i qf[A::KS];
+  A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
+  const float c = p.scale * kAttnLog2e;
+  typename A::Along along = A::along(lane);
+  typename A::Across across = A::across(lane);
+  along.add(lds);
+  across.add(lds);
+  floatx16 acc[A::DB], s_even[KB], s_odd[KB];
+#pragma unroll
+  for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
+  float m = -INFINITY, sum = 0.0f, shift = 0.0f;       // m is a maximum times c, as it was rounded
+
+  auto scores = [&](floatx16 (&s)[KB], auto parity) {
+    constexpr unsigned at = decltype(parity)::value * TILE;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[b][v] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s[b], A::read_along(along, at, b, ks), qf[ks]);
+    }
+  };
+  auto hide = [&](floatx16 (&s)[KB], int tile) {       // what a row does not see
+    const int k0 = k_begin + tile * TK;
+    if (k0 >= to.lo && k0 + TK - 1 <= from.hi && r_wave + 32 <= packed) return;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[b][v] = (unsigned)(k0 + 4 * h - lo + (32 * b + 8 * (v >> 2) + (v & 3))) <= span ? s[b][v] : -INFINITY;
+  };
+  auto weights = [&](floatx16 (&s)[KB], v4i (&pf)[KB][A::SS]) {
+    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[b][v] = attn_exp2(__builtin_fmaf(s[b][v], c, -shift));
+        part[v & 3] += s[b][v];
+      }
+      A::pack(s[b], pf[b]);
+    }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+  };
+  auto values = [&](const v4i (&pf)[KB][A::SS], auto parity) {
+    constexpr unsigned at = (2 + decltype(parity)::value) * TILE;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int ss = 0; ss < A::SS; ++ss)
+#pragma unroll
+        for (int db = 0; db < A::DB; ++db) A::E::mma(acc[db], A::read_across(across, at, b, ss, db), pf[b][ss]);
+  };
+  auto maximum = [&](const floatx16 (&s)[KB]) {
+    float part[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) part[v & 3] = fmaxf(part[v & 3], s[b][v]);
+    return fmaxf(attn_max_halves(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]))) * c, m);
+  };
+  auto rescale = [&](float most) {
+    if (attn_any(most > m)) {
+      shift = most == -INFINITY ? 0.0f : most;         // (nothing seen so far: every term is 0)
+      const float less = attn_exp2(m - shift);
+      sum *= less;
+#pragma unroll
+      for (int db = 0; db < A::DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[db][v] *= less;
+      m = most;
+    }
+  };
+  // An order of the instructions between two of these points: LDS reads ahead of the products that take them, vector work between.
+  auto ahead = [&](auto products, auto reads, auto first, auto vector, auto trans) {
+    if constexpr (DT != kF32) {
+      constexpr int N = decltype(products)::value, R = decltype(reads)::value, F = decltype(first)::value;
+      __builtin_amdgcn_sched_group_barrier(0x100, F, 0);
+      attn_for<0, N>([&](auto i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        constexpr int left = R - F - decltype(i)::value * (R / N);
+        if constexpr (left > 0) __builtin_amdgcn_sched_group_barrier(0x100, left < R / N ? left : R / N, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, decltype(vector)::value, 0);
+        if constexpr (decltype(trans)::value > 0) __builtin_amdgcn_sched_group_barrier(0x400, decltype(trans)::value, 0);
+      });
+    }
+  };
+  // Scores of tile `tile` (of parity P) into `now`, while `before` becomes weights of the values of the tile before it.
+  auto step = [&](floatx16 (&before)[KB], floatx16 (&now)[KB], int tile, auto parity) {
+    constexpr int P = decltype(parity)::value;
+    attn_meet<0>();                                    // keys of this tile and values of the one before are here, and everybody is this far
+    if (tile + 1 < tiles) request(k_base, p.k_stride, tile + 1, (1 - P) * TILE);
+    request(v_base, p.v_stride, tile, (2 + P) * TILE);
+    v4i pf[KB][A::SS];
+    __builtin_amdgcn_sched_barrier(0);
+    scores(now, parity);
+    weights(before, pf);
+    ahead(attn_c<KB * A::KS>, attn_c<KB * A::KS>, attn_c<3>, attn_c<5>, attn_c<2>);
+    __builtin_amdgcn_sched_barrier(0);
+    hide(now, tile);
+    __builtin_amdgcn_sched_barrier(0);
+    values(pf, attn_c<1 - P>);
+    const float most = maximum(now);
+    ahead(attn_c<KB * A::SS * A::DB>, attn_c<2 * KB * A::SS * A::DB>, attn_c<6>, attn_c<2>, attn_c<0>);
+    __builtin_amdgcn_sched_barrier(0);
+    rescale(most);
+  };
+  auto finish = [&](floatx16 (&before)[KB], auto parity) {
+    v4i pf[KB][A::SS];
+    attn_meet<0>();
+    weights(before, pf);
+    values(pf, parity);
+  };
+  attn_meet<0>();
+  if (tiles > 1) request(k_base, p.k_stride, 1, TILE);
+  request(v_base, p.v_stride, 0, 2 * TILE);
+  scores(s_even, attn_c<0>);
+  hide(s_even, 0);
+  rescale(maximum(s_even));
+  int tile = 1;
+  for (; tile + 1 < tiles; tile += 2) {
+    step(s_even, s_odd, tile, attn_c<1>);
+    step(s_odd, s_even, tile + 1, attn_c<0>);
+  }
+  if (tile < tiles) {
+    step(s_even, s_odd, tile, attn_c<1>);
+    finish(s_odd, attn_c<1>);
+  } else {
+    finish(s_even, attn_c<0>);
+  }
+  sum = attn_add_halves(sum);
+  if (!there) return;
+  const float per = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;      // (NaN stays)
+  if (p.lse && h == 0) p.lse[(int64_t)(first + i) * p.heads + head] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
+  T* const out = static_cast<T*>(p.out) + (row * p.heads + head) * p.d;
+#pragma unroll
+  for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], per);
+}
+
+// ---- gradient of the queries -----------------------------------------------------------------------------------------------------------
 // A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.
-template <int DT, int DP, int NW, bool VEC, bool BACKWARD>
+template <int DT, int DP, int NW, bool VEC>
 __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
@@ -102,11 +291,11 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   };
 
   request(0);
-  v4i qf[A::KS], gf[BACKWARD ? A::KS : 1];
+  v4i qf[A::KS], gf[A::KS];
   A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
   const float c = p.scale * kAttnLog2e;
   float lse2 = 0.0f, delta = 0.0f;
-  if constexpr (BACKWARD) {
+  {
     const int64_t at = (row * p.heads + head) * p.d;
     A::template read_row<VEC>(static_cast<const T*>(p.d_o) + at, p.d, h, there, gf);
     v4i of[A::KS];
@@ -132,7 +321,6 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   for (int db = 0; db < A::DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
-  float m = -INFINITY, sum = 0.0f;                     // m is a maximum times c, as it was rounded
 
   for (int tile = 0; tile < tiles; ++tile) {
     attn_meet<0>();                                   // this tile is here, and everybody is done with the one before
@@ -151,39 +339,7 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     }
     auto visible = [&](int b, int v) { return (unsigned)(k0 + 4 * h - lo + (32 * b + 8 * (v >> 2) + (v & 3))) <= span; };
     v4i pf[KB][A::SS];
-    if constexpr (!BACKWARD) {
-      if (!whole) {
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) s[b][v] = visible(b, v) ? s[b][v] : -INFINITY;
-      }
-      float most = s[0][0];
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) most = fmaxf(most, s[b][v]);
-      most = fmaxf(attn_max_halves(most) * c, m);
-      const float shift = most == -INFINITY ? 0.0f : most;      // (nothing seen so far: every term is 0)
-      if (attn_any(most > m)) {
-        const float less = attn_exp2(m - shift);
-        sum *= less;
-#pragma unroll
-        for (int db = 0; db < A::DB; ++db)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) acc[db][v] *= less;
-        m = most;
-      }
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s[b][v] = attn_exp2(__builtin_fmaf(s[b][v], c, -shift));
-          sum += s[b][v];
-        }
-        A::pack(s[b], pf[b]);
-      }
-    } else {
+    {
       floatx16 g[KB];
 #pragma unroll
       for (int b = 0; b < KB; ++b) {
@@ -199,29 +355,18 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
         A::pack(s[b], pf[b]);
       }
     }
-    // forward: values times probabilities; backward: keys times the gradients of the scores
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int ss = 0; ss < A::SS; ++ss)
 #pragma unroll
         for (int db = 0; db < A::DB; ++db)
-          A::E::mma(acc[db], A::read_across(across, BACKWARD ? at_k : at_v, b, ss, db), pf[b][ss]);
+          A::E::mma(acc[db], A::read_across(across, at_k, b, ss, db), pf[b][ss]);
   }
-  if constexpr (!BACKWARD) {
-    sum = attn_add_halves(sum);
-    if (!there) return;
-    const float per = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;      // (NaN stays)
-    if (p.lse && h == 0) p.lse[(int64_t)(first + i) * p.heads + head] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
-    T* const out = static_cast<T*>(p.out) + (row * p.heads + head) * p.d;
+  if (!there) return;
+  T* const out = static_cast<T*>(p.dq) + row * p.dq_stride + (int64_t)head * p.d;
 #pragma unroll
-    for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], per);
-  } else {
-    if (!there) return;
-    T* const out = static_cast<T*>(p.dq) + row * p.dq_stride + (int64_t)head * p.d;
-#pragma unroll
-    for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
-  }
+  for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
 }
 
 // ---- gradients of keys and values ------------------------------------------------------------------------------------------------------
@@ -351,8 +496,8 @@ template <class Kernel> static hipError_t attn_start(Kernel kernel, int threads,
 
 template <int DT, int DP, int NW, bool VEC> static hipError_t attn_start_rows(int what, const AttnParams& p, hipStream_t s) {
   constexpr int lds = 2 * 2 * (DT == kF32 ? 32 : 64) * AttnTile<DT, DP>::RB;
-  return what == kAttnForward ? attn_start(attn_rows_kernel<DT, DP, NW, VEC, false>, 64 * NW, lds, p, s)
-                              : attn_start(attn_rows_kernel<DT, DP, NW, VEC, true>, 64 * NW, lds, p, s);
+  return what == kAttnForward ? attn_start(attn_forward_kernel<DT, DP, NW, VEC>, 64 * NW, lds, p, s)
+                              : attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, lds, p, s);
 }
 
 template <int DT, int DP, bool VEC> static hipError_t attn_start_width(int what, const AttnParams& p, int waves, hipStream_t s) {
@@ -360,7 +505,7 @@ template <int DT, int DP, bool VEC> static hipError_t attn_start_width(int what,
     constexpr int lds = 2 * (2 * 32 * AttnTile<DT, DP>::RB + 2 * 32 * 4);
     return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, lds, p, s);
   }
-  return attn_start_rows<DT, DP, 4, VEC>(what, p, s);
+  return waves == 8 ? attn_start_rows<DT, DP, 8, VEC>(what, p, s) : attn_start_rows<DT, DP, 4, VEC>(what, p, s);
 }
 
 template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, bool vec, hipStream_t s) {

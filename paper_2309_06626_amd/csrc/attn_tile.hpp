@@ -71,8 +71,19 @@ template <int DT, int DP> struct AttnTile {
   }
 
   // Lane addresses within a tile, worked out once; what depends on the block of 32 rows is an offset.
-  struct Along { unsigned at[KS]; };
-  struct Across { unsigned at[EB == 2 ? 2 * DB : 16]; };
+  template <int N> struct Lanes {
+    unsigned at[N];
+    // the tiles' base, kept as it is, so that what is added to it goes into the instructions
+    __device__ __forceinline__ void add(unsigned base) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        at[i] += base;
+        asm volatile("" : "+v"(at[i]));
+      }
+    }
+  };
+  typedef Lanes<KS> Along;
+  typedef Lanes<EB == 2 ? 2 * DB : 16> Across;
 
   static __device__ __forceinline__ Along along(int lane) {
     Along a;
