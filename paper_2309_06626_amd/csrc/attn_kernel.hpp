@@ -95,16 +95,25 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   const T* const k_base = static_cast<const T*>(p.k) + (int64_t)w.head * p.d;
   const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
   const unsigned lds = attn_lds(smem);
-  auto request = [&](const T* base, int64_t stride, int tile, unsigned at) {
+  // rows as they follow each other, of all channels, have their offsets worked out once; the end of a sequence takes the general way
+  const bool plain = VEC && !p.map && p.d == DP && p.k_stride <= A::kMostStride && p.v_stride <= A::kMostStride;
+  const auto k_off = A::template offsets<TK, NT>(plain ? p.k_stride : 0), v_off = A::template offsets<TK, NT>(plain ? p.v_stride : 0);
+  auto request = [&](const T* base, int64_t stride, const auto& off, int tile, unsigned at) {
     const int k0 = k_begin + tile * TK;
-    A::template request<TK, NT, VEC>(lds + at, p.d, [=, &p](int r) -> const T* {
-      const int j = k0 + r;
-      if (j >= n) return nullptr;
-      return base + (p.map ? p.map[first + j] : first + j) * stride;
-    });
+    if (plain && k0 + TK <= n) {
+      A::template request_rows<TK, NT>(lds + at, base + (first + k0) * stride, off);
+    } else {
+      A::template request<TK, NT, VEC>(lds + at, p.d, [=, &p](int r) -> const T* {
+        const int j = k0 + r;
+        if (j >= n) return nullptr;
+        return base + (p.map ? p.map[first + j] : first + j) * stride;
+      });
+    }
   };
+  auto request_k = [&](int tile, unsigned at) { request(k_base, p.k_stride, k_off, tile, at); };
+  auto request_v = [&](int tile, unsigned at) { request(v_base, p.v_stride, v_off, tile, at); };
 
-  request(k_base, p.k_stride, 0, 0);
+  request_k(0, 0);
   v4i qf[A::KS];
   A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
   const float c = p.scale * kAttnLog2e;
@@ -168,7 +177,8 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     return fmaxf(attn_max_halves(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]))) * c, m);
   };
   auto rescale = [&](float most) {
-    if (attn_any(most > m)) {
+    // (a maximum that grew by less than 2^8 stays: weights of up to 256 are as good as those of up to 1)
+    if (attn_any(most > m + 8.0f)) {
       shift = most == -INFINITY ? 0.0f : most;         // (nothing seen so far: every term is 0)
       const float less = attn_exp2(m - shift);
       sum *= less;
@@ -197,19 +207,23 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   auto step = [&](floatx16 (&before)[KB], floatx16 (&now)[KB], int tile, auto parity) {
     constexpr int P = decltype(parity)::value;
     attn_meet<0>();                                    // keys of this tile and values of the one before are here, and everybody is this far
-    if (tile + 1 < tiles) request(k_base, p.k_stride, tile + 1, (1 - P) * TILE);
-    request(v_base, p.v_stride, tile, (2 + P) * TILE);
+    if (tile + 1 < tiles) request_k(tile + 1, (1 - P) * TILE);
+    request_v(tile, (2 + P) * TILE);
     v4i pf[KB][A::SS];
     __builtin_amdgcn_sched_barrier(0);
     scores(now, parity);
     weights(before, pf);
-    ahead(attn_c<KB * A::KS>, attn_c<KB * A::KS>, attn_c<3>, attn_c<5>, attn_c<2>);
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int ss = 0; ss < A::SS; ++ss) asm volatile("" : "+v"(pf[b][ss]));      // (formed here, not where they are taken)
+    ahead(attn_c<KB * A::KS>, attn_c<KB * A::KS>, attn_c<3>, attn_c<24 / A::KS>, attn_c<16 / A::KS>);
     __builtin_amdgcn_sched_barrier(0);
     hide(now, tile);
     __builtin_amdgcn_sched_barrier(0);
     values(pf, attn_c<1 - P>);
     const float most = maximum(now);
-    ahead(attn_c<KB * A::SS * A::DB>, attn_c<2 * KB * A::SS * A::DB>, attn_c<6>, attn_c<2>, attn_c<0>);
+    ahead(attn_c<KB * A::SS * A::DB>, attn_c<2 * KB * A::SS * A::DB>, attn_c<6>, attn_c<(4 * 4 + A::DB - 1) / A::DB>, attn_c<0>);
     __builtin_amdgcn_sched_barrier(0);
     rescale(most);
   };
@@ -220,8 +234,8 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     values(pf, parity);
   };
   attn_meet<0>();
-  if (tiles > 1) request(k_base, p.k_stride, 1, TILE);
-  request(v_base, p.v_stride, 0, 2 * TILE);
+  if (tiles > 1) request_k(1, TILE);
+  request_v(0, 2 * TILE);
   scores(s_even, attn_c<0>);
   hide(s_even, 0);
   rescale(maximum(s_even));

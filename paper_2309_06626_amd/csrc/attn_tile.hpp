@@ -26,6 +26,11 @@ __device__ __forceinline__ void attn_dma4(const void* src, unsigned lds_base) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(lds_base), "v"(src) : "memory");
 }
 
+// the same with a base that all lanes share and 32-bit offsets
+__device__ __forceinline__ void attn_dma16(const void* base, unsigned offset, unsigned lds_base) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds_base), "v"(offset), "s"(base) : "memory");
+}
+
 // All of this wavefront's transfers but the youngest N have landed and its LDS accesses are done; then the same holds for all.
 template <int N> __device__ __forceinline__ void attn_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
@@ -181,6 +186,25 @@ template <int DT, int DP> struct AttnTile {
       for (int v = 0; v < 16; ++v)
         if (c0 + v < d) row[c0 + v] = r[v];
     }
+  }
+
+  // The same of rows that lie `stride` entries apart and of DP channels: offsets of a lane's transfers, worked out once, from the first row.
+  template <int ROWS, int NT> struct Offsets { unsigned at[ROWS * GROUPS / NT]; };
+  template <int ROWS, int NT> static __device__ __forceinline__ Offsets<ROWS, NT> offsets(int64_t stride) {
+    Offsets<ROWS, NT> o;
+#pragma unroll
+    for (int j = 0; j < ROWS * GROUPS / NT; ++j) {
+      const int at = j * NT + threadIdx.x, r = at / GROUPS;
+      o.at[j] = (unsigned)(r * (int)stride * EB + ((at % GROUPS) ^ key(r)) * 16);
+    }
+    return o;
+  }
+  static constexpr int64_t kMostStride = (1 << 23) / EB;      // entries: offsets within 128 rows fit 31 bits
+  template <int ROWS, int NT>
+  static __device__ __forceinline__ void request_rows(unsigned tile, const T* first, const Offsets<ROWS, NT>& o) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int j = 0; j < ROWS * GROUPS / NT; ++j) attn_dma16(first, o.at[j], tile + (j * NT + wave * 64) * 16);
   }
 
   // Transfer of ROWS rows by NT lanes: `place(r)` is the row's address in memory, null for a row of zeros.
