@@ -243,7 +243,7 @@ sc_status sparse_attn_plan(const sc_attn_desc* desc, int64_t seqs, const int64_t
     plan->desc = *desc;
     plan->end = starts[seqs];
     plan->version = rows ? rows->version : 0;
-    plan->waves = starts[seqs] * (desc->heads / desc->kv_heads) >= 512 * seqs ? 8 : 4;
+    plan->waves = desc->dtype != SC_F32 && starts[seqs] * (desc->heads / desc->kv_heads) >= 512 * seqs ? 8 : 4;
     st = sc::attn_plan(plan, seqs, starts, rows, static_cast<unsigned char*>(workspace_dev), static_cast<hipStream_t>(hip_stream));
   } catch (const std::bad_alloc&) {
     sc::note_hip_error((int32_t)hipErrorOutOfMemory);

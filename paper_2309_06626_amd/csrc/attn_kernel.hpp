@@ -68,7 +68,7 @@ __device__ __forceinline__ AttnSpan attn_rows(const AttnParams& p, int j, int n)
 // A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.  While the matrix unit multiplies the keys of one tile, the
 // vector unit takes the exponentials of the tile before, and while it multiplies their values, the maximum of this one.
 template <int DT, int DP, int NW, bool VEC>
-__global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn_forward_kernel(const AttnParams p) {
+__global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4) ? 1 : 2) : 2) void attn_forward_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
   constexpr int NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32;
@@ -96,9 +96,9 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
   const unsigned lds = attn_lds(smem);
   // rows as they follow each other, of all channels, have their offsets worked out once; the end of a sequence takes the general way
-  const bool plain = VEC && !p.map && p.d == DP && p.k_stride <= A::kMostStride && p.v_stride <= A::kMostStride;
-  const auto k_off = A::template offsets<TK, NT>(plain ? p.k_stride : 0), v_off = A::template offsets<TK, NT>(plain ? p.v_stride : 0);
-  auto request = [&](const T* base, int64_t stride, const auto& off, int tile, unsigned at) {
+  const bool plain = VEC && !p.map && p.d == DP && p.k_stride == p.v_stride && p.k_stride <= A::kMostStride;
+  const auto off = A::template offsets<TK, NT>(plain ? p.k_stride : 0);
+  auto request = [&](const T* base, int64_t stride, int tile, unsigned at) {
     const int k0 = k_begin + tile * TK;
     if (plain && k0 + TK <= n) {
       A::template request_rows<TK, NT>(lds + at, base + (first + k0) * stride, off);
@@ -110,8 +110,8 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
       });
     }
   };
-  auto request_k = [&](int tile, unsigned at) { request(k_base, p.k_stride, k_off, tile, at); };
-  auto request_v = [&](int tile, unsigned at) { request(v_base, p.v_stride, v_off, tile, at); };
+  auto request_k = [&](int tile, unsigned at) { request(k_base, p.k_stride, tile, at); };
+  auto request_v = [&](int tile, unsigned at) { request(v_base, p.v_stride, tile, at); };
 
   request_k(0, 0);
   v4i qf[A::KS];
@@ -147,17 +147,20 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
       for (int v = 0; v < 16; ++v) s[b][v] = (unsigned)(k0 + 4 * h - lo + (32 * b + 8 * (v >> 2) + (v & 3))) <= span ? s[b][v] : -INFINITY;
   };
   auto weights = [&](floatx16 (&s)[KB], v4i (&pf)[KB][A::SS]) {
-    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[b][v] = attn_exp2(__builtin_fmaf(s[b][v], c, -shift));
-        part[v & 3] += s[b][v];
-      }
+      for (int v = 0; v < 16; ++v) s[b][v] = attn_exp2(__builtin_fmaf(s[b][v], c, -shift));
       A::pack(s[b], pf[b]);
     }
-    sum += (part[0] + part[1]) + (part[2] + part[3]);
+  };
+  auto add_up = [&](const floatx16 (&s)[KB], auto from, auto to) {      // blocks from .. to
+    float part[4] = {sum, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int b = decltype(from)::value; b < decltype(to)::value; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) part[v & 3] += s[b][v];
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
   };
   auto values = [&](const v4i (&pf)[KB][A::SS], auto parity) {
     constexpr unsigned at = (2 + decltype(parity)::value) * TILE;
@@ -189,6 +192,8 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
       m = most;
     }
   };
+  // blocks whose weights are added up beside the scores, the others beside the values: as the vector unit has room and registers last
+  constexpr int EARLY = VEC && DP > 64 ? 0 : KB;
   // An order of the instructions between two of these points: LDS reads ahead of the products that take them, vector work between.
   auto ahead = [&](auto products, auto reads, auto first, auto vector, auto trans) {
     if constexpr (DT != kF32) {
@@ -213,17 +218,20 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     __builtin_amdgcn_sched_barrier(0);
     scores(now, parity);
     weights(before, pf);
+    add_up(before, attn_c<0>, attn_c<EARLY>);
+    asm volatile("" : "+v"(sum));                      // (formed here, not where they are taken)
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
-      for (int ss = 0; ss < A::SS; ++ss) asm volatile("" : "+v"(pf[b][ss]));      // (formed here, not where they are taken)
-    ahead(attn_c<KB * A::KS>, attn_c<KB * A::KS>, attn_c<3>, attn_c<24 / A::KS>, attn_c<16 / A::KS>);
+      for (int ss = 0; ss < A::SS; ++ss) asm volatile("" : "+v"(pf[b][ss]));
+    ahead(attn_c<KB * A::KS>, attn_c<KB * A::KS>, attn_c<3>, attn_c<EARLY ? 40 / A::KS : 24 / A::KS>, attn_c<16 / A::KS>);
     __builtin_amdgcn_sched_barrier(0);
     hide(now, tile);
     __builtin_amdgcn_sched_barrier(0);
     values(pf, attn_c<1 - P>);
+    add_up(before, attn_c<EARLY>, attn_c<KB>);
     const float most = maximum(now);
-    ahead(attn_c<KB * A::SS * A::DB>, attn_c<2 * KB * A::SS * A::DB>, attn_c<6>, attn_c<(4 * 4 + A::DB - 1) / A::DB>, attn_c<0>);
+    ahead(attn_c<KB * A::SS * A::DB>, attn_c<2 * KB * A::SS * A::DB>, attn_c<6>, attn_c<EARLY ? 8 / A::DB : 16 / A::DB>, attn_c<0>);
     __builtin_amdgcn_sched_barrier(0);
     rescale(most);
   };
@@ -232,6 +240,7 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     attn_meet<0>();
     weights(before, pf);
     values(pf, parity);
+    add_up(before, attn_c<0>, attn_c<KB>);
   };
   attn_meet<0>();
   if (tiles > 1) request_k(1, TILE);
@@ -251,21 +260,47 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     finish(s_even, attn_c<0>);
   }
   sum = attn_add_halves(sum);
-  if (!there) return;
+  // (the row's place is worked out again: registers are short in between)
+  int again = threadIdx.x;
+  asm volatile("" : "+v"(again));
+  const int r_out = r_wave + (again & 31);
+  if (r_out >= packed) return;
+  const int i_out = r_out / p.group, head_out = w.head * p.group + (r_out - i_out * p.group);
+  const int64_t row_out = p.map ? p.map[first + i_out] : first + i_out;
   const float per = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;      // (NaN stays)
-  if (p.lse && h == 0) p.lse[(int64_t)(first + i) * p.heads + head] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
-  T* const out = static_cast<T*>(p.out) + (row * p.heads + head) * p.d;
+  if (p.lse && again % 64 < 32) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
+  T* const out = static_cast<T*>(p.out) + (row_out * p.heads + head_out) * p.d;
 #pragma unroll
-  for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], per);
+  for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * ((again >> 5) & 1), p.d, acc[db], per);
 }
 
-// ---- gradient of the queries -----------------------------------------------------------------------------------------------------------
-// A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.
+// ---- gradients ---------------------------------------------------------------------------------------------------------------------------
+// Both kernels go in steps of 32 rows of what passes by.  While the matrix unit forms the scores and the products with the result's gradient of
+// the next step, the vector unit makes probabilities and gradients of scores of this one; then those are multiplied.  Tiles (one or two
+// steps) lie in three places in LDS: one whose second half is still multiplied, the next, and one on its way.
+
+// An order of the instructions of a step: A products with one LDS read each (and vector work beside them), then B with R reads each, every read
+// three products ahead of the one that takes it; FIRST other reads before.
+template <int A, int B, int R, int FIRST, int VECTOR> __device__ __forceinline__ void attn_order_step() {
+  __builtin_amdgcn_sched_group_barrier(0x100, FIRST + 3, 0);
+  attn_for<0, A + B>([&](auto at) {
+    constexpr int i = decltype(at)::value;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (i + 3 < A) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    else if constexpr (i + 3 < A + B) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+    if constexpr (i < A) {
+      __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 16 / A, 0);
+    }
+  });
+}
+
+// Gradient of the queries: a wavefront has 32 packed rows, one a lane and half; keys and values pass by.
 template <int DT, int DP, int NW, bool VEC>
-__global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
+__global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
-  constexpr int NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32, STAGES = 2;
+  constexpr int NT = 64 * NW, HALVES = DT == kF32 ? 1 : 2, TK = 32 * HALVES;
   constexpr int TILE = TK * A::RB, STAGE = 2 * TILE;
   extern __shared__ __align__(16) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
@@ -273,12 +308,11 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   const AttnWork w = attn_work(p);
   const int n = w.item.rows, first = w.item.first, packed = n * p.group;
   const int r0 = w.item.tile * 32 * NW, r_wave = r0 + wave * 32, r = r_wave + l32;
-  const bool there = r < packed;
+  const bool there = r < packed, any = r_wave < packed;
   const int i = there ? r / p.group : 0, head = w.head * p.group + (there ? r - i * p.group : 0);
   const int64_t row = p.map ? p.map[first + i] : first + i;
   const AttnSpan mine = attn_keys(p, i, n);
   // of the whole wavefront and workgroup: rows are in ascending order, and so are both ends of what they see
-  const bool any = r_wave < packed;
   const AttnSpan from = attn_keys(p, any ? r_wave / p.group : 0, n), to = attn_keys(p, any ? (min(r_wave + 32, packed) - 1) / p.group : 0, n);
   const int k_begin = attn_keys(p, r0 / p.group, n).lo / TK * TK;
   const int k_end = attn_keys(p, (min(r0 + 32 * NW, packed) - 1) / p.group, n).hi + 1;
@@ -290,21 +324,27 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   const T* const k_base = static_cast<const T*>(p.k) + (int64_t)w.head * p.d;
   const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
   const unsigned lds = attn_lds(smem);
-  auto request = [&](int tile) {
+  const bool plain = VEC && !p.map && p.d == DP && p.k_stride == p.v_stride && p.k_stride <= A::kMostStride;
+  const auto off = A::template offsets<TK, NT>(plain ? p.k_stride : 0);
+  auto request = [&](int tile, unsigned stage) {
     const int k0 = k_begin + tile * TK;
-    const unsigned at = lds + (tile % STAGES) * STAGE;
-    auto place = [&](const T* base, int64_t stride) {
-      return [=, &p](int r) -> const T* {
-        const int j = k0 + r;
-        if (j >= n) return nullptr;
-        return base + (p.map ? p.map[first + j] : first + j) * stride;
+    if (plain && k0 + TK <= n) {
+      A::template request_rows<TK, NT>(lds + stage, k_base + (first + k0) * p.k_stride, off);
+      A::template request_rows<TK, NT>(lds + stage + TILE, v_base + (first + k0) * p.k_stride, off);
+    } else {
+      auto place = [&](const T* base, int64_t stride) {
+        return [=, &p](int r) -> const T* {
+          const int j = k0 + r;
+          if (j >= n) return nullptr;
+          return base + (p.map ? p.map[first + j] : first + j) * stride;
+        };
       };
-    };
-    A::template request<TK, NT, VEC>(at, p.d, place(k_base, p.k_stride));
-    A::template request<TK, NT, VEC>(at + TILE, p.d, place(v_base, p.v_stride));
+      A::template request<TK, NT, VEC>(lds + stage, p.d, place(k_base, p.k_stride));
+      A::template request<TK, NT, VEC>(lds + stage + TILE, p.d, place(v_base, p.v_stride));
+    }
   };
+  request(0, 0);
 
-  request(0);
   v4i qf[A::KS], gf[A::KS];
   A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
   const float c = p.scale * kAttnLog2e;
@@ -328,54 +368,96 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
     lse2 = there ? attn_lse2(p.lse[stat]) : 0.0f;
   }
 
-  const typename A::Along along = A::along(lane);
-  const typename A::Across across = A::across(lane);
-  floatx16 acc[A::DB];
+  typename A::Along along = A::along(lane);
+  typename A::Across across = A::across(lane);
+  along.add(lds);
+  across.add(lds);
+  floatx16 acc[A::DB], s_even, g_even, s_odd, g_odd;
 #pragma unroll
   for (int db = 0; db < A::DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
 
-  for (int tile = 0; tile < tiles; ++tile) {
-    attn_meet<0>();                                   // this tile is here, and everybody is done with the one before
-    if (tile + 1 < tiles) request(tile + 1);
-    const int k0 = k_begin + tile * TK;
-    if (!any || k0 > to.hi || k0 + TK <= from.lo) continue;
-    const bool whole = k0 >= to.lo && k0 + TK - 1 <= from.hi && r_wave + 32 <= packed;
-    const unsigned at_k = lds + (tile % STAGES) * STAGE, at_v = at_k + TILE;
-    floatx16 s[KB];
+  auto products = [&](floatx16& s, floatx16& g, unsigned stage, int half) {
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
+    for (int v = 0; v < 16; ++v) s[v] = g[v] = 0.0f;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[b][v] = 0.0f;
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, stage, half, ks), qf[ks]);
 #pragma unroll
-      for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s[b], A::read_along(along, at_k, b, ks), qf[ks]);
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, stage + TILE, half, ks), gf[ks]);
+  };
+  auto hide = [&](floatx16& s, int k0) {               // what a row does not see
+    if (k0 >= to.lo && k0 + 31 <= from.hi && r_wave + 32 <= packed) return;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = (unsigned)(k0 + 4 * h - lo + (8 * (v >> 2) + (v & 3))) <= span ? s[v] : -INFINITY;
+  };
+  auto form = [&](const floatx16& s, floatx16& g, v4i (&pf)[A::SS]) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) g[v] = attn_exp2(__builtin_fmaf(s[v], c, -lse2)) * (g[v] - delta);
+    A::pack(g, pf);
+  };
+  auto take = [&](const v4i (&pf)[A::SS], unsigned stage, int half) {
+#pragma unroll
+    for (int ss = 0; ss < A::SS; ++ss)
+#pragma unroll
+      for (int db = 0; db < A::DB; ++db) A::E::mma(acc[db], A::read_across(across, stage, half, ss, db), pf[ss]);
+  };
+  // a step of `half` of the tile at `stage`, from key k0 on, with the next one's products beside it
+  auto step = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next, int k0, unsigned stage, int half, unsigned stage_next, int half_next) {
+    v4i pf[A::SS];
+    hide(s, k0);
+    __builtin_amdgcn_sched_barrier(0);
+    products(s_next, g_next, stage_next, half_next);
+    form(s, g, pf);
+    take(pf, stage, half);
+    if constexpr (DT != kF32) attn_order_step<2 * A::KS, A::SS * A::DB, 2, 0, 64 / (2 * A::KS)>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto last = [&](floatx16& s, floatx16& g, int k0, unsigned stage, int half) {
+    v4i pf[A::SS];
+    hide(s, k0);
+    form(s, g, pf);
+    take(pf, stage, half);
+  };
+  unsigned here = 0, there_next = STAGE;               // places of this tile and of the next one
+  auto turn = [&]() {
+    here = there_next;
+    there_next = there_next == 2 * STAGE ? 0 : there_next + STAGE;
+  };
+  attn_meet<0>();
+  if (tiles > 1) request(1, STAGE);
+  products(s_even, g_even, 0, 0);
+  if constexpr (HALVES == 2) {
+    int k0 = k_begin;
+    for (int tile = 0; tile + 1 < tiles; ++tile, k0 += TK) {
+      step(s_even, g_even, s_odd, g_odd, k0, here, 0, here, 1);
+      attn_meet<0>();                                  // the next tile is here, and nobody is in the one before this any more
+      if (tile + 2 < tiles) request(tile + 2, there_next == 2 * STAGE ? 0 : there_next + STAGE);
+      step(s_odd, g_odd, s_even, g_even, k0 + 32, here, 1, there_next, 0);
+      turn();
     }
-    auto visible = [&](int b, int v) { return (unsigned)(k0 + 4 * h - lo + (32 * b + 8 * (v >> 2) + (v & 3))) <= span; };
-    v4i pf[KB][A::SS];
-    {
-      floatx16 g[KB];
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) g[b][v] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g[b], A::read_along(along, at_v, b, ks), gf[ks]);
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float e = attn_exp2(__builtin_fmaf(s[b][v], c, -lse2));
-          s[b][v] = (whole || visible(b, v) ? e : 0.0f) * (g[b][v] - delta);
-        }
-        A::pack(s[b], pf[b]);
-      }
+    step(s_even, g_even, s_odd, g_odd, k0, here, 0, here, 1);
+    last(s_odd, g_odd, k0 + 32, here, 1);
+  } else {
+    int tile = 0, k0 = k_begin;
+    auto one = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next) {
+      attn_meet<0>();
+      if (tile + 2 < tiles) request(tile + 2, there_next == 2 * STAGE ? 0 : there_next + STAGE);
+      step(s, g, s_next, g_next, k0, here, 0, there_next, 0);
+      turn();
+      ++tile;
+      k0 += TK;
+    };
+    while (tile + 2 < tiles) {
+      one(s_even, g_even, s_odd, g_odd);
+      one(s_odd, g_odd, s_even, g_even);
     }
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-      for (int ss = 0; ss < A::SS; ++ss)
-#pragma unroll
-        for (int db = 0; db < A::DB; ++db)
-          A::E::mma(acc[db], A::read_across(across, at_k, b, ss, db), pf[b][ss]);
+    if (tile + 1 < tiles) {
+      one(s_even, g_even, s_odd, g_odd);
+      last(s_odd, g_odd, k0, here, 0);
+    } else {
+      last(s_even, g_even, k0, here, 0);
+    }
   }
   if (!there) return;
   T* const out = static_cast<T*>(p.dq) + row * p.dq_stride + (int64_t)head * p.d;
@@ -383,13 +465,12 @@ __global__ __launch_bounds__(64 * NW, (DT == kF32 && DP > 64) ? 1 : 2) void attn
   for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
 }
 
-// ---- gradients of keys and values ------------------------------------------------------------------------------------------------------
-// A wavefront has 32 keys, one a lane and half; packed rows of queries and of the result's gradient pass by in tiles.
+// Gradients of keys and values: a wavefront has 32 keys, one a lane and half; packed rows of queries and of the result's gradient pass by.
 template <int DT, int DP, bool VEC>
 __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
-  constexpr int NW = kAttnKeyWaves, NT = 64 * NW, TQ = 32, STAGES = 2;
+  constexpr int NW = kAttnKeyWaves, NT = 64 * NW, HALVES = DT == kF32 ? 1 : 2, TQ = 32 * HALVES;
   constexpr int TILE = TQ * A::RB, STATS = 2 * TQ * 4, STAGE = 2 * TILE + STATS;
   extern __shared__ __align__(16) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
@@ -407,17 +488,14 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
   const int tiles = (r_end - r_begin + TQ - 1) / TQ;
   const int lo = there ? mine.lo * group : 0x40000000;
   const unsigned span = there ? (mine.hi - mine.lo + 1) * group - 1 : 0;
-  const int wave_lo = from.lo * group, wave_hi = (to.hi + 1) * group - 1;          // rows that see any key of the wavefront
-  const int all_lo = to.lo * group, all_hi = (from.hi + 1) * group - 1;            // rows that see all of them
+  const int all_lo = to.lo * group, all_hi = (from.hi + 1) * group - 1;            // rows that see all of the wavefront's keys
 
   const T* const q_base = static_cast<const T*>(p.q) + (int64_t)w.head * group * p.d;
   const T* const g_base = static_cast<const T*>(p.d_o) + (int64_t)w.head * group * p.d;
   const unsigned lds = attn_lds(smem);
   const float c = p.scale * kAttnLog2e;
-  float stat = 0.0f;      // one of lse (lanes 0 .. 31) and delta (32 .. 63) of the next tile's rows
-  auto request = [&](int tile) {
+  auto request = [&](int tile, unsigned stage) {
     const int r0 = r_begin + tile * TQ, i0 = r0 / group, rem = r0 - i0 * group;
-    const unsigned at = lds + (tile % STAGES) * STAGE;
     auto place = [&](const T* base, int64_t stride) {
       return [=, &p](int r) -> const T* {
         const int past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
@@ -425,67 +503,117 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
         return base + (p.map ? p.map[first + i] : first + i) * stride + (rem + r - past * group) * p.d;
       };
     };
-    A::template request<TQ, NT, VEC>(at, p.d, place(q_base, p.q_stride));
-    A::template request<TQ, NT, VEC>(at + TILE, p.d, place(g_base, (int64_t)p.heads * p.d));
-    if (t < 64) {
-      const int past = (int)((unsigned)(rem + l32) * p.magic >> 20), i = i0 + past;
-      const int64_t of = (int64_t)(first + i) * p.heads + w.head * group + (rem + l32 - past * group);
-      stat = i < n ? (h ? p.delta[of] : attn_lse2(p.lse[of])) : 0.0f;
-      *(__attribute__((address_space(3))) float*)(uint64_t)(at + 2 * TILE + t * 4) = stat;
+    A::template request<TQ, NT, VEC>(lds + stage, p.d, place(q_base, p.q_stride));
+    A::template request<TQ, NT, VEC>(lds + stage + TILE, p.d, place(g_base, (int64_t)p.heads * p.d));
+    // lse of the tile's rows, then delta
+    if (t < 2 * TQ) {
+      const int r = t % TQ, past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
+      const int64_t of = (int64_t)(first + i) * p.heads + w.head * group + (rem + r - past * group);
+      const float stat = i < n ? (t >= TQ ? p.delta[of] : attn_lse2(p.lse[of])) : 0.0f;
+      *(__attribute__((address_space(3))) float*)(uint64_t)(lds + stage + 2 * TILE + t * 4) = stat;
     }
   };
-  request(0);
+  request(0, 0);
 
   v4i kf[A::KS], vf[A::KS];
   A::template read_row<VEC>(static_cast<const T*>(p.k) + row * p.k_stride + (int64_t)w.head * p.d, p.d, h, there, kf);
   A::template read_row<VEC>(static_cast<const T*>(p.v) + row * p.v_stride + (int64_t)w.head * p.d, p.d, h, there, vf);
-  const typename A::Along along = A::along(lane);
-  const typename A::Across across = A::across(lane);
-  floatx16 dk[A::DB], dv[A::DB];
+  typename A::Along along = A::along(lane);
+  typename A::Across across = A::across(lane);
+  along.add(lds);
+  across.add(lds);
+  const unsigned at_stats = lds + 2 * TILE + 16 * h;
+  floatx16 dk[A::DB], dv[A::DB], s_even, g_even, s_odd, g_odd;
 #pragma unroll
   for (int db = 0; db < A::DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.0f;
 
   typedef __attribute__((address_space(3))) const v4f lds_v4f;
-  for (int tile = 0; tile < tiles; ++tile) {
-    attn_meet<0>();
-    if (tile + 1 < tiles) request(tile + 1);
-    const int r0 = r_begin + tile * TQ;
-    if (!any || r0 > wave_hi || r0 + TQ <= wave_lo) continue;
-    const bool whole = r0 >= all_lo && r0 + TQ - 1 <= all_hi && j_wave + 32 <= n;
-    const unsigned at_q = lds + (tile % STAGES) * STAGE, at_g = at_q + TILE, at_s = at_g + TILE;
-    floatx16 s, g;
+  auto products = [&](floatx16& s, floatx16& g, unsigned stage, int half) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = g[v] = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, at_q, 0, ks), kf[ks]);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, stage, half, ks), kf[ks]);
+    if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, at_g, 0, ks), vf[ks]);
-    v4i pf[A::SS], df[A::SS];
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, stage + TILE, half, ks), vf[ks]);
+  };
+  auto hide = [&](floatx16& s, int r0) {               // keys that a row does not see
+    if (r0 >= all_lo && r0 + 31 <= all_hi && j_wave + 32 <= n) return;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = (unsigned)(r0 + 4 * h - lo + (8 * (v >> 2) + (v & 3))) <= span ? s[v] : -INFINITY;
+  };
+  auto form = [&](floatx16& s, floatx16& g, unsigned stage, int half, v4i (&pf)[A::SS], v4i (&df)[A::SS]) {
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-      const v4f lse2 = *(lds_v4f*)(uint64_t)(at_s + (8 * a + 4 * h) * 4), delta = *(lds_v4f*)(uint64_t)(at_s + (TQ + 8 * a + 4 * h) * 4);
+      const v4f lse2 = *(lds_v4f*)(uint64_t)(at_stats + stage + (32 * half + 8 * a) * 4);
+      const v4f delta = *(lds_v4f*)(uint64_t)(at_stats + stage + (TQ + 32 * half + 8 * a) * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int v = 4 * a + e;
-        const bool seen = whole || (unsigned)(r0 + 4 * h - lo + (8 * a + e)) <= span;
-        const float pr = seen ? attn_exp2(__builtin_fmaf(s[v], c, -lse2[e])) : 0.0f;
-        s[v] = pr;
-        g[v] = pr * (g[v] - delta[e]);
+        s[v] = attn_exp2(__builtin_fmaf(s[v], c, -lse2[e]));
+        g[v] = s[v] * (g[v] - delta[e]);
       }
     }
     A::pack(s, pf);
     A::pack(g, df);
+  };
+  auto take = [&](const v4i (&pf)[A::SS], const v4i (&df)[A::SS], unsigned stage, int half) {
 #pragma unroll
     for (int ss = 0; ss < A::SS; ++ss) {
-      __builtin_amdgcn_sched_barrier(0);      // (operands are read a product's worth ahead, not all at once into registers that are not there)
+      if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);      // (operands are read as they are taken: there is no room for all)
 #pragma unroll
       for (int db = 0; db < A::DB; ++db) {
-        A::E::mma(dv[db], A::read_across(across, at_g, 0, ss, db), pf[ss]);
-        A::E::mma(dk[db], A::read_across(across, at_q, 0, ss, db), df[ss]);
+        A::E::mma(dv[db], A::read_across(across, stage + TILE, half, ss, db), pf[ss]);
+        A::E::mma(dk[db], A::read_across(across, stage, half, ss, db), df[ss]);
       }
+    }
+  };
+  auto step = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next, int r0, unsigned stage, int half, unsigned stage_next, int half_next) {
+    v4i pf[A::SS], df[A::SS];
+    hide(s, r0);
+    __builtin_amdgcn_sched_barrier(0);
+    products(s_next, g_next, stage_next, half_next);
+    form(s, g, stage, half, pf, df);
+    take(pf, df, stage, half);
+    if constexpr (DT != kF32) attn_order_step<2 * A::KS, 2 * A::SS * A::DB, 2, 8, 72 / (2 * A::KS)>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto last = [&](floatx16& s, floatx16& g, int r0, unsigned stage, int half) {
+    v4i pf[A::SS], df[A::SS];
+    hide(s, r0);
+    form(s, g, stage, half, pf, df);
+    take(pf, df, stage, half);
+  };
+  unsigned here = 0, there_next = STAGE;               // places of this tile and of the next one
+  auto turn = [&]() {
+    here = there_next;
+    there_next = there_next == 2 * STAGE ? 0 : there_next + STAGE;
+  };
+  if constexpr (HALVES == 2) {
+    attn_meet<0>();
+    if (tiles > 1) request(1, STAGE);
+    products(s_even, g_even, 0, 0);
+    int r0 = r_begin;
+    for (int tile = 0; tile + 1 < tiles; ++tile, r0 += TQ) {
+      step(s_even, g_even, s_odd, g_odd, r0, here, 0, here, 1);
+      attn_meet<0>();                                  // the next tile is here, and nobody is in the one before this any more
+      if (tile + 2 < tiles) request(tile + 2, there_next == 2 * STAGE ? 0 : there_next + STAGE);
+      step(s_odd, g_odd, s_even, g_even, r0 + 32, here, 1, there_next, 0);
+      turn();
+    }
+    step(s_even, g_even, s_odd, g_odd, r0, here, 0, here, 1);
+    last(s_odd, g_odd, r0 + 32, here, 1);
+  } else {
+    // floats: the products take all of the time, and registers two sets of results do not have
+    for (int tile = 0; tile < tiles; ++tile) {
+      attn_meet<0>();
+      if (tile + 1 < tiles) request(tile + 1, there_next);
+      products(s_even, g_even, here, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      last(s_even, g_even, r_begin + tile * TQ, here, 0);
+      turn();
     }
   }
   if (!there) return;
@@ -509,17 +637,20 @@ template <class Kernel> static hipError_t attn_start(Kernel kernel, int threads,
 }
 
 template <int DT, int DP, int NW, bool VEC> static hipError_t attn_start_rows(int what, const AttnParams& p, hipStream_t s) {
-  constexpr int lds = 2 * 2 * (DT == kF32 ? 32 : 64) * AttnTile<DT, DP>::RB;
-  return what == kAttnForward ? attn_start(attn_forward_kernel<DT, DP, NW, VEC>, 64 * NW, lds, p, s)
-                              : attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, lds, p, s);
+  constexpr int tile = (DT == kF32 ? 32 : 64) * AttnTile<DT, DP>::RB;
+  return what == kAttnForward ? attn_start(attn_forward_kernel<DT, DP, NW, VEC>, 64 * NW, 4 * tile, p, s)
+                              : attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, 6 * tile, p, s);
 }
 
 template <int DT, int DP, bool VEC> static hipError_t attn_start_width(int what, const AttnParams& p, int waves, hipStream_t s) {
   if (what == kAttnBackwardKV) {
-    constexpr int lds = 2 * (2 * 32 * AttnTile<DT, DP>::RB + 2 * 32 * 4);
+    constexpr int rows = DT == kF32 ? 32 : 64, lds = 3 * (2 * rows * AttnTile<DT, DP>::RB + 2 * rows * 4);
     return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, lds, p, s);
   }
-  return waves == 8 ? attn_start_rows<DT, DP, 8, VEC>(what, p, s) : attn_start_rows<DT, DP, 4, VEC>(what, p, s);
+  if constexpr (DT != kF32) {
+    if (waves == 8) return attn_start_rows<DT, DP, 8, VEC>(what, p, s);
+  }
+  return attn_start_rows<DT, DP, 4, VEC>(what, p, s);
 }
 
 template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, bool vec, hipStream_t s) {
