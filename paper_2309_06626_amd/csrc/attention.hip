@@ -303,7 +303,7 @@ sc_status sparse_attn_backward_workspace_bytes(const sc_attn* plan, size_t* byte
   if (!bytes) return SC_ERR_NULL;
   *bytes = 0;
   if (!plan) return SC_ERR_NULL;
-  *bytes = 256 + sc::attn_up((size_t)plan->kept * plan->desc.heads * 4);
+  *bytes = 256 + 2 * sc::attn_up((size_t)plan->kept * plan->desc.heads * 4);
   return SC_OK;
 }
 
@@ -343,12 +343,13 @@ sc_status sparse_attn_backward(const sc_attn* plan, const sc_rows* rows, int32_t
   p.dk_stride = dk_stride;
   p.dv_stride = dv_stride;
   p.lse = const_cast<float*>(lse_dev);
-  p.delta = static_cast<float*>(workspace_dev);
+  p.stats[0] = static_cast<float*>(workspace_dev);
+  p.stats[1] = p.stats[0] + sc::attn_up((size_t)plan->kept * d.heads * 4) / 4;
   hipError_t e = hipSuccess;
   if (plan->n_row_items > 0) {
     p.items = plan->row_items;
     p.n_items = plan->n_row_items;
-    e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->waves, vec, s);      // (leaves delta for the keys)
+    e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->waves, vec, s);      // (leaves statistics for the keys)
     p.items = plan->key_items;
     p.n_items = plan->n_key_items;
     if (e == hipSuccess) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardKV, p, plan->waves, vec, s);

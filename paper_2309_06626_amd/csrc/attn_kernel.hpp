@@ -364,8 +364,8 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
     }
     delta = attn_add_halves(delta);
     const int64_t stat = (int64_t)(first + i) * p.heads + head;
-    if (there && h == 0) p.delta[stat] = delta;
     lse2 = there ? attn_lse2(p.lse[stat]) : 0.0f;
+    if (there) p.stats[h][stat] = h ? delta : lse2;      // (for the keys)
   }
 
   typename A::Along along = A::along(lane);
@@ -494,23 +494,34 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
   const T* const g_base = static_cast<const T*>(p.d_o) + (int64_t)w.head * group * p.d;
   const unsigned lds = attn_lds(smem);
   const float c = p.scale * kAttnLog2e;
+  // rows of whole groups that follow each other, of all channels, have their offsets worked out once
+  const int64_t g_stride = (int64_t)p.heads * p.d;
+  const bool plain = VEC && !p.map && p.d == DP && TQ % group == 0 && p.q_stride <= A::kMostStride && g_stride <= A::kMostStride;
+  const auto q_off = A::template offsets<TQ, NT>(plain ? p.q_stride : 0, plain ? group : 1), g_off = A::template offsets<TQ, NT>(plain ? g_stride : 0, plain ? group : 1);
   auto request = [&](int tile, unsigned stage) {
     const int r0 = r_begin + tile * TQ, i0 = r0 / group, rem = r0 - i0 * group;
-    auto place = [&](const T* base, int64_t stride) {
-      return [=, &p](int r) -> const T* {
-        const int past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
-        if (i >= n) return nullptr;
-        return base + (p.map ? p.map[first + i] : first + i) * stride + (rem + r - past * group) * p.d;
+    if (plain && r0 + TQ <= n * group) {
+      A::template request_rows<TQ, NT>(lds + stage, q_base + (first + i0) * p.q_stride, q_off);
+      A::template request_rows<TQ, NT>(lds + stage + TILE, g_base + (first + i0) * g_stride, g_off);
+    } else {
+      auto place = [&](const T* base, int64_t stride) {
+        return [=, &p](int r) -> const T* {
+          const int past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
+          if (i >= n) return nullptr;
+          return base + (p.map ? p.map[first + i] : first + i) * stride + (rem + r - past * group) * p.d;
+        };
       };
-    };
-    A::template request<TQ, NT, VEC>(lds + stage, p.d, place(q_base, p.q_stride));
-    A::template request<TQ, NT, VEC>(lds + stage + TILE, p.d, place(g_base, (int64_t)p.heads * p.d));
-    // lse of the tile's rows, then delta
-    if (t < 2 * TQ) {
-      const int r = t % TQ, past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
-      const int64_t of = (int64_t)(first + i) * p.heads + w.head * group + (rem + r - past * group);
-      const float stat = i < n ? (t >= TQ ? p.delta[of] : attn_lse2(p.lse[of])) : 0.0f;
-      *(__attribute__((address_space(3))) float*)(uint64_t)(lds + stage + 2 * TILE + t * 4) = stat;
+      A::template request<TQ, NT, VEC>(lds + stage, p.d, place(q_base, p.q_stride));
+      A::template request<TQ, NT, VEC>(lds + stage + TILE, p.d, place(g_base, g_stride));
+    }
+    // lse of the tile's rows (in exponents of 2), then delta: the first wavefront's transfers
+    if (wave == 0) {
+#pragma unroll
+      for (int part = 0; part < 2 * TQ; part += 64) {
+        const int x = part + lane, r = x % TQ, past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
+        const float* of = p.stats[x / TQ] + (int64_t)(first + i) * p.heads + w.head * group + (rem + r - past * group);
+        attn_dma4(i < n ? (const void*)of : (const void*)&attn_zeros, lds + stage + 2 * TILE + part * 4);
+      }
     }
   };
   request(0, 0);
