@@ -26,7 +26,7 @@ namespace sc {
 
 void note_hip_error(int32_t code);
 
-static hipError_t attn_dispatch(int dtype, int what, const AttnParams& p, int waves, bool vec, hipStream_t s) {
+static hipError_t attn_dispatch(int dtype, int what, const AttnParams& p, int waves, int vec, hipStream_t s) {
   if (dtype == SC_BF16) return attn_launch<kBF16>(what, p, waves, vec, s);
   if (dtype == SC_F16) return attn_launch<kF16>(what, p, waves, vec, s);
   return attn_launch<kF32>(what, p, waves, vec, s);
@@ -46,33 +46,20 @@ __global__ __launch_bounds__(256) void attn_starts_kernel(const int32_t* __restr
   out[i] = lo;
 }
 
-// zeros in the dropped rows of up to three outputs; a wavefront a row
-struct AttnZeros {
-  void* out[3];
-  int64_t stride[3], width[3];      // bytes
-};
-template <typename T>
-__global__ __launch_bounds__(256) void attn_zero_kernel(const int32_t* __restrict__ slot, int64_t rows, AttnZeros z) {
-  for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4) {
-    if (slot && slot[r] >= 0) continue;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      T* row = reinterpret_cast<T*>(static_cast<unsigned char*>(z.out[k]) + r * z.stride[k]);
-      for (int64_t i = threadIdx.x & 63; i < z.width[k] / (int64_t)sizeof(T); i += 64) row[i] = T{};
-    }
-  }
-}
-
-static hipError_t attn_zero_dropped(const sc_rows* set, int64_t rows, const AttnZeros& z, hipStream_t s) {
-  if (!set || set->kept == set->rows || rows == 0) return hipSuccess;
-  uintptr_t all = 0;
-  for (int k = 0; k < 3; ++k) all |= (uintptr_t)z.out[k] | (uintptr_t)z.stride[k] | (uintptr_t)z.width[k];
-  const unsigned grid = (unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 22);
-  const int32_t* slot = set->kept ? set->slot : nullptr;
-  typedef int v4 __attribute__((ext_vector_type(4)));
-  if (all % 16 == 0) attn_zero_kernel<v4><<<dim3(grid), dim3(256), 0, s>>>(slot, rows, z);
-  else attn_zero_kernel<uint16_t><<<dim3(grid), dim3(256), 0, s>>>(slot, rows, z);
-  return hipGetLastError();
+// Zeros in the dropped rows of up to three outputs (of null and 0 bytes where there are fewer).
+static void attn_zeros_of(const sc_rows* set, int64_t rows, std::initializer_list<void*> out, std::initializer_list<int64_t> stride,
+                          std::initializer_list<int64_t> width, AttnZeros* z) {
+  *z = {};
+  if (!set || set->kept == set->rows || rows == 0) return;
+  z->slot = set->kept ? set->slot : nullptr;
+  z->rows = rows;
+  std::copy(out.begin(), out.end(), z->out);
+  std::copy(stride.begin(), stride.end(), z->stride);
+  std::copy(width.begin(), width.end(), z->width);
+  uint64_t all = 0;
+  for (int k = 0; k < 3; ++k) all |= (uint64_t)(uintptr_t)z->out[k] | (uint64_t)z->stride[k] | (uint64_t)z->width[k];
+  z->vec = all % 16 == 0;
+  z->blocks = (int32_t)std::min<int64_t>((rows + 31) / 32, 512);
 }
 
 static size_t attn_up(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -176,15 +163,16 @@ static sc_status attn_check_call(const sc_attn* plan, const sc_rows* rows, int32
 
 struct AttnMatrix { const void* at; int64_t stride; int32_t heads; };      // [rows][heads][d]
 
-static sc_status attn_check_matrices(const sc_attn* plan, std::initializer_list<AttnMatrix> ms, bool* vec) {
+static sc_status attn_check_matrices(const sc_attn* plan, std::initializer_list<AttnMatrix> ms, int* vec) {
   const int eb = plan->desc.dtype == SC_F32 ? 4 : 2;
-  *vec = plan->desc.d * eb % 16 == 0;
+  uint64_t all = (uint64_t)plan->desc.d * eb;
   for (const AttnMatrix& m : ms) {
     if (plan->kept > 0 && !m.at) return SC_ERR_NULL;
     if (m.stride < (int64_t)m.heads * plan->desc.d || m.stride > ((int64_t)1 << 40)) return SC_ERR_BAD_SHAPE;
     if ((uintptr_t)m.at % eb) return SC_ERR_ALIGN;
-    if ((uintptr_t)m.at % 16 || m.stride * eb % 16) *vec = false;
+    all |= (uint64_t)(uintptr_t)m.at | (uint64_t)m.stride * eb;
   }
+  *vec = all % 16 == 0 ? 2 : all % 4 == 0 ? 1 : 0;
   return SC_OK;
 }
 
@@ -272,7 +260,7 @@ sc_status sparse_attn_run(const sc_attn* plan, const sc_rows* rows, int32_t row_
   sc_status st = sc::attn_check_call(plan, rows, row_format);
   if (st != SC_OK) return st;
   const sc_attn_desc& d = plan->desc;
-  bool vec;
+  int vec;
   st = sc::attn_check_matrices(plan, {{q_dev, q_stride, d.heads}, {k_dev, k_stride, d.kv_heads}, {v_dev, v_stride, d.kv_heads}}, &vec);
   if (st != SC_OK) return st;
   if (plan->end > 0 && !o_dev && (plan->kept > 0 || row_format == SC_ROWS_DENSE)) return SC_ERR_NULL;
@@ -290,11 +278,11 @@ sc_status sparse_attn_run(const sc_attn* plan, const sc_rows* rows, int32_t row_
   p.items = plan->row_items;
   p.n_items = plan->n_row_items;
   hipError_t e = hipSuccess;
-  if (p.n_items > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnForward, p, plan->waves, vec, s);
-  if (e == hipSuccess && row_format == SC_ROWS_DENSE) {
+  if (row_format == SC_ROWS_DENSE) {
     const int64_t width = (int64_t)d.heads * d.d * (d.dtype == SC_F32 ? 4 : 2);
-    e = sc::attn_zero_dropped(rows, plan->end, {{o_dev, nullptr, nullptr}, {width, 0, 0}, {width, 0, 0}}, s);
+    sc::attn_zeros_of(rows, plan->end, {o_dev}, {width}, {width}, &p.zeros);
   }
+  if (p.n_items > 0 || p.zeros.blocks > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnForward, p, plan->waves, vec, s);
   if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
   return SC_OK;
 }
@@ -315,7 +303,7 @@ sc_status sparse_attn_backward(const sc_attn* plan, const sc_rows* rows, int32_t
   sc_status st = sc::attn_check_call(plan, rows, row_format);
   if (st != SC_OK) return st;
   const sc_attn_desc& d = plan->desc;
-  bool vec;
+  int vec;
   st = sc::attn_check_matrices(plan, {{q_dev, q_stride, d.heads}, {k_dev, k_stride, d.kv_heads}, {v_dev, v_stride, d.kv_heads},
                                       {dq_dev, dq_stride, d.heads}, {dk_dev, dk_stride, d.kv_heads}, {dv_dev, dv_stride, d.kv_heads}}, &vec);
   if (st != SC_OK) return st;
@@ -345,19 +333,18 @@ sc_status sparse_attn_backward(const sc_attn* plan, const sc_rows* rows, int32_t
   p.lse = const_cast<float*>(lse_dev);
   p.stats[0] = static_cast<float*>(workspace_dev);
   p.stats[1] = p.stats[0] + sc::attn_up((size_t)plan->kept * d.heads * 4) / 4;
-  hipError_t e = hipSuccess;
-  if (plan->n_row_items > 0) {
-    p.items = plan->row_items;
-    p.n_items = plan->n_row_items;
-    e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->waves, vec, s);      // (leaves statistics for the keys)
-    p.items = plan->key_items;
-    p.n_items = plan->n_key_items;
-    if (e == hipSuccess) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardKV, p, plan->waves, vec, s);
-  }
-  if (e == hipSuccess && row_format == SC_ROWS_DENSE) {
+  p.items = plan->row_items;
+  p.n_items = plan->n_row_items;
+  if (row_format == SC_ROWS_DENSE) {
     const int64_t eb = d.dtype == SC_F32 ? 4 : 2, q = d.heads * eb * d.d, kv = d.kv_heads * eb * d.d;
-    e = sc::attn_zero_dropped(rows, plan->end, {{dq_dev, dk_dev, dv_dev}, {dq_stride * eb, dk_stride * eb, dv_stride * eb}, {q, kv, kv}}, s);
+    sc::attn_zeros_of(rows, plan->end, {dq_dev, dk_dev, dv_dev}, {dq_stride * eb, dk_stride * eb, dv_stride * eb}, {q, kv, kv}, &p.zeros);
   }
+  hipError_t e = hipSuccess;
+  if (p.n_items > 0 || p.zeros.blocks > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->waves, vec, s);      // (leaves statistics for the keys)
+  p.zeros.blocks = 0;
+  p.items = plan->key_items;
+  p.n_items = plan->n_key_items;
+  if (e == hipSuccess && p.n_items > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardKV, p, plan->waves, vec, s);
   if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
   return SC_OK;
 }

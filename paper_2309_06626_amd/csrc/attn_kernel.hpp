@@ -25,6 +25,10 @@ template <int I, int N, class Fn> __device__ __forceinline__ void attn_for(Fn&& 
   }
 }
 
+// How rows are read, the VEC of the kernels: by entries (0), 4 bytes (1) or 16 (2); plain ones, besides, are of 64 or 128 channels and follow
+// each other at a distance that offsets of 32 bits span.
+constexpr int kAttnPlain = 3;
+
 // Consecutive workgroups go round the eight dies.  Where the key-value heads are a multiple of eight, each die takes heads of its own, whose
 // keys and values stay in its L2; otherwise heads are neighbours.  Items come with the longest first.
 struct AttnWork { AttnItem item; int head; };
@@ -40,6 +44,25 @@ __device__ __forceinline__ AttnWork attn_work(const AttnParams& p) {
     item = b / p.kv_heads;
   }
   return {p.items[item], head};
+}
+
+// The workgroups behind those of the items write the zeros of dropped rows, a wavefront a row.  True for such a one.
+template <int NW> __device__ __forceinline__ bool attn_zeros_of_dropped(const AttnParams& p) {
+  const int block = (int)blockIdx.x - p.n_items * p.kv_heads;
+  if (block < 0) return false;
+  for (int64_t r = (int64_t)block * NW + (threadIdx.x >> 6); r < p.zeros.rows; r += (int64_t)p.zeros.blocks * NW) {
+    if (p.zeros.slot && p.zeros.slot[r] >= 0) continue;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      unsigned char* const row = static_cast<unsigned char*>(p.zeros.out[k]) + r * p.zeros.stride[k];
+      if (p.zeros.vec) {
+        for (int64_t i = (threadIdx.x & 63) * 16; i < p.zeros.width[k]; i += 1024) *reinterpret_cast<v4i*>(row + i) = v4i{0, 0, 0, 0};
+      } else {
+        for (int64_t i = (threadIdx.x & 63) * 2; i < p.zeros.width[k]; i += 128) *reinterpret_cast<uint16_t*>(row + i) = 0;
+      }
+    }
+  }
+  return true;
 }
 
 // Keys that row i of a sequence of n rows sees: lo .. hi.
@@ -64,18 +87,28 @@ __device__ __forceinline__ AttnSpan attn_rows(const AttnParams& p, int j, int n)
   return s;
 }
 
+// Rows of the tensors that hold kept rows first + j0 .. + 63 of a sequence of n, a lane each (-1: none).  Asked for a tile ahead: a look-up at
+// the place where it is taken would wait for all transfers on their way.
+__device__ __forceinline__ int attn_look_up(const AttnParams& p, int first, int j0, int n) {
+  const int j = j0 + (threadIdx.x & 63);
+  if (j >= n) return -1;
+  return p.map ? p.map[first + j] : first + j;
+}
+
 // ---- forward ---------------------------------------------------------------------------------------------------------------------------
 // A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.  While the matrix unit multiplies the keys of one tile, the
 // vector unit takes the exponentials of the tile before, and while it multiplies their values, the maximum of this one.
-template <int DT, int DP, int NW, bool VEC>
-__global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4) ? 1 : 2) : 2) void attn_forward_kernel(const AttnParams p) {
+template <int DT, int DP, int NW, int VEC>
+__global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (VEC < 2 && NW == 4) ? 1 : 2) : 2) void attn_forward_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
-  constexpr int NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32;
+  constexpr bool PLAIN = VEC == kAttnPlain;
+  constexpr int LOADS = PLAIN ? 2 : VEC, NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32;
   constexpr int TILE = TK * A::RB;                     // LDS: two tiles of keys, two of values
   extern __shared__ __align__(16) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
 
+  if (attn_zeros_of_dropped<NW>(p)) return;
   const AttnWork w = attn_work(p);
   const int n = w.item.rows, first = w.item.first, packed = n * p.group;
   const int r0 = w.item.tile * 32 * NW, r_wave = r0 + wave * 32, r = r_wave + l32;
@@ -95,27 +128,31 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4)
   const T* const k_base = static_cast<const T*>(p.k) + (int64_t)w.head * p.d;
   const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
   const unsigned lds = attn_lds(smem);
-  // rows as they follow each other, of all channels, have their offsets worked out once; the end of a sequence takes the general way
-  const bool plain = VEC && !p.map && p.d == DP && p.k_stride == p.v_stride && p.k_stride <= A::kMostStride;
-  const auto off = A::template offsets<TK, NT>(plain ? p.k_stride : 0);
-  auto request = [&](const T* base, int64_t stride, int tile, unsigned at) {
+  // rows that follow each other have their offsets worked out once; the end of a sequence takes the general way
+  const auto off = A::template offsets<TK, NT>(PLAIN ? p.k_stride : 0);
+  auto request = [&](const T* base, int64_t stride, int tile, int rows, unsigned at) {
     const int k0 = k_begin + tile * TK;
-    if (plain && k0 + TK <= n) {
+    if (PLAIN && k0 + TK <= n) {
       A::template request_rows<TK, NT>(lds + at, base + (first + k0) * stride, off);
     } else {
-      A::template request<TK, NT, VEC>(lds + at, p.d, [=, &p](int r) -> const T* {
-        const int j = k0 + r;
-        if (j >= n) return nullptr;
-        return base + (p.map ? p.map[first + j] : first + j) * stride;
+      A::template request<TK, NT, LOADS>(lds + at, p.d, [=](int r) -> const T* {
+        if constexpr (PLAIN) return k0 + r < n ? base + (first + k0 + r) * stride : nullptr;
+        const int row = __shfl(rows, r);
+        return row < 0 ? nullptr : base + row * stride;
       });
     }
   };
-  auto request_k = [&](int tile, unsigned at) { request(k_base, p.k_stride, tile, at); };
-  auto request_v = [&](int tile, unsigned at) { request(v_base, p.v_stride, tile, at); };
+  int rows_k = 0, rows_v = 0;                          // rows of the next tile of keys, and of values
+  auto look_up = [&](int tile) {
+    if constexpr (!PLAIN) rows_k = attn_look_up(p, first, k_begin + tile * TK, n);
+  };
+  auto request_k = [&](int tile, unsigned at) { request(k_base, p.k_stride, tile, rows_k, at); };
+  auto request_v = [&](int tile, unsigned at) { request(v_base, p.v_stride, tile, rows_v, at); };
+  look_up(0);
 
   request_k(0, 0);
   v4i qf[A::KS];
-  A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
+  A::template read_row<LOADS>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
   const float c = p.scale * kAttnLog2e;
   typename A::Along along = A::along(lane);
   typename A::Across across = A::across(lane);
@@ -193,7 +230,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4)
     }
   };
   // blocks whose weights are added up beside the scores, the others beside the values: as the vector unit has room and registers last
-  constexpr int EARLY = VEC && DP > 64 ? 0 : KB;
+  constexpr int EARLY = VEC >= 2 && DP > 64 ? 0 : KB;
   // An order of the instructions between two of these points: LDS reads ahead of the products that take them, vector work between.
   auto ahead = [&](auto products, auto reads, auto first, auto vector, auto trans) {
     if constexpr (DT != kF32) {
@@ -214,6 +251,8 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4)
     attn_meet<0>();                                    // keys of this tile and values of the one before are here, and everybody is this far
     if (tile + 1 < tiles) request_k(tile + 1, (1 - P) * TILE);
     request_v(tile, (2 + P) * TILE);
+    rows_v = rows_k;
+    look_up(tile + 2);
     v4i pf[KB][A::SS];
     __builtin_amdgcn_sched_barrier(0);
     scores(now, parity);
@@ -242,9 +281,13 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4)
     values(pf, parity);
     add_up(before, attn_c<0>, attn_c<KB>);
   };
+  rows_v = rows_k;
+  look_up(1);
   attn_meet<0>();
   if (tiles > 1) request_k(1, TILE);
   request_v(0, 2 * TILE);
+  rows_v = rows_k;
+  look_up(2);
   scores(s_even, attn_c<0>);
   hide(s_even, 0);
   rescale(maximum(s_even));
@@ -271,7 +314,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (!VEC && NW == 4)
   if (p.lse && again % 64 < 32) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
   T* const out = static_cast<T*>(p.out) + (row_out * p.heads + head_out) * p.d;
 #pragma unroll
-  for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * ((again >> 5) & 1), p.d, acc[db], per);
+  for (int db = 0; db < A::DB; ++db) A::template write_16<LOADS>(out, 32 * db + 16 * ((again >> 5) & 1), p.d, acc[db], per);
 }
 
 // ---- gradients ---------------------------------------------------------------------------------------------------------------------------
@@ -296,15 +339,17 @@ template <int A, int B, int R, int FIRST, int VECTOR> __device__ __forceinline__
 }
 
 // Gradient of the queries: a wavefront has 32 packed rows, one a lane and half; keys and values pass by.
-template <int DT, int DP, int NW, bool VEC>
+template <int DT, int DP, int NW, int VEC>
 __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
-  constexpr int NT = 64 * NW, HALVES = DT == kF32 ? 1 : 2, TK = 32 * HALVES;
+  constexpr bool PLAIN = VEC == kAttnPlain;
+  constexpr int LOADS = PLAIN ? 2 : VEC, NT = 64 * NW, HALVES = DT == kF32 ? 1 : 2, TK = 32 * HALVES;
   constexpr int TILE = TK * A::RB, STAGE = 2 * TILE;
   extern __shared__ __align__(16) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
 
+  if (attn_zeros_of_dropped<NW>(p)) return;
   const AttnWork w = attn_work(p);
   const int n = w.item.rows, first = w.item.first, packed = n * p.group;
   const int r0 = w.item.tile * 32 * NW, r_wave = r0 + wave * 32, r = r_wave + l32;
@@ -324,36 +369,37 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
   const T* const k_base = static_cast<const T*>(p.k) + (int64_t)w.head * p.d;
   const T* const v_base = static_cast<const T*>(p.v) + (int64_t)w.head * p.d;
   const unsigned lds = attn_lds(smem);
-  const bool plain = VEC && !p.map && p.d == DP && p.k_stride == p.v_stride && p.k_stride <= A::kMostStride;
-  const auto off = A::template offsets<TK, NT>(plain ? p.k_stride : 0);
+  const auto off = A::template offsets<TK, NT>(PLAIN ? p.k_stride : 0);
+  int rows = PLAIN ? 0 : attn_look_up(p, first, k_begin, n);      // of the next tile
   auto request = [&](int tile, unsigned stage) {
     const int k0 = k_begin + tile * TK;
-    if (plain && k0 + TK <= n) {
+    if (PLAIN && k0 + TK <= n) {
       A::template request_rows<TK, NT>(lds + stage, k_base + (first + k0) * p.k_stride, off);
       A::template request_rows<TK, NT>(lds + stage + TILE, v_base + (first + k0) * p.k_stride, off);
     } else {
       auto place = [&](const T* base, int64_t stride) {
-        return [=, &p](int r) -> const T* {
-          const int j = k0 + r;
-          if (j >= n) return nullptr;
-          return base + (p.map ? p.map[first + j] : first + j) * stride;
+        return [=](int r) -> const T* {
+          if constexpr (PLAIN) return k0 + r < n ? base + (first + k0 + r) * stride : nullptr;
+          const int row = __shfl(rows, r);
+          return row < 0 ? nullptr : base + row * stride;
         };
       };
-      A::template request<TK, NT, VEC>(lds + stage, p.d, place(k_base, p.k_stride));
-      A::template request<TK, NT, VEC>(lds + stage + TILE, p.d, place(v_base, p.v_stride));
+      A::template request<TK, NT, LOADS>(lds + stage, p.d, place(k_base, p.k_stride));
+      A::template request<TK, NT, LOADS>(lds + stage + TILE, p.d, place(v_base, p.v_stride));
     }
+    if constexpr (!PLAIN) rows = attn_look_up(p, first, k0 + TK, n);
   };
   request(0, 0);
 
   v4i qf[A::KS], gf[A::KS];
-  A::template read_row<VEC>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
+  A::template read_row<LOADS>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
   const float c = p.scale * kAttnLog2e;
   float lse2 = 0.0f, delta = 0.0f;
   {
     const int64_t at = (row * p.heads + head) * p.d;
-    A::template read_row<VEC>(static_cast<const T*>(p.d_o) + at, p.d, h, there, gf);
+    A::template read_row<LOADS>(static_cast<const T*>(p.d_o) + at, p.d, h, there, gf);
     v4i of[A::KS];
-    A::template read_row<VEC>(static_cast<const T*>(p.o) + at, p.d, h, there, of);
+    A::template read_row<LOADS>(static_cast<const T*>(p.o) + at, p.d, h, there, of);
 #pragma unroll
     for (int ks = 0; ks < A::KS; ++ks) {
       T a[A::V], b[A::V];
@@ -462,15 +508,16 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
   if (!there) return;
   T* const out = static_cast<T*>(p.dq) + row * p.dq_stride + (int64_t)head * p.d;
 #pragma unroll
-  for (int db = 0; db < A::DB; ++db) A::template write_16<VEC>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
+  for (int db = 0; db < A::DB; ++db) A::template write_16<LOADS>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
 }
 
 // Gradients of keys and values: a wavefront has 32 keys, one a lane and half; packed rows of queries and of the result's gradient pass by.
-template <int DT, int DP, bool VEC>
+template <int DT, int DP, int VEC>
 __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
-  constexpr int NW = kAttnKeyWaves, NT = 64 * NW, HALVES = DT == kF32 ? 1 : 2, TQ = 32 * HALVES;
+  constexpr bool PLAIN = VEC == kAttnPlain;
+  constexpr int LOADS = PLAIN ? 2 : VEC, NW = kAttnKeyWaves, NT = 64 * NW, HALVES = DT == kF32 ? 1 : 2, TQ = 32 * HALVES;
   constexpr int TILE = TQ * A::RB, STATS = 2 * TQ * 4, STAGE = 2 * TILE + STATS;
   extern __shared__ __align__(16) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
@@ -494,26 +541,25 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
   const T* const g_base = static_cast<const T*>(p.d_o) + (int64_t)w.head * group * p.d;
   const unsigned lds = attn_lds(smem);
   const float c = p.scale * kAttnLog2e;
-  // rows of whole groups that follow each other, of all channels, have their offsets worked out once
   const int64_t g_stride = (int64_t)p.heads * p.d;
-  const bool plain = VEC && !p.map && p.d == DP && TQ % group == 0 && p.q_stride <= A::kMostStride && g_stride <= A::kMostStride;
-  const auto q_off = A::template offsets<TQ, NT>(plain ? p.q_stride : 0, plain ? group : 1), g_off = A::template offsets<TQ, NT>(plain ? g_stride : 0, plain ? group : 1);
+  const auto q_off = A::template offsets<TQ, NT>(PLAIN ? p.q_stride : 0, PLAIN ? group : 1), g_off = A::template offsets<TQ, NT>(PLAIN ? g_stride : 0, PLAIN ? group : 1);
+  int rows = PLAIN ? 0 : attn_look_up(p, first, r_begin / group, n);      // of the next tile
   auto request = [&](int tile, unsigned stage) {
     const int r0 = r_begin + tile * TQ, i0 = r0 / group, rem = r0 - i0 * group;
-    if (plain && r0 + TQ <= n * group) {
+    if (PLAIN && r0 + TQ <= n * group) {
       A::template request_rows<TQ, NT>(lds + stage, q_base + (first + i0) * p.q_stride, q_off);
       A::template request_rows<TQ, NT>(lds + stage + TILE, g_base + (first + i0) * g_stride, g_off);
     } else {
       auto place = [&](const T* base, int64_t stride) {
         return [=, &p](int r) -> const T* {
-          const int past = (int)((unsigned)(rem + r) * p.magic >> 20), i = i0 + past;
-          if (i >= n) return nullptr;
-          return base + (p.map ? p.map[first + i] : first + i) * stride + (rem + r - past * group) * p.d;
+          const int past = (int)((unsigned)(rem + r) * p.magic >> 20), row = PLAIN ? (i0 + past < n ? first + i0 + past : -1) : __shfl(rows, past);
+          return row < 0 ? nullptr : base + row * stride + (rem + r - past * group) * p.d;
         };
       };
-      A::template request<TQ, NT, VEC>(lds + stage, p.d, place(q_base, p.q_stride));
-      A::template request<TQ, NT, VEC>(lds + stage + TILE, p.d, place(g_base, g_stride));
+      A::template request<TQ, NT, LOADS>(lds + stage, p.d, place(q_base, p.q_stride));
+      A::template request<TQ, NT, LOADS>(lds + stage + TILE, p.d, place(g_base, g_stride));
     }
+    if constexpr (!PLAIN) rows = attn_look_up(p, first, (r0 + TQ) / group, n);
     // lse of the tile's rows (in exponents of 2), then delta: the first wavefront's transfers
     if (wave == 0) {
 #pragma unroll
@@ -527,8 +573,8 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
   request(0, 0);
 
   v4i kf[A::KS], vf[A::KS];
-  A::template read_row<VEC>(static_cast<const T*>(p.k) + row * p.k_stride + (int64_t)w.head * p.d, p.d, h, there, kf);
-  A::template read_row<VEC>(static_cast<const T*>(p.v) + row * p.v_stride + (int64_t)w.head * p.d, p.d, h, there, vf);
+  A::template read_row<LOADS>(static_cast<const T*>(p.k) + row * p.k_stride + (int64_t)w.head * p.d, p.d, h, there, kf);
+  A::template read_row<LOADS>(static_cast<const T*>(p.v) + row * p.v_stride + (int64_t)w.head * p.d, p.d, h, there, vf);
   typename A::Along along = A::along(lane);
   typename A::Across across = A::across(lane);
   along.add(lds);
@@ -632,8 +678,8 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
   T* const out_v = static_cast<T*>(p.dv) + row * p.dv_stride + (int64_t)w.head * p.d;
 #pragma unroll
   for (int db = 0; db < A::DB; ++db) {
-    A::template write_16<VEC>(out_k, 32 * db + 16 * h, p.d, dk[db], p.scale);
-    A::template write_16<VEC>(out_v, 32 * db + 16 * h, p.d, dv[db], 1.0f);
+    A::template write_16<LOADS>(out_k, 32 * db + 16 * h, p.d, dk[db], p.scale);
+    A::template write_16<LOADS>(out_v, 32 * db + 16 * h, p.d, dv[db], 1.0f);
   }
 }
 
@@ -643,17 +689,17 @@ template <class Kernel> static hipError_t attn_start(Kernel kernel, int threads,
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  kernel<<<dim3((unsigned)((int64_t)p.n_items * p.kv_heads)), dim3(threads), lds, s>>>(p);
+  kernel<<<dim3((unsigned)((int64_t)p.n_items * p.kv_heads + p.zeros.blocks)), dim3(threads), lds, s>>>(p);
   return hipGetLastError();
 }
 
-template <int DT, int DP, int NW, bool VEC> static hipError_t attn_start_rows(int what, const AttnParams& p, hipStream_t s) {
+template <int DT, int DP, int NW, int VEC> static hipError_t attn_start_rows(int what, const AttnParams& p, hipStream_t s) {
   constexpr int tile = (DT == kF32 ? 32 : 64) * AttnTile<DT, DP>::RB;
   return what == kAttnForward ? attn_start(attn_forward_kernel<DT, DP, NW, VEC>, 64 * NW, 4 * tile, p, s)
                               : attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, 6 * tile, p, s);
 }
 
-template <int DT, int DP, bool VEC> static hipError_t attn_start_width(int what, const AttnParams& p, int waves, hipStream_t s) {
+template <int DT, int DP, int VEC> static hipError_t attn_start_width(int what, const AttnParams& p, int waves, hipStream_t s) {
   if (what == kAttnBackwardKV) {
     constexpr int rows = DT == kF32 ? 32 : 64, lds = 3 * (2 * rows * AttnTile<DT, DP>::RB + 2 * rows * 4);
     return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, lds, p, s);
@@ -664,9 +710,22 @@ template <int DT, int DP, bool VEC> static hipError_t attn_start_width(int what,
   return attn_start_rows<DT, DP, 4, VEC>(what, p, s);
 }
 
-template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, bool vec, hipStream_t s) {
-  if (p.d <= 64) return vec ? attn_start_width<DT, 64, true>(what, p, waves, s) : attn_start_width<DT, 64, false>(what, p, waves, s);
-  return vec ? attn_start_width<DT, 128, true>(what, p, waves, s) : attn_start_width<DT, 128, false>(what, p, waves, s);
+template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, int vec, hipStream_t s) {
+  auto start = [&](auto level) {
+    constexpr int VEC = decltype(level)::value;
+    return p.d <= 64 ? attn_start_width<DT, 64, VEC>(what, p, waves, s) : attn_start_width<DT, 128, VEC>(what, p, waves, s);
+  };
+  if (vec == 2) {
+    const int64_t most = AttnTile<DT, 64>::kMostStride;
+    const bool plain = !p.map && (p.d == 64 || p.d == 128) &&
+                       (what == kAttnBackwardKV ? (DT == kF32 ? 32 : 64) % p.group == 0 && p.q_stride <= most && (int64_t)p.heads * p.d <= most
+                                                : p.k_stride == p.v_stride && p.k_stride <= most);
+    return plain ? start(attn_c<kAttnPlain>) : start(attn_c<2>);
+  }
+  if constexpr (DT != kF32) {
+    if (vec == 0) return start(attn_c<0>);
+  }
+  return start(attn_c<1>);
 }
 
 }  // namespace sc

@@ -10,6 +10,14 @@ struct AttnItem {      // a workgroup's share: a tile of a sequence
   int32_t tile, pad;
 };
 
+struct AttnZeros {                     // dropped rows of up to three dense outputs
+  const int32_t* slot;                 // null: every row is dropped
+  int64_t rows;
+  void* out[3];
+  int64_t stride[3], width[3];         // bytes
+  int32_t blocks, vec;                 // workgroups that write them (0: none); whole 16-byte groups
+};
+
 struct AttnParams {
   const void *q, *k, *v, *o, *d_o;
   void *out, *dq, *dk, *dv;
@@ -22,10 +30,11 @@ struct AttnParams {
   int32_t causal, window;              // window 0: none
   uint32_t magic;                      // ceil(2^20 / group)
   float scale;
+  AttnZeros zeros;
 };
 
-// waves: wavefronts of a workgroup; vec: all rows are whole 16-byte groups
-template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, bool vec, hipStream_t s);
+// waves: wavefronts of a workgroup; vec: rows are whole 16-byte groups (2), 4-byte ones (1) or neither (0)
+template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, int vec, hipStream_t s);
 
 constexpr int kAttnKeyWaves = 4;                            // wavefronts of a workgroup of the keys' gradients, 32 keys each
 enum { kAttnForward, kAttnBackwardQ, kAttnBackwardKV };

@@ -153,13 +153,13 @@ template <int DT, int DP> struct AttnTile {
   }
 
   // a lane's share of a row in memory (channel groups 2 ks + h), as second operand of the products along; zeros beyond d
-  template <bool VEC> static __device__ __forceinline__ void read_row(const T* row, int d, int h, bool there, v4i (&f)[KS]) {
+  template <int VEC> static __device__ __forceinline__ void read_row(const T* row, int d, int h, bool there, v4i (&f)[KS]) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) f[ks] = group<VEC>(row, (2 * ks + h) * V, d, there);
   }
-  template <bool VEC> static __device__ __forceinline__ v4i group(const T* row, int c, int d, bool there) {
+  template <int VEC> static __device__ __forceinline__ v4i group(const T* row, int c, int d, bool there) {
     v4i g = {0, 0, 0, 0};
-    if constexpr (VEC) {
+    if constexpr (VEC == 2) {
       if (there && c < d) g = *reinterpret_cast<const v4i*>(row + c);
     } else {
       T e[V];
@@ -171,11 +171,11 @@ template <int DT, int DP> struct AttnTile {
   }
 
   // 16 channels from c0 on of a row, from a lane's results
-  template <bool VEC> static __device__ __forceinline__ void write_16(T* row, int c0, int d, const floatx16& o, float factor) {
+  template <int VEC> static __device__ __forceinline__ void write_16(T* row, int c0, int d, const floatx16& o, float factor) {
     T r[16];
 #pragma unroll
     for (int v = 0; v < 16; ++v) r[v] = E::from_float(o[v] * factor);
-    if constexpr (VEC) {
+    if constexpr (VEC == 2) {
       v4i g[EB];
       __builtin_memcpy(g, r, sizeof(r));
 #pragma unroll
@@ -210,19 +210,29 @@ template <int DT, int DP> struct AttnTile {
 
   // Transfer of ROWS rows by NT lanes: `place(r)` is the row's address in memory, null for a row of zeros.
   template <int ROWS, int NT> static constexpr int transfers() { return ROWS * GROUPS / NT; }
-  template <int ROWS, int NT, bool VEC, class Place>
+  template <int ROWS, int NT, int VEC, class Place>
   static __device__ __forceinline__ void request(unsigned tile, int d, Place&& place) {
     constexpr int J = ROWS * GROUPS / NT;
     static_assert(J >= 1 && ROWS * GROUPS % NT == 0, "whole transfers");
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    if constexpr (VEC == 1) {      // 4 bytes a lane
+      constexpr int WORDS = RB / 4, PER = 4 / EB;
+#pragma unroll
+      for (int j = 0; j < 4 * J; ++j) {
+        const int at = j * NT + t, r = at / WORDS, word = at % WORDS, c = (((word >> 2) ^ key(r)) << 2 | (word & 3)) * PER;
+        const T* row = place(r);
+        attn_dma4(row && c < d ? (const void*)(row + c) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 4);
+      }
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int at = j * NT + t, r = at / GROUPS, g = (at % GROUPS) ^ key(r);
       const T* row = place(r);
-      if constexpr (VEC) {
+      if constexpr (VEC == 2) {
         attn_dma16(row && g * V < d ? (const void*)(row + g * V) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 16);
       } else {
-        *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<false>(row, g * V, d, row != nullptr);
+        *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<0>(row, g * V, d, row != nullptr);
       }
     }
   }

@@ -58,8 +58,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
   const int group = p.heads / p.kv_heads, col = block * 32 + l32, q_head = head * group + col;
   const bool there = col < group;
   v4i qf[A::KS];
-  if (p.vec) A::template read_row<true>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
-  else A::template read_row<false>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
+  if (p.vec) A::template read_row<2>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
+  else A::template read_row<0>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
   __syncthreads();
 
   const unsigned lds = attn_lds(smem) + wave * (LDS_WAVE + SCALES), at_scales = lds + LDS_WAVE;

@@ -67,6 +67,12 @@ CASES = [  # lengths, heads, kv heads, d, dtype, causal, window, share of rows k
     ([40, 0, 0, 24], 2, 2, 64, "bf16", True, 0, 0.0, 0, 4),
     ([513], 2, 1, 128, "bf16", False, 100, 1.0, 0, 0),
     ([3] * 50, 8, 8, 64, "f16", True, 0, 0.7, 0, 0),
+    ([150, 40], 6, 3, 50, "bf16", True, 0, 0.8, 0, 2),
+    ([150, 40], 4, 4, 110, "f16", False, 0, 1.0, 0, 0),
+    ([600], 8, 2, 128, "bf16", True, 0, 1.0, 0, 0),
+    ([600, 550], 4, 1, 64, "f16", True, 200, 0.9, 0, 0),
+    ([550], 3, 1, 125, "bf16", True, 0, 1.0, 0, 0),
+    ([700], 2, 1, 66, "bf16", False, 0, 1.0, 0, 0),
 ]
 
 
@@ -137,7 +143,7 @@ def test_packed_forward_and_gradients(c):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("pad", [1, 8])
+@pytest.mark.parametrize("pad", [1, 2, 8])
 def test_rows_with_gaps(dtype, pad):
     packed_check(([70, 33], 4, 2, 64, dtype, True, 0, 0.8, 0, 1), 3, pad)
 
