@@ -217,22 +217,27 @@ template <int DT, int DP> struct AttnTile {
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     if constexpr (VEC == 1) {      // 4 bytes a lane
       constexpr int WORDS = RB / 4, PER = 4 / EB;
+      const void* from[4 * J];
 #pragma unroll
       for (int j = 0; j < 4 * J; ++j) {
         const int at = j * NT + t, r = at / WORDS, word = at % WORDS, c = (((word >> 2) ^ key(r)) << 2 | (word & 3)) * PER;
         const T* row = place(r);
-        attn_dma4(row && c < d ? (const void*)(row + c) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 4);
+        from[j] = row && c < d ? (const void*)(row + c) : (const void*)&attn_zeros;
       }
+#pragma unroll
+      for (int j = 0; j < 4 * J; ++j) attn_dma4(from[j], tile + (j * NT + wave * 64) * 4);
       return;
     }
+    const T* from[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) from[j] = place((j * NT + t) / GROUPS);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      const int at = j * NT + t, r = at / GROUPS, g = (at % GROUPS) ^ key(r);
-      const T* row = place(r);
+      const int at = j * NT + t, g = (at % GROUPS) ^ key(at / GROUPS);
       if constexpr (VEC == 2) {
-        attn_dma16(row && g * V < d ? (const void*)(row + g * V) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 16);
+        attn_dma16(from[j] && g * V < d ? (const void*)(from[j] + g * V) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 16);
       } else {
-        *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<0>(row, g * V, d, row != nullptr);
+        *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<0>(from[j], g * V, d, from[j] != nullptr);
       }
     }
   }
