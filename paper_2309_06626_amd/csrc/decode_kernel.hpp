@@ -13,15 +13,58 @@
 
 namespace sc {
 
-// 8-bit codes as entries of the type: whole numbers up to 127 are exact in all of them.
-template <typename T> __device__ __forceinline__ void decode_widen(v4i codes, T (&out)[16]) {
+// 8-bit codes as entries of the type: whole numbers up to 127 are exact in it.
+__device__ __forceinline__ void decode_widen(v4i codes, float (&out)[16]) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) out[i] = (T)(float)(int8_t)(codes[i >> 2] >> (8 * (i & 3)));
+  for (int i = 0; i < 16; ++i) out[i] = (float)(int8_t)(codes[i >> 2] >> (8 * (i & 3)));
+}
+// A byte below a half's 0x64 is 1 024 and the byte: code + 128 of these bytes, two at a time, less 1 152.
+__device__ __forceinline__ void decode_widen(v4i codes, _Float16 (&out)[16]) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned bytes = (unsigned)codes[i] ^ 0x80808080u;
+    const f16x2 less = {(_Float16)1152, (_Float16)1152};
+    const f16x2 low = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, bytes, 0x04010400u)) - less;
+    const f16x2 high = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, bytes, 0x04030402u)) - less;
+    out[4 * i] = low[0];
+    out[4 * i + 1] = low[1];
+    out[4 * i + 2] = high[0];
+    out[4 * i + 3] = high[1];
+  }
+}
+
+// What a lane holds of a row of q, as f16: in units of a power of two, so that the largest entry is between 2^13 and 2^14 (none is lost that
+// is not below 2^-37 of it).  Returns the unit.
+template <class From, class To, int KS> __device__ __forceinline__ float decode_narrow(const v4i (&from)[KS], v4i (&to)[KS]) {
+  float x[KS][8], most = 0.0f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    From e[8];
+    __builtin_memcpy(e, &from[ks], 16);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[ks][i] = (float)e[i];
+      most = fmaxf(most, fabsf(x[ks][i]));
+    }
+  }
+  most = attn_max_halves(most);
+  const int up = most > 0.0f && most <= 3.4e38f ? min(14 - __builtin_amdgcn_frexp_expf(most), 100) : 0;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    To e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = (To)__builtin_amdgcn_ldexpf(x[ks][i], up);
+    __builtin_memcpy(&to[ks], e, 16);
+  }
+  return __builtin_amdgcn_ldexpf(1.0f, -up);
 }
 
 template <int DT, int DP, bool BITS8>
-__global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const DecodeParams p) {
-  using A = AttnTile<DT, DP>;
+__global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) void decode_kernel(const DecodeParams p) {
+  using IO = typename Elem<DT>::T;                             // of q and o
+  constexpr int CT = BITS8 && DT == kBF16 ? kF16 : DT;         // codes are multiplied in f16, which they are widened to in the fewest operations
+  using A = AttnTile<CT, DP>;
   using T = typename A::T;
   constexpr int TILE = 32 * A::RB, STAGES = BITS8 || A::RB > 256 ? 1 : 2, SCALES = 2 * 32 * 4;
   constexpr int LDS_WAVE = 2 * TILE * STAGES;
@@ -58,8 +101,20 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
   const int group = p.heads / p.kv_heads, col = block * 32 + l32, q_head = head * group + col;
   const bool there = col < group;
   v4i qf[A::KS];
-  if (p.vec) A::template read_row<2>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
-  else A::template read_row<0>(static_cast<const T*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d, p.d, h, there, qf);
+  float c = p.scale * 1.4426950408889634f;                     // of a product of q and k; of this lane's row
+  {
+    using Q = AttnTile<DT, DP>;
+    v4i f[Q::KS];
+    const IO* const q = static_cast<const IO*>(p.q) + (row * p.heads + (there ? q_head : 0)) * p.d;
+    if (p.vec) Q::template read_row<2>(q, p.d, h, there, f);
+    else Q::template read_row<0>(q, p.d, h, there, f);
+    if constexpr (CT != DT) {
+      c = fmaxf(c * decode_narrow<IO, T>(f, qf), 1e-37f);      // (not 0, whatever the scale: what is not seen is -infinity times it)
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < A::KS; ++ks) qf[ks] = f[ks];
+    }
+  }
   __syncthreads();
 
   const unsigned lds = attn_lds(smem) + wave * (LDS_WAVE + SCALES), at_scales = lds + LDS_WAVE;
@@ -73,17 +128,17 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
   };
   const unsigned char *const k_pages = static_cast<const unsigned char*>(p.k_pages), *const v_pages = static_cast<const unsigned char*>(p.v_pages);
   // entries as they are: straight into LDS
-  auto request = [&](int i, int at_row) {
-    const unsigned at = lds + (i % STAGES) * 2 * TILE;
+  auto request = [&](const unsigned char* pages, unsigned at, int at_row) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int place = j * 64 + lane, r = place / A::GROUPS, g = (place % A::GROUPS) ^ A::key(r);
       const int64_t of = __shfl(at_row, r);
       const bool in = of >= 0 && g * 16 < p.row_bytes;
-      attn_dma16(in ? (const void*)(k_pages + of * p.row_bytes + g * 16) : (const void*)&attn_zeros, at + j * 1024);
-      attn_dma16(in ? (const void*)(v_pages + of * p.row_bytes + g * 16) : (const void*)&attn_zeros, at + TILE + j * 1024);
+      attn_dma16(in ? (const void*)(pages + of * p.row_bytes + g * 16) : (const void*)&attn_zeros, at + j * 1024);
     }
   };
+  auto request_k = [&](int i, int at_row) { request(k_pages, lds + (i % STAGES) * TILE, at_row); };
+  auto request_v = [&](int i, int at_row) { request(v_pages, lds + (STAGES + i % STAGES) * TILE, at_row); };
   // codes: into registers, widened on the way to LDS
   constexpr int CG = DP / 16, CJ = BITS8 ? 32 * CG / 64 : 1;   // 16-byte groups of a row, and transfers of a tile
   struct Codes { v4i k[CJ], v[CJ]; float k_scale, v_scale; };
@@ -104,21 +159,23 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
     return c;
   };
   auto widen = [&](const Codes& c) {
+    if constexpr (BITS8) {
 #pragma unroll
-    for (int j = 0; j < CJ; ++j) {
-      const int place = j * 64 + lane, r = place / CG, g = place % CG;
+      for (int j = 0; j < CJ; ++j) {
+        const int place = j * 64 + lane, r = place / CG, g = place % CG;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        T e[16];
-        decode_widen(k ? c.v[j] : c.k[j], e);
-        v4i w[A::EB];
-        __builtin_memcpy(w, e, sizeof(e));
+        for (int k = 0; k < 2; ++k) {
+          T e[16];
+          decode_widen(k ? c.v[j] : c.k[j], e);
+          v4i w[A::EB];
+          __builtin_memcpy(w, e, sizeof(e));
 #pragma unroll
-        for (int i = 0; i < A::EB; ++i)
-          *(__attribute__((address_space(3))) v4i*)(uint64_t)(lds + k * TILE + r * A::RB + (((g * A::EB + i) ^ A::key(r)) << 4)) = w[i];
+          for (int i = 0; i < A::EB; ++i)
+            *(__attribute__((address_space(3))) v4i*)(uint64_t)(lds + k * TILE * STAGES + r * A::RB + (((g * A::EB + i) ^ A::key(r)) << 4)) = w[i];
+        }
       }
+      *(__attribute__((address_space(3))) float*)(uint64_t)(at_scales + lane * 4) = h ? c.v_scale : c.k_scale;
     }
-    *(__attribute__((address_space(3))) float*)(uint64_t)(at_scales + lane * 4) = h ? c.v_scale : c.k_scale;
   };
 
   const typename A::Along along = A::along(lane);
@@ -128,43 +185,63 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
   for (int db = 0; db < A::DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
-  const float c = p.scale * 1.4426950408889634f;
   float m = -INFINITY, sum = 0.0f;                             // m is a maximum times c, as it was rounded
-  float unit = 0.0f;                                           // of SC_F16 and codes: acc is in units of it, see below
+  float unit = 0.0f;                                           // of codes in f16: acc is in units of it, see below
 
   typedef __attribute__((address_space(3))) const v4f lds_v4f;
-  int row_now = mine > 0 ? cache_row(0) : -1, row_next = -1;
+  // Entries as they are: with two places for keys and two for values, whatever is in LDS is asked for again as soon as it has been multiplied, so
+  // that three transfers of a tile are on their way all the time.  All but the youngest of them have landed, when N are waited for:
+  auto wait = [&](int on_their_way) {
+    if (on_their_way >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * J <= 63 ? 3 * J : 63) : "memory");
+    else if (on_their_way == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * J <= 63 ? 2 * J : 63) : "memory");
+    else if (on_their_way == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(J) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  };
+  int rows[3] = {-1, -1, -1};                                  // of this tile and of the two behind it
+  if (mine > 0) rows[0] = cache_row(0);
+  if (mine > 1) rows[1] = cache_row(1);
   Codes codes;
   if constexpr (BITS8) {
-    if (mine > 0) codes = fetch(row_now);
-  } else {
-    if (STAGES > 1 && mine > 0) request(0, row_now);
+    if (mine > 0) codes = fetch(rows[0]);
+  } else if constexpr (STAGES > 1) {
+    if (mine > 0) {
+      request_k(0, rows[0]);
+      request_v(0, rows[0]);
+    }
+    if (mine > 1) {
+      request_k(1, rows[1]);
+      request_v(1, rows[1]);
+    }
   }
   for (int i = 0; i < mine; ++i) {
-    if (i + 1 < mine) row_next = cache_row(i + 1);
-    const uint64_t seen = __ballot(row_now >= 0);
+    const int left = mine - 1 - i;                             // tiles behind this one
+    const uint64_t seen = __ballot(rows[0] >= 0);
+    rows[2] = left > 1 ? cache_row(i + 2) : -1;
     if constexpr (BITS8) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the tile before is in registers)
       widen(codes);
-      if (i + 1 < mine) codes = fetch(row_next);
+      if (left > 0) codes = fetch(rows[1]);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    } else if constexpr (STAGES == 1) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      request_k(i, rows[0]);
+      request_v(i, rows[0]);
+      wait(0);
     } else {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the tile before last is in registers)
-      if (STAGES == 1) request(i, row_now);
-      if (STAGES > 1 && i + 1 < mine) {
-        request(i + 1, row_next);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * J <= 63 ? 2 * J : 63) : "memory");
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
+      wait(left > 0 ? 3 : 1);
     }
-    row_now = row_next;
-    const unsigned at_k = lds + (i % STAGES) * 2 * TILE, at_v = at_k + TILE;
+    const unsigned at_k = lds + (i % STAGES) * TILE, at_v = lds + (STAGES + i % STAGES) * TILE;
     floatx16 s;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, at_k, 0, ks), qf[ks]);
+    if constexpr (!BITS8 && STAGES > 1) {
+      if (left > 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        request_k(i + 2, rows[2]);
+      }
+    }
     if constexpr (BITS8) {
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
@@ -195,7 +272,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
       // weights of the codes: p times the value's scale.  In f16 they are taken in units of a power of two near the largest scale so far,
       // so that they keep their digits whatever the values' size.
       float per_unit = 1.0f;
-      if constexpr (DT == kF16) {
+      if constexpr (CT == kF16) {
         float big = *(__attribute__((address_space(3))) const float*)(uint64_t)(at_scales + (32 + l32) * 4);
         big = __builtin_isfinite(big) ? big : 0.0f;
 #pragma unroll
@@ -211,7 +288,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
       for (int a = 0; a < 4; ++a) {
         const v4f v_scale = *(lds_v4f*)(uint64_t)(at_scales + (32 + 8 * a + 4 * h) * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * a + e] *= DT == kF16 ? v_scale[e] * per_unit : v_scale[e];
+        for (int e = 0; e < 4; ++e) s[4 * a + e] *= CT == kF16 ? v_scale[e] * per_unit : v_scale[e];
       }
     }
     if (attn_any(less != 1.0f)) {
@@ -222,12 +299,21 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
     }
     v4i pf[A::SS];
     A::pack(s, pf);
+    if constexpr (!BITS8 && STAGES > 1) wait(left > 1 ? 3 : 2 * left);
 #pragma unroll
     for (int ss = 0; ss < A::SS; ++ss)
 #pragma unroll
       for (int db = 0; db < A::DB; ++db) A::E::mma(acc[db], A::read_across(across, at_v, 0, ss, db), pf[ss]);
+    if constexpr (!BITS8 && STAGES > 1) {
+      if (left > 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        request_v(i + 2, rows[2]);
+      }
+    }
+    rows[0] = rows[1];
+    rows[1] = rows[2];
   }
-  if constexpr (BITS8 && DT == kF16) {
+  if constexpr (BITS8 && CT == kF16) {
 #pragma unroll
     for (int db = 0; db < A::DB; ++db)
 #pragma unroll
@@ -273,7 +359,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
     }
     const int64_t head_row = row * p.heads + head * group + block * 32 + q;
     if (p.splits == 1) {
-      if (ch < p.d) static_cast<T*>(p.o)[head_row * p.d + ch] = A::E::from_float(all == 0.0f ? 0.0f : out / all);
+      if (ch < p.d) static_cast<IO*>(p.o)[head_row * p.d + ch] = Elem<DT>::from_float(all == 0.0f ? 0.0f : out / all);
     } else {
       p.part_o[(head_row * p.splits + split) * DP + ch] = out;
       if (ch == 0) {
@@ -284,27 +370,45 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 1) void decode_kernel(const Deco
   }
 }
 
-// the stretches' shares of a head, in order
-template <int DT, int DP> __global__ __launch_bounds__(DP) void decode_join_kernel(const DecodeParams p) {
+// The stretches' shares of a head, in a fixed order: eight teams of lanes take every eighth one each, four channels a lane.
+template <int DT, int DP> __global__ __launch_bounds__(2 * DP) void decode_join_kernel(const DecodeParams p) {
   using T = typename Elem<DT>::T;
+  constexpr int LANES = DP / 4, TEAMS = 8;
+  __shared__ v4f s_out[TEAMS][LANES];
+  __shared__ float s_all[TEAMS];
   const int64_t head_row = blockIdx.x;
-  const int ch = threadIdx.x;
+  const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
   const float* const stat = p.part_m + head_row * p.splits * 2;
   float top = -INFINITY;
+#pragma unroll 8
   for (int s = 0; s < p.splits; ++s) top = fmaxf(top, stat[2 * s]);
-  float all = 0.0f, out = 0.0f;
-  for (int s = 0; s < p.splits; ++s) {
-    const float sum = stat[2 * s + 1];
-    if (sum == 0.0f) continue;
-    const float f = attn_exp2(stat[2 * s] - top);
+  float all = 0.0f;
+  v4f out = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = team; s < p.splits; s += TEAMS) {
+    const float sum = stat[2 * s + 1], f = sum == 0.0f ? 0.0f : attn_exp2(stat[2 * s] - top);
+    const v4f part = *reinterpret_cast<const v4f*>(p.part_o + (head_row * p.splits + s) * DP + 4 * lane);
     all += sum * f;
-    out += p.part_o[(head_row * p.splits + s) * DP + ch] * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] += part[e] * f;
   }
-  if (ch < p.d) static_cast<T*>(p.o)[head_row * p.d + ch] = Elem<DT>::from_float(all == 0.0f ? 0.0f : out / all);
+  s_out[team][lane] = out;
+  if (lane == 0) s_all[team] = all;
+  __syncthreads();
+  if (team != 0) return;
+#pragma unroll
+  for (int i = 1; i < TEAMS; ++i) {
+    all += s_all[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] += s_out[i][lane][e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (4 * lane + e < p.d) static_cast<T*>(p.o)[head_row * p.d + 4 * lane + e] = Elem<DT>::from_float(all == 0.0f ? 0.0f : out[e] / all);
 }
 
 template <int DT, int DP, bool BITS8> static hipError_t decode_start(const DecodeParams& p, hipStream_t s) {
-  using A = AttnTile<DT, DP>;
+  using A = AttnTile<BITS8 && DT == kBF16 ? kF16 : DT, DP>;
   constexpr int wave = 2 * 32 * A::RB * (BITS8 || A::RB > 256 ? 1 : 2) + 2 * 32 * 4, join = kDecodeWaves * 32 * (DP + 2) * 4;
   constexpr int lds = (kDecodeWaves * wave + kDecodePages * 4) > join ? kDecodeWaves * wave + kDecodePages * 4 : join;
   static_assert(lds <= 160 * 1024, "LDS of a compute unit");
@@ -314,7 +418,7 @@ template <int DT, int DP, bool BITS8> static hipError_t decode_start(const Decod
     if (e != hipSuccess) return e;
   }
   kernel<<<dim3((unsigned)(p.rows * p.blocks * p.kv_heads * p.splits)), dim3(64 * kDecodeWaves), lds, s>>>(p);
-  if (p.splits > 1) decode_join_kernel<DT, DP><<<dim3((unsigned)(p.rows * p.heads)), dim3(DP), 0, s>>>(p);
+  if (p.splits > 1) decode_join_kernel<DT, DP><<<dim3((unsigned)(p.rows * p.heads)), dim3(2 * DP), 0, s>>>(p);
   return hipGetLastError();
 }
 

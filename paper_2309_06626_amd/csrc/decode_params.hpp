@@ -6,7 +6,7 @@
 namespace sc {
 
 constexpr int kDecodeWaves = 4;         // wavefronts of a workgroup
-constexpr int kDecodePages = 4096;      // entries of the page table that a workgroup holds
+constexpr int kDecodePages = 2048;      // entries of the page table that a workgroup holds (two with codes fit a compute unit's LDS)
 
 struct DecodeParams {
   const void *q, *k_pages, *v_pages;
