@@ -191,11 +191,11 @@ template <int DT, int DP> struct AttnTile {
   // The same of rows of DP channels, `group` of them together and such groups `stride` entries apart: offsets of a lane's transfers, worked out
   // once, from the first row.
   template <int ROWS, int NT> struct Offsets { unsigned at[ROWS * GROUPS / NT]; };
-  template <int ROWS, int NT> static __device__ __forceinline__ Offsets<ROWS, NT> offsets(int64_t stride, int group = 1) {
+  template <int ROWS, int NT> static __device__ __forceinline__ Offsets<ROWS, NT> offsets(int64_t stride, int group = 1, int t = threadIdx.x) {
     Offsets<ROWS, NT> o;
 #pragma unroll
     for (int j = 0; j < ROWS * GROUPS / NT; ++j) {
-      const int at = j * NT + threadIdx.x, r = at / GROUPS;
+      const int at = j * NT + t, r = at / GROUPS;
       o.at[j] = (unsigned)(r / group * (int)stride * EB + r % group * RB + ((at % GROUPS) ^ key(r)) * 16);
     }
     return o;

@@ -128,7 +128,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
   };
   const unsigned char *const k_pages = static_cast<const unsigned char*>(p.k_pages), *const v_pages = static_cast<const unsigned char*>(p.v_pages);
   // entries as they are: straight into LDS
+  const bool near = p.shift >= 5 && p.row_bytes == A::RB;      // a tile whose rows are all there is one piece of memory
+  const auto off = A::template offsets<32, 64>(DP, 1, lane);
   auto request = [&](const unsigned char* pages, unsigned at, int at_row) {
+    if (near && __ballot(at_row < 0) == 0) {
+      const int64_t of = __builtin_amdgcn_readfirstlane(at_row);
+#pragma unroll
+      for (int j = 0; j < J; ++j) attn_dma16(pages + of * A::RB, off.at[j], at + j * 1024);
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int place = j * 64 + lane, r = place / A::GROUPS, g = (place % A::GROUPS) ^ A::key(r);
