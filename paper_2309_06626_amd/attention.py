@@ -16,7 +16,8 @@ from . import block as K
 from .block import (DTYPE_CODE, SC_BF16, SC_F16, SC_F32, SC_ROWS_COMPACT, SC_ROWS_DENSE, TORCH_DTYPE, RowSet, ScError,  # noqa: F401
                     sparse_rows_info, sparse_rows_plan, sparse_rows_set_mask)
 
-_F32, _I8 = torch.float32, torch.int8
+_F32, _I8, _I64, _I32 = torch.float32, torch.int8, torch.int64, torch.int32
+_current_device = K._current_device
 
 
 class sc_attn_desc(ctypes.Structure):
@@ -69,12 +70,25 @@ def make_kv_desc(kv_heads, d, page_rows, pages, dtype=SC_BF16, bits=0) -> sc_kv_
     return sc_kv_desc(kv_heads, d, page_rows, pages, dtype, bits)
 
 
-def _matrix(t: torch.Tensor, what: str, rows: Optional[int], width: int, dtype: torch.dtype) -> Tuple[int, int]:
-    """Address and stride of `rows` (None: any number of) rows of `width` entries that lie together; a row may have several dimensions."""
+def _matrix(t: torch.Tensor, what: str, rows: int, width: int, dtype: torch.dtype) -> Tuple[int, int]:
+    """Address and stride of `rows` rows of `width` entries that lie together; a row may have several dimensions.  The calls for single tokens
+    spend as long here as on the GPU: two cases that hold nearly always first, the reason looked for afterwards."""
+    if t.dtype is dtype and t.is_cuda and t.get_device() == _current_device():
+        shape = t.shape
+        if shape and shape[0] == rows:
+            if t.is_contiguous():
+                if t.numel() == rows * width:
+                    return t.data_ptr(), width
+            elif len(shape) == 2 and shape[1] == width:
+                stride, inner = t.stride()
+                if inner == 1:
+                    return t.data_ptr(), stride
     if t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
+    if t.get_device() != _current_device():
+        raise ValueError(f"{what} is on another device than the current one")
     if t.dim() < 2:
         raise ValueError(f"{what} must have rows")
     inner = 1
@@ -84,7 +98,7 @@ def _matrix(t: torch.Tensor, what: str, rows: Optional[int], width: int, dtype: 
         inner *= size
     if inner != width:
         raise ValueError(f"a row of {what} has {inner} entries, the call needs {width}")
-    if rows is not None and t.shape[0] != rows:
+    if t.shape[0] != rows:
         raise ValueError(f"{what} has {t.shape[0]} rows, the call needs {rows}")
     stride = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
     return t.data_ptr(), stride
@@ -98,7 +112,7 @@ class AttnPlan:
 
     def __init__(self, handle: int, desc: sc_attn_desc, workspace: torch.Tensor):
         self.handle = handle
-        self.desc = desc
+        self.desc = sc_attn_desc.from_buffer_copy(desc)
         self.workspace = workspace
         end, kept = ctypes.c_int64(), ctypes.c_int64()
         B._check(lib().sparse_attn_info(handle, ctypes.byref(end), ctypes.byref(kept)), "sparse_attn_info")
@@ -225,7 +239,8 @@ class KvCache:
             t = torch.zeros(shape, dtype=_F32, device=device) if t is None else t
             return t, K._tensor(t, what, math.prod(shape), _F32)
 
-        self.desc, self.type = desc, K._elem(desc)
+        self.desc, self.type = sc_kv_desc.from_buffer_copy(desc), K._elem(desc)
+        self._reference, self._width = ctypes.byref(self.desc), desc.kv_heads * desc.d
         (self.k_pages, k), (self.v_pages, v) = pages(k_pages, "k_pages"), pages(v_pages, "v_pages")
         (self.k_scales, ks), (self.v_scales, vs) = scales(k_scales, "k_scales"), scales(v_scales, "v_scales")
         self._addresses = (k, v, ks, vs)
@@ -233,10 +248,11 @@ class KvCache:
 
 def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:
     """k, v: [rows, ...] with rows of kv_heads * d entries that lie together; slots: int64[rows], places page * page_rows + row."""
-    d, n = cache.desc, slots.numel()
-    width = d.kv_heads * d.d
-    status = lib().sparse_kv_write(ctypes.byref(d), n, *_matrix(k, "k", n, width, cache.type), *_matrix(v, "v", n, width, cache.type),
-                                   K._tensor(slots, "slots", n, torch.int64), *cache._addresses, K._stream_handle(stream))
+    n, width, t = slots.numel(), cache._width, cache.type
+    k_at, k_stride = _matrix(k, "k", n, width, t)
+    v_at, v_stride = _matrix(v, "v", n, width, t)
+    status = lib().sparse_kv_write(cache._reference, n, k_at, k_stride, v_at, v_stride, K._tensor(slots, "slots", n, _I64), *cache._addresses,
+                                   K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_kv_write")
     return cache
@@ -244,10 +260,11 @@ def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:
 
 def sparse_kv_read(cache: KvCache, slots, k, v, stream=None):
     """Rows of the cache at slots into k and v; zeros where a slot is not in the cache."""
-    d, n = cache.desc, slots.numel()
-    width = d.kv_heads * d.d
-    status = lib().sparse_kv_read(ctypes.byref(d), n, K._tensor(slots, "slots", n, torch.int64), *cache._addresses,
-                                  *_matrix(k, "k", n, width, cache.type), *_matrix(v, "v", n, width, cache.type), K._stream_handle(stream))
+    n, width, t = slots.numel(), cache._width, cache.type
+    k_at, k_stride = _matrix(k, "k", n, width, t)
+    v_at, v_stride = _matrix(v, "v", n, width, t)
+    status = lib().sparse_kv_read(cache._reference, n, K._tensor(slots, "slots", n, _I64), *cache._addresses, k_at, k_stride, v_at, v_stride,
+                                  K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_kv_read")
     return k, v
@@ -270,12 +287,12 @@ def sparse_attn_decode(desc: sc_attn_desc, cache: KvCache, q, table, lengths, o,
         raise ValueError("the descriptors' types differ")
     if table.dim() != 2 or table.shape[0] != n:
         raise ValueError(f"table must be [{n}, pages of a sequence]")
-    tensor = K._tensor
+    tensor, width = K._tensor, table.shape[1]
     at, size = K._workspace(workspace)
     status = lib().sparse_attn_decode(
-        ctypes.byref(desc), ctypes.byref(cache.desc), n, tensor(q, "q", n * wide, t), tensor(table, "table", table.numel(), torch.int32),
-        table.shape[1], tensor(lengths, "lengths", n, torch.int32), *cache._addresses, tensor(o, "o", n * wide, t), at, size,
-        K._stream_handle(stream))
+        ctypes.byref(desc), cache._reference, n, _matrix(q, "q", n, wide, t)[0] if q.is_contiguous() else tensor(q, "q", n * wide, t),
+        tensor(table, "table", n * width, _I32), width, tensor(lengths, "lengths", n, _I32), *cache._addresses, tensor(o, "o", n * wide, t), at,
+        size, K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_attn_decode")
     return o

@@ -94,17 +94,26 @@ template <typename T, bool BITS8, bool VEC> __global__ __launch_bounds__(256) vo
       for (int s = 1; s < kKvLanes; s <<= 1) most = max(most, (unsigned)__shfl_xor((int)most, s));
       const bool finite = most < 0x7f800000u;
       const float scale = finite ? fmaxf(__fdiv_rn(__builtin_bit_cast(float, most), 127.0f), 0x1p-126f) : __builtin_nanf("");
-      uint64_t codes = 0;
+      // x / scale by a product may lie on the other side of a half: what is left of x is exact there, and decides
+      const float per = finite ? __fdiv_rn(1.0f, scale) : 0.0f, half = 0.5f * scale;
+      float code[kKvChannels], left[kKvChannels], most_left = 0.0f;
 #pragma unroll
       for (int i = 0; i < kKvChannels; ++i) {
-        // the quotient rounded may lie on the other side of a half: what is left of x is exact, and decides
-        float code = finite ? rintf(__fdiv_rn(x[k][i], scale)) : 0.0f;
-        const float left = finite ? __builtin_fmaf(-code, scale, x[k][i]) : 0.0f, half = 0.5f * scale;
-        const bool odd = (int)code & 1;
-        if (left > half || (left == half && odd)) code += 1.0f;
-        if (left < -half || (left == -half && odd)) code -= 1.0f;
-        codes |= (uint64_t)(uint8_t)(int8_t)(int)code << (8 * i);
+        code[i] = finite ? rintf(x[k][i] * per) : 0.0f;
+        left[i] = __builtin_fmaf(-code[i], scale, x[k][i]);
+        most_left = fmaxf(most_left, fabsf(left[i]));
       }
+      if (most_left >= half) {
+#pragma unroll
+        for (int i = 0; i < kKvChannels; ++i) {
+          const bool odd = (int)code[i] & 1;
+          if (left[i] > half || (left[i] == half && odd)) code[i] += 1.0f;
+          else if (left[i] < -half || (left[i] == -half && odd)) code[i] -= 1.0f;
+        }
+      }
+      uint64_t codes = 0;
+#pragma unroll
+      for (int i = 0; i < kKvChannels; ++i) codes |= (uint64_t)(uint8_t)(int8_t)(int)code[i] << (8 * i);
       if (c < p.entries) *reinterpret_cast<uint64_t*>(static_cast<int8_t*>(p.pages[k]) + at * p.entries + c) = codes;
       if (c == 0) p.scales[k][at] = scale;
     } else {

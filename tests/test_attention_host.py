@@ -206,6 +206,10 @@ class Recorder:
 class OnDevice(torch.Tensor):
     """A host tensor that says it is on the device."""
     is_cuda = True
+    device_index = 0
+
+    def get_device(self):
+        return self.device_index
 
 
 def fake(*shape, dtype=torch.bfloat16):
@@ -217,6 +221,7 @@ def recorder(monkeypatch):
     r = Recorder()
     monkeypatch.setattr(A, "lib", lambda: r)
     monkeypatch.setattr(A.K, "_stream_handle", lambda stream: 0)
+    monkeypatch.setattr(A, "_current_device", lambda: 0)
     return r
 
 
@@ -246,6 +251,10 @@ def test_binding_looks_at_rows_types_and_strides(recorder):
                 lambda: A.sparse_attn_run(plan, q[0], k, k, o)):
         with pytest.raises(ValueError):
             bad()
+    elsewhere = fake(10, 2, 64)
+    elsewhere.device_index = 1
+    with pytest.raises(ValueError, match="another device"):
+        A.sparse_attn_run(plan, q, elsewhere, k, o)
     plan.handle = None
     with pytest.raises(ValueError, match="closed"):
         A.sparse_attn_run(plan, q, k, k, o)
