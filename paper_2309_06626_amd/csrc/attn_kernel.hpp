@@ -322,20 +322,27 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (VEC < 2 && NW ==
 // the next step, the vector unit makes probabilities and gradients of scores of this one; then those are multiplied.  Tiles (one or two
 // steps) lie in three places in LDS: one whose second half is still multiplied, the next, and one on its way.
 
-// An order of the instructions of a step: A products with one LDS read each (and vector work beside them), then B with R reads each, every read
-// three products ahead of the one that takes it; FIRST other reads before.
-template <int A, int B, int R, int FIRST, int VECTOR> __device__ __forceinline__ void attn_order_step() {
+// Orders of the instructions of a step.  Products of scores: N, a read of LDS each (FIRST others before, MORE behind, of the products that
+// follow), and the vector unit's work beside them.  Products across: N, two reads each, of which FIRST have been there before.
+template <int N, int FIRST, int MORE, int VECTOR> __device__ __forceinline__ void attn_order_scores() {
   __builtin_amdgcn_sched_group_barrier(0x100, FIRST + 3, 0);
-  attn_for<0, A + B>([&](auto at) {
+  attn_for<0, N>([&](auto at) {
     constexpr int i = decltype(at)::value;
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if constexpr (i + 3 < A) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    else if constexpr (i + 3 < A + B) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-    if constexpr (i < A) {
-      __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, 16 / A, 0);
-    }
+    __builtin_amdgcn_sched_group_barrier(0x100, i + 3 < N ? 1 : (MORE + 2) / 3, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);
+    __builtin_amdgcn_sched_group_barrier(0x400, 16 / N, 0);
   });
+}
+template <int N, int FIRST> __device__ __forceinline__ void attn_order_across() {
+  attn_for<0, N>([&](auto at) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (decltype(at)::value + FIRST < N) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+  });
+}
+template <int N> __device__ __forceinline__ void attn_keep(v4i (&f)[N]) {      // what has been formed by here stays formed here
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
 }
 
 // Gradient of the queries: a wavefront has 32 packed rows, one a lane and half; keys and values pass by.
@@ -424,13 +431,15 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
 
-  auto products = [&](floatx16& s, floatx16& g, unsigned stage, int half) {
+  // (the tile that scores are formed of is where `along` points, that of the products across where `across` does)
+  auto products = [&](floatx16& s, floatx16& g, auto half) {
+    constexpr int H = decltype(half)::value;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = g[v] = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, stage, half, ks), qf[ks]);
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, 0, H, ks), qf[ks]);
 #pragma unroll
-    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, stage + TILE, half, ks), gf[ks]);
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, TILE, H, ks), gf[ks]);
   };
   auto hide = [&](floatx16& s, int k0) {               // what a row does not see
     if (k0 >= to.lo && k0 + 31 <= from.hi && r_wave + 32 <= packed) return;
@@ -442,55 +451,72 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
     for (int v = 0; v < 16; ++v) g[v] = attn_exp2(__builtin_fmaf(s[v], c, -lse2)) * (g[v] - delta);
     A::pack(g, pf);
   };
-  auto take = [&](const v4i (&pf)[A::SS], unsigned stage, int half) {
+  constexpr int EARLY = DT == kF32 ? 0 : 2;            // operands across that are read before
+  auto early = [&](v4i (&of)[EARLY + 1], auto half) {
+#pragma unroll
+    for (int db = 0; db < EARLY; ++db) of[db] = A::read_across(across, 0, decltype(half)::value, 0, db);
+  };
+  auto take = [&](const v4i (&pf)[A::SS], const v4i (&of)[EARLY + 1], auto half) {
 #pragma unroll
     for (int ss = 0; ss < A::SS; ++ss)
 #pragma unroll
-      for (int db = 0; db < A::DB; ++db) A::E::mma(acc[db], A::read_across(across, stage, half, ss, db), pf[ss]);
+      for (int db = 0; db < A::DB; ++db)
+        A::E::mma(acc[db], ss == 0 && db < EARLY ? of[db] : A::read_across(across, 0, decltype(half)::value, ss, db), pf[ss]);
   };
-  // a step of `half` of the tile at `stage`, from key k0 on, with the next one's products beside it
-  auto step = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next, int k0, unsigned stage, int half, unsigned stage_next, int half_next) {
-    v4i pf[A::SS];
+  // a step of `half` of a tile, from key k0 on, with the next one's products beside it
+  auto step = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next, int k0, auto half, auto half_next) {
+    v4i pf[A::SS], of[EARLY + 1] = {};
     hide(s, k0);
     __builtin_amdgcn_sched_barrier(0);
-    products(s_next, g_next, stage_next, half_next);
+    products(s_next, g_next, half_next);
     form(s, g, pf);
-    take(pf, stage, half);
-    if constexpr (DT != kF32) attn_order_step<2 * A::KS, A::SS * A::DB, 2, 0, 64 / (2 * A::KS)>();
+    early(of, half);
+    if constexpr (DT != kF32) {
+      attn_keep(pf);
+      attn_keep(of);
+      attn_order_scores<2 * A::KS, 0, 2 * EARLY, 64 / (2 * A::KS)>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    take(pf, of, half);
+    if constexpr (DT != kF32) attn_order_across<A::SS * A::DB, EARLY>();
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto last = [&](floatx16& s, floatx16& g, int k0, unsigned stage, int half) {
-    v4i pf[A::SS];
+  auto last = [&](floatx16& s, floatx16& g, int k0, auto half) {
+    v4i pf[A::SS], of[EARLY + 1] = {};
     hide(s, k0);
     form(s, g, pf);
-    take(pf, stage, half);
+    early(of, half);
+    take(pf, of, half);
   };
-  unsigned here = 0, there_next = STAGE;               // places of this tile and of the next one
-  auto turn = [&]() {
-    here = there_next;
-    there_next = there_next == 2 * STAGE ? 0 : there_next + STAGE;
+  unsigned place = 0;                                  // of the tile that `along` points into
+  auto turn = [&]() {                                  // on to the next tile
+    const unsigned by = place == 2 * STAGE ? 0u - 2 * STAGE : STAGE;
+    place += by;
+    along.add(by);
+    return by;
   };
   attn_meet<0>();
   if (tiles > 1) request(1, STAGE);
-  products(s_even, g_even, 0, 0);
+  products(s_even, g_even, attn_c<0>);
+  int k0 = k_begin, tile = 0;
   if constexpr (HALVES == 2) {
-    int k0 = k_begin;
-    for (int tile = 0; tile + 1 < tiles; ++tile, k0 += TK) {
-      step(s_even, g_even, s_odd, g_odd, k0, here, 0, here, 1);
+    for (; tile + 1 < tiles; ++tile, k0 += TK) {
+      step(s_even, g_even, s_odd, g_odd, k0, attn_c<0>, attn_c<1>);
       attn_meet<0>();                                  // the next tile is here, and nobody is in the one before this any more
-      if (tile + 2 < tiles) request(tile + 2, there_next == 2 * STAGE ? 0 : there_next + STAGE);
-      step(s_odd, g_odd, s_even, g_even, k0 + 32, here, 1, there_next, 0);
-      turn();
+      const unsigned by = turn();
+      if (tile + 2 < tiles) request(tile + 2, place == 2 * STAGE ? 0 : place + STAGE);
+      step(s_odd, g_odd, s_even, g_even, k0 + 32, attn_c<1>, attn_c<0>);
+      across.add(by);
     }
-    step(s_even, g_even, s_odd, g_odd, k0, here, 0, here, 1);
-    last(s_odd, g_odd, k0 + 32, here, 1);
+    step(s_even, g_even, s_odd, g_odd, k0, attn_c<0>, attn_c<1>);
+    last(s_odd, g_odd, k0 + 32, attn_c<1>);
   } else {
-    int tile = 0, k0 = k_begin;
     auto one = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next) {
       attn_meet<0>();
-      if (tile + 2 < tiles) request(tile + 2, there_next == 2 * STAGE ? 0 : there_next + STAGE);
-      step(s, g, s_next, g_next, k0, here, 0, there_next, 0);
-      turn();
+      const unsigned by = turn();
+      if (tile + 2 < tiles) request(tile + 2, place == 2 * STAGE ? 0 : place + STAGE);
+      step(s, g, s_next, g_next, k0, attn_c<0>, attn_c<0>);
+      across.add(by);
       ++tile;
       k0 += TK;
     };
@@ -500,9 +526,9 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
     }
     if (tile + 1 < tiles) {
       one(s_even, g_even, s_odd, g_odd);
-      last(s_odd, g_odd, k0, here, 0);
+      last(s_odd, g_odd, k0, attn_c<0>);
     } else {
-      last(s_even, g_even, k0, here, 0);
+      last(s_even, g_even, k0, attn_c<0>);
     }
   }
   if (!there) return;
@@ -513,7 +539,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
 
 // Gradients of keys and values: a wavefront has 32 keys, one a lane and half; packed rows of queries and of the result's gradient pass by.
 template <int DT, int DP, int VEC>
-__global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys_kernel(const AttnParams p) {
+__global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 || DT == kF32 ? 1 : 2) void attn_keys_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
   constexpr bool PLAIN = VEC == kAttnPlain;
@@ -579,7 +605,7 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
   typename A::Across across = A::across(lane);
   along.add(lds);
   across.add(lds);
-  const unsigned at_stats = lds + 2 * TILE + 16 * h;
+  unsigned at_stats = lds + 2 * TILE + 16 * h;
   floatx16 dk[A::DB], dv[A::DB], s_even, g_even, s_odd, g_odd;
 #pragma unroll
   for (int db = 0; db < A::DB; ++db)
@@ -587,90 +613,123 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 ? 1 : 2) void attn_keys
     for (int v = 0; v < 16; ++v) dk[db][v] = dv[db][v] = 0.0f;
 
   typedef __attribute__((address_space(3))) const v4f lds_v4f;
-  auto products = [&](floatx16& s, floatx16& g, unsigned stage, int half) {
+  // (the tile that scores are formed of is where `along` points, that of the products across where `across` does)
+  auto products = [&](floatx16& s, floatx16& g, auto half) {
+    constexpr int H = decltype(half)::value;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = g[v] = 0.0f;
 #pragma unroll
-    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, stage, half, ks), kf[ks]);
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(s, A::read_along(along, 0, H, ks), kf[ks]);
     if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, stage + TILE, half, ks), vf[ks]);
+    for (int ks = 0; ks < A::KS; ++ks) A::E::mma(g, A::read_along(along, TILE, H, ks), vf[ks]);
   };
   auto hide = [&](floatx16& s, int r0) {               // keys that a row does not see
     if (r0 >= all_lo && r0 + 31 <= all_hi && j_wave + 32 <= n) return;
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = (unsigned)(r0 + 4 * h - lo + (8 * (v >> 2) + (v & 3))) <= span ? s[v] : -INFINITY;
   };
-  auto form = [&](floatx16& s, floatx16& g, unsigned stage, int half, v4i (&pf)[A::SS], v4i (&df)[A::SS]) {
+  struct Stats { v4f lse2[4], delta[4]; };             // of a step's rows
+  auto stats_of = [&](auto half) {
+    constexpr int H = decltype(half)::value;
+    Stats of;
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-      const v4f lse2 = *(lds_v4f*)(uint64_t)(at_stats + stage + (32 * half + 8 * a) * 4);
-      const v4f delta = *(lds_v4f*)(uint64_t)(at_stats + stage + (TQ + 32 * half + 8 * a) * 4);
+      of.lse2[a] = *(lds_v4f*)(uint64_t)(at_stats + (32 * H + 8 * a) * 4);
+      of.delta[a] = *(lds_v4f*)(uint64_t)(at_stats + (TQ + 32 * H + 8 * a) * 4);
+    }
+    return of;
+  };
+  auto form = [&](floatx16& s, floatx16& g, const Stats& of, v4i (&pf)[A::SS], v4i (&df)[A::SS]) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int v = 4 * a + e;
-        s[v] = attn_exp2(__builtin_fmaf(s[v], c, -lse2[e]));
-        g[v] = s[v] * (g[v] - delta[e]);
-      }
+    for (int v = 0; v < 16; ++v) {
+      s[v] = attn_exp2(__builtin_fmaf(s[v], c, -of.lse2[v >> 2][v & 3]));
+      g[v] = s[v] * (g[v] - of.delta[v >> 2][v & 3]);
     }
     A::pack(s, pf);
     A::pack(g, df);
   };
-  auto take = [&](const v4i (&pf)[A::SS], const v4i (&df)[A::SS], unsigned stage, int half) {
+  constexpr int EARLY = DT == kF32 ? 0 : 1;            // pairs of operands across that are read before
+  auto early = [&](v4i (&of)[2 * EARLY + 1], auto half) {
+#pragma unroll
+    for (int db = 0; db < EARLY; ++db) {
+      of[2 * db] = A::read_across(across, TILE, decltype(half)::value, 0, db);
+      of[2 * db + 1] = A::read_across(across, 0, decltype(half)::value, 0, db);
+    }
+  };
+  auto take = [&](const v4i (&pf)[A::SS], const v4i (&df)[A::SS], const v4i (&of)[2 * EARLY + 1], auto half) {
+    constexpr int H = decltype(half)::value;
 #pragma unroll
     for (int ss = 0; ss < A::SS; ++ss) {
       if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);      // (operands are read as they are taken: there is no room for all)
 #pragma unroll
       for (int db = 0; db < A::DB; ++db) {
-        A::E::mma(dv[db], A::read_across(across, stage + TILE, half, ss, db), pf[ss]);
-        A::E::mma(dk[db], A::read_across(across, stage, half, ss, db), df[ss]);
+        const bool there = ss == 0 && db < EARLY;
+        A::E::mma(dv[db], there ? of[2 * db] : A::read_across(across, TILE, H, ss, db), pf[ss]);
+        A::E::mma(dk[db], there ? of[2 * db + 1] : A::read_across(across, 0, H, ss, db), df[ss]);
       }
     }
   };
-  auto step = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next, int r0, unsigned stage, int half, unsigned stage_next, int half_next) {
-    v4i pf[A::SS], df[A::SS];
+  auto step = [&](floatx16& s, floatx16& g, floatx16& s_next, floatx16& g_next, int r0, auto half, auto half_next) {
+    v4i pf[A::SS], df[A::SS], of[2 * EARLY + 1] = {};
+    const Stats of_rows = stats_of(half);
     hide(s, r0);
     __builtin_amdgcn_sched_barrier(0);
-    products(s_next, g_next, stage_next, half_next);
-    form(s, g, stage, half, pf, df);
-    take(pf, df, stage, half);
-    if constexpr (DT != kF32) attn_order_step<2 * A::KS, 2 * A::SS * A::DB, 2, 8, 72 / (2 * A::KS)>();
+    products(s_next, g_next, half_next);
+    form(s, g, of_rows, pf, df);
+    early(of, half);
+    if constexpr (DT != kF32) {
+      attn_keep(pf);
+      attn_keep(df);
+      attn_keep(of);
+      attn_order_scores<2 * A::KS, 0, 4 * EARLY, 80 / (2 * A::KS)>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    take(pf, df, of, half);
+    if constexpr (DT != kF32) attn_order_across<2 * A::SS * A::DB, 2 * EARLY>();
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto last = [&](floatx16& s, floatx16& g, int r0, unsigned stage, int half) {
-    v4i pf[A::SS], df[A::SS];
+  auto last = [&](floatx16& s, floatx16& g, int r0, auto half) {
+    v4i pf[A::SS], df[A::SS], of[2 * EARLY + 1] = {};
     hide(s, r0);
-    form(s, g, stage, half, pf, df);
-    take(pf, df, stage, half);
+    form(s, g, stats_of(half), pf, df);
+    early(of, half);
+    take(pf, df, of, half);
   };
-  unsigned here = 0, there_next = STAGE;               // places of this tile and of the next one
-  auto turn = [&]() {
-    here = there_next;
-    there_next = there_next == 2 * STAGE ? 0 : there_next + STAGE;
+  unsigned place = 0;                                  // of the tile that `along` points into
+  auto turn = [&]() {                                  // on to the next tile
+    const unsigned by = place == 2 * STAGE ? 0u - 2 * STAGE : STAGE;
+    place += by;
+    along.add(by);
+    return by;
   };
+  int r0 = r_begin, tile = 0;
   if constexpr (HALVES == 2) {
     attn_meet<0>();
     if (tiles > 1) request(1, STAGE);
-    products(s_even, g_even, 0, 0);
-    int r0 = r_begin;
-    for (int tile = 0; tile + 1 < tiles; ++tile, r0 += TQ) {
-      step(s_even, g_even, s_odd, g_odd, r0, here, 0, here, 1);
+    products(s_even, g_even, attn_c<0>);
+    for (; tile + 1 < tiles; ++tile, r0 += TQ) {
+      step(s_even, g_even, s_odd, g_odd, r0, attn_c<0>, attn_c<1>);
       attn_meet<0>();                                  // the next tile is here, and nobody is in the one before this any more
-      if (tile + 2 < tiles) request(tile + 2, there_next == 2 * STAGE ? 0 : there_next + STAGE);
-      step(s_odd, g_odd, s_even, g_even, r0 + 32, here, 1, there_next, 0);
-      turn();
+      const unsigned by = turn();
+      if (tile + 2 < tiles) request(tile + 2, place == 2 * STAGE ? 0 : place + STAGE);
+      step(s_odd, g_odd, s_even, g_even, r0 + 32, attn_c<1>, attn_c<0>);
+      across.add(by);
+      at_stats += by;
     }
-    step(s_even, g_even, s_odd, g_odd, r0, here, 0, here, 1);
-    last(s_odd, g_odd, r0 + 32, here, 1);
+    step(s_even, g_even, s_odd, g_odd, r0, attn_c<0>, attn_c<1>);
+    last(s_odd, g_odd, r0 + 32, attn_c<1>);
   } else {
     // floats: the products take all of the time, and registers two sets of results do not have
-    for (int tile = 0; tile < tiles; ++tile) {
+    for (; tile < tiles; ++tile, r0 += TQ) {
       attn_meet<0>();
-      if (tile + 1 < tiles) request(tile + 1, there_next);
-      products(s_even, g_even, here, 0);
+      if (tile + 1 < tiles) request(tile + 1, place == 2 * STAGE ? 0 : place + STAGE);
+      products(s_even, g_even, attn_c<0>);
       __builtin_amdgcn_sched_barrier(0);
-      last(s_even, g_even, r_begin + tile * TQ, here, 0);
-      turn();
+      last(s_even, g_even, r0, attn_c<0>);
+      const unsigned by = turn();
+      across.add(by);
+      at_stats += by;
     }
   }
   if (!there) return;
