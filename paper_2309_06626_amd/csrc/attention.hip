@@ -17,19 +17,19 @@ struct sc_attn {
   sc_attn_desc desc;
   int64_t end, kept;               // rows of the sequences, and how many of them are kept
   uint64_t version;                // of the row set; 0: none
-  int32_t waves;
-  const sc::AttnItem *row_items, *key_items;
-  int32_t n_row_items, n_key_items;
+  sc::AttnTiles forward, backward;
+  const sc::AttnItem* items[3];    // of the forward pass, the queries' gradient, and that of keys and values
+  int32_t n_items[3];
 };
 
 namespace sc {
 
 void note_hip_error(int32_t code);
 
-static hipError_t attn_dispatch(int dtype, int what, const AttnParams& p, int waves, int vec, hipStream_t s) {
-  if (dtype == SC_BF16) return attn_launch<kBF16>(what, p, waves, vec, s);
-  if (dtype == SC_F16) return attn_launch<kF16>(what, p, waves, vec, s);
-  return attn_launch<kF32>(what, p, waves, vec, s);
+static hipError_t attn_dispatch(int dtype, int what, const AttnParams& p, AttnTiles t, int vec, hipStream_t s) {
+  if (dtype == SC_BF16) return attn_launch<kBF16>(what, p, t, vec, s);
+  if (dtype == SC_F16) return attn_launch<kF16>(what, p, t, vec, s);
+  return attn_launch<kF32>(what, p, t, vec, s);
 }
 
 // kept rows before each start
@@ -64,7 +64,7 @@ static void attn_zeros_of(const sc_rows* set, int64_t rows, std::initializer_lis
 
 static size_t attn_up(size_t n) { return (n + 255) & ~(size_t)255; }
 static int64_t attn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int kAttnRowsLeast = 32;      // packed rows of the smallest tile
+constexpr int kAttnRowsLeast = 128;      // packed rows of the smallest tile
 
 sc_status check_attn(const sc_attn_desc* d) {
   if (!d) return SC_ERR_NULL;
@@ -82,13 +82,14 @@ static AttnLayout attn_layout(const sc_attn_desc* d, int64_t seqs, int64_t rows)
   const int64_t group = d->heads / d->kv_heads;
   AttnLayout l;
   l.starts = attn_up((size_t)(seqs + 1) * 4);
-  l.row_items = attn_up((size_t)(rows * group / kAttnRowsLeast + seqs) * sizeof(AttnItem));
+  l.row_items = attn_up((size_t)(rows * group / kAttnRowsLeast + seqs) * sizeof(AttnItem));      // (twice: forward and backward)
   l.key_items = attn_up((size_t)(rows / (32 * kAttnKeyWaves) + seqs) * sizeof(AttnItem));
   return l;
 }
 
 // Tiles of `per` packed rows of every sequence, longest first.
-static void attn_items(const std::vector<int32_t>& starts, const sc_attn_desc& d, int64_t per, bool keys, std::vector<AttnItem>& items) {
+// Returns what a tile sees on average.
+static int64_t attn_items(const std::vector<int32_t>& starts, const sc_attn_desc& d, int64_t per, bool keys, std::vector<AttnItem>& items) {
   const int64_t group = keys ? 1 : d.heads / d.kv_heads;
   items.clear();
   std::vector<int64_t> work;
@@ -112,6 +113,9 @@ static void attn_items(const std::vector<int32_t>& starts, const sc_attn_desc& d
   std::vector<AttnItem> sorted(items.size());
   for (size_t i = 0; i < order.size(); ++i) sorted[i] = items[order[i]];
   items.swap(sorted);
+  int64_t all = 0;
+  for (int64_t w : work) all += w;
+  return work.empty() ? 0 : all / (int64_t)work.size();
 }
 
 static sc_status attn_plan(sc_attn* plan, int64_t seqs, const int64_t* starts, const sc_rows* set, unsigned char* w, hipStream_t s) {
@@ -134,17 +138,27 @@ static sc_status attn_plan(sc_attn* plan, int64_t seqs, const int64_t* starts, c
   }
   if (e != hipSuccess) { note_hip_error((int32_t)e); return SC_ERR_HIP; }
   plan->kept = at.back();
-  std::vector<AttnItem> row_items, key_items;
-  attn_items(at, plan->desc, 32 * plan->waves, false, row_items);
-  attn_items(at, plan->desc, 32 * kAttnKeyWaves, true, key_items);
-  plan->n_row_items = (int32_t)row_items.size();
-  plan->n_key_items = (int32_t)key_items.size();
+  // Workgroups of eight wavefronts read keys and values half as often; those of four leave less undone at a sequence's ends, and two run on a
+  // compute unit side by side (8 192 rows that see 4 096 on average: 494 and 510 us; 23 sequences, window 1 024: 145 and 136).  The queries' gradient
+  // has LDS for one of either: eight where they are filled (4 x 2 048 rows: 346 and 370 us).  Narrow heads of short sequences take tiles of
+  // 32 keys, whose registers allow three workgroups (64 x 98 rows, 12 heads of 64: 15.1 and 18 us; 16 x 1 024: 77 and 75).
+  const sc_attn_desc& d = plan->desc;
+  const bool wide = d.dtype != SC_F32;
+  std::vector<AttnItem> items[3];
+  const int64_t seen = attn_items(at, d, 128, false, items[0]);
+  plan->forward = {wide && seen >= 2048 ? 8 : 4, d.d <= 64 && seen <= 256 ? 32 : 64};
+  plan->backward = {wide && plan->kept * (d.heads / d.kv_heads) >= 512 * seqs ? 8 : 4, 64};
+  if (plan->forward.waves == 8) attn_items(at, d, 256, false, items[0]);
+  attn_items(at, d, 32 * plan->backward.waves, false, items[1]);
+  attn_items(at, d, 32 * kAttnKeyWaves, true, items[2]);
   unsigned char* to = w + 2 * l.starts;
-  plan->row_items = reinterpret_cast<const AttnItem*>(to);
-  plan->key_items = reinterpret_cast<const AttnItem*>(to + l.row_items);
-  if (!row_items.empty()) {
-    e = hipMemcpyAsync(to, row_items.data(), row_items.size() * sizeof(AttnItem), hipMemcpyHostToDevice, s);
-    if (e == hipSuccess) e = hipMemcpyAsync(to + l.row_items, key_items.data(), key_items.size() * sizeof(AttnItem), hipMemcpyHostToDevice, s);
+  for (int k = 0; k < 3; ++k) {
+    plan->items[k] = reinterpret_cast<const AttnItem*>(to);
+    plan->n_items[k] = (int32_t)items[k].size();
+    if (e == hipSuccess && !items[k].empty()) e = hipMemcpyAsync(to, items[k].data(), items[k].size() * sizeof(AttnItem), hipMemcpyHostToDevice, s);
+    to += k < 2 ? l.row_items : l.key_items;
+  }
+  if (!items[0].empty()) {
     const hipError_t waited = hipStreamSynchronize(s);
     if (e == hipSuccess) e = waited;
   }
@@ -205,7 +219,7 @@ sc_status sparse_attn_workspace_bytes(const sc_attn_desc* desc, int64_t seqs, in
       rows * (desc->heads / desc->kv_heads) > (1 << 30) || (rows * (desc->heads / desc->kv_heads) / sc::kAttnRowsLeast + seqs) * desc->kv_heads > (1 << 23))
     return SC_ERR_BAD_SHAPE;
   const sc::AttnLayout l = sc::attn_layout(desc, seqs, rows);
-  *bytes = 2 * l.starts + l.row_items + l.key_items;
+  *bytes = 2 * l.starts + 2 * l.row_items + l.key_items;
   return SC_OK;
 }
 
@@ -231,7 +245,6 @@ sc_status sparse_attn_plan(const sc_attn_desc* desc, int64_t seqs, const int64_t
     plan->desc = *desc;
     plan->end = starts[seqs];
     plan->version = rows ? rows->version : 0;
-    plan->waves = desc->dtype != SC_F32 && starts[seqs] * (desc->heads / desc->kv_heads) >= 512 * seqs ? 8 : 4;
     st = sc::attn_plan(plan, seqs, starts, rows, static_cast<unsigned char*>(workspace_dev), static_cast<hipStream_t>(hip_stream));
   } catch (const std::bad_alloc&) {
     sc::note_hip_error((int32_t)hipErrorOutOfMemory);
@@ -275,14 +288,14 @@ sc_status sparse_attn_run(const sc_attn* plan, const sc_rows* rows, int32_t row_
   p.v_stride = v_stride;
   p.out = o_dev;
   p.lse = lse_dev;
-  p.items = plan->row_items;
-  p.n_items = plan->n_row_items;
+  p.items = plan->items[0];
+  p.n_items = plan->n_items[0];
   hipError_t e = hipSuccess;
   if (row_format == SC_ROWS_DENSE) {
     const int64_t width = (int64_t)d.heads * d.d * (d.dtype == SC_F32 ? 4 : 2);
     sc::attn_zeros_of(rows, plan->end, {o_dev}, {width}, {width}, &p.zeros);
   }
-  if (p.n_items > 0 || p.zeros.blocks > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnForward, p, plan->waves, vec, s);
+  if (p.n_items > 0 || p.zeros.blocks > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnForward, p, plan->forward, vec, s);
   if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
   return SC_OK;
 }
@@ -333,18 +346,18 @@ sc_status sparse_attn_backward(const sc_attn* plan, const sc_rows* rows, int32_t
   p.lse = const_cast<float*>(lse_dev);
   p.stats[0] = static_cast<float*>(workspace_dev);
   p.stats[1] = p.stats[0] + sc::attn_up((size_t)plan->kept * d.heads * 4) / 4;
-  p.items = plan->row_items;
-  p.n_items = plan->n_row_items;
+  p.items = plan->items[1];
+  p.n_items = plan->n_items[1];
   if (row_format == SC_ROWS_DENSE) {
     const int64_t eb = d.dtype == SC_F32 ? 4 : 2, q = d.heads * eb * d.d, kv = d.kv_heads * eb * d.d;
     sc::attn_zeros_of(rows, plan->end, {dq_dev, dk_dev, dv_dev}, {dq_stride * eb, dk_stride * eb, dv_stride * eb}, {q, kv, kv}, &p.zeros);
   }
   hipError_t e = hipSuccess;
-  if (p.n_items > 0 || p.zeros.blocks > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->waves, vec, s);      // (leaves statistics for the keys)
+  if (p.n_items > 0 || p.zeros.blocks > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardQ, p, plan->backward, vec, s);      // (leaves statistics for the keys)
   p.zeros.blocks = 0;
-  p.items = plan->key_items;
-  p.n_items = plan->n_key_items;
-  if (e == hipSuccess && p.n_items > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardKV, p, plan->waves, vec, s);
+  p.items = plan->items[2];
+  p.n_items = plan->n_items[2];
+  if (e == hipSuccess && p.n_items > 0) e = sc::attn_dispatch(d.dtype, sc::kAttnBackwardKV, p, plan->backward, vec, s);
   if (e != hipSuccess) { sc::note_hip_error((int32_t)e); return SC_ERR_HIP; }
   return SC_OK;
 }

@@ -2,5 +2,5 @@
 #include "attn_kernel.hpp"
 
 namespace sc {
-template hipError_t attn_launch<kF16>(int what, const AttnParams& p, int waves, int vec, hipStream_t s);
+template hipError_t attn_launch<kF16>(int what, const AttnParams& p, AttnTiles t, int vec, hipStream_t s);
 }  // namespace sc

@@ -98,12 +98,12 @@ __device__ __forceinline__ int attn_look_up(const AttnParams& p, int first, int 
 // ---- forward ---------------------------------------------------------------------------------------------------------------------------
 // A wavefront has 32 packed rows, one a lane and half; keys pass by in tiles.  While the matrix unit multiplies the keys of one tile, the
 // vector unit takes the exponentials of the tile before, and while it multiplies their values, the maximum of this one.
-template <int DT, int DP, int NW, int VEC>
-__global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (VEC < 2 && NW == 4) ? 1 : 2) : 2) void attn_forward_kernel(const AttnParams p) {
+template <int DT, int DP, int NW, int TK, int VEC>
+__global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW == 4)) ? 1 : 2) void attn_forward_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
   constexpr bool PLAIN = VEC == kAttnPlain;
-  constexpr int LOADS = PLAIN ? 2 : VEC, NT = 64 * NW, TK = DT == kF32 ? 32 : 64, KB = TK / 32;
+  constexpr int LOADS = PLAIN ? 2 : VEC, NT = 64 * NW, KB = TK / 32;
   constexpr int TILE = TK * A::RB;                     // LDS: two tiles of keys, two of values
   extern __shared__ __align__(16) unsigned char smem[];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), h = lane >> 5, l32 = lane & 31;
@@ -151,6 +151,8 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (VEC < 2 && NW ==
   look_up(0);
 
   request_k(0, 0);
+  rows_v = rows_k;
+  request_v(0, 2 * TILE);
   v4i qf[A::KS];
   A::template read_row<LOADS>(static_cast<const T*>(p.q) + row * p.q_stride + (int64_t)head * p.d, p.d, h, there, qf);
   const float c = p.scale * kAttnLog2e;
@@ -281,11 +283,9 @@ __global__ __launch_bounds__(64 * NW, DP > 64 ? (DT == kF32 || (VEC < 2 && NW ==
     values(pf, parity);
     add_up(before, attn_c<0>, attn_c<KB>);
   };
-  rows_v = rows_k;
   look_up(1);
   attn_meet<0>();
   if (tiles > 1) request_k(1, TILE);
-  request_v(0, 2 * TILE);
   rows_v = rows_k;
   look_up(2);
   scores(s_even, attn_c<0>);
@@ -752,27 +752,28 @@ template <class Kernel> static hipError_t attn_start(Kernel kernel, int threads,
   return hipGetLastError();
 }
 
-template <int DT, int DP, int NW, int VEC> static hipError_t attn_start_rows(int what, const AttnParams& p, hipStream_t s) {
-  constexpr int tile = (DT == kF32 ? 32 : 64) * AttnTile<DT, DP>::RB;
-  return what == kAttnForward ? attn_start(attn_forward_kernel<DT, DP, NW, VEC>, 64 * NW, 4 * tile, p, s)
-                              : attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, 6 * tile, p, s);
-}
-
-template <int DT, int DP, int VEC> static hipError_t attn_start_width(int what, const AttnParams& p, int waves, hipStream_t s) {
-  if (what == kAttnBackwardKV) {
-    constexpr int rows = DT == kF32 ? 32 : 64, lds = 3 * (2 * rows * AttnTile<DT, DP>::RB + 2 * rows * 4);
-    return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, lds, p, s);
-  }
+template <int DT, int DP, int VEC> static hipError_t attn_start_width(int what, const AttnParams& p, AttnTiles t, hipStream_t s) {
+  using A = AttnTile<DT, DP>;
+  constexpr int rows = DT == kF32 ? 32 : 64;                 // of a tile that passes by
+  if (what == kAttnBackwardKV) return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, 3 * (2 * rows * A::RB + 2 * rows * 4), p, s);
+  auto start = [&](auto waves) {
+    constexpr int NW = decltype(waves)::value;
+    if (what == kAttnBackwardQ) return attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, 6 * rows * A::RB, p, s);
+    if constexpr (DT != kF32 && DP == 64 && NW == 4) {
+      if (t.keys == 32) return attn_start(attn_forward_kernel<DT, DP, NW, 32, VEC>, 64 * NW, 4 * 32 * A::RB, p, s);
+    }
+    return attn_start(attn_forward_kernel<DT, DP, NW, rows, VEC>, 64 * NW, 4 * rows * A::RB, p, s);
+  };
   if constexpr (DT != kF32) {
-    if (waves == 8) return attn_start_rows<DT, DP, 8, VEC>(what, p, s);
+    if (t.waves == 8) return start(attn_c<8>);
   }
-  return attn_start_rows<DT, DP, 4, VEC>(what, p, s);
+  return start(attn_c<4>);
 }
 
-template <int DT> hipError_t attn_launch(int what, const AttnParams& p, int waves, int vec, hipStream_t s) {
+template <int DT> hipError_t attn_launch(int what, const AttnParams& p, AttnTiles t, int vec, hipStream_t s) {
   auto start = [&](auto level) {
     constexpr int VEC = decltype(level)::value;
-    return p.d <= 64 ? attn_start_width<DT, 64, VEC>(what, p, waves, s) : attn_start_width<DT, 128, VEC>(what, p, waves, s);
+    return p.d <= 64 ? attn_start_width<DT, 64, VEC>(what, p, t, s) : attn_start_width<DT, 128, VEC>(what, p, t, s);
   };
   if (vec == 2) {
     const int64_t most = AttnTile<DT, 64>::kMostStride;
