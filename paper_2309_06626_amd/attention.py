@@ -222,7 +222,7 @@ def sparse_kv_row_entries(desc: sc_kv_desc) -> int:
 
 class KvCache:
     """The tensors of a cache: k_pages and v_pages [pages, kv_heads, page_rows, row entries], of 8-bit caches int8 with float scales
-    [pages, kv_heads, page_rows].  Those that are not given are made, with zeros."""
+    [pages, kv_heads, page_rows].  Those that are not given are made, with zeros.  They stay those of the object's making."""
 
     def __init__(self, desc: sc_kv_desc, k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None,
                  k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None, device="cuda"):
@@ -243,7 +243,7 @@ class KvCache:
         self._reference, self._width = ctypes.byref(self.desc), desc.kv_heads * desc.d
         (self.k_pages, k), (self.v_pages, v) = pages(k_pages, "k_pages"), pages(v_pages, "v_pages")
         (self.k_scales, ks), (self.v_scales, vs) = scales(k_scales, "k_scales"), scales(v_scales, "v_scales")
-        self._addresses = (k, v, ks, vs)
+        self._addresses, self._held = (k, v, ks, vs), (self.k_pages, self.v_pages, self.k_scales, self.v_scales)
 
 
 def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:

@@ -10,7 +10,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <new>
 #include <vector>
 
 struct sc_attn {
@@ -147,7 +146,7 @@ static sc_status attn_plan(sc_attn* plan, int64_t seqs, const int64_t* starts, c
   std::vector<AttnItem> items[3];
   const int64_t seen = attn_items(at, d, 128, false, items[0]);
   plan->forward = {wide && seen >= 2048 ? 8 : 4, d.d <= 64 && seen <= 256 ? 32 : 64};
-  plan->backward = {wide && plan->kept * (d.heads / d.kv_heads) >= 512 * seqs ? 8 : 4, 64};
+  plan->backward = {wide && d.d % 8 == 0 && plan->kept * (d.heads / d.kv_heads) >= 512 * seqs ? 8 : 4, 64};
   if (plan->forward.waves == 8) attn_items(at, d, 256, false, items[0]);
   attn_items(at, d, 32 * plan->backward.waves, false, items[1]);
   attn_items(at, d, 32 * kAttnKeyWaves, true, items[2]);
@@ -246,7 +245,7 @@ sc_status sparse_attn_plan(const sc_attn_desc* desc, int64_t seqs, const int64_t
     plan->end = starts[seqs];
     plan->version = rows ? rows->version : 0;
     st = sc::attn_plan(plan, seqs, starts, rows, static_cast<unsigned char*>(workspace_dev), static_cast<hipStream_t>(hip_stream));
-  } catch (const std::bad_alloc&) {
+  } catch (...) {      // (there is no memory for them)
     sc::note_hip_error((int32_t)hipErrorOutOfMemory);
     st = SC_ERR_HIP;
   }

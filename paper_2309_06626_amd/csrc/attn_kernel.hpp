@@ -347,7 +347,7 @@ template <int N> __device__ __forceinline__ void attn_keep(v4i (&f)[N]) {      /
 
 // Gradient of the queries: a wavefront has 32 packed rows, one a lane and half; keys and values pass by.
 template <int DT, int DP, int NW, int VEC>
-__global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
+__global__ __launch_bounds__(64 * NW, DT == kF32 || (DP > 64 && NW == 4) ? 1 : 2) void attn_rows_kernel(const AttnParams p) {
   using A = AttnTile<DT, DP>;
   using T = typename A::T;
   constexpr bool PLAIN = VEC == kAttnPlain;
@@ -392,7 +392,9 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
         };
       };
       A::template request<TK, NT, LOADS>(lds + stage, p.d, place(k_base, p.k_stride));
+      __builtin_amdgcn_sched_barrier(0);
       A::template request<TK, NT, LOADS>(lds + stage + TILE, p.d, place(v_base, p.v_stride));
+      __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!PLAIN) rows = attn_look_up(p, first, k0 + TK, n);
   };
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
     delta = attn_add_halves(delta);
     const int64_t stat = (int64_t)(first + i) * p.heads + head;
     lse2 = there ? attn_lse2(p.lse[stat]) : 0.0f;
-    if (there) p.stats[h][stat] = h ? delta : lse2;      // (for the keys)
+    if (there && h == 0) p.stats[0][stat] = lse2;        // (for the keys)
   }
 
   typename A::Along along = A::along(lane);
@@ -430,6 +432,9 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
   for (int db = 0; db < A::DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
+  // delta again, as sum_j p (do . v_j): what o as it is stored makes of it is off by that tensor's rounding, one error of all the row's
+  // gradients of scores.  Here they have to be formed before the sum is there; the keys' gradients have it.
+  float part[2] = {0.0f, 0.0f};
 
   // (the tile that scores are formed of is where `along` points, that of the products across where `across` does)
   auto products = [&](floatx16& s, floatx16& g, auto half) {
@@ -448,10 +453,14 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
   };
   auto form = [&](const floatx16& s, floatx16& g, v4i (&pf)[A::SS]) {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) g[v] = attn_exp2(__builtin_fmaf(s[v], c, -lse2)) * (g[v] - delta);
+    for (int v = 0; v < 16; ++v) {
+      const float e = attn_exp2(__builtin_fmaf(s[v], c, -lse2));
+      part[v & 1] = __builtin_fmaf(e, g[v], part[v & 1]);
+      g[v] = e * (g[v] - delta);
+    }
     A::pack(g, pf);
   };
-  constexpr int EARLY = DT == kF32 ? 0 : 2;            // operands across that are read before
+  constexpr int EARLY = DT == kF32 || VEC < 2 ? 0 : 2; // operands across that are read before
   auto early = [&](v4i (&of)[EARLY + 1], auto half) {
 #pragma unroll
     for (int db = 0; db < EARLY; ++db) of[db] = A::read_across(across, 0, decltype(half)::value, 0, db);
@@ -474,7 +483,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
     if constexpr (DT != kF32) {
       attn_keep(pf);
       attn_keep(of);
-      attn_order_scores<2 * A::KS, 0, 2 * EARLY, 64 / (2 * A::KS)>();
+      attn_order_scores<2 * A::KS, 0, 2 * EARLY, 80 / (2 * A::KS)>();
     }
     __builtin_amdgcn_sched_barrier(0);
     take(pf, of, half);
@@ -531,10 +540,17 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || NW == 4) ? 1 : 2
       last(s_even, g_even, k0, attn_c<0>);
     }
   }
-  if (!there) return;
-  T* const out = static_cast<T*>(p.dq) + row * p.dq_stride + (int64_t)head * p.d;
+  delta = attn_add_halves(part[0] + part[1]);
+  // (the row's place is worked out again: registers are short in between)
+  int again = threadIdx.x;
+  asm volatile("" : "+v"(again));
+  const int r_out = r_wave + (again & 31), h_out = (again >> 5) & 1;
+  if (r_out >= packed) return;
+  const int i_out = r_out / p.group, head_out = w.head * p.group + (r_out - i_out * p.group);
+  if (h_out == 0) p.stats[1][(int64_t)(first + i_out) * p.heads + head_out] = delta;
+  T* const out = static_cast<T*>(p.dq) + (p.map ? p.map[first + i_out] : first + i_out) * p.dq_stride + (int64_t)head_out * p.d;
 #pragma unroll
-  for (int db = 0; db < A::DB; ++db) A::template write_16<LOADS>(out, 32 * db + 16 * h, p.d, acc[db], p.scale);
+  for (int db = 0; db < A::DB; ++db) A::template write_16<LOADS>(out, 32 * db + 16 * h_out, p.d, acc[db], p.scale);
 }
 
 // Gradients of keys and values: a wavefront has 32 keys, one a lane and half; packed rows of queries and of the result's gradient pass by.
@@ -758,7 +774,9 @@ template <int DT, int DP, int VEC> static hipError_t attn_start_width(int what, 
   if (what == kAttnBackwardKV) return attn_start(attn_keys_kernel<DT, DP, VEC>, 64 * kAttnKeyWaves, 3 * (2 * rows * A::RB + 2 * rows * 4), p, s);
   auto start = [&](auto waves) {
     constexpr int NW = decltype(waves)::value;
-    if (what == kAttnBackwardQ) return attn_start(attn_rows_kernel<DT, DP, NW, VEC>, 64 * NW, 6 * rows * A::RB, p, s);
+    // (4-byte transfers of eight wavefronts need more registers than there are: entries, where strides alone ask for them)
+    constexpr int LOADS = VEC == 1 && NW == 8 ? 0 : VEC;
+    if (what == kAttnBackwardQ) return attn_start(attn_rows_kernel<DT, DP, NW, LOADS>, 64 * NW, 6 * rows * A::RB, p, s);
     if constexpr (DT != kF32 && DP == 64 && NW == 4) {
       if (t.keys == 32) return attn_start(attn_forward_kernel<DT, DP, NW, 32, VEC>, 64 * NW, 4 * 32 * A::RB, p, s);
     }
