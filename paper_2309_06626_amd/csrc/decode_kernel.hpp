@@ -34,6 +34,19 @@ __device__ __forceinline__ void decode_widen(v4i codes, _Float16 (&out)[16]) {
   }
 }
 
+// largest of the 32 lanes of a half wavefront (positive numbers)
+__device__ __forceinline__ float decode_max32(float v) {
+  auto with = [&](auto control) {
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, false)));
+  };
+  with(std::integral_constant<int, 0xB1>{});       // quad_perm [1, 0, 3, 2]
+  with(std::integral_constant<int, 0x4E>{});       // quad_perm [2, 3, 0, 1]
+  with(std::integral_constant<int, 0x141>{});      // mirrored within 8
+  with(std::integral_constant<int, 0x140>{});      // within 16
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+
 // What a lane holds of a row of q, as f16: in units of a power of two, so that the largest entry is between 2^13 and 2^14 (none is lost that
 // is not below 2^-37 of it).  Returns the unit.
 template <class From, class To, int KS> __device__ __forceinline__ float decode_narrow(const v4i (&from)[KS], v4i (&to)[KS]) {
@@ -267,10 +280,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
 #pragma unroll
     for (int v = 1; v < 16; ++v) top = fmaxf(top, s[v]);
     top = fmaxf(attn_max_halves(top) * c, m);
-    const float shift = top == -INFINITY ? 0.0f : top;         // (nothing seen so far: every term is 0)
-    float less = attn_any(top > m) ? attn_exp2(m - shift) : 1.0f;
-    m = top;
-    sum *= less;
+    // (a maximum that grew by less than 2^8 stays: weights of up to 256 are as good as those of up to 1)
+    float less = 1.0f;
+    if (attn_any(top > m + 8.0f)) {
+      less = attn_exp2(m - (top == -INFINITY ? 0.0f : top));
+      m = top;
+      sum *= less;
+    }
+    const float shift = m == -INFINITY ? 0.0f : m;             // (nothing seen so far: every term is 0)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       s[v] = attn_exp2(__builtin_fmaf(s[v], c, -shift));
@@ -283,8 +300,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
       if constexpr (CT == kF16) {
         float big = *(__attribute__((address_space(3))) const float*)(uint64_t)(at_scales + (32 + l32) * 4);
         big = __builtin_isfinite(big) ? big : 0.0f;
-#pragma unroll
-        for (int x = 1; x < 32; x <<= 1) big = fmaxf(big, __shfl_xor(big, x));
+        big = decode_max32(big);
         const float least = __builtin_bit_cast(float, (unsigned)(__builtin_bit_cast(unsigned, big) & 0x7f800000u));
         if (least > unit) {
           less *= unit / least;      // (powers of two; 0 at first)
