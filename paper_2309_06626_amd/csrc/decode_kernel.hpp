@@ -5,6 +5,12 @@
 // A workgroup takes the query heads of one key-value head (up to 32 of them) and a stretch of the sequence, of which its wavefronts take every
 // fourth tile of 32 keys each, on their own: keys by heads are one 32 x 32 product, whose results, rounded, are an operand of the next.
 // Maximum, sum and result of the wavefronts are joined in LDS, those of the stretches by a second launch, both in a fixed order.
+//
+// Bound by memory: a tile is 16 KB of 16-bit entries for 16 products, of whose columns a group of query heads fills some.  Entries go straight
+// into LDS, where a wavefront has two tiles of keys and two of values, of which three are on their way.  Measured, 8 key-value heads of
+// 128 in bf16: 64 sequences of 4 096 to 8 192 rows 289 us (5.6 TB/s; a plain copy 6.3), one of 100 000 rows 79 (5.2 TB/s).  Codes go through
+// registers, where they are widened; 33 sequences of up to 4 000 rows, 4 heads: 29 us (2.4 TB/s), bound by the longest stretch's chain of
+// widening, products and exponentials.
 #pragma once
 #include "attn_tile.hpp"
 #include "decode_params.hpp"
