@@ -73,6 +73,10 @@ CASES = [  # lengths, heads, kv heads, d, dtype, causal, window, share of rows k
     ([600, 550], 4, 1, 64, "f16", True, 200, 0.9, 0, 0),
     ([550], 3, 1, 125, "bf16", True, 0, 1.0, 0, 0),
     ([700], 2, 1, 66, "bf16", False, 0, 1.0, 0, 0),
+    ([5, 1, 9], 512, 1, 16, "f16", True, 0, 1.0, 0, 1),
+    ([40], 48, 1, 64, "bf16", True, 7, 0.7, 0, 0),
+    ([33, 70], 14, 2, 128, "bf16", False, 0, 1.0, 0, 0),
+    ([70, 30], 64, 1, 128, "f32", True, 0, 1.0, 0, 0),
 ]
 
 
@@ -146,6 +150,64 @@ def test_packed_forward_and_gradients(c):
 @pytest.mark.parametrize("pad", [1, 2, 8])
 def test_rows_with_gaps(dtype, pad):
     packed_check(([70, 33], 4, 2, 64, dtype, True, 0, 0.8, 0, 1), 3, pad)
+
+
+@pytest.mark.parametrize("pad", [1, 2, 8])
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_rows_with_gaps(d, pad):
+    packed_check(([600], 4, 2, d, "bf16", True, 0, 1.0, 0, 0), 5, pad)
+
+
+def test_keys_and_values_of_different_strides_and_far_apart():
+    """Queries follow each other, keys and values lie at other distances, the values' beyond what the offsets of plain rows span."""
+    n, d = 90, 64
+    g = gen(31)
+    x = {"q": normal(g, n, 2, d, dtype="bf16"), "k": normal(g, n, 1, d, dtype="bf16"), "v": normal(g, n, 1, d, dtype="bf16"), "do": normal(g, n, 2, d, dtype="bf16")}
+    want, bound = O.packed((2, 1, d, "bf16", True, 0, 0.125), [0, n], torch.ones(n, dtype=torch.bool), x["q"], x["k"], x["v"], x["do"])
+    plan = A.sparse_attn_plan(A.make_attn_desc(2, 1, d), [0, n])
+    ws = torch.empty(A.sparse_attn_backward_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+    q, do = dev(x["q"], "bf16"), dev(x["do"], "bf16")
+    for k_wide, v_wide in ((64, 200), (72, 64), (64, (1 << 22) + 8), ((1 << 22) + 8, (1 << 22) + 8)):
+        k, v, dk, dv = (torch.empty(n, w, dtype=torch.bfloat16, device=DEV)[:, :d] for w in (k_wide, v_wide, k_wide, v_wide))
+        k.copy_(x["k"][:, 0])
+        v.copy_(x["v"][:, 0])
+        o, lse, dq = nans(n, 2, d, dtype="bf16"), nans(n, 2), nans(n, 2, d, dtype="bf16")
+        A.sparse_attn_run(plan, q, k, v, o, lse)
+        A.sparse_attn_backward(plan, q, k, v, o, lse, do, dq, dk, dv, ws)
+        for name, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+            inside(t.reshape(want[name].shape), want[name], bound[name], name)
+
+
+def test_no_sequences_and_empty_ones():
+    x, o = nans(3, 2, 64, dtype="bf16"), nans(3, 2, 64, dtype="bf16")
+    for starts in ([0], [0, 0, 0]):
+        plan = A.sparse_attn_plan(A.make_attn_desc(2, 2, 64), starts)
+        assert (plan.end, plan.kept) == (0, 0)
+        ws = torch.empty(A.sparse_attn_backward_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+        lse, grads = torch.empty(0, 2, device=DEV), [nans(3, 2, 64, dtype="bf16") for _ in range(3)]
+        A.sparse_attn_run(plan, x, x, x, o, lse)
+        A.sparse_attn_backward(plan, x, x, x, o, lse, x, *grads, ws)
+        torch.cuda.synchronize()
+        assert all(torch.isnan(t).all() for t in (o, *grads))
+
+
+def test_many_short_sequences():
+    """Whole numbers: every row of a sequence of equal keys is the mean of the values so far."""
+    lens = [i % 4 for i in range(30000)]
+    starts = starts_of(lens)
+    n = starts[-1]
+    q = torch.zeros(n, 2, 64, dtype=torch.bfloat16, device=DEV)
+    v = torch.randint(-8, 9, (n, 1, 64), device=DEV, generator=torch.Generator(DEV).manual_seed(1)).to(torch.bfloat16)
+    plan = A.sparse_attn_plan(A.make_attn_desc(2, 1, 64), starts)
+    o = nans(n, 2, 64, dtype="bf16")
+    A.sparse_attn_run(plan, q, torch.zeros_like(v), v, o)
+    first = torch.tensor(starts[:-1], device=DEV).repeat_interleave(torch.tensor(lens, device=DEV))
+    at = torch.arange(n, device=DEV)
+    total = v[:, 0].double().cumsum(0)
+    before = torch.where((first > 0)[:, None], total[(first - 1).clamp_min(0)], torch.zeros_like(total))
+    want = ((total - before) / (at - first + 1)[:, None]).cpu()
+    inside(o[:, 0], want, 2.0 ** -8 * want.abs() + 2.0 ** -20, "o")
+    assert same(o[:, 0], o[:, 1])
 
 
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 95, 96, 127, 128, 129, 191, 192, 193, 255, 256, 257])
@@ -395,6 +457,11 @@ DECODES = [  # lengths, heads, kv heads, d, page rows, dtype, bits, window, spar
     ([5000], 9, 3, 96, 2, "bf16", 0, 0, 0),
     ([70] * 40, 8, 8, 64, 32, "f16", 0, 0, 0),
     ([3000, 2999], 70, 2, 128, 256, "bf16", 8, 1000, 0),
+    ([37, 20], 512, 1, 32, 16, "f16", 0, 0, 0),
+    ([37, 20], 512, 1, 32, 16, "bf16", 8, 0, 0),
+    ([1500], 4, 4, 16, 65536, "bf16", 0, 0, 0),
+    ([9000], 2, 1, 64, 1, "f32", 8, 0, 3),
+    ([6000, 11], 8, 1, 128, 64, "f32", 0, 4000, 0),
 ]
 
 
@@ -477,6 +544,23 @@ def test_decode_of_pages_that_are_not_there_and_lengths_beyond_the_table():
     got = decode_call(c, cache, table, [-1, -(2 ** 31), 0, 2 ** 31 - 1], q)
     assert (got[:3] == 0).all()
     inside(got[3:], want[3:], bound[3:], "o")
+
+
+def test_decode_without_pages_and_of_many_rows():
+    cache = cache_of(1, 64, 16, 2, "bf16", 0)
+    desc = A.make_attn_desc(2, 1, 64)
+    rows = 70000
+    q, o = torch.randn(rows, 2, 64, device=DEV).to(torch.bfloat16), nans(rows, 2, 64, dtype="bf16")
+    ws = torch.empty(A.sparse_attn_decode_workspace_bytes(desc, cache.desc, rows, 1), dtype=torch.uint8, device=DEV)
+    lengths = torch.full((rows,), 5, dtype=torch.int32, device=DEV)
+    A.sparse_attn_decode(desc, cache, q, torch.empty(rows, 0, dtype=torch.int32, device=DEV), lengths, o, ws)
+    assert (o == 0).all()
+    v = torch.randint(-8, 9, (5, 1, 64), device=DEV).to(torch.bfloat16)      # equal keys: the values' mean
+    A.sparse_kv_write(cache, torch.zeros_like(v), v, torch.arange(16, 21, device=DEV))
+    table = torch.full((rows, 1), 1, dtype=torch.int32, device=DEV)
+    A.sparse_attn_decode(desc, cache, q, table, lengths, o, ws)
+    want = (v[:, 0].double().mean(0)).cpu().expand(rows, 2, 64)
+    inside(o, want, 2.0 ** -8 * want.abs() + 2.0 ** -20, "o")
 
 
 @pytest.mark.parametrize("bits", [0, 8])
