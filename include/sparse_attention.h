@@ -29,7 +29,7 @@ typedef struct {
   int32_t dtype;           /* sc_dtype */
   int32_t causal;          /* 0/1: row i sees keys j <= i only */
   int32_t window;          /* 0, or row i sees keys with |i - j| < window only */
-  float scale;             /* of q . k; finite and > 0 */
+  float scale;             /* of q . k; > 0 and at most 2^127 */
 } sc_attn_desc;
 
 /* ---- attention over packed sequences ----------------------------------------------------------------------------------------------
@@ -41,7 +41,9 @@ typedef struct {
  * sparse_rows_set_mask the row set needs a new plan: runs with the old one are refused (SC_ERR_MASK_COUNT).
  * q, o: [rows][heads][d], k, v: [rows][kv_heads][d], with row_format = SC_ROWS_COMPACT of the kept rows alone.
  * lse: float[kept][heads], log sum exp of the scores, for the backward pass; NULL in inference.  kept: of sparse_attn_info.
- * A row of q that is not finite is lost, and no other; of k or v, the rows of its sequence are (their dk and dv too). */
+ * A row of q that is not finite loses what is made of it, and no other; one of k or v what is made of its sequence (its dk and dv too).  A row
+ * all of whose scores are -infinity gives zeros.
+ * rows * heads / kv_heads <= 2^30, rows * heads <= 2^36, (rows * heads / kv_heads / 128 + seqs) * kv_heads < 2^23 - 512. */
 typedef struct sc_attn sc_attn;
 
 /* Bytes for plans of up to `seqs` sequences of up to `rows` rows in all. */
@@ -95,7 +97,8 @@ sc_status sparse_kv_read(const sc_kv_desc* desc, int64_t rows, const int64_t* sl
  * lies in page table[r][j / page_rows] (int32[rows][table_width]).  lengths[r] <= 0: o is zero; beyond table_width * page_rows: what the
  * table holds.  Rows of a page that is not in the cache are not there: no weight, nothing read.
  * What lies in the cache behind a sequence's length is not looked at, whatever it is.  A key or value that is not finite loses the heads
- * that read it in this row of q, and no other row. */
+ * that read it in this row of q, and no other row.  rows * heads < 2^24, and so is the number of workgroups, which the sequences' longest
+ * length that table_width allows multiplies. */
 sc_status sparse_attn_decode_workspace_bytes(const sc_attn_desc* desc, const sc_kv_desc* cache, int64_t rows, int64_t table_width,
                                              size_t* bytes);
 sc_status sparse_attn_decode(const sc_attn_desc* desc, const sc_kv_desc* cache, int64_t rows, const void* q_dev, const int32_t* table_dev,

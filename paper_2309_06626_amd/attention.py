@@ -104,6 +104,14 @@ def _matrix(t: torch.Tensor, what: str, rows: int, width: int, dtype: torch.dtyp
     return t.data_ptr(), stride
 
 
+def _same_device(*tensors: Optional[torch.Tensor]):
+    """The library launches on the current device, whose kernels fault on another one's memory."""
+    here = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("a tensor of the call is on another device than the current one")
+
+
 # ---- attention over packed sequences -----------------------------------------------------------------------------------
 
 
@@ -136,6 +144,12 @@ def _open(plan: AttnPlan) -> int:
     return plan.handle
 
 
+def _open_both(plan: AttnPlan, rows: Optional[RowSet]):
+    handles = _open(plan), K._handle(rows)
+    _same_device(plan.workspace, None if rows is None else rows.workspace)
+    return handles
+
+
 def sparse_attn_workspace_bytes(desc: sc_attn_desc, seqs: int, rows: int) -> int:
     n = ctypes.c_size_t()
     B._check(lib().sparse_attn_workspace_bytes(ctypes.byref(desc), seqs, rows, ctypes.byref(n)), "sparse_attn_workspace_bytes")
@@ -155,8 +169,10 @@ def sparse_attn_plan(desc: sc_attn_desc, starts: Sequence[int], rows: Optional[R
     if workspace is None:
         workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device if rows is None else rows.workspace.device)
     at, size = K._workspace(workspace)
+    set_handle = K._handle(rows)
+    _same_device(workspace, None if rows is None else rows.workspace)
     out = ctypes.c_void_p()
-    B._check(lib().sparse_attn_plan(ctypes.byref(desc), seqs, (ctypes.c_int64 * len(starts))(*starts), K._handle(rows), at, size,
+    B._check(lib().sparse_attn_plan(ctypes.byref(desc), seqs, (ctypes.c_int64 * len(starts))(*starts), set_handle, at, size,
                                     K._stream_handle(stream), ctypes.byref(out)), "sparse_attn_plan")
     return AttnPlan(out.value, desc, workspace)
 
@@ -174,7 +190,9 @@ def _attn_rows(plan: AttnPlan, rows: Optional[RowSet], row_format: int, q: torch
 
 
 def _flat(t: torch.Tensor, what: str, numel: int, dtype: torch.dtype) -> int:
-    return K._tensor(t, what, numel, dtype)
+    at = K._tensor(t, what, numel, dtype)
+    _same_device(t)
+    return at
 
 
 def sparse_attn_run(plan: AttnPlan, q, k, v, o, lse=None, rows: Optional[RowSet] = None, row_format: int = SC_ROWS_DENSE, stream=None):
@@ -184,7 +202,7 @@ def sparse_attn_run(plan: AttnPlan, q, k, v, o, lse=None, rows: Optional[RowSet]
     n = _attn_rows(plan, rows, row_format, q)
     wide, narrow = d.heads * d.d, d.kv_heads * d.d
     status = lib().sparse_attn_run(
-        _open(plan), K._handle(rows), row_format, *_matrix(q, "q", n, wide, t), *_matrix(k, "k", n, narrow, t), *_matrix(v, "v", n, narrow, t),
+        *_open_both(plan, rows), row_format, *_matrix(q, "q", n, wide, t), *_matrix(k, "k", n, narrow, t), *_matrix(v, "v", n, narrow, t),
         _flat(o, "o", n * wide, t), None if lse is None else _flat(lse, "lse", plan.kept * d.heads, _F32), K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_attn_run")
@@ -204,8 +222,9 @@ def sparse_attn_backward(plan: AttnPlan, q, k, v, o, lse, do, dq, dk, dv, worksp
     n = _attn_rows(plan, rows, row_format, q)
     wide, narrow = d.heads * d.d, d.kv_heads * d.d
     at, size = K._workspace(workspace)
+    _same_device(workspace)
     B._check(lib().sparse_attn_backward(
-        _open(plan), K._handle(rows), row_format, *_matrix(q, "q", n, wide, t), *_matrix(k, "k", n, narrow, t), *_matrix(v, "v", n, narrow, t),
+        *_open_both(plan, rows), row_format, *_matrix(q, "q", n, wide, t), *_matrix(k, "k", n, narrow, t), *_matrix(v, "v", n, narrow, t),
         _flat(o, "o", n * wide, t), _flat(lse, "lse", plan.kept * d.heads, _F32), _flat(do, "do", n * wide, t),
         *_matrix(dq, "dq", n, wide, t), *_matrix(dk, "dk", n, narrow, t), *_matrix(dv, "dv", n, narrow, t), at, size,
         K._stream_handle(stream)), "sparse_attn_backward")
@@ -244,6 +263,15 @@ class KvCache:
         (self.k_pages, k), (self.v_pages, v) = pages(k_pages, "k_pages"), pages(v_pages, "v_pages")
         (self.k_scales, ks), (self.v_scales, vs) = scales(k_scales, "k_scales"), scales(v_scales, "v_scales")
         self._addresses, self._held = (k, v, ks, vs), (self.k_pages, self.v_pages, self.k_scales, self.v_scales)
+        self.device_index = self.k_pages.get_device()
+        if any(t is not None and t.get_device() != self.device_index for t in self._held):
+            raise ValueError("the cache's tensors are on different devices")
+
+
+def _cache_and(cache: KvCache, *tensors: torch.Tensor):
+    here = _current_device()
+    if cache.device_index != here or any([t.get_device() != here for t in tensors]):
+        raise ValueError("the cache or a tensor of the call is on another device than the current one")
 
 
 def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:
@@ -251,7 +279,9 @@ def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:
     n, width, t = slots.numel(), cache._width, cache.type
     k_at, k_stride = _matrix(k, "k", n, width, t)
     v_at, v_stride = _matrix(v, "v", n, width, t)
-    status = lib().sparse_kv_write(cache._reference, n, k_at, k_stride, v_at, v_stride, K._tensor(slots, "slots", n, _I64), *cache._addresses,
+    slots_at = K._tensor(slots, "slots", n, _I64)
+    _cache_and(cache, slots)
+    status = lib().sparse_kv_write(cache._reference, n, k_at, k_stride, v_at, v_stride, slots_at, *cache._addresses,
                                    K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_kv_write")
@@ -263,7 +293,9 @@ def sparse_kv_read(cache: KvCache, slots, k, v, stream=None):
     n, width, t = slots.numel(), cache._width, cache.type
     k_at, k_stride = _matrix(k, "k", n, width, t)
     v_at, v_stride = _matrix(v, "v", n, width, t)
-    status = lib().sparse_kv_read(cache._reference, n, K._tensor(slots, "slots", n, _I64), *cache._addresses, k_at, k_stride, v_at, v_stride,
+    slots_at = K._tensor(slots, "slots", n, _I64)
+    _cache_and(cache, slots)
+    status = lib().sparse_kv_read(cache._reference, n, slots_at, *cache._addresses, k_at, k_stride, v_at, v_stride,
                                   K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_kv_read")
@@ -289,10 +321,10 @@ def sparse_attn_decode(desc: sc_attn_desc, cache: KvCache, q, table, lengths, o,
         raise ValueError(f"table must be [{n}, pages of a sequence]")
     tensor, width = K._tensor, table.shape[1]
     at, size = K._workspace(workspace)
-    status = lib().sparse_attn_decode(
-        ctypes.byref(desc), cache._reference, n, _matrix(q, "q", n, wide, t)[0] if q.is_contiguous() else tensor(q, "q", n * wide, t),
-        tensor(table, "table", n * width, _I32), width, tensor(lengths, "lengths", n, _I32), *cache._addresses, tensor(o, "o", n * wide, t), at,
-        size, K._stream_handle(stream))
+    of = (_matrix(q, "q", n, wide, t)[0] if q.is_contiguous() else tensor(q, "q", n * wide, t), tensor(table, "table", n * width, _I32), width,
+          tensor(lengths, "lengths", n, _I32), *cache._addresses, tensor(o, "o", n * wide, t), at, size)
+    _cache_and(cache, table, lengths, o, workspace)
+    status = lib().sparse_attn_decode(ctypes.byref(desc), cache._reference, n, *of, K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_attn_decode")
     return o

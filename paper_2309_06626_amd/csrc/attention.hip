@@ -70,7 +70,7 @@ sc_status check_attn(const sc_attn_desc* d) {
   if (d->dtype != SC_F32 && d->dtype != SC_F16 && d->dtype != SC_BF16) return SC_ERR_UNSUPPORTED;
   if (d->causal != 0 && d->causal != 1) return SC_ERR_UNSUPPORTED;
   if (d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > 512 || d->heads > (1 << 20)) return SC_ERR_BAD_SHAPE;
-  if (d->d < 1 || d->window < 0 || !std::isfinite(d->scale) || !(d->scale > 0.0f)) return SC_ERR_BAD_SHAPE;
+  if (d->d < 1 || d->window < 0 || !std::isfinite(d->scale) || !(d->scale > 0.0f) || d->scale > 0x1p127f) return SC_ERR_BAD_SHAPE;      // (kernels take it in exponents of 2)
   if (d->d > 128) return SC_ERR_UNSUPPORTED;
   return SC_OK;
 }
@@ -213,9 +213,9 @@ sc_status sparse_attn_workspace_bytes(const sc_attn_desc* desc, int64_t seqs, in
   *bytes = 0;
   const sc_status st = sc::check_attn(desc);
   if (st != SC_OK) return st;
-  // packed rows and workgroups are counted in 32 bits, of which tiles need a few
+  // packed rows are counted in 32 bits, of which tiles need a few; a launch of workgroups of 512 lanes, those of zeros among them, has fewer than 2^32
   if (seqs < 0 || rows < 0 || seqs > (1 << 24) || rows > 0x7fffffff || rows * desc->heads > ((int64_t)1 << 36) ||
-      rows * (desc->heads / desc->kv_heads) > (1 << 30) || (rows * (desc->heads / desc->kv_heads) / sc::kAttnRowsLeast + seqs) * desc->kv_heads > (1 << 23))
+      rows * (desc->heads / desc->kv_heads) > (1 << 30) || (rows * (desc->heads / desc->kv_heads) / sc::kAttnRowsLeast + seqs) * desc->kv_heads >= (1 << 23) - 512)
     return SC_ERR_BAD_SHAPE;
   const sc::AttnLayout l = sc::attn_layout(desc, seqs, rows);
   *bytes = 2 * l.starts + 2 * l.row_items + l.key_items;

@@ -43,7 +43,7 @@ static sc_status decode_check(const sc_attn_desc* desc, const sc_kv_desc* cache,
   if (rows < 0 || table_width < 0 || rows > (1 << 24) || table_width > 0x7fffffff || table_width * cache->page_rows > 0x7fffffff) return SC_ERR_BAD_SHAPE;
   // a launch has fewer than 2^32 lanes
   const int64_t blocks = (desc->heads / desc->kv_heads + 31) / 32;
-  if (rows * blocks * desc->kv_heads * decode_splits(desc, cache, rows, table_width) >= (1 << 24) || rows * desc->heads >= (1 << 25)) return SC_ERR_BAD_SHAPE;
+  if (rows * blocks * desc->kv_heads * decode_splits(desc, cache, rows, table_width) >= (1 << 24) || rows * desc->heads >= (1 << 24)) return SC_ERR_BAD_SHAPE;
   return SC_OK;
 }
 

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
     if (p.vec) Q::template read_row<2>(q, p.d, h, there, f);
     else Q::template read_row<0>(q, p.d, h, there, f);
     if constexpr (CT != DT) {
-      c = fmaxf(c * decode_narrow<IO, T>(f, qf), 1e-37f);      // (not 0, whatever the scale: what is not seen is -infinity times it)
+      c = fminf(fmaxf(c * decode_narrow<IO, T>(f, qf), 1e-37f), 3e38f);      // (neither 0 nor infinite, whatever the scale: scores are, times it)
     } else {
 #pragma unroll
       for (int ks = 0; ks < A::KS; ++ks) qf[ks] = f[ks];

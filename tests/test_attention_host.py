@@ -45,7 +45,7 @@ def test_every_entry_point_is_exported_and_declared_with_its_arguments():
 BAD_ATTN = [("heads", 0, B.SC_ERR_BAD_SHAPE), ("kv_heads", 0, B.SC_ERR_BAD_SHAPE), ("kv_heads", 3, B.SC_ERR_BAD_SHAPE), ("heads", 513 * 2, B.SC_ERR_BAD_SHAPE),
             ("d", 0, B.SC_ERR_BAD_SHAPE), ("d", 129, B.SC_ERR_UNSUPPORTED), ("dtype", 3, B.SC_ERR_UNSUPPORTED), ("causal", 2, B.SC_ERR_UNSUPPORTED),
             ("window", -1, B.SC_ERR_BAD_SHAPE), ("scale", 0.0, B.SC_ERR_BAD_SHAPE), ("scale", -1.0, B.SC_ERR_BAD_SHAPE),
-            ("scale", float("nan"), B.SC_ERR_BAD_SHAPE), ("scale", float("inf"), B.SC_ERR_BAD_SHAPE)]
+            ("scale", float("nan"), B.SC_ERR_BAD_SHAPE), ("scale", float("inf"), B.SC_ERR_BAD_SHAPE), ("scale", 2.0 ** 127 * 1.5, B.SC_ERR_BAD_SHAPE)]
 BAD_KV = [("kv_heads", 0, B.SC_ERR_BAD_SHAPE), ("d", 0, B.SC_ERR_BAD_SHAPE), ("d", 129, B.SC_ERR_UNSUPPORTED), ("page_rows", 0, B.SC_ERR_BAD_SHAPE),
           ("page_rows", 24, B.SC_ERR_BAD_SHAPE), ("page_rows", 1 << 17, B.SC_ERR_BAD_SHAPE), ("pages", 0, B.SC_ERR_BAD_SHAPE),
           ("pages", 1 << 30, B.SC_ERR_BAD_SHAPE), ("dtype", -1, B.SC_ERR_UNSUPPORTED), ("bits", 4, B.SC_ERR_UNSUPPORTED)]
@@ -89,6 +89,9 @@ def test_plans_refuse():
     for seqs, rows in ((-1, 5), (1, -1), (1, 1 << 31), (1 << 25, 5)):
         assert L.sparse_attn_workspace_bytes(ctypes.byref(d), seqs, rows, ctypes.byref(size)) == B.SC_ERR_BAD_SHAPE
     assert L.sparse_attn_workspace_bytes(ctypes.byref(A.make_attn_desc(512, 1, 64)), 1, 1 << 22, ctypes.byref(size)) == B.SC_ERR_BAD_SHAPE
+    most = (1 << 23) - 512      # workgroups, of sequences of a row and of two key-value heads
+    for seqs, status in ((most // 2 - 1, B.SC_OK), (most // 2, B.SC_ERR_BAD_SHAPE)):
+        assert L.sparse_attn_workspace_bytes(ctypes.byref(d), seqs, 0, ctypes.byref(size)) == status
     assert L.sparse_attn_workspace_bytes(ctypes.byref(d), 3, 1000, ctypes.byref(size)) == B.SC_OK and size.value > 0
     need = size.value
 
@@ -173,6 +176,8 @@ def test_decode_calls_refuse():
     assert nbytes() == B.SC_OK
     need = size.value
     assert nbytes(rows=-1) == nbytes(width=-1) == nbytes(width=1 << 30) == nbytes(rows=1 << 25) == B.SC_ERR_BAD_SHAPE and size.value == 0
+    ones = A.make_kv_desc(2, 64, 1, 10)      # stretches of 2 000 pages: a second launch has a workgroup for every head
+    assert nbytes(rows=(1 << 22) - 1, width=1, cache=ones) == B.SC_OK and nbytes(rows=1 << 22, width=1, cache=ones) == B.SC_ERR_BAD_SHAPE
     for other in (A.make_kv_desc(1, 64, 16, 10), A.make_kv_desc(2, 32, 16, 10), A.make_kv_desc(2, 64, 16, 10, dtype=A.SC_F16)):
         assert nbytes(cache=other) == B.SC_ERR_BAD_SHAPE
     assert L.sparse_attn_decode_workspace_bytes(ctypes.byref(d), ctypes.byref(kv), 1, 1, None) == B.SC_ERR_NULL
@@ -265,6 +270,49 @@ def test_binding_looks_at_rows_types_and_strides(recorder):
         A.sparse_attn_run(plan, q, k, k, o, rows=closed)
     assert len(recorder.calls) == 2
     plan.handle = None
+
+
+def test_binding_looks_at_devices(recorder, monkeypatch):
+    """Of every tensor of a call, and of those that plans, row sets and caches hold."""
+    def other(t):
+        t.device_index = 1
+        return t
+
+    d, bf, f32, u8 = A.make_attn_desc(4, 2, 64), torch.bfloat16, torch.float32, torch.uint8
+    plan, rows = plan_of(d, 10, 10), A.RowSet.__new__(A.RowSet)
+    plan.workspace, rows.workspace, rows.handle, rows.rows, rows.kept = fake(64, dtype=u8), fake(64, dtype=u8), FAKE, 10, 10
+    cache = A.KvCache.__new__(A.KvCache)
+    cache.desc, cache.type, cache._width, cache._reference, cache._addresses, cache.device_index = A.make_kv_desc(2, 64, 16, 9), bf, 128, None, (0,) * 4, 0
+
+    def calls():
+        wide, narrow, ws = (10, 4, 64), (10, 2, 64), (64,)
+        kept = (plan.workspace, rows.workspace)
+        yield lambda *t: A.sparse_attn_run(plan, *t, rows=rows), [wide, narrow, narrow, wide], [bf] * 4, kept
+        yield lambda *t: A.sparse_attn_run(plan, *t, rows=rows), [wide, narrow, narrow, wide, (10, 4)], [bf] * 4 + [f32], kept
+        yield (lambda *t: A.sparse_attn_backward(plan, *t, rows=rows), [wide, narrow, narrow, wide, (10, 4), wide, wide, narrow, narrow, ws],
+               [bf] * 4 + [f32] + [bf] * 4 + [u8], kept)
+        yield lambda *t: A.sparse_kv_write(cache, *t), [narrow, narrow, (10,)], [bf, bf, torch.int64], (cache,)
+        yield lambda s, k, v: A.sparse_kv_read(cache, s, k, v), [(10,), narrow, narrow], [torch.int64, bf, bf], (cache,)
+        yield lambda *t: A.sparse_attn_decode(d, cache, *t), [wide, (10, 3), (10,), wide, ws], [bf, torch.int32, torch.int32, bf, u8], (cache,)
+
+    for call, shapes, types, helds in calls():
+        tensors = lambda: [fake(*s, dtype=t) for s, t in zip(shapes, types)]  # noqa: E731,B023
+        call(*tensors())
+        done = len(recorder.calls)
+        for i in range(len(shapes)):
+            with pytest.raises(ValueError, match="another device"):
+                ts = tensors()
+                other(ts[i])
+                call(*ts)
+        for held in helds:
+            held.device_index = 1
+            with pytest.raises(ValueError, match="another device"):
+                call(*tensors())
+            held.device_index = 0
+        assert len(recorder.calls) == done
+    with pytest.raises(ValueError, match="different devices"):
+        A.KvCache(A.make_kv_desc(2, 64, 16, 9), fake(0), other(fake(0)))      # (the recorder has rows of no entries)
+    plan.handle = rows.handle = None
 
 
 def test_binding_looks_at_starts():

@@ -723,3 +723,71 @@ def test_on_another_stream():
     A.sparse_attn_run(plan, q, k, v, o, stream=stream)
     stream.synchronize()
     assert same(o, want["o"])
+
+
+def test_two_calls_at_once():
+    """One plan and one cache on two streams, with outputs and workspaces of their own."""
+    c = ([900, 30, 1100], 8, 2, 128, "bf16", True, 0, 1.0, 0, 0)
+    starts, rows, keep, x = case_inputs(c, 6)
+    plan = A.sparse_attn_plan(A.make_attn_desc(8, 2, 128), starts)
+    sets = [{n: dev(t if s == 0 else t.flip(0), "bf16").reshape(rows, -1, 128) for n, t in x.items() if n in ("q", "k", "v", "do")} for s in range(2)]
+    dc = ([700, 1900, 64], 8, 2, 128, 16, "bf16", 8, 0, 0)
+    cache, table, dq, _, _ = decode_inputs(dc, 7)
+    table, desc, lens = table.to(DEV), A.make_attn_desc(8, 2, 128), torch.tensor(dc[0], dtype=torch.int32, device=DEV)
+    ask, size = [dev(dq, "bf16"), dev(dq.flip(0), "bf16")], A.sparse_attn_decode_workspace_bytes(desc, cache.desc, 3, table.shape[1])
+
+    def buffers():
+        b = {"o": nans(rows, 8, 128, dtype="bf16"), "lse": nans(rows, 8), "dq": nans(rows, 8, 128, dtype="bf16"), "dk": nans(rows, 2, 128, dtype="bf16"),
+             "dv": nans(rows, 2, 128, dtype="bf16"), "token": nans(3, 8, 128, dtype="bf16")}
+        return b, [torch.empty(max(n, 16), dtype=torch.uint8, device=DEV) for n in (A.sparse_attn_backward_workspace_bytes(plan), size)]
+
+    def go(i, b, ws, stream=None):
+        s = sets[i]
+        A.sparse_attn_run(plan, s["q"], s["k"], s["v"], b["o"], b["lse"], stream=stream)
+        A.sparse_attn_backward(plan, s["q"], s["k"], s["v"], b["o"], b["lse"], s["do"], b["dq"], b["dk"], b["dv"], ws[0], stream=stream)
+        A.sparse_attn_decode(desc, cache, ask[i], table, lens, b["token"], ws[1], stream=stream)
+
+    want = []
+    for i in range(2):
+        b, ws = buffers()
+        go(i, b, ws)
+        want.append(b)
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [buffers(), buffers()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i in range(2):
+            go(i, *got[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for name, t in want[i].items():
+            assert same(got[i][0][name], t), (i, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_scores_of_minus_infinity(dtype):
+    """A key whose score is -infinity has no weight; a row of such scores alone gives zeros, and so does a token."""
+    n, d = 70, 64
+    q, k = torch.ones(n, 1, d), torch.zeros(n, 1, d)
+    v = torch.arange(n).float().reshape(n, 1, 1).expand(n, 1, d).contiguous()
+    lost = torch.tensor([0, 1, 5, 64])
+    k[lost, 0, 3] = -float("inf")
+    plan = A.sparse_attn_plan(A.make_attn_desc(1, 1, d, A.DTYPE_CODE[dtype]), [0, n])
+    o, lse = nans(n, 1, d, dtype=dtype), nans(n, 1)
+    A.sparse_attn_run(plan, dev(q, dtype), dev(k, dtype), dev(v, dtype), o, lse)
+    some = torch.ones(n).index_fill(0, lost, 0)
+    count = some.cumsum(0)
+    want = ((some * torch.arange(n)).double().cumsum(0) / count.clamp_min(1)).reshape(n, 1, 1).expand(n, 1, d)
+    step = torch.finfo(O.TORCH[dtype]).eps / 2 + 4 * O.E      # weights are 1; of the result, of 1 / sum, of the product and of the shares' join
+    inside(o, want, step * want.abs(), "o")
+    assert (lse.cpu()[count == 0] == -float("inf")).all()
+    inside(lse[2:], count[2:].double().log()[:, None], 8 * O.E * count[2:].double().log()[:, None] + 2.0 ** -22, "lse")
+    cache = cache_of(1, d, 16, 5, dtype, 0)
+    A.sparse_kv_write(cache, dev(k, dtype), dev(v, dtype), torch.arange(n, device=DEV))
+    desc = A.make_attn_desc(1, 1, d, plan.desc.dtype)
+    lengths = torch.tensor([1, 2, 3, 6, 70, 0], dtype=torch.int32, device=DEV)
+    table = torch.arange(5, dtype=torch.int32, device=DEV).repeat(6, 1)
+    ws = torch.empty(A.sparse_attn_decode_workspace_bytes(desc, cache.desc, 6, 5), dtype=torch.uint8, device=DEV)
+    token = nans(6, 1, d, dtype=dtype)
+    A.sparse_attn_decode(desc, cache, dev(q[:6], dtype), table, lengths, token, ws)
+    want = torch.stack([want[i - 1] if i else torch.zeros_like(want[0]) for i in lengths.tolist()])
+    inside(token, want, step * want.abs(), "token")
