@@ -26,6 +26,11 @@ namespace sc {
 void note_hip_error(int32_t code);
 
 static hipError_t attn_dispatch(int dtype, int what, const AttnParams& p, AttnTiles t, int vec, hipStream_t s) {
+  if (t.waves == 1) {
+    if (dtype == SC_BF16) return attn_few_launch<kBF16>(what, p, vec, s);
+    if (dtype == SC_F16) return attn_few_launch<kF16>(what, p, vec, s);
+    return attn_few_launch<kF32>(what, p, vec, s);
+  }
   if (dtype == SC_BF16) return attn_launch<kBF16>(what, p, t, vec, s);
   if (dtype == SC_F16) return attn_launch<kF16>(what, p, t, vec, s);
   return attn_launch<kF32>(what, p, t, vec, s);
@@ -64,6 +69,7 @@ static void attn_zeros_of(const sc_rows* set, int64_t rows, std::initializer_lis
 static size_t attn_up(size_t n) { return (n + 255) & ~(size_t)255; }
 static int64_t attn_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int kAttnRowsLeast = 128;      // packed rows of the smallest tile
+constexpr int kAttnFew = 2048;           // most workgroups of the tiles for few rows
 
 sc_status check_attn(const sc_attn_desc* d) {
   if (!d) return SC_ERR_NULL;
@@ -81,8 +87,8 @@ static AttnLayout attn_layout(const sc_attn_desc* d, int64_t seqs, int64_t rows)
   const int64_t group = d->heads / d->kv_heads;
   AttnLayout l;
   l.starts = attn_up((size_t)(seqs + 1) * 4);
-  l.row_items = attn_up((size_t)(rows * group / kAttnRowsLeast + seqs) * sizeof(AttnItem));      // (twice: forward and backward)
-  l.key_items = attn_up((size_t)(rows / (32 * kAttnKeyWaves) + seqs) * sizeof(AttnItem));
+  l.row_items = attn_up((size_t)(rows * group / kAttnRowsLeast + seqs + kAttnFew) * sizeof(AttnItem));      // (twice: forward and backward)
+  l.key_items = attn_up((size_t)(rows / (32 * kAttnKeyWaves) + seqs + kAttnFew) * sizeof(AttnItem));
   return l;
 }
 
@@ -147,9 +153,21 @@ static sc_status attn_plan(sc_attn* plan, int64_t seqs, const int64_t* starts, c
   const int64_t seen = attn_items(at, d, 128, false, items[0]);
   plan->forward = {wide && seen >= 2048 ? 8 : 4, d.d <= 64 && seen <= 256 ? 32 : 64};
   plan->backward = {wide && d.d % 8 == 0 && plan->kept * (d.heads / d.kv_heads) >= 512 * seqs ? 8 : 4, 64};
-  if (plan->forward.waves == 8) attn_items(at, d, 256, false, items[0]);
+  // Few rows: tiles of 32, whose workgroup's wavefronts share what passes by.  Gradients up to 1 024 workgroups (16 heads on 4: 2 048 rows of 128 in
+  // 16 bits, training 367 and 235 us, 16 x 128 rows 50.9 and 49.3; 8 heads of 64 floats: 512 rows 175 and 93, 8 x 512 184 and 159, 16 x 512 253 and
+  // 269), of long sequences in 16 bits up to 2 048 (4 096 rows 734 and 591, 32 x 128 rows 63 and 83).  Forward of floats alone, up to 512, where it takes
+  // those 93 us to 71 (8 x 512, 1 024 workgroups of heads of 128: 343 and 364); in 16 bits it gains nothing (1 024 rows alone: 21 and 33).
+  int64_t row_tiles = 0, key_tiles = 0;
+  for (int64_t i = 0; i < seqs; ++i) {
+    row_tiles += attn_ceil((int64_t)(at[i + 1] - at[i]) * (d.heads / d.kv_heads), 32);
+    key_tiles += attn_ceil(at[i + 1] - at[i], 32);
+  }
+  const bool few = row_tiles * d.kv_heads <= 512 && !wide, few_backward = std::max(row_tiles, key_tiles) * d.kv_heads <= (wide && seen >= 1024 ? kAttnFew : 1024);
+  if (few) plan->forward.waves = 1;
+  if (few_backward) plan->backward.waves = 1;
+  if (plan->forward.waves != 4) attn_items(at, d, 32 * plan->forward.waves, false, items[0]);
   attn_items(at, d, 32 * plan->backward.waves, false, items[1]);
-  attn_items(at, d, 32 * kAttnKeyWaves, true, items[2]);
+  attn_items(at, d, few_backward ? 32 : 32 * kAttnKeyWaves, true, items[2]);
   unsigned char* to = w + 2 * l.starts;
   for (int k = 0; k < 3; ++k) {
     plan->items[k] = reinterpret_cast<const AttnItem*>(to);

@@ -34,12 +34,13 @@ struct AttnParams {
 };
 
 struct AttnTiles {
-  int32_t waves;                       // wavefronts of a workgroup, 32 packed rows each
+  int32_t waves;                       // wavefronts of a workgroup, 32 packed rows each; 1: four that share 32
   int32_t keys;                        // of a tile that passes by (forward)
 };
 
 // vec: rows are whole 16-byte groups (2), 4-byte ones (1) or neither (0)
 template <int DT> hipError_t attn_launch(int what, const AttnParams& p, AttnTiles t, int vec, hipStream_t s);
+template <int DT> hipError_t attn_few_launch(int what, const AttnParams& p, int vec, hipStream_t s);
 
 constexpr int kAttnKeyWaves = 4;                            // wavefronts of a workgroup of the keys' gradients, 32 keys each
 enum { kAttnForward, kAttnBackwardQ, kAttnBackwardKV };

@@ -161,6 +161,20 @@ template <int DT, int DP> struct AttnTile {
     v4i g = {0, 0, 0, 0};
     if constexpr (VEC == 2) {
       if (there && c < d) g = *reinterpret_cast<const v4i*>(row + c);
+    } else if (d >= V) {
+      // whatever the alignment; a group that the row ends in is that of the row's end, moved down
+      const int at = min(c, d - V);
+      if (there && c < d) __builtin_memcpy(&g, row + at, 16);
+      if (d % V) {
+        const int down = (c - at) * EB;
+        if (EB == 2) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) g[i] = down & 2 ? (int)((unsigned)g[i] >> 16 | (unsigned)(i < 3 ? g[i < 3 ? i + 1 : i] : 0) << 16) : g[i];
+        }
+        g = down & 4 ? v4i{g[1], g[2], g[3], 0} : g;
+        g = down & 8 ? v4i{g[2], g[3], 0, 0} : g;
+        if (c >= d) g = v4i{0, 0, 0, 0};
+      }
     } else {
       T e[V];
 #pragma unroll
@@ -183,8 +197,17 @@ template <int DT, int DP> struct AttnTile {
         if (c0 + i * V < d) *reinterpret_cast<v4i*>(row + c0 + i * V) = g[i];
     } else {
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (c0 + v < d) row[c0 + v] = r[v];
+      for (int i = 0; i < EB; ++i) write_group(row, c0 + i * V, d, r + i * V);
+    }
+  }
+  // a 16-byte group whatever the alignment, of which the row may hold a part
+  static __device__ __forceinline__ void write_group(T* row, int c, int d, const T* r) {
+    if (c + V <= d) {
+      __builtin_memcpy(row + c, r, 16);
+    } else {
+#pragma unroll
+      for (int v = 0; v < V - 1; ++v)
+        if (c + v < d) row[c + v] = r[v];
     }
   }
 
@@ -211,34 +234,44 @@ template <int DT, int DP> struct AttnTile {
   // Transfer of ROWS rows by NT lanes: `place(r)` is the row's address in memory, null for a row of zeros.
   template <int ROWS, int NT> static constexpr int transfers() { return ROWS * GROUPS / NT; }
   template <int ROWS, int NT, int VEC, class Place>
-  static __device__ __forceinline__ void request(unsigned tile, int d, Place&& place) {
+  static __device__ __forceinline__ void request(unsigned tile, int d, Place&& place, int t = threadIdx.x) {
     constexpr int J = ROWS * GROUPS / NT;
     static_assert(J >= 1 && ROWS * GROUPS % NT == 0, "whole transfers");
-    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    // (a wavefront that transfers alone has many addresses: eight at a time)
+    constexpr int TRANSFERS = VEC == 1 ? 4 * J : J, STEP = NT == 64 && TRANSFERS > 8 ? 8 : TRANSFERS;
     if constexpr (VEC == 1) {      // 4 bytes a lane
       constexpr int WORDS = RB / 4, PER = 4 / EB;
-      const void* from[4 * J];
+#pragma unroll 1
+      for (int j0 = 0; j0 < TRANSFERS; j0 += STEP) {
+        const void* from[STEP];
 #pragma unroll
-      for (int j = 0; j < 4 * J; ++j) {
-        const int at = j * NT + t, r = at / WORDS, word = at % WORDS, c = (((word >> 2) ^ key(r)) << 2 | (word & 3)) * PER;
-        const T* row = place(r);
-        from[j] = row && c < d ? (const void*)(row + c) : (const void*)&attn_zeros;
+        for (int j = 0; j < STEP; ++j) {
+          const int at = (j0 + j) * NT + t, r = at / WORDS, word = at % WORDS, c = (((word >> 2) ^ key(r)) << 2 | (word & 3)) * PER;
+          const T* row = place(r);
+          from[j] = row && c < d ? (const void*)(row + c) : (const void*)&attn_zeros;
+        }
+#pragma unroll
+        for (int j = 0; j < STEP; ++j) attn_dma4(from[j], tile + ((j0 + j) * NT + wave * 64) * 4);
+        if constexpr (STEP < TRANSFERS) __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int j = 0; j < 4 * J; ++j) attn_dma4(from[j], tile + (j * NT + wave * 64) * 4);
       return;
     }
-    const T* from[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) from[j] = place((j * NT + t) / GROUPS);
+    for (int j0 = 0; j0 < TRANSFERS; j0 += STEP) {
+      const T* from[STEP];
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int at = j * NT + t, g = (at % GROUPS) ^ key(at / GROUPS);
-      if constexpr (VEC == 2) {
-        attn_dma16(from[j] && g * V < d ? (const void*)(from[j] + g * V) : (const void*)&attn_zeros, tile + (j * NT + wave * 64) * 16);
-      } else {
-        *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<0>(from[j], g * V, d, from[j] != nullptr);
+      for (int j = 0; j < STEP; ++j) from[j] = place(((j0 + j) * NT + t) / GROUPS);
+#pragma unroll
+      for (int j = 0; j < STEP; ++j) {
+        const int at = (j0 + j) * NT + t, g = (at % GROUPS) ^ key(at / GROUPS);
+        if constexpr (VEC == 2) {
+          attn_dma16(from[j] && g * V < d ? (const void*)(from[j] + g * V) : (const void*)&attn_zeros, tile + ((j0 + j) * NT + wave * 64) * 16);
+        } else {
+          *(__attribute__((address_space(3))) v4i*)(uint64_t)(tile + at * 16) = group<0>(from[j], g * V, d, from[j] != nullptr);
+        }
       }
+      if constexpr (STEP < TRANSFERS) __builtin_amdgcn_sched_barrier(0);
     }
   }
 };

@@ -77,6 +77,9 @@ CASES = [  # lengths, heads, kv heads, d, dtype, causal, window, share of rows k
     ([40], 48, 1, 64, "bf16", True, 7, 0.7, 0, 0),
     ([33, 70], 14, 2, 128, "bf16", False, 0, 1.0, 0, 0),
     ([70, 30], 64, 1, 128, "f32", True, 0, 1.0, 0, 0),
+    ([900, 41], 3, 1, 41, "f32", True, 0, 0.6, 0, 2),
+    ([700, 650], 4, 2, 63, "bf16", False, 0, 0.7, 0, 0),
+    ([1100], 2, 2, 128, "f16", True, 300, 0.7, 1, 0),
 ]
 
 
@@ -122,11 +125,17 @@ def packed_call(c, starts, keep, x, rows_set=None, pad=0, stream=None):
     return plan, at, dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv)
 
 
-def packed_check(c, seed, pad=0):
+def packed_check(c, seed, pad=0, times=1):
     lens, heads, kv, d, dtype, causal, window, share, fmt, tail = c
     starts, rows, keep, x = case_inputs(c, seed)
-    plan, at, got = packed_call(c, starts, keep, x, pad=pad)
     want, bound = O.packed((heads, kv, d, dtype, causal, window, 1 / math.sqrt(d)), starts, keep, x["q"], x["k"], x["v"], x["do"])
+    if times > 1:      # the sequences again and again
+        end = starts[-1]
+        again = lambda t: torch.cat([t[:end]] * times + [t[end:]])  # noqa: E731
+        keep, x, want, bound = again(keep), {n: again(t) for n, t in x.items()}, {n: again(t) for n, t in want.items()}, {n: again(t) for n, t in bound.items()}
+        starts = starts_of(lens * times)
+        c = (lens * times, *c[1:])
+    plan, at, got = packed_call(c, starts, keep, x, pad=pad)
     inside_rows = at < starts[-1]
     kept_rows = keep.nonzero()[:, 0]
     kept_rows = kept_rows[kept_rows < starts[-1]]
@@ -150,6 +159,13 @@ def test_packed_forward_and_gradients(c):
 @pytest.mark.parametrize("pad", [1, 2, 8])
 def test_rows_with_gaps(dtype, pad):
     packed_check(([70, 33], 4, 2, 64, dtype, True, 0, 0.8, 0, 1), 3, pad)
+
+
+@pytest.mark.parametrize("c", [c for c in CASES if c[0] != [700, 650]], ids=lambda c: "-".join(map(str, [sum(c[0]), len(c[0]), *c[1:]])))
+def test_many_of_them(c):
+    """Few rows are cut into smaller tiles than many: more than 2 048 tiles of 32, kept rows counted."""
+    tiles = sum(-(-int(n * c[7] * 0.8) * c[1] // c[2] // 32) for n in c[0]) * c[2]
+    packed_check(c, sum(c[0]) + c[3], times=2049 // max(tiles, 1) + 1 if c[7] else 2)
 
 
 @pytest.mark.parametrize("pad", [1, 2, 8])
