@@ -3,7 +3,11 @@
 // A workgroup takes 32 packed rows (or keys) in place of 128 or 256, and its four wavefronts every fourth block of 32 of what passes by, each on its
 // own: a transfer, two or four products and the softmax between, without a meeting.  Their shares (of the forward pass with maxima and sums) are joined
 // in LDS at the end, in a fixed order.  Keys and values are read four times as often, which does not matter as long as a compute unit has no more than
-// a few workgroups.  Bound by the latency of one wavefront's steps: 8 x 196 rows, 4 heads of 64 floats, training ... us.
+// a few workgroups.
+//
+// Bound by the latency of a wavefront's steps, of which it has a quarter as many.  Training, gradients and in floats the forward pass by these kernels:
+// 2 048 rows, 16 heads of 128 on 4 in bf16, 235 us (367 with tiles of 128 and 256 rows); 512 rows, 8 heads of 64 floats, 71 (175); 8 x 196 rows of
+// which 30 % are dropped, 10 heads of 41 floats, 84 (105), where transfers of 4 bytes a lane and their addresses are half of it (40 channels: 57).
 #pragma once
 #include "attn_kernel.hpp"
 
@@ -101,7 +105,7 @@ template <class A, int VEC, class T> __device__ __forceinline__ auto few_place(c
 }
 
 // The workgroup's own rows of N tensors, `at` being that of a lane (null: none).  Where rows are not whole 16-byte groups, a lane that read a row by
-// itself would ask for a cache line an entry (10 heads of 41 floats, 8 x 137 rows, training: ... and ... us): they come as tiles, one a wavefront,
+// itself would ask for a cache line an entry (the 84 us above 91): they come as tiles, one a wavefront,
 // into the places where what passes by will lie.
 template <class F, int VEC, int N, class T>
 __device__ __forceinline__ void few_own(const AttnParams& p, unsigned lds, const T* const (&at)[N], v4i (&f)[N][F::A::KS]) {

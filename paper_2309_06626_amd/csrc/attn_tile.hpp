@@ -162,7 +162,8 @@ template <int DT, int DP> struct AttnTile {
     if constexpr (VEC == 2) {
       if (there && c < d) g = *reinterpret_cast<const v4i*>(row + c);
     } else if (d >= V) {
-      // whatever the alignment; a group that the row ends in is that of the row's end, moved down
+      // whatever the alignment; a group that the row ends in is that of the row's end, moved down (entry by entry the training of 16 x 512 rows, 16
+      // heads of 63 in f16, took 290 us in place of 162)
       const int at = min(c, d - V);
       if (there && c < d) __builtin_memcpy(&g, row + at, 16);
       if (d % V) {
@@ -238,7 +239,8 @@ template <int DT, int DP> struct AttnTile {
     constexpr int J = ROWS * GROUPS / NT;
     static_assert(J >= 1 && ROWS * GROUPS % NT == 0, "whole transfers");
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    // (a wavefront that transfers alone has many addresses: eight at a time)
+    // (a wavefront that transfers alone has many addresses: eight at a time, and code that is read once costs as much as what it does: written
+    // out, the gradients of 8 x 137 rows, 10 heads of 41 floats, took 90 us in place of 84)
     constexpr int TRANSFERS = VEC == 1 ? 4 * J : J, STEP = NT == 64 && TRANSFERS > 8 ? 8 : TRANSFERS;
     if constexpr (VEC == 1) {      // 4 bytes a lane
       constexpr int WORDS = RB / 4, PER = 4 / EB;
