@@ -268,10 +268,8 @@ class KvCache:
             raise ValueError("the cache's tensors are on different devices")
 
 
-def _cache_and(cache: KvCache, *tensors: torch.Tensor):
-    here = _current_device()
-    if cache.device_index != here or any([t.get_device() != here for t in tensors]):
-        raise ValueError("the cache or a tensor of the call is on another device than the current one")
+def _elsewhere():
+    raise ValueError("the cache or a tensor of the call is on another device than the current one")
 
 
 def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:
@@ -280,7 +278,8 @@ def sparse_kv_write(cache: KvCache, k, v, slots, stream=None) -> KvCache:
     k_at, k_stride = _matrix(k, "k", n, width, t)
     v_at, v_stride = _matrix(v, "v", n, width, t)
     slots_at = K._tensor(slots, "slots", n, _I64)
-    _cache_and(cache, slots)
+    if not cache.device_index == _current_device() == slots.get_device():
+        _elsewhere()
     status = lib().sparse_kv_write(cache._reference, n, k_at, k_stride, v_at, v_stride, slots_at, *cache._addresses,
                                    K._stream_handle(stream))
     if status:
@@ -294,7 +293,8 @@ def sparse_kv_read(cache: KvCache, slots, k, v, stream=None):
     k_at, k_stride = _matrix(k, "k", n, width, t)
     v_at, v_stride = _matrix(v, "v", n, width, t)
     slots_at = K._tensor(slots, "slots", n, _I64)
-    _cache_and(cache, slots)
+    if not cache.device_index == _current_device() == slots.get_device():
+        _elsewhere()
     status = lib().sparse_kv_read(cache._reference, n, slots_at, *cache._addresses, k_at, k_stride, v_at, v_stride,
                                   K._stream_handle(stream))
     if status:
@@ -323,7 +323,8 @@ def sparse_attn_decode(desc: sc_attn_desc, cache: KvCache, q, table, lengths, o,
     at, size = K._workspace(workspace)
     of = (_matrix(q, "q", n, wide, t)[0] if q.is_contiguous() else tensor(q, "q", n * wide, t), tensor(table, "table", n * width, _I32), width,
           tensor(lengths, "lengths", n, _I32), *cache._addresses, tensor(o, "o", n * wide, t), at, size)
-    _cache_and(cache, table, lengths, o, workspace)
+    if not cache.device_index == _current_device() == table.get_device() == lengths.get_device() == o.get_device() == workspace.get_device():
+        _elsewhere()
     status = lib().sparse_attn_decode(ctypes.byref(desc), cache._reference, n, *of, K._stream_handle(stream))
     if status:
         raise ScError(status, "sparse_attn_decode")

@@ -174,6 +174,12 @@ def test_long_rows_with_gaps(d, pad):
     packed_check(([600], 4, 2, d, "bf16", True, 0, 1.0, 0, 0), 5, pad)
 
 
+@pytest.mark.parametrize("pad", [1, 2, 8])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f16"), (96, "f32")])
+def test_many_long_rows_with_gaps(d, dtype, pad):
+    packed_check(([600], 4, 2, d, dtype, True, 0, 1.0, 0, 0), 5, pad, times=28)
+
+
 def test_keys_and_values_of_different_strides_and_far_apart():
     """Queries follow each other, keys and values lie at other distances, the values' beyond what the offsets of plain rows span."""
     n, d = 90, 64
@@ -192,6 +198,23 @@ def test_keys_and_values_of_different_strides_and_far_apart():
         A.sparse_attn_backward(plan, q, k, v, o, lse, do, dq, dk, dv, ws)
         for name, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
             inside(t.reshape(want[name].shape), want[name], bound[name], name)
+
+
+def test_many_tiles_with_offsets_beyond_32_bits():
+    n, heads, kv, d, stride = 1100, 32, 16, 64, (1 << 21) + 8
+    g = gen(32)
+    x = {name: normal(g, n, h, d, dtype="bf16") for name, h in (("q", heads), ("k", kv), ("v", kv), ("do", heads))}
+    want, bound = O.packed((heads, kv, d, "bf16", True, 0, 0.125), [0, n], torch.ones(n, dtype=torch.bool), x["q"], x["k"], x["v"], x["do"])
+    plan = A.sparse_attn_plan(A.make_attn_desc(heads, kv, d), [0, n])
+    ws = torch.empty(A.sparse_attn_backward_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+    q, k, v, dq, dk, dv = (torch.empty(n, stride, dtype=torch.bfloat16, device=DEV)[:, :h * d] for h in (heads, kv, kv) * 2)
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        t.copy_(dev(x[name], "bf16").flatten(1))
+    o, lse = nans(n, heads, d, dtype="bf16"), nans(n, heads)
+    A.sparse_attn_run(plan, q, k, v, o, lse)
+    A.sparse_attn_backward(plan, q, k, v, o, lse, dev(x["do"], "bf16"), dq, dk, dv, ws)
+    for name, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+        inside(t.reshape(want[name].shape), want[name], bound[name], name)
 
 
 def test_no_sequences_and_empty_ones():
@@ -266,6 +289,28 @@ def test_rows_that_do_not_count_are_not_looked_at():
     for n in ("o", "dq", "dk", "dv"):
         for a, b in ((starts[0], starts[1]), (starts[2], starts[3])):
             assert same(clean[n][a:b], got[n][a:b])
+
+
+@pytest.mark.parametrize("dtype,times", [("f32", 1), ("f32", 30), ("bf16", 30)])
+@pytest.mark.parametrize("d", [64, 41])
+def test_rows_that_do_not_count_of_few_and_many(dtype, times, d):
+    """The same where tiles are those of few rows and of many: bits again, in both formats, with NaN in rows that do not count."""
+    c = ([90, 61, 40] * times, 6, 2, d, dtype, True, 0, 0.7, 0, 3)
+    starts, rows, keep, x = case_inputs(c, 6)
+    _, _, clean = packed_call(c, starts, keep, x)
+    _, at, compact = packed_call(c[:8] + (1, 3), starts, keep, x)
+    inside_rows = at < starts[-1]
+    for t in x.values():
+        t[~keep] = float("nan")
+        t[starts[-1]:] = float("nan")
+    _, _, got = packed_call(c, starts, keep, x)
+    assert all(same(clean[n], got[n]) for n in clean) and same(clean["lse"], compact["lse"])
+    assert all(same(clean[n][at[inside_rows].to(DEV)], compact[n][inside_rows.to(DEV)]) for n in ("o", "dq", "dk", "dv"))
+    assert all(torch.isfinite(clean[n][:starts[-1]]).all() for n in ("o", "dq", "dk", "dv"))
+    for t in x.values():
+        t[starts[-2]:starts[-1]] = float("inf")
+    _, _, got = packed_call(c, starts, keep, x)
+    assert all(same(clean[n][:starts[-2]], got[n][:starts[-2]]) for n in ("o", "dq", "dk", "dv"))
 
 
 def test_a_query_that_is_not_finite_is_lost_alone():
@@ -725,6 +770,36 @@ def test_training_step_in_a_graph(d):
             inside_rows = slice(0, starts[-1])
             assert all(same(sets[which][n][inside_rows], eager[n][inside_rows]) for n in ("o", "dq", "dk", "dv"))
             assert same(sets[which]["lse"], eager["lse"])
+
+
+@pytest.mark.parametrize("dtype,times", [("f32", 1), ("f32", 30), ("bf16", 30)])
+def test_graphs_of_few_and_many(dtype, times):
+    c = ([90, 61, 8] * times, 6, 2, 72, dtype, True, 0, 1.0, 0, 0)
+    starts, rows, _, x = case_inputs(c, 5)
+    plan = A.sparse_attn_plan(A.make_attn_desc(6, 2, 72, A.DTYPE_CODE[dtype]), starts)
+    ws = torch.empty(A.sparse_attn_backward_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+
+    def buffers():
+        b = {n: torch.zeros(rows, h, 72, dtype=O.TORCH[dtype], device=DEV) for n, h in (("q", 6), ("k", 2), ("v", 2), ("o", 6), ("do", 6), ("dq", 6), ("dk", 2), ("dv", 2))}
+        b["lse"] = torch.zeros(rows, 6, device=DEV)
+        return b
+
+    def step(b):
+        A.sparse_attn_run(plan, b["q"], b["k"], b["v"], b["o"], b["lse"])
+        A.sparse_attn_backward(plan, b["q"], b["k"], b["v"], b["o"], b["lse"], b["do"], b["dq"], b["dk"], b["dv"], ws)
+
+    captured, eager, graph = buffers(), buffers(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for turn in range(3):
+        for n, t in x.items():
+            eager[n].copy_(dev(t.roll(turn, 0), dtype))
+            captured[n].copy_(eager[n])
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        assert all(same(captured[n], eager[n]) for n in ("o", "lse", "dq", "dk", "dv"))
 
 
 def test_on_another_stream():
