@@ -42,7 +42,7 @@ typedef struct {
  * q, o: [rows][heads][d], k, v: [rows][kv_heads][d], with row_format = SC_ROWS_COMPACT of the kept rows alone.
  * lse: float[kept][heads], log sum exp of the scores, for the backward pass; NULL in inference.  kept: of sparse_attn_info.
  * A row of q that is not finite loses what is made of it, and no other; one of k or v what is made of its sequence (its dk and dv too).  A row
- * all of whose scores are -infinity gives zeros.
+ * all of whose scores are -infinity gives zeros, has zeros for its gradient and adds nothing to dk and dv.
  * rows * heads / kv_heads <= 2^30, rows * heads <= 2^36, (rows * heads / kv_heads / 128 + seqs) * kv_heads < 2^23 - 512. */
 typedef struct sc_attn sc_attn;
 

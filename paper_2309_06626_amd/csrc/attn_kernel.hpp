@@ -22,9 +22,10 @@
 namespace sc {
 
 constexpr float kAttnLog2e = 1.4426950408889634f;
-// a row's lse, and what is taken off in the exponent of 2: in 64 bits, because the error of either is one of all the row's probabilities
+// a row's lse, and what is taken off in the exponent of 2: in 64 bits, because the error of either is one of all the row's probabilities.  A row
+// whose scores are all -infinity has none: less 0, in place of less its lse, they are 0.
 __device__ __forceinline__ float attn_lse(float m, float sum) { return (float)((double)m * 0.6931471805599453 + (double)__builtin_logf(sum)); }
-__device__ __forceinline__ float attn_lse2(float lse) { return (float)((double)lse * 1.4426950408889634); }
+__device__ __forceinline__ float attn_lse2(float lse) { return lse == -INFINITY ? 0.0f : (float)((double)lse * 1.4426950408889634); }
 
 template <int N> constexpr std::integral_constant<int, N> attn_c{};
 template <int I, int N, class Fn> __device__ __forceinline__ void attn_for(Fn&& f) {

@@ -1,0 +1,68 @@
+"""Attention operators at the limits of their numbers: scores that leave a float's range, small weights beside a large one, values of very different
+sizes in 8 bits, rows that are not finite; and the kernels of few and of many rows and of long sequences at the same tests."""
+import math
+
+import pytest
+import torch
+
+import attention_oracle as O
+from paper_2309_06626_amd import attention as A
+from test_gpu_attention import DEV, cache_of, case_inputs, decode_call, decode_oracle, dev, gen, inside, nans, normal, packed_call, packed_check, same, starts_of
+
+pytestmark = pytest.mark.gpu
+
+
+def train(desc, dtype, starts, x):
+    """One training step of whole sequences: o, lse, dq, dk, dv."""
+    plan = A.sparse_attn_plan(desc, starts)
+    on = {n: dev(t, dtype) for n, t in x.items()}
+    got = {"o": torch.empty_like(on["q"]), "lse": nans(plan.kept, desc.heads)}
+    got.update({"d" + n: torch.full_like(on[n], float("nan")) for n in "qkv"})
+    ws = torch.empty(A.sparse_attn_backward_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+    A.sparse_attn_run(plan, on["q"], on["k"], on["v"], got["o"], got["lse"])
+    A.sparse_attn_backward(plan, on["q"], on["k"], on["v"], got["o"], got["lse"], on["do"], got["dq"], got["dk"], got["dv"], ws)
+    return got
+
+
+# ---- scores beyond a float's range -------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("times", [1, 80])
+@pytest.mark.parametrize("d", [64, 72, 128])
+def test_gradients_of_rows_whose_scores_are_minus_infinity(dtype, times, d):
+    """The first rows' products with all keys that they see leave a float's range: o is 0, and so are dq and what they add to dk and dv.  Other rows see
+    these keys as any other.  (The oracle takes a row's contributions away with its gradient.)"""
+    c = ([70, 33], 4, 2, d, dtype, True, 0, 1.0, 0, 0)
+    starts, rows, keep, x = case_inputs(c, 41)
+    lost = torch.tensor([0, 1, 2, 70, 71])
+    x["q"][..., 0] = x["k"][..., 0] = 0
+    x["q"][lost, :, 0], x["k"][lost, :, 0] = 2.0 ** 100, -(2.0 ** 100)
+    without = x["do"].clone()
+    without[lost] = 0
+    want, bound = O.packed((4, 2, d, dtype, True, 0, 1 / math.sqrt(d)), starts, keep, x["q"], x["k"], x["v"], without)
+    again = lambda t: torch.cat([t] * times)  # noqa: E731
+    got = train(A.make_attn_desc(4, 2, d, A.DTYPE_CODE[dtype]), dtype, starts_of([70, 33] * times), {n: again(t) for n, t in x.items()})
+    kept = torch.ones(rows, dtype=torch.bool).index_fill(0, lost, False).repeat(times)
+    for n in ("o", "dq", "dk", "dv"):
+        mine = kept if n in ("o", "dq") else torch.ones_like(kept)
+        inside(got[n][mine.to(DEV)], again(want[n])[mine], again(bound[n])[mine], n)
+    for n in ("o", "dq"):
+        assert (got[n][~kept.to(DEV)] == 0).all(), n
+    assert (got["lse"][~kept.to(DEV)] == -math.inf).all()
+
+
+@pytest.mark.parametrize("times", [1, 400])
+def test_gradients_of_rows_whose_scores_are_minus_infinity_in_f16(times):
+    """The same by the scale; rows see themselves alone, so that nothing else is multiplied by it."""
+    n, d = 70, 64
+    g = gen(7)
+    x = {name: torch.zeros(n, 1, d, dtype=torch.float64) for name in "qk"}
+    x["v"], x["do"] = normal(g, n, 1, d, dtype="f16"), normal(g, n, 1, d, dtype="f16")
+    lost = torch.tensor([0, 5, 31, 32, 69])
+    x["q"][lost, 0, 0], x["k"][lost, 0, 0] = 2.0 ** 15, -(2.0 ** 15)
+    x = {name: torch.cat([t] * times) for name, t in x.items()}
+    got = train(A.make_attn_desc(1, 1, d, A.SC_F16, window=1, scale=2.0 ** 100), "f16", starts_of([n] * times), x)
+    some = torch.ones(n).index_fill(0, lost, 0).repeat(times)[:, None, None].double()
+    assert torch.equal(got["o"].double().cpu(), x["v"] * some) and torch.equal(got["dv"].double().cpu(), x["do"] * some)
+    assert (got["dq"] == 0).all() and (got["dk"] == 0).all()
