@@ -42,7 +42,8 @@ typedef struct {
  * q, o: [rows][heads][d], k, v: [rows][kv_heads][d], with row_format = SC_ROWS_COMPACT of the kept rows alone.
  * lse: float[kept][heads], log sum exp of the scores, for the backward pass; NULL in inference.  kept: of sparse_attn_info.
  * A row of q that is not finite loses what is made of it, and no other; one of k or v what is made of its sequence (its dk and dv too).  A row
- * all of whose scores are -infinity gives zeros, has zeros for its gradient and adds nothing to dk and dv.
+ * all of whose scores are -infinity gives zeros, has zeros for its gradient and adds nothing to dk and dv; one whose largest score is beyond a float's
+ * range is NaN, as one that is not finite.
  * rows * heads / kv_heads <= 2^30, rows * heads <= 2^36, (rows * heads / kv_heads / 128 + seqs) * kv_heads < 2^23 - 512. */
 typedef struct sc_attn sc_attn;
 
@@ -97,8 +98,8 @@ sc_status sparse_kv_read(const sc_kv_desc* desc, int64_t rows, const int64_t* sl
  * lies in page table[r][j / page_rows] (int32[rows][table_width]).  lengths[r] <= 0: o is zero; beyond table_width * page_rows: what the
  * table holds.  Rows of a page that is not in the cache are not there: no weight, nothing read.
  * What lies in the cache behind a sequence's length is not looked at, whatever it is.  A key or value that is not finite loses the heads
- * that read it in this row of q, and no other row.  rows * heads < 2^24, and so is the number of workgroups, which the sequences' longest
- * length that table_width allows multiplies. */
+ * that read it in this row of q, and no other row; a score beyond a float's range is as above.  rows * heads < 2^24, and so is the number of
+ * workgroups, which the sequences' longest length that table_width allows multiplies. */
 sc_status sparse_attn_decode_workspace_bytes(const sc_attn_desc* desc, const sc_kv_desc* cache, int64_t rows, int64_t table_width,
                                              size_t* bytes);
 sc_status sparse_attn_decode(const sc_attn_desc* desc, const sc_kv_desc* cache, int64_t rows, const void* q_dev, const int32_t* table_dev,

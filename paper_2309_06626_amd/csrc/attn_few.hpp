@@ -255,6 +255,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
       all += part * f;
       F::add(shares, v, r_out, c0, f, x);
     }
+    all = attn_total(top, all);
     const int i_out = (r0 + r_out) / p.group, head_out = w.head * p.group + (r0 + r_out - i_out * p.group);
     const int64_t row_out = p.map ? p.map[first + i_out] : first + i_out;
     if (p.lse && c0 == 0) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = all == 0.0f ? -INFINITY : attn_lse(top, all);

@@ -323,6 +323,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW =
   if (r_out >= packed) return;
   const int i_out = r_out / p.group, head_out = w.head * p.group + (r_out - i_out * p.group);
   const int64_t row_out = p.map ? p.map[first + i_out] : first + i_out;
+  sum = attn_total(m, sum);
   const float per = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;      // (NaN stays)
   if (p.lse && again % 64 < 32) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
   T* const out = static_cast<T*>(p.out) + (row_out * p.heads + head_out) * p.d;

@@ -10,6 +10,7 @@
 #pragma once
 #include "mma_common.hpp"
 
+#include <math.h>
 #include <type_traits>
 
 namespace sc {
@@ -44,6 +45,10 @@ __device__ __forceinline__ unsigned attn_lds(const void* p) {
 
 __device__ __forceinline__ float attn_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bool attn_any(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
+// A row's sum of weights, m being what its largest score became as an exponent.  No weight at all is a row that sees nothing but scores of -infinity;
+// with any other m the score, as it was scaled, left a float's range, and the row is lost.
+__device__ __forceinline__ float attn_total(float m, float sum) { return sum == 0.0f && m != -INFINITY ? __builtin_nanf("") : sum; }
 
 // a value and that of the lane in the other half of the wavefront, in the same order in both
 __device__ __forceinline__ void attn_halves(float v, float& low, float& high) {

@@ -389,6 +389,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
     }
     const int64_t head_row = row * p.heads + head * group + block * 32 + q;
     if (p.splits == 1) {
+      all = attn_total(top, all);
       if (ch < p.d) static_cast<IO*>(p.o)[head_row * p.d + ch] = Elem<DT>::from_float(all == 0.0f ? 0.0f : out / all);
     } else {
       p.part_o[(head_row * p.splits + split) * DP + ch] = out;
@@ -432,6 +433,7 @@ template <int DT, int DP> __global__ __launch_bounds__(2 * DP) void decode_join_
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] += s_out[i][lane][e];
   }
+  all = attn_total(top, all);
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (4 * lane + e < p.d) static_cast<T*>(p.o)[head_row * p.d + 4 * lane + e] = Elem<DT>::from_float(all == 0.0f ? 0.0f : out[e] / all);

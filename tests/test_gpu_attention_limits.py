@@ -66,3 +66,56 @@ def test_gradients_of_rows_whose_scores_are_minus_infinity_in_f16(times):
     some = torch.ones(n).index_fill(0, lost, 0).repeat(times)[:, None, None].double()
     assert torch.equal(got["o"].double().cpu(), x["v"] * some) and torch.equal(got["dv"].double().cpu(), x["do"] * some)
     assert (got["dq"] == 0).all() and (got["dk"] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,times", [(70, 1), (70, 600), (2100, 1)])
+def test_a_score_beyond_a_floats_range_is_not_an_empty_row(dtype, n, times):
+    """A score that is +infinity once it is scaled makes its row NaN, and no other; it is not a row without weights."""
+    d = 64
+    x = {name: torch.zeros(n, 2, d, dtype=torch.float64) for name in "qk"}
+    v = (torch.arange(n) % 7).double().reshape(n, 1, 1).expand(n, 2, d)
+    lost = torch.tensor([3, 64])
+    x["q"][lost, 0, 0], x["k"][5, :, 0] = 2.0 ** 15, 2.0 ** 15
+    desc = A.make_attn_desc(2, 2, d, A.DTYPE_CODE[dtype], causal=False, scale=2.0 ** 100)
+    plan = A.sparse_attn_plan(desc, starts_of([n] * times))
+    q, k, w = (dev(t.repeat(times, 1, 1), dtype) for t in (x["q"], x["k"], v))
+    o, lse = torch.zeros_like(q), torch.zeros(plan.kept, 2, device=DEV)
+    A.sparse_attn_run(plan, q, k, w, o, lse)
+    ok = torch.ones(n, 2, dtype=torch.bool)
+    ok[lost, 0] = False
+    ok = ok.repeat(times, 1).to(DEV)
+    mean = v[:, 0].mean(0)
+    # weights are 1: the sums are exact, the quotient's three roundings are floats', the result's the type's
+    step = torch.finfo(O.TORCH[dtype]).eps / 2 + 4 * O.E
+    inside(o[ok], mean.expand(int(ok.sum()), d), step * mean.expand(int(ok.sum()), d), "o")
+    inside(lse[ok], torch.full((int(ok.sum()),), math.log(n), dtype=torch.float64), torch.full((int(ok.sum()),), 8 * O.E * (1 + math.log(n))), "lse")
+    assert torch.isnan(o[~ok]).all() and torch.isnan(lse[~ok]).all()
+
+
+@pytest.mark.parametrize("dtype,bits", [("bf16", 0), ("f16", 0), ("f32", 0), ("bf16", 8), ("f16", 8), ("f32", 8)])
+@pytest.mark.parametrize("n,requests", [(1, 3), (300, 2), (3000, 2), (300, 900)])
+def test_a_tokens_score_beyond_a_floats_range_is_not_an_empty_row(dtype, bits, n, requests):
+    """The same of single tokens, whose shares of wavefronts and stretches are joined; with 900 requests there is one stretch."""
+    d = 64
+    cache = cache_of(1, d, 16, -(-n // 16), dtype, bits)
+    k = torch.zeros(n, 1, d, dtype=torch.float64)
+    k[n // 2, 0, 0] = 2.0 ** 15
+    v = (torch.arange(n) % 7 + 1.0).reshape(n, 1, 1).expand(n, 1, d)
+    A.sparse_kv_write(cache, dev(k, dtype), dev(v, dtype), torch.arange(n, device=DEV))
+    q = torch.zeros(requests, 2, d)
+    q[1::2, 0, 0] = 2.0 ** 15
+    desc = A.make_attn_desc(2, 1, d, A.DTYPE_CODE[dtype], scale=2.0 ** 100)
+    table = torch.arange(-(-n // 16), dtype=torch.int32, device=DEV).repeat(requests, 1)
+    ws = torch.empty(A.sparse_attn_decode_workspace_bytes(desc, cache.desc, requests, table.shape[1]), dtype=torch.uint8, device=DEV)
+    o = torch.zeros(requests, 2, d, dtype=O.TORCH[dtype], device=DEV)
+    A.sparse_attn_decode(desc, cache, dev(q, dtype), table, torch.full((requests,), n, dtype=torch.int32, device=DEV), o, ws)
+    assert torch.isnan(o[1::2, 0]).all()
+    held = v[:, 0, 0].double()
+    if bits:
+        codes, scale = O.quantised(v[:, 0].double())
+        held = codes[:, 0] * scale.double()
+    # weights are 1; in 8 bits they are products with a scale, rounded to the type
+    step = torch.finfo(O.TORCH[dtype]).eps / 2 + (O.U["f16" if dtype == "bf16" else dtype] if bits else 0) + O.acc(n)
+    for got in (o[::2, 0], o[:, 1]):
+        inside(got, held.mean().expand(got.shape), step * held.mean().expand(got.shape), "o")
