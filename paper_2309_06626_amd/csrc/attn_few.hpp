@@ -209,12 +209,15 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[db][v] *= less;
     }
-    const float shift = m == -INFINITY ? 0.0f : m;     // (nothing seen so far: every term is 0)
+    static_assert(DT == kF32, "weights of f16 would be formed larger");
+    const float shift = attn_shift<false>(m);
+    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};          // (one weight after the other is lost beside a large sum)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       s[v] = attn_exp2(__builtin_fmaf(s[v], c, -shift));
-      sum += s[v];
+      part[v & 3] += s[v];
     }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
     v4i pf[A::SS];
     A::pack(s, pf);
     if (more) few_wait<J>();
@@ -258,7 +261,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
     all = attn_total(top, all);
     const int i_out = (r0 + r_out) / p.group, head_out = w.head * p.group + (r0 + r_out - i_out * p.group);
     const int64_t row_out = p.map ? p.map[first + i_out] : first + i_out;
-    if (p.lse && c0 == 0) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = all == 0.0f ? -INFINITY : attn_lse(top, all);
+    if (p.lse && c0 == 0) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = all == 0.0f ? -INFINITY : attn_lse<DT>(top, all);
     const float per = all > 0.0f ? 1.0f / all : all == 0.0f ? 0.0f : all;      // (NaN stays)
     F::write(static_cast<T*>(p.out) + (row_out * p.heads + head_out) * p.d, c0, p.d, x, per);
   }

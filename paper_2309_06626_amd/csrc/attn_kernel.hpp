@@ -24,7 +24,10 @@ namespace sc {
 constexpr float kAttnLog2e = 1.4426950408889634f;
 // a row's lse, and what is taken off in the exponent of 2: in 64 bits, because the error of either is one of all the row's probabilities.  A row
 // whose scores are all -infinity has none: less 0, in place of less its lse, they are 0.
-__device__ __forceinline__ float attn_lse(float m, float sum) { return (float)((double)m * 0.6931471805599453 + (double)__builtin_logf(sum)); }
+template <int DT> __device__ __forceinline__ float attn_lse(float shift, float sum) {
+  if constexpr (DT == kF16) return (float)(((double)shift + kAttnUp) * 0.6931471805599453 + (double)__builtin_logf(__builtin_amdgcn_ldexpf(sum, -kAttnUp)));
+  return (float)((double)shift * 0.6931471805599453 + (double)__builtin_logf(sum));
+}
 __device__ __forceinline__ float attn_lse2(float lse) { return lse == -INFINITY ? 0.0f : (float)((double)lse * 1.4426950408889634); }
 
 template <int N> constexpr std::integral_constant<int, N> attn_c{};
@@ -206,13 +209,14 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW =
       A::pack(s[b], pf[b]);
     }
   };
-  auto add_up = [&](const floatx16 (&s)[KB], auto from, auto to) {      // blocks from .. to
-    float part[4] = {sum, 0.0f, 0.0f, 0.0f};
+  auto add_up = [&](const floatx16 (&s)[KB], auto from, auto to) {      // blocks from .. to, by themselves first: one weight after the other is lost beside a large sum
+    if constexpr (decltype(from)::value == decltype(to)::value) return;
+    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int b = decltype(from)::value; b < decltype(to)::value; ++b)
 #pragma unroll
       for (int v = 0; v < 16; ++v) part[v & 3] += s[b][v];
-    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
   };
   auto values = [&](const v4i (&pf)[KB][A::SS], auto parity) {
     constexpr unsigned at = (2 + decltype(parity)::value) * TILE;
@@ -234,8 +238,8 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW =
   auto rescale = [&](float most) {
     // (a maximum that grew by less than 2^8 stays: weights of up to 256 are as good as those of up to 1)
     if (attn_any(most > m + 8.0f)) {
-      shift = most == -INFINITY ? 0.0f : most;         // (nothing seen so far: every term is 0)
-      const float less = attn_exp2(m - shift);
+      const float next = attn_shift<DT == kF16>(most), less = m == -INFINITY ? 0.0f : attn_exp2(shift - next);
+      shift = next;
       sum *= less;
 #pragma unroll
       for (int db = 0; db < A::DB; ++db)
@@ -325,7 +329,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW =
   const int64_t row_out = p.map ? p.map[first + i_out] : first + i_out;
   sum = attn_total(m, sum);
   const float per = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;      // (NaN stays)
-  if (p.lse && again % 64 < 32) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = sum == 0.0f ? -INFINITY : attn_lse(m, sum);
+  if (p.lse && again % 64 < 32) p.lse[(int64_t)(first + i_out) * p.heads + head_out] = sum == 0.0f ? -INFINITY : attn_lse<DT>(shift, sum);
   T* const out = static_cast<T*>(p.out) + (row_out * p.heads + head_out) * p.d;
 #pragma unroll
   for (int db = 0; db < A::DB; ++db) A::template write_16<LOADS>(out, 32 * db + 16 * ((again >> 5) & 1), p.d, acc[db], per);

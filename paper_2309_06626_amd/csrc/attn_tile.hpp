@@ -46,6 +46,16 @@ __device__ __forceinline__ unsigned attn_lds(const void* p) {
 __device__ __forceinline__ float attn_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bool attn_any(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
 
+// f16 holds numbers from 2^-24 on, those below 2^-14 with fewer digits, up to 65 504.  Weights that become operands of it are therefore formed 2^6 times
+// as large: with the 2^8 by which a maximum that stays may be passed, the largest are 2^14, and those down to 2^-31 of the largest are not lost
+// (100 000 of 2^-25 beside it are 0.3 % of their sum).
+constexpr int kAttnUp = 6;
+// What is taken off in the exponent of 2, m being what the largest score so far became there: 0 where nothing has been seen, so that every term is 0.
+// (An m in whose rounding the 2^6 would be lost stays as it is.)
+template <bool UP> __device__ __forceinline__ float attn_shift(float m) {
+  return m == -INFINITY ? 0.0f : UP && fabsf(m) < 0x1p20f ? m - kAttnUp : m;
+}
+
 // A row's sum of weights, m being what its largest score became as an exponent.  No weight at all is a row that sees nothing but scores of -infinity;
 // with any other m the score, as it was scaled, left a float's range, and the row is lost.
 __device__ __forceinline__ float attn_total(float m, float sum) { return sum == 0.0f && m != -INFINITY ? __builtin_nanf("") : sum; }

@@ -212,7 +212,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
   for (int db = 0; db < A::DB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
-  float m = -INFINITY, sum = 0.0f;                             // m is a maximum times c, as it was rounded
+  constexpr bool UP = DT == kF16 && !BITS8;                    // (the weights of codes are taken in units)
+  float m = -INFINITY, sum = 0.0f, shift = 0.0f;               // m is a maximum times c, as it was rounded
   float unit = 0.0f;                                           // of codes in f16: acc is in units of it, see below
 
   typedef __attribute__((address_space(3))) const v4f lds_v4f;
@@ -289,16 +290,19 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
     // (a maximum that grew by less than 2^8 stays: weights of up to 256 are as good as those of up to 1)
     float less = 1.0f;
     if (attn_any(top > m + 8.0f)) {
-      less = attn_exp2(m - (top == -INFINITY ? 0.0f : top));
+      const float next = attn_shift<UP>(top);
+      less = m == -INFINITY ? 0.0f : attn_exp2(shift - next);
+      shift = next;
       m = top;
       sum *= less;
     }
-    const float shift = m == -INFINITY ? 0.0f : m;             // (nothing seen so far: every term is 0)
+    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};                  // (one weight after the other is lost beside a large sum)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       s[v] = attn_exp2(__builtin_fmaf(s[v], c, -shift));
-      sum += s[v];
+      part[v & 3] += s[v];
     }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
     if constexpr (BITS8) {
       // weights of the codes: p times the value's scale.  In f16 they are taken in units of a power of two near the largest scale so far,
       // so that they keep their digits whatever the values' size.
@@ -368,7 +372,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
         *reinterpret_cast<v4f*>(s_acc + (wave * 32 + l32) * DP + 32 * db + 16 * h + 4 * q) = part;
       }
     if (h == 0) {
-      s_max[wave * 32 + l32] = m;
+      s_max[wave * 32 + l32] = m == -INFINITY ? m : shift;
       s_sum[wave * 32 + l32] = sum;
     }
   }

@@ -119,3 +119,45 @@ def test_a_tokens_score_beyond_a_floats_range_is_not_an_empty_row(dtype, bits, n
     step = torch.finfo(O.TORCH[dtype]).eps / 2 + (O.U["f16" if dtype == "bf16" else dtype] if bits else 0) + O.acc(n)
     for got in (o[::2, 0], o[:, 1]):
         inside(got, held.mean().expand(got.shape), step * held.mean().expand(got.shape), "o")
+
+
+# ---- small weights beside a large one ----------------------------------------------------------------------------------
+
+SCORE = 17.359375      # beside it, a score of 0 has 2^-25.04 of the weight: below half of f16's smallest number
+
+
+def one_large_weight(n, d=64):
+    x = {"q": torch.zeros(n, 1, d), "k": torch.zeros(n, 1, d), "v": torch.ones(n, 1, d), "do": torch.full((n, 1, d), 2.0 ** -4)}
+    x["q"][:, 0, 0], x["k"][0, 0, 0] = 1, SCORE
+    return train(A.make_attn_desc(1, 1, d, A.SC_F16, causal=False, scale=1.0), "f16", [0, n], x)
+
+
+@pytest.mark.parametrize("n", [65536, 100000])
+def test_many_small_weights_beside_a_large_one_in_f16(n):
+    """One key has most of the weight, the others the rest, 0.3 % of it: o is 1 as all values are."""
+    got = one_large_weight(n)
+    # The result's rounding; weights below f16's normal numbers, half of 2^-24 in units of 2^-6; the numerator is n / 16 additions to a float and the sum
+    # n / 32 to another, half a step each
+    off = O.U["f16"] + n * 2.0 ** -31 + (n / 16 + n / 32) * O.E
+    inside(got["o"], torch.ones(n, 1, 64, dtype=torch.float64), torch.full((n, 1, 64), off), "o")
+    lse = torch.full((n, 1), SCORE + math.log1p((n - 1) * math.exp(-SCORE)), dtype=torch.float64)
+    inside(got["lse"], lse, 8 * O.E * (1 + lse) + n / 32 * O.E, "lse")
+
+
+def test_many_small_weights_beside_a_large_one_in_f16_of_single_tokens():
+    """The same of 800 000 rows of a cache, whose wavefronts have one large weight each."""
+    n, d, page, requests = 800000, 64, 4096, 768
+    cache = cache_of(1, d, page, -(-n // page), "f16", 0)
+    k, v = torch.zeros(n, 1, d, dtype=torch.float16, device=DEV), torch.ones(n, 1, d, dtype=torch.float16, device=DEV)
+    k[torch.tensor([0, 32, 64, 96], device=DEV), 0, 0] = SCORE
+    A.sparse_kv_write(cache, k, v, torch.arange(n, device=DEV))
+    q = torch.zeros(requests, 1, d, dtype=torch.float16, device=DEV)
+    q[:, 0, 0] = 1
+    desc = A.make_attn_desc(1, 1, d, A.SC_F16, scale=1.0)
+    table = torch.arange(-(-n // page), dtype=torch.int32, device=DEV).repeat(requests, 1)
+    ws = torch.empty(A.sparse_attn_decode_workspace_bytes(desc, cache.desc, requests, table.shape[1]), dtype=torch.uint8, device=DEV)
+    o = nans(requests, 1, d, dtype="f16")
+    A.sparse_attn_decode(desc, cache, q, table, torch.full((requests,), n, dtype=torch.int32, device=DEV), o, ws)
+    # as above; a wavefront adds up a quarter of the rows
+    off = O.U["f16"] + n / 4 * 2.0 ** -31 + (n / 64 + n / 128) * O.E
+    inside(o, torch.ones(requests, 1, d, dtype=torch.float64), torch.full((requests, 1, d), off), "o")
