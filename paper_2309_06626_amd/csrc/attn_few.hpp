@@ -300,7 +300,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
                               there ? static_cast<const T*>(p.d_o) + own_place : nullptr, there ? static_cast<const T*>(p.o) + own_place : nullptr};
   few_own<F, VEC>(p, attn_lds(smem), own_at, own_f);
   const float c = p.scale * kAttnLog2e;
-  float lse2 = 0.0f, delta = 0.0f;
+  float lse2 = 0.0f, keys_lse2 = 0.0f, delta = 0.0f;
   const int64_t stat = (int64_t)(first + i) * p.heads + head;
   {
     lse2 = there ? p.lse[stat] : 0.0f;
@@ -313,6 +313,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
       for (int e = 0; e < A::V; ++e) delta += (float)a[e] * (float)b[e];
     }
     delta = attn_add_halves(delta);
+    keys_lse2 = attn_lse2(lse2, kAttnKeysUp<DT>);
     lse2 = attn_lse2(lse2);
   }
   __builtin_amdgcn_sched_barrier(0);
@@ -372,7 +373,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
   __syncthreads();
   F::put(shares, wave, l32, h, acc);
   if (h == 0) s_delta[wave * 32 + l32] = delta;
-  if (wave == 0 && h == 0 && there) p.stats[0][stat] = lse2;
+  if (wave == 0 && h == 0 && there) p.stats[0][stat] = keys_lse2;
   __syncthreads();
   const int c0 = t % F::LANES * F::CH;
 #pragma unroll 4
@@ -380,7 +381,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
     float x[F::CH];
     F::sum(shares, r_out, c0, x);
     const int i_out = (r0 + r_out) / p.group, head_out = w.head * p.group + (r0 + r_out - i_out * p.group);
-    if (c0 == 0) p.stats[1][(int64_t)(first + i_out) * p.heads + head_out] = (s_delta[r_out] + s_delta[32 + r_out]) + (s_delta[64 + r_out] + s_delta[96 + r_out]);
+    if (c0 == 0) p.stats[1][(int64_t)(first + i_out) * p.heads + head_out] = ((s_delta[r_out] + s_delta[32 + r_out]) + (s_delta[64 + r_out] + s_delta[96 + r_out])) * kAttnKeysUnit<DT>;
     const int64_t row_out = p.map ? p.map[first + i_out] : first + i_out;
     F::write(static_cast<T*>(p.dq) + row_out * p.dq_stride + (int64_t)head_out * p.d, c0, p.d, x, p.scale);
   }
@@ -468,7 +469,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
       for (int e = 0; e < 4; ++e) {
         const int v = 4 * a + e;
         s[v] = attn_exp2(__builtin_fmaf(s[v], c, -lse2[e]));
-        g[v] = s[v] * (g[v] - delta[e]);
+        g[v] = attn_keys_ds<DT>(s[v], g[v], delta[e]);
       }
     }
     A::pack(s, pf);
@@ -508,7 +509,7 @@ template <int DT, int DP, int VEC> __global__ __launch_bounds__(64 * kFewWaves, 
       F::write(static_cast<T*>(out) + row_out * stride + (int64_t)w.head * p.d, c0, p.d, x, factor);
     }
   };
-  join(dv, p.dv, p.dv_stride, 1.0f);
+  join(dv, p.dv, p.dv_stride, kAttnKeysUnit<DT>);
   join(dk, p.dk, p.dk_stride, p.scale);
 }
 

@@ -28,7 +28,16 @@ template <int DT> __device__ __forceinline__ float attn_lse(float shift, float s
   if constexpr (DT == kF16) return (float)(((double)shift + kAttnUp) * 0.6931471805599453 + (double)__builtin_logf(__builtin_amdgcn_ldexpf(sum, -kAttnUp)));
   return (float)((double)shift * 0.6931471805599453 + (double)__builtin_logf(sum));
 }
-__device__ __forceinline__ float attn_lse2(float lse) { return lse == -INFINITY ? 0.0f : (float)((double)lse * 1.4426950408889634); }
+__device__ __forceinline__ float attn_lse2(float lse, int up = 0) { return (float)((lse == -INFINITY ? 0.0 : (double)lse * 1.4426950408889634) - up); }
+
+// The keys' gradients take probabilities as operands.  f16's are formed 2^14 times as large, so that those down to 2^-28 keep their digits and those
+// to 2^-39 are not lost (65 536 rows with 2^-25 each are 2^-9 of their gradients); their lse and delta are written for it, dv is divided by it.
+template <int DT> constexpr int kAttnKeysUp = DT == kF16 ? 14 : 0;
+template <int DT> constexpr float kAttnKeysUnit = DT == kF16 ? 0x1p-14f : 1.0f;
+// gradient of a score: p (do . v - delta)
+template <int DT> __device__ __forceinline__ float attn_keys_ds(float p, float g, float delta) {
+  return p * (DT == kF16 ? __builtin_fmaf(g, kAttnKeysUnit<DT>, -delta) : g - delta);
+}
 
 template <int N> constexpr std::integral_constant<int, N> attn_c{};
 template <int I, int N, class Fn> __device__ __forceinline__ void attn_for(Fn&& f) {
@@ -438,7 +447,7 @@ __global__ __launch_bounds__(64 * NW, DT == kF32 || (DP > 64 && NW == 4) ? 1 : 2
     delta = attn_add_halves(delta);
     const int64_t stat = (int64_t)(first + i) * p.heads + head;
     lse2 = there ? attn_lse2(p.lse[stat]) : 0.0f;
-    if (there && h == 0) p.stats[0][stat] = lse2;        // (for the keys)
+    if (there && h == 0) p.stats[0][stat] = attn_lse2(p.lse[stat], kAttnKeysUp<DT>);      // (for the keys)
   }
 
   typename A::Along along = A::along(lane);
@@ -565,7 +574,7 @@ __global__ __launch_bounds__(64 * NW, DT == kF32 || (DP > 64 && NW == 4) ? 1 : 2
   const int r_out = r_wave + (again & 31), h_out = (again >> 5) & 1;
   if (r_out >= packed) return;
   const int i_out = r_out / p.group, head_out = w.head * p.group + (r_out - i_out * p.group);
-  if (h_out == 0) p.stats[1][(int64_t)(first + i_out) * p.heads + head_out] = delta;
+  if (h_out == 0) p.stats[1][(int64_t)(first + i_out) * p.heads + head_out] = delta * kAttnKeysUnit<DT>;
   T* const out = static_cast<T*>(p.dq) + (p.map ? p.map[first + i_out] : first + i_out) * p.dq_stride + (int64_t)head_out * p.d;
 #pragma unroll
   for (int db = 0; db < A::DB; ++db) A::template write_16<LOADS>(out, 32 * db + 16 * h_out, p.d, acc[db], p.scale);
@@ -678,7 +687,7 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 || DT == kF32 ? 1 : 2) 
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       s[v] = attn_exp2(__builtin_fmaf(s[v], c, -of.lse2[v >> 2][v & 3]));
-      g[v] = s[v] * (g[v] - of.delta[v >> 2][v & 3]);
+      g[v] = attn_keys_ds<DT>(s[v], g[v], of.delta[v >> 2][v & 3]);
     }
     A::pack(s, pf);
     A::pack(g, df);
@@ -772,7 +781,7 @@ __global__ __launch_bounds__(64 * kAttnKeyWaves, DP > 64 || DT == kF32 ? 1 : 2) 
 #pragma unroll
   for (int db = 0; db < A::DB; ++db) {
     A::template write_16<LOADS>(out_k, 32 * db + 16 * h, p.d, dk[db], p.scale);
-    A::template write_16<LOADS>(out_v, 32 * db + 16 * h, p.d, dv[db], 1.0f);
+    A::template write_16<LOADS>(out_v, 32 * db + 16 * h, p.d, dv[db], kAttnKeysUnit<DT>);
   }
 }
 

@@ -23,7 +23,7 @@ struct AttnParams {
   void *out, *dq, *dk, *dv;
   int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;      // entries from row to row; o and d_o are [rows][heads][d]
   float* lse;                          // [kept][heads]
-  float* stats[2];                     // the same of the backward pass: lse in exponents of 2, and delta
+  float* stats[2];                     // of the backward pass, as the keys' gradients take them: lse in exponents of 2, and delta
   const int32_t* map;                  // row of the tensors that holds a kept row; null: row r is kept row r
   const AttnItem* items;
   int32_t n_items, heads, kv_heads, group, d;

@@ -161,3 +161,13 @@ def test_many_small_weights_beside_a_large_one_in_f16_of_single_tokens():
     # as above; a wavefront adds up a quarter of the rows
     off = O.U["f16"] + n / 4 * 2.0 ** -31 + (n / 64 + n / 128) * O.E
     inside(o, torch.ones(requests, 1, d, dtype=torch.float64), torch.full((requests, 1, d), off), "o")
+
+
+@pytest.mark.parametrize("n", [65536, 100000])
+def test_many_small_probabilities_of_a_key_in_f16(n):
+    """The gradients of the other values: many rows' probabilities of 2^-25.  65 536 rows go by the small tiles of the gradients, 100 000 by the large ones."""
+    got = one_large_weight(n)["dv"][1:]
+    small = math.exp(-SCORE)
+    dv = torch.full(got.shape, n * small / (1 + (n - 1) * small) * 2.0 ** -4, dtype=torch.float64)
+    # a probability's and the result's rounding; what makes a probability: lse and the score, twice each, and lse's sum; n / 16 additions of n equal terms
+    inside(got, dv, dv * (2 * O.U["f16"] + 4 * 8 * O.E * (1 + SCORE) + (n / 32 + n / 16) * O.E), "dv")
