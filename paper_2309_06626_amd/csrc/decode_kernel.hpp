@@ -40,18 +40,9 @@ __device__ __forceinline__ void decode_widen(v4i codes, _Float16 (&out)[16]) {
   }
 }
 
-// largest of the 32 lanes of a half wavefront (positive numbers)
-__device__ __forceinline__ float decode_max32(float v) {
-  auto with = [&](auto control) {
-    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, false)));
-  };
-  with(std::integral_constant<int, 0xB1>{});       // quad_perm [1, 0, 3, 2]
-  with(std::integral_constant<int, 0x4E>{});       // quad_perm [2, 3, 0, 1]
-  with(std::integral_constant<int, 0x141>{});      // mirrored within 8
-  with(std::integral_constant<int, 0x140>{});      // within 16
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
-  return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
-}
+// power of two at or below x (of normal numbers), and 1 / x of such a power
+__device__ __forceinline__ float decode_pow2(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, x) & 0x7f800000u); }
+__device__ __forceinline__ float decode_per(float pow2) { return __builtin_bit_cast(float, 0x7f000000u - __builtin_bit_cast(unsigned, pow2)); }
 
 // What a lane holds of a row of q, as f16: in units of a power of two, so that the largest entry is between 2^13 and 2^14 (none is lost that
 // is not below 2^-37 of it).  Returns the unit.
@@ -214,7 +205,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
     for (int v = 0; v < 16; ++v) acc[db][v] = 0.0f;
   constexpr bool UP = DT == kF16 && !BITS8;                    // (the weights of codes are taken in units)
   float m = -INFINITY, sum = 0.0f, shift = 0.0f;               // m is a maximum times c, as it was rounded
-  float unit = 0.0f;                                           // of codes in f16: acc is in units of it, see below
+  float unit = 0.0f, peak = 0.0f;                              // of codes in f16: acc is in units of it, see below
 
   typedef __attribute__((address_space(3))) const v4f lds_v4f;
   // Entries as they are: with two places for keys and two for values, whatever is in LDS is asked for again as soon as it has been multiplied, so
@@ -304,25 +295,28 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
     }
     sum += (part[0] + part[1]) + (part[2] + part[3]);
     if constexpr (BITS8) {
-      // weights of the codes: p times the value's scale.  In f16 they are taken in units of a power of two near the largest scale so far,
-      // so that they keep their digits whatever the values' size.
-      float per_unit = 1.0f;
-      if constexpr (CT == kF16) {
-        float big = *(__attribute__((address_space(3))) const float*)(uint64_t)(at_scales + (32 + l32) * 4);
-        big = __builtin_isfinite(big) ? big : 0.0f;
-        big = decode_max32(big);
-        const float least = __builtin_bit_cast(float, (unsigned)(__builtin_bit_cast(unsigned, big) & 0x7f800000u));
-        if (least > unit) {
-          less *= unit / least;      // (powers of two; 0 at first)
-          unit = least;
-        }
-        per_unit = unit > 0.0f ? 1.0f / unit : 0.0f;
-      }
+      // weights of the codes: p times the value's scale
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const v4f v_scale = *(lds_v4f*)(uint64_t)(at_scales + (32 + 8 * a + 4 * h) * 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[4 * a + e] *= CT == kF16 ? v_scale[e] * per_unit : v_scale[e];
+        for (int e = 0; e < 4; ++e) s[4 * a + e] *= v_scale[e];
+      }
+      if constexpr (CT == kF16) {
+        // in f16 in units of a power of two, 2^-6 to 2^-14 of this head's largest one so far (not of the largest scale, whose row may have no weight), so
+        // that they keep their digits whatever the values' size, and those down to 2^-30 of the largest are not lost
+        float big = s[0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) big = fmaxf(big, s[v]);
+        peak = fmaxf(peak * less, attn_max_halves(big));
+        if (attn_any(peak > unit * 0x1p14f || less != 1.0f)) {
+          const float next = decode_pow2(fminf(fmaxf(peak, 0x1p-119f), 0x1p127f)) * 0x1p-6f;
+          less = less * unit * decode_per(next);      // (0 at first)
+          unit = next;
+        }
+        const float per_unit = decode_per(unit);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] *= per_unit;
       }
     }
     if (attn_any(less != 1.0f)) {

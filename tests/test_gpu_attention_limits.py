@@ -171,3 +171,36 @@ def test_many_small_probabilities_of_a_key_in_f16(n):
     dv = torch.full(got.shape, n * small / (1 + (n - 1) * small) * 2.0 ** -4, dtype=torch.float64)
     # a probability's and the result's rounding; what makes a probability: lse and the score, twice each, and lse's sum; n / 16 additions of n equal terms
     inside(got, dv, dv * (2 * O.U["f16"] + 4 * 8 * O.E * (1 + SCORE) + (n / 32 + n / 16) * O.E), "dv")
+
+
+# ---- values of very different sizes in 8 bits --------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype,small", [("bf16", 1e-4), ("bf16", 1e-5), ("bf16", 1e-30), ("f16", 1e-3), ("f16", 1e-4), ("f32", 1e-5)])
+@pytest.mark.parametrize("requests", [1, 400])
+@pytest.mark.parametrize("large", [(0, 1), (150, 151), (290, 291), (0, 128), (100, 164)])
+def test_8_bit_values_beside_larger_ones_that_have_no_weight(dtype, small, large, requests, monkeypatch):
+    """Rows of large values that the token hardly sees take no digits from those that it sees.  Of 400 tokens one stretch is made, whose wavefronts have three
+    tiles each, a first one of large values alone among them."""
+    monkeypatch.setitem(O.SUB, "f16", 0.0)      # (weights keep their digits: the loss that is left is in the bound below)
+    n, d = 300, 64
+    c = ([n], 8, 2, d, 16, dtype, 8, 0, 0)
+    g = gen(12)
+    cache = cache_of(2, d, 16, 21, dtype, 8)
+    table, j = torch.arange(20, dtype=torch.int32)[None], torch.arange(n)
+    k, v = normal(g, n, 2, d, dtype=dtype), (normal(g, n, 2, d) * small).to(O.TORCH[dtype]).double()
+    k[..., 0] = 0
+    k[slice(*large), :, 0] = -60
+    v[slice(*large)] = normal(g, large[1] - large[0], 2, d, dtype=dtype) * 1024
+    A.sparse_kv_write(cache, dev(k, dtype), dev(v, dtype), j.to(DEV))
+    (k, _), (v, scales) = ((codes * scale.double()[..., None], scale.double()) for codes, scale in map(O.quantised, (k, v)))
+    q = normal(g, 1, 8, d, dtype=dtype)
+    q[..., 0] = 16      # scores of -120 and less
+    got = decode_call(c, cache, table.repeat(requests, 1), [n] * requests, q.repeat(requests, 1, 1))
+    want, bound = decode_oracle(c, q, [k], [v])
+    # f16's half steps below its normal numbers, 2^-25, in units of 2^-6 of the largest weight and scale, times codes up to 127
+    for h in range(8):
+        p = O.attend(q[0, h][None], k[:, h // 4], v[:, h // 4], 1 / 8, torch.ones(1, n, dtype=torch.bool))[2][0]
+        bound[0, h] += n * 2.0 ** -31 * 127 * (p * scales[:, h // 4]).max()
+    inside(got[:1], want, bound, "o")
+    assert same(got, got[:1].expand_as(got))
