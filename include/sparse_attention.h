@@ -11,7 +11,8 @@
  * contiguous and aligned to 16 bytes; q, k, v and their gradients have a stride of their own from row to row (in entries, at least the
  * row's own length; so that they may be parts of one product's rows) and the alignment of an entry, 16-byte groups being the fast path.
  * Scores, softmax statistics and sums are floats; probabilities and the gradients of scores are rounded to the tensors' type, as
- * operands of the next product (SC_F16: gradients of scores beyond 65 504 are infinite); every result is rounded once.
+ * operands of the next product (to f16 where values are 8-bit codes of 16-bit types; SC_F16: gradients of scores beyond 65 504 are infinite and
+ * below 2^-25 zero); every result is rounded once.
  */
 #ifndef SPARSE_ATTENTION_H_
 #define SPARSE_ATTENTION_H_
@@ -41,9 +42,11 @@ typedef struct {
  * sparse_rows_set_mask the row set needs a new plan: runs with the old one are refused (SC_ERR_MASK_COUNT).
  * q, o: [rows][heads][d], k, v: [rows][kv_heads][d], with row_format = SC_ROWS_COMPACT of the kept rows alone.
  * lse: float[kept][heads], log sum exp of the scores, for the backward pass; NULL in inference.  kept: of sparse_attn_info.
- * A row of q that is not finite loses what is made of it, and no other; one of k or v what is made of its sequence (its dk and dv too).  A row
- * all of whose scores are -infinity gives zeros, has zeros for its gradient and adds nothing to dk and dv; one whose largest score is beyond a float's
- * range is NaN, as one that is not finite.
+ * A row of q that is not finite loses its o and dq, one of do its dq, and no other row's; either loses dk and dv of the keys that it sees, and may
+ * lose those of all keys of its sequence and key-value head.  A row of k or v that is not finite loses what is made of its sequence and key-value
+ * head.  A row of q all of whose scores are -infinity gives zeros, has zeros for its gradient and adds nothing to dk and dv; one whose largest
+ * score is beyond a float's range is NaN, as one that is not finite.  Scores and lse are floats, which limits probabilities: those of the gradients
+ * are off by 2^-24 of lse's size relatively, and from scores of 2^24 on weights of f16 may leave its range.
  * rows * heads / kv_heads <= 2^30, rows * heads <= 2^36, (rows * heads / kv_heads / 128 + seqs) * kv_heads < 2^23 - 512. */
 typedef struct sc_attn sc_attn;
 

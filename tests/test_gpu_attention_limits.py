@@ -204,3 +204,25 @@ def test_8_bit_values_beside_larger_ones_that_have_no_weight(dtype, small, large
         bound[0, h] += n * 2.0 ** -31 * 127 * (p * scales[:, h // 4]).max()
     inside(got[:1], want, bound, "o")
     assert same(got, got[:1].expand_as(got))
+
+
+# ---- rows that are not finite ------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("which", ["q", "do"])
+@pytest.mark.parametrize("dtype,times", [("bf16", 1), ("bf16", 40), ("f32", 1), ("f32", 40)])
+def test_a_row_that_is_not_finite_loses_its_keys_gradients(which, dtype, times):
+    """A NaN row of q or of do loses its own o (q) and dq, and dk and dv of its sequence's key-value head; all else keeps its bits."""
+    c = ([90, 61, 40] * times, 4, 2, 64, dtype, True, 0, 1.0, 0, 0)
+    starts, rows, keep, x = case_inputs(c, 8)
+    _, _, clean = packed_call(c, starts, keep, x)
+    x[which][40, 1] = float("nan")                       # key-value head 0
+    _, _, got = packed_call(c, starts, keep, x)
+    own = torch.zeros(rows, 4, dtype=torch.bool, device=DEV)
+    own[40, 1] = True
+    for n in ("o", "lse", "dq"):
+        mine = own if n == "dq" or which == "q" else torch.zeros_like(own)
+        assert same(clean[n][~mine], got[n][~mine]) and torch.isnan(got[n][mine]).all(), n
+    for n in ("dk", "dv"):
+        assert same(clean[n][90:], got[n][90:]) and same(clean[n][:90, 1], got[n][:90, 1]), n
+        assert torch.isnan(got[n][:41, 0]).all(), n
