@@ -226,3 +226,109 @@ def test_a_row_that_is_not_finite_loses_its_keys_gradients(which, dtype, times):
     for n in ("dk", "dv"):
         assert same(clean[n][90:], got[n][90:]) and same(clean[n][:90, 1], got[n][:90, 1]), n
         assert torch.isnan(got[n][:41, 0]).all(), n
+
+
+# ---- every kernel, below and above the limits of the small tiles ---------------------------------------------------------
+
+LONG = [  # tiles that see 2 048 keys or more on average
+    ([2100], 2, 1, 64, "bf16", False, 0, 1.0, 0, 0),
+    ([2100], 2, 2, 128, "f16", False, 0, 1.0, 0, 3),
+    ([2600, 40, 0, 300], 2, 1, 128, "bf16", False, 0, 1.0, 0, 0),
+    ([2400], 3, 1, 64, "f16", False, 0, 0.9, 0, 1),
+    ([2500, 70], 2, 1, 128, "bf16", False, 0, 0.9, 1, 2),
+    ([4500], 2, 1, 64, "bf16", True, 0, 1.0, 0, 0),
+    ([3100], 1, 1, 128, "f16", False, 2200, 1.0, 0, 0),
+    ([2200], 2, 1, 40, "f16", False, 0, 1.0, 0, 0),
+    ([2200], 2, 1, 66, "bf16", False, 0, 1.0, 0, 0),
+    ([2111], 3, 1, 41, "bf16", False, 0, 0.98, 0, 0),
+    ([2111], 1, 1, 127, "f16", False, 0, 1.0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("c", LONG, ids=lambda c: "-".join(map(str, [sum(c[0]), len(c[0]), *c[1:]])))
+def test_tiles_that_see_many_keys(c):
+    packed_check(c, 3 * sum(c[0]) + c[3])
+
+
+@pytest.mark.parametrize("pad", [1, 2, 8])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f16")])
+def test_tiles_that_see_many_keys_of_rows_with_gaps(d, dtype, pad):
+    packed_check(([2100], 2, 1, d, dtype, False, 0, 1.0, 0, 0), 5, pad)
+
+
+def many(c):
+    """How often the sequences have to come for more than 2 048 tiles of 32."""
+    return 2049 // (sum(-(-n * c[1] // c[2] // 32) for n in c[0]) * c[2]) + 1
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 95, 96, 127, 128, 129, 191, 192, 193, 255, 256, 257])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_end_of_a_tile_of_many(n, dtype):
+    c = ([n, n], 2, 1, 64, dtype, n % 2 == 0, 0, 1.0, 0, 0)
+    packed_check(c, n, times=many(c))
+
+
+@pytest.mark.parametrize("window", [1, 2, 31, 32, 33, 64, 65, 200, 1 << 30])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_windows_of_many(window, causal, dtype):
+    c = ([150], 3, 1, 64, dtype, causal, window, 1.0, 0, 0)
+    packed_check(c, window % 97, times=many(c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,heads,kv,d,causal", [(300, 4, 4, 64, True), (300, 8, 2, 128, True), (190, 4, 4, 40, True), (190, 6, 2, 41, True), (2100, 1, 1, 128, False)])
+@pytest.mark.parametrize("of_many", [False, True])
+def test_results_are_as_near_as_their_operands_allow_of_few_and_many(dtype, n, heads, kv, d, causal, of_many):
+    """Probabilities and gradients of scores are rounded once, as operands of products, and results once more, whichever tiles form them.  dq's scores have
+    a delta from o as it is stored; dk's have not: with that delta dk would be off by as much more as dq is."""
+    c = ([n], heads, kv, d, dtype, causal, 0, 1.0, 0, 0)
+    times = many(c) if of_many else 1
+    starts, rows, keep, x = case_inputs(c, 23)
+    _, _, got = packed_call(([n] * times, *c[1:]), starts_of([n] * times), keep.repeat(times), {name: t.repeat(times, 1, 1) for name, t in x.items()})
+    want, _ = O.packed((heads, kv, d, dtype, causal, 0, 1 / math.sqrt(d)), starts, keep, x["q"], x["k"], x["v"], x["do"])
+    once = lambda v: v.to(O.TORCH[dtype]).double()  # noqa: E731
+    near = {name: torch.zeros_like(want[name]) for name in ("o", "dq", "dk", "dv")}
+    visible = O.seen(n, causal, 0)
+    for h in range(heads):
+        j, scale = h * kv // heads, 1 / math.sqrt(d)
+        q, k, v, do = x["q"][:, h], x["k"][:, j], x["v"][:, j], x["do"][:, h]
+        o, _, p = O.attend(q, k, v, scale, visible)
+        near["o"][:, h] = once(p) @ v
+        dp = do @ v.T
+        near["dq"][:, h] = once(p * (dp - (do * once(once(p) @ v)).sum(1, keepdim=True))) @ k * scale
+        near["dk"][:, j] += once(p * (dp - (do * o).sum(1, keepdim=True))).T @ q * scale
+        near["dv"][:, j] += once(p).T @ do
+    for name in near:
+        ideal = (once(near[name]) - want[name]).norm()
+        off = (got[name].double().cpu().view(times, *want[name].shape) - want[name]).flatten(1).norm(dim=1)
+        assert (off <= 1.1 * ideal).all(), f"{name}: {(off.max() / ideal):.3f}"
+
+
+def test_training_steps_of_many_rows_at_once():
+    """One plan on two streams, more than 2 048 tiles of 32: the gradients' large tiles, too, keep to their own workspaces."""
+    c = ([900, 30, 1100] * 5, 8, 2, 128, "bf16", True, 0, 1.0, 0, 0)
+    starts, rows, keep, x = case_inputs(c, 6)
+    plan = A.sparse_attn_plan(A.make_attn_desc(8, 2, 128), starts)
+    sets = [{n: dev(t if s == 0 else t.flip(0), "bf16") for n, t in x.items()} for s in range(2)]
+
+    def buffers():
+        b = {"o": nans(rows, 8, 128, dtype="bf16"), "lse": nans(rows, 8), "dq": nans(rows, 8, 128, dtype="bf16"), "dk": nans(rows, 2, 128, dtype="bf16"),
+             "dv": nans(rows, 2, 128, dtype="bf16")}
+        return b, torch.empty(A.sparse_attn_backward_workspace_bytes(plan), dtype=torch.uint8, device=DEV)
+
+    def go(s, b, ws, stream=None):
+        A.sparse_attn_run(plan, s["q"], s["k"], s["v"], b["o"], b["lse"], stream=stream)
+        A.sparse_attn_backward(plan, s["q"], s["k"], s["v"], b["o"], b["lse"], s["do"], b["dq"], b["dk"], b["dv"], ws, stream=stream)
+
+    want, got = [buffers(), buffers()], [buffers(), buffers()]
+    for s, (b, ws) in zip(sets, want):
+        go(s, b, ws)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, (b, ws), stream in zip(sets, got, streams):
+            go(s, b, ws, stream)
+    torch.cuda.synchronize()
+    for (a, _), (b, _) in zip(want, got):
+        assert all(same(a[n], b[n]) for n in a)
