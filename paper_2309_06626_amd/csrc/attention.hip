@@ -129,13 +129,13 @@ static sc_status attn_plan(sc_attn* plan, int64_t seqs, const int64_t* starts, c
   for (int64_t i = 0; i <= seqs; ++i) at[i] = (int32_t)starts[i];
   hipError_t e = hipSuccess;
   if (set && set->kept != set->rows && plan->end > 0) {
+    std::vector<int32_t> kept(at.size());      // (before the copies: what throws between them and the wait would give back memory that they use)
     int32_t *in = reinterpret_cast<int32_t*>(w), *out = reinterpret_cast<int32_t*>(w + l.starts);
     e = hipMemcpyAsync(in, at.data(), at.size() * 4, hipMemcpyHostToDevice, s);
     if (e == hipSuccess) {
       attn_starts_kernel<<<dim3((unsigned)(at.size() + 255) / 256), dim3(256), 0, s>>>(in, (int)at.size(), set->row_idx, (int32_t)set->kept, out);
       e = hipGetLastError();
     }
-    std::vector<int32_t> kept(at.size());
     if (e == hipSuccess) e = hipMemcpyAsync(kept.data(), out, kept.size() * 4, hipMemcpyDeviceToHost, s);
     const hipError_t waited = hipStreamSynchronize(s);      // (also after an error: the copies read and write these vectors)
     if (e == hipSuccess) e = waited;
