@@ -219,12 +219,13 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW =
     }
   };
   auto add_up = [&](const floatx16 (&s)[KB], auto from, auto to) {      // blocks from .. to, by themselves first: one weight after the other is lost beside a large sum
-    if constexpr (decltype(from)::value == decltype(to)::value) return;
-    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int B0 = decltype(from)::value, B1 = decltype(to)::value;
+    if constexpr (B0 == B1) return;
+    float part[4] = {s[B0 % KB][0], s[B0 % KB][1], s[B0 % KB][2], s[B0 % KB][3]};
 #pragma unroll
-    for (int b = decltype(from)::value; b < decltype(to)::value; ++b)
+    for (int b = B0; b < B1; ++b)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) part[v & 3] += s[b][v];
+      for (int v = b == B0 ? 4 : 0; v < 16; ++v) part[v & 3] += s[b][v];
     sum += (part[0] + part[1]) + (part[2] + part[3]);
   };
   auto values = [&](const v4i (&pf)[KB][A::SS], auto parity) {

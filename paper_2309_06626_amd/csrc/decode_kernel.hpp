@@ -302,11 +302,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves, BITS8 && DT != kF32 ? 2 : 1) voi
       sum *= less;
       if constexpr (!BITS8) rescale();
     }
-    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};                  // (one weight after the other is lost beside a large sum)
+    float part[4];                                             // (one weight after the other is lost beside a large sum)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       s[v] = attn_exp2(__builtin_fmaf(s[v], c, -shift));
-      part[v & 3] += s[v];
+      part[v & 3] = v < 4 ? s[v] : part[v & 3] + s[v];
     }
     sum += (part[0] + part[1]) + (part[2] + part[3]);
     if constexpr (BITS8) {
