@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * NW, DP > 64 && (DT == kF32 || (VEC < 2 && NW =
     return fmaxf(attn_max_halves(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]))) * c, m);
   };
   auto rescale = [&](float most) {
-    // (a maximum that grew by less than 2^8 stays: weights of up to 256 are as good as those of up to 1)
+    // (a maximum that grew by less than 2^8 stays, as is published of such kernels: weights of up to 256 are as good as those of up to 1)
     if (attn_any(most > m + 8.0f)) {
       const float next = attn_shift<DT == kF16>(most), less = m == -INFINITY ? 0.0f : attn_exp2(shift - next);
       shift = next;

@@ -15,11 +15,12 @@ sc_status check_attn(const sc_attn_desc* d);
 
 static int decode_width(int d) { return d <= 64 ? 64 : 128; }
 
-// Stretches of the longest sequence that the table allows; how long the sequences are is known on the device alone.  Workgroups of entries fill a
-// compute unit's LDS, of codes two do.  Few sequences: as many stretches as run at once (100 000 rows, 8 key-value heads: 32 stretches 79 us,
-// 64 89, 96 100; 33 sequences of up to 4 000 rows in 8 bits, 4 heads: 2 39 us, 4 29.7, 6 32).  Many, whose lengths differ: three times as many
-// (64 sequences of 4 096 to 8 192 rows, 8 heads: 1 316 us, 2 306, 4 304).  A stretch has a tile for each wavefront at least, and no more pages
-// than a workgroup holds.
+// Stretches of the longest sequence that the table allows; how long the sequences are is known on the device alone.  A workgroup of entries above 64
+// channels fills a compute unit's LDS, of codes of 16-bit types two do.  (Two of 16-bit entries of up to 64 channels would fit as well; they are counted as
+// those above.)  Few sequences: as many stretches as run at once (100 000 rows, 8 key-value heads: 32 stretches 79 us, 64 89, 96 100; 33 sequences of up
+// to 4 000 rows in 8 bits, 4 heads: 2 39 us, 4 29.7, 6 32).  Many, whose lengths differ: three times as many (64 sequences of 4 096 to 8 192 rows, 8
+// heads: 1 316 us, 2 306, 4 304).  Between the two, where the number of stretches jumps from 2 to 6, nothing was measured.  A stretch has a tile for each
+// wavefront at least, and no more pages than a workgroup holds.
 static int64_t decode_splits(const sc_attn_desc* d, const sc_kv_desc* cache, int64_t rows, int64_t table_width) {
   const int64_t blocks = (d->heads / d->kv_heads + 31) / 32, base = std::max<int64_t>(rows * blocks * d->kv_heads, 1);
   int64_t keys = table_width * cache->page_rows;

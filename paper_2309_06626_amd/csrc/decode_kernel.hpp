@@ -7,9 +7,10 @@
 // Maximum, sum and result of the wavefronts are joined in LDS, those of the stretches by a second launch, both in a fixed order.
 //
 // Bound by memory: a tile is 16 KB of 16-bit entries for 16 products, of whose columns a group of query heads fills some.  Entries go straight
-// into LDS, where a wavefront has two tiles of keys and two of values, of which three are on their way.  Measured, 8 key-value heads of
-// 128 in bf16: 64 sequences of 4 096 to 8 192 rows 289 us (5.6 TB/s; a plain copy 6.3), one of 100 000 rows 79 (5.2 TB/s).  Codes go through
-// registers, where they are widened; 33 sequences of up to 4 000 rows, 4 heads: 29 us (2.4 TB/s), bound by the longest stretch's chain of
+// into LDS, where a wavefront has two tiles of keys and two of values, of which three are on their way (of floats above 64 channels one of each, asked
+// for when both have been multiplied).  Measured, 8 key-value heads in bf16: 64 sequences of 4 096 to 8 192 rows 288 us with heads of 128 (5.6 TB/s;
+// a plain copy 6.3), 152 of 64 (5.3), one of 100 000 rows 79 (5.2) and 44 (4.7); in floats, of the 64 sequences, 640 (5.0) and 442 (3.6).  Codes go
+// through registers, where they are widened; 33 sequences of up to 4 000 rows, 4 heads: 28.3 us (2.5 TB/s), bound by the longest stretch's chain of
 // widening, products and exponentials.
 #pragma once
 #include "attn_tile.hpp"
