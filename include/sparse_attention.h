@@ -101,8 +101,9 @@ sc_status sparse_kv_read(const sc_kv_desc* desc, int64_t rows, const int64_t* sl
  * lies in page table[r][j / page_rows] (int32[rows][table_width]).  lengths[r] <= 0: o is zero; beyond table_width * page_rows: what the
  * table holds.  Rows of a page that is not in the cache are not there: no weight, nothing read.
  * What lies in the cache behind a sequence's length is not looked at, whatever it is.  A key or value that is not finite loses the heads
- * that read it in this row of q, and no other row; a score beyond a float's range is as above.  rows * heads < 2^24, and so is the number of
- * workgroups, which the sequences' longest length that table_width allows multiplies. */
+ * that read it in this row of q, and no other row; a score beyond a float's range is as above.  Against 8-bit codes a head's row of q in SC_BF16 is
+ * taken in f16, in units of its largest entry: entries below 2^-28 of that lose digits.  rows * heads < 2^24, and so is the number of workgroups, which
+ * the sequences' longest length that table_width allows multiplies. */
 sc_status sparse_attn_decode_workspace_bytes(const sc_attn_desc* desc, const sc_kv_desc* cache, int64_t rows, int64_t table_width,
                                              size_t* bytes);
 sc_status sparse_attn_decode(const sc_attn_desc* desc, const sc_kv_desc* cache, int64_t rows, const void* q_dev, const int32_t* table_dev,
